@@ -44,7 +44,9 @@ typedef struct CUstream_st *hsa_stream_t;
 
 typedef enum {
     HSA_BF16 = 0,   /* bfloat16 storage, fp32 accumulation */
-    HSA_F32 = 1     /* fp32 storage and arithmetic */
+    HSA_F32 = 1,    /* fp32 storage and arithmetic */
+    HSA_E4M3 = 2    /* 8-bit KV cache: e4m3 codes with one power of two per row; only where
+                       a call names it */
 } hsa_dtype;
 
 typedef enum {
@@ -315,6 +317,86 @@ int hsa_active_attention_prefix(const void *q, const int32_t *q_idx, int n_activ
  * D, so one buffer serves every call of a given D on that device. */
 size_t hsa_active_attention_workspace_bytes(int n_active, int N, int H, int D,
                                             hsa_dtype dtype);
+
+/* ------------------------------------------------- the KV cache in 8 bits */
+
+/* A KV cache of N rows of H heads x D values in half the bytes of bf16.  The row of
+ * one token and head is held as D e4m3 codes (OCP 8-bit floating point, 4 exponent
+ * and 3 fraction bits) and one scale byte s, and stands for code * 2^(s - 127):
+ *   codes   [N, H, D], one byte each;   scales  [N, H], one byte each.
+ * Written from values x: with a the largest |x_d| of the row, e is the least integer
+ * with a * 2^-e <= 448, at least -100; s = e + 127 and the codes are x * 2^-e rounded
+ * to nearest, ties to even.  The values held are exact in bf16 and fp32.  A magnitude
+ * above 1.875 * 2^127 counts as that.  A NaN or infinite element is stored as NaN and
+ * reported (HSA_ERR_NONFINITE); its row goes by the largest finite element.
+ *
+ * hsa_kv_quant_scatter: the KV-cache synchronisation (Sec. 2.3, step 2; see
+ * hsa_kv_sync_scatter) into an 8-bit cache: row idx[j] of the caches takes fresh
+ * row j, one launch for K and V.
+ *   k_cache, v_cache  device, codes [N, H, D], updated in place.
+ *   k_scale, v_scale  device, scales [N, H], updated in place (any alignment).
+ *   k_fresh, v_fresh  device, [n_active, H, D] of dtype (HSA_BF16 or HSA_F32).
+ *   idx               device, int32 [n_active], distinct values in [0, N).  For a
+ *                     cache in pages [n_pages, page, H, D] that is N = n_pages * page
+ *                     rows, idx[j] = page id * page + place in the page.
+ *   table             device, fp32 [table_rows, D/2, 2] or NULL: K is first rotated
+ *                     as hsa_rope_rows does (HSA_BF16 only), fresh row j by table row
+ *                     table_idx[j], or idx[j] where table_idx is NULL.  The cache then
+ *                     holds what hsa_kv_sync_scatter_rope would have written, in 8
+ *                     bits.  table_idx needs a table.
+ * An idx entry outside [0, N), or a table row outside [0, table_rows), skips its row
+ * (HSA_ERR_INDEX).
+ *
+ * hsa_kv_dequant_gather: rows idx[j] of the cache (rows 0 .. n-1 where idx is NULL,
+ * n <= N) as [n, H, D] of dtype (HSA_BF16 or HSA_F32), for the attention calls below;
+ * one bf16 buffer of a layer's size then serves every layer.  An idx entry outside
+ * [0, N) leaves its output rows untouched (HSA_ERR_INDEX).
+ *
+ * Both: D a multiple of 8 up to 256, n * H < 2^31, pointers but the scales 16-byte
+ * aligned. */
+int hsa_kv_quant_scatter(void *k_cache, void *v_cache, uint8_t *k_scale, uint8_t *v_scale,
+                         const void *k_fresh, const void *v_fresh, const int32_t *idx,
+                         int n_active, int N, int H, int D, hsa_dtype dtype,
+                         const float *table, const int32_t *table_idx, int table_rows,
+                         hsa_stream_t stream);
+int hsa_kv_dequant_gather(const void *k_cache, const void *v_cache, const uint8_t *k_scale,
+                          const uint8_t *v_scale, const int32_t *idx, int n, int N, int H,
+                          int D, void *k_out, void *v_out, hsa_dtype dtype,
+                          hsa_stream_t stream);
+
+/* ------------------------------- attention over paged caches, packed prompts */
+
+/* Attention of the n_new newest tokens of each of `batch` sequences over caches held
+ * in pages, with grouped heads: query head h reads K/V head h / (Hq / Hkv), and
+ *   out[b, i, h, :] = sum_j softmax_j(scale * <q[b,i,h], k_j>) v_j
+ * over the keys j < seq_lens[b] - n_new + i + 1 of sequence b (so the newest tokens
+ * are causal among themselves; their K/V are in the cache already).  A row without
+ * keys is zero.  scale <= 0 selects 1/sqrt(D).
+ *   q            device, bf16 [batch, n_new, Hq, D].
+ *   k_pages,     device, [n_pages, page_size, Hkv, D] of cache_dtype: HSA_BF16, or
+ *   v_pages      HSA_E4M3 as hsa_kv_quant_scatter writes it, with
+ *   k_scale,     device, scales [n_pages, page_size, Hkv] (HSA_E4M3; else NULL).
+ *   v_scale
+ *   page_table   device, int32 [batch, max_pages]: key j of sequence b is row
+ *                j % page_size of page page_table[b, j / page_size].  Entries past a
+ *                sequence's last page are not read, nor rows past its last key.
+ *   seq_lens     device, int32 [batch], in [0, max_pages * page_size]; a value
+ *                outside is taken as the nearer end and reported (HSA_ERR_INDEX).
+ *   out          device, bf16 [batch, n_new, Hq, D], written.
+ *   workspace    device, >= hsa_paged_attention_workspace_bytes(...) bytes, 16-byte
+ *                aligned, overwritten; calls (and captured graphs) sharing one must
+ *                not overlap on the GPU.  Its size depends on D and the device only.
+ * D in {64, 128}; page_size a power of two; max_pages * page_size < 2^31 - 256.  A
+ * page id outside [0, n_pages) reads as rows of zeros (HSA_ERR_INDEX).  Two launches;
+ * the result does not depend on what else runs.  A flat cache of N rows is a cache of
+ * ceil(N / page_size) pages with the identity as its table. */
+int hsa_paged_attention(const void *q, int batch, int n_new, int Hq, const void *k_pages,
+                        const void *v_pages, const uint8_t *k_scale, const uint8_t *v_scale,
+                        int n_pages, int page_size, int Hkv, int D, hsa_dtype cache_dtype,
+                        const int32_t *page_table, int max_pages, const int32_t *seq_lens,
+                        float scale, void *out, void *workspace, size_t workspace_bytes,
+                        hsa_stream_t stream);
+size_t hsa_paged_attention_workspace_bytes(int batch, int n_new, int Hq, int Hkv, int D);
 
 /* ------------------------------------------------------- a6 cached Euler */
 

@@ -27,6 +27,8 @@ __all__ = [
     "hsa_active_attention", "hsa_active_attention_prefix",
     "hsa_active_attention_workspace_bytes",
     "hsa_cached_euler", "hsa_cached_euler_l1rel",
+    "HSA_E4M3", "hsa_kv_quant_scatter", "hsa_kv_dequant_gather",
+    "hsa_paged_attention", "hsa_paged_attention_workspace_bytes",
     "hsa_get_device_error", "hsa_launch_count", "hsa_test_inject_attention_stall",
     "hsa_test_f32_cluster",
 ]
@@ -34,7 +36,7 @@ __all__ = [
 _HERE = os.path.dirname(os.path.abspath(__file__))
 library_path = os.path.join(_HERE, "libhsa.so")
 
-HSA_BF16, HSA_F32 = 0, 1
+HSA_BF16, HSA_F32, HSA_E4M3 = 0, 1, 2
 HSA_PARTITION_STATIC_MAX_TOKENS = 524288
 STATUS = {0: "HSA_OK", -1: "HSA_ERR_INVALID_ARG", -2: "HSA_ERR_NOT_DIVISOR",
           -3: "HSA_ERR_BAD_COUNTS", -4: "HSA_ERR_UNSUPPORTED", -5: "HSA_ERR_NONFINITE",
@@ -84,6 +86,11 @@ _SIGS = {
     "hsa_cached_euler": ([_c_p, _c_p, _c_p, _c_p, _c_int, _c_int, _c_int, _c_f, _c_p], _c_int),
     "hsa_cached_euler_l1rel": ([_c_p, _c_p, _c_p, _c_p, _c_int, _c_int, _c_int, _c_f, _c_p,
                                 _c_f, _c_p], _c_int),
+    "hsa_kv_quant_scatter": ([_c_p] * 7 + [_c_int] * 5 + [_c_p, _c_p, _c_int, _c_p], _c_int),
+    "hsa_kv_dequant_gather": ([_c_p] * 5 + [_c_int] * 4 + [_c_p, _c_p, _c_int, _c_p], _c_int),
+    "hsa_paged_attention": ([_c_p, _c_int, _c_int, _c_int] + [_c_p] * 4 + [_c_int] * 5 +
+                            [_c_p, _c_int, _c_p, _c_f, _c_p, _c_p, _c_sz, _c_p], _c_int),
+    "hsa_paged_attention_workspace_bytes": ([_c_int] * 5, _c_sz),
     "hsa_get_device_error": ([_c_p], _c_int),
     "hsa_launch_count": ([], ctypes.c_ulonglong),
     "hsa_test_inject_attention_stall": ([_c_int], _c_int),
@@ -160,6 +167,33 @@ def _dtype_code(t: torch.Tensor) -> int:
     if t.dtype == torch.float32:
         return HSA_F32
     raise TypeError(f"unsupported dtype {t.dtype}")
+
+
+def _want(name, t, dtype, *shape, optional=False):
+    """Refuses a tensor that is not a contiguous device tensor of the current device with
+    this dtype (or one of a tuple) and shape (None: any size); returns its address.  What
+    C cannot see of a tensor is checked here."""
+    if t is None:
+        if optional:
+            return None
+        raise TypeError(f"{name} is missing")
+    if t.dtype is not dtype and not (isinstance(dtype, tuple) and t.dtype in dtype):
+        raise TypeError(f"{name} has dtype {t.dtype}, not {dtype}")
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, not on the current CUDA device")
+    if t.dim() != len(shape) or any(w is not None and n != w for n, w in zip(t.shape, shape)):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, not "
+                         f"{tuple('any' if w is None else w for w in shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} is not contiguous")
+    return t.data_ptr()
+
+
+def _scratch(t):
+    """Address and bytes of a workspace (None: none)."""
+    if t is None:
+        return None, 0
+    return _want("workspace", t.view(-1), t.dtype, None), t.numel() * t.element_size()
 
 
 # ---------------------------------------------------------- host helpers
@@ -341,6 +375,87 @@ def hsa_cached_euler_l1rel(x, v_cache, v_fresh, pos, dsigma: float, stat, weight
     _check(lib().hsa_cached_euler_l1rel(_p(x), _p(v_cache), _p(v_fresh), _p(pos), n_fresh, N, C,
                                         float(dsigma), _p(stat), float(weight),
                                         _stream(stream)), "hsa_cached_euler_l1rel")
+
+
+# ------------------------------------------------ 8-bit cache, paged attention
+
+_CODES = (torch.float8_e4m3fn, torch.uint8)
+_FLOATS = (torch.bfloat16, torch.float32)
+
+
+def hsa_kv_quant_scatter(k_cache, v_cache, k_scale, v_scale, k_fresh, v_fresh, idx, n_active: int,
+                         table=None, table_idx=None, stream=None) -> None:
+    """Fresh rows [n, H, D] (bf16 or fp32) into rows idx of an 8-bit cache: codes [N, H, D]
+    (float8_e4m3fn or uint8) and scale bytes [N, H] (uint8); a cache in pages [P, page, H, D]
+    with scales [P, page, H] counts as P * page rows.  table: K is rotated first (bf16), by
+    the table's rows table_idx (idx where that is None)."""
+    H, D = k_cache.shape[-2:]
+    lead = k_cache.shape[:-2]
+    N = lead.numel()
+    dt = k_fresh.dtype
+    if idx.dim() != 1 or not 0 <= n_active <= min(idx.numel(), k_fresh.shape[0]):
+        raise ValueError("idx or k_fresh holds fewer than n_active rows")
+    rows = k_fresh.shape[0]
+    ids = None
+    if table_idx is not None:
+        ids = _want("table_idx", table_idx, torch.int32, None)
+        if table_idx.numel() < n_active:
+            raise ValueError("table_idx holds fewer than n_active rows")
+    _check(lib().hsa_kv_quant_scatter(
+        _want("k_cache", k_cache, _CODES, *lead, H, D), _want("v_cache", v_cache, _CODES, *lead, H, D),
+        _want("k_scale", k_scale, torch.uint8, *lead, H),
+        _want("v_scale", v_scale, torch.uint8, *lead, H),
+        _want("k_fresh", k_fresh, _FLOATS, rows, H, D), _want("v_fresh", v_fresh, dt, rows, H, D),
+        _want("idx", idx, torch.int32, None), n_active, N, H, D, _dtype_code(k_fresh),
+        _want("table", table, torch.float32, None, D // 2, 2, optional=True), ids,
+        0 if table is None else table.shape[0], _stream(stream)), "hsa_kv_quant_scatter")
+
+
+def hsa_kv_dequant_gather(k_cache, v_cache, k_scale, v_scale, idx, n: int, k_out, v_out,
+                          stream=None) -> None:
+    """k_out[:n], v_out[:n] ([>= n, H, D], bf16 or fp32) <- rows idx[:n] of an 8-bit cache
+    (idx None: rows 0 .. n-1); the cache as for hsa_kv_quant_scatter."""
+    H, D = k_cache.shape[-2:]
+    lead = k_cache.shape[:-2]
+    if not 0 <= n <= k_out.shape[0] or (idx is not None and n > idx.numel()):
+        raise ValueError("idx or k_out holds fewer than n rows")
+    rows = k_out.shape[0]
+    _check(lib().hsa_kv_dequant_gather(
+        _want("k_cache", k_cache, _CODES, *lead, H, D), _want("v_cache", v_cache, _CODES, *lead, H, D),
+        _want("k_scale", k_scale, torch.uint8, *lead, H),
+        _want("v_scale", v_scale, torch.uint8, *lead, H),
+        _want("idx", idx, torch.int32, None, optional=True), n, lead.numel(), H, D,
+        _want("k_out", k_out, _FLOATS, rows, H, D), _want("v_out", v_out, k_out.dtype, rows, H, D),
+        _dtype_code(k_out), _stream(stream)), "hsa_kv_dequant_gather")
+
+
+def hsa_paged_attention_workspace_bytes(batch: int, n_new: int, Hq: int, Hkv: int, D: int) -> int:
+    return lib().hsa_paged_attention_workspace_bytes(batch, n_new, Hq, Hkv, D)
+
+
+def hsa_paged_attention(q, k_pages, v_pages, page_table, seq_lens, out, k_scale=None, v_scale=None,
+                        scale: float = 0.0, workspace=None, stream=None) -> None:
+    """out = attention of the newest tokens q [batch, n_new, Hq, D] over each sequence's
+    seq_lens[b] keys, held in pages [n_pages, page, Hkv, D] named by page_table [batch,
+    max_pages]; bf16 pages, or 8-bit ones (float8_e4m3fn or uint8) with their scale bytes
+    [n_pages, page, Hkv].  workspace: uint8 device tensor of at least
+    hsa_paged_attention_workspace_bytes(...) bytes."""
+    B, n_new, Hq, D = q.shape
+    n_pages, page, Hkv, _ = k_pages.shape
+    f8 = k_scale is not None
+    kind = _CODES if f8 else torch.bfloat16
+    where, size = _scratch(workspace)
+    _check(lib().hsa_paged_attention(
+        _want("q", q, torch.bfloat16, B, n_new, Hq, D), B, n_new, Hq,
+        _want("k_pages", k_pages, kind, n_pages, page, Hkv, D),
+        _want("v_pages", v_pages, kind, n_pages, page, Hkv, D),
+        _want("k_scale", k_scale, torch.uint8, n_pages, page, Hkv, optional=True),
+        _want("v_scale", v_scale, torch.uint8, n_pages, page, Hkv, optional=not f8),
+        n_pages, page, Hkv, D, HSA_E4M3 if f8 else HSA_BF16,
+        _want("page_table", page_table, torch.int32, B, None), page_table.shape[1],
+        _want("seq_lens", seq_lens, torch.int32, B), float(scale),
+        _want("out", out, torch.bfloat16, B, n_new, Hq, D), where, size, _stream(stream)),
+        "hsa_paged_attention")
 
 
 def hsa_get_device_error(stream=None) -> int:
