@@ -756,9 +756,10 @@ def profiled_traffic(w, n_of):
     with fewer heads; heads are independent, so a launch's traffic scales with
     H."""
     path = os.path.join(ROOT, "profiles", f"attention_{w.name}.md")
-    src = os.path.join(ROOT, "paper_2605_06892_gb300", "csrc", "hsa_attention.cu")
+    src = os.path.join(ROOT, "paper_2605_06892_gb300", "csrc")
     try:
-        digest = code_digest(open(src).read())
+        digest = code_digest("\n".join(open(os.path.join(src, f)).read()
+                                       for f in ("hsa_tc.cuh", "hsa_attention.cu")))
         per_head, sha = {}, None
         for line in open(path):
             if line.startswith("code_sha256:"):

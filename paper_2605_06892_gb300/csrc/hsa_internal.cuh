@@ -94,6 +94,9 @@ int launch_attention_f32(const void *q, const int32_t *q_idx, int n_active, cons
                          int rows2, int H, int D, float scale, void *out, cudaStream_t stream,
                          unsigned *err);
 
+// The mode of the attention's test hook (hsa_test.h).
+int attention_stall();
+
 // Number of lanes that cooperate on one row of `vecs` 16-byte vectors:
 // a power of two, at most 32.
 inline int lanes_per_row(long long vecs) {

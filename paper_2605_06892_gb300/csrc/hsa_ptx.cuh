@@ -1,4 +1,4 @@
-// PTX wrappers shared by the two attention kernels.
+// PTX wrappers shared by the attention kernels.
 #pragma once
 
 #include <stdint.h>
