@@ -398,6 +398,39 @@ int hsa_paged_attention(const void *q, int batch, int n_new, int Hq, const void 
                         hsa_stream_t stream);
 size_t hsa_paged_attention_workspace_bytes(int batch, int n_new, int Hq, int Hkv, int D);
 
+/* Attention of whole prompts: `batch` sequences packed one behind the other, with
+ * grouped heads: query head h reads K/V head h / (Hq / Hkv).  Sequence b has the query
+ * rows cu_q[b] .. cu_q[b+1]-1 and the key rows cu_k[b] .. cu_k[b+1]-1, Lq and Lk of
+ * them; its query i stands at position p = i + Lk - Lq (its keys may begin before its
+ * queries: a prompt continued) and sees
+ *   mask == 0   all Lk keys;
+ *   mask == F   the keys below (floor(p / F) + 1) * F: causal by frames of F tokens,
+ *               plainly causal for F = 1.
+ * A row that sees no key is zero.  What a row does not see does not reach it, NaN and
+ * infinities included.  scale <= 0 selects 1/sqrt(D).
+ *   q, k, v      device, bf16: token rows of Hq (Hkv, Hkv) heads x D values, q_row
+ *                (k_row, v_row) elements from one token to the next: Hq * D where they
+ *                are compact, more in a fused projection's output; multiples of 8.
+ *   cu_q, cu_k   device, int32 [batch + 1], not falling, within [0, total_q] and
+ *                [0, total_k]; other values are moved inside and reported
+ *                (HSA_ERR_INDEX; what is computed is then unspecified).
+ *   total_q,     rows that q and out (k and v) hold; rows before cu[0] or from
+ *   total_k      cu[batch] on are neither read nor written.
+ *   out          device, bf16 [total_q, Hq, D] compact, written; overlaps no input.
+ *   dtype        HSA_BF16.
+ *   workspace    device, optional (NULL = none), >=
+ *                hsa_packed_attention_workspace_bytes(...) bytes, 16-byte aligned: lets
+ *                calls with few rows and long keys be cut along the keys and joined (a
+ *                second launch).  Overwritten; calls (and captured graphs) sharing one
+ *                must not overlap on the GPU.  Its size depends on D and the device.
+ * D in {64, 128}; pointers but cu_q and cu_k 16-byte aligned. */
+int hsa_packed_attention(const void *q, long long q_row, const void *k, long long k_row,
+                         const void *v, long long v_row, const int32_t *cu_q,
+                         const int32_t *cu_k, int batch, int total_q, int total_k, int Hq,
+                         int Hkv, int D, int mask, float scale, void *out, hsa_dtype dtype,
+                         void *workspace, size_t workspace_bytes, hsa_stream_t stream);
+size_t hsa_packed_attention_workspace_bytes(int Hq, int Hkv, int D);
+
 /* ------------------------------------------------------- a6 cached Euler */
 
 /* Cached Euler update (Sec. 2.4, Eq. 6) of all N tokens in one pass: when

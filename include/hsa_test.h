@@ -16,7 +16,8 @@ extern "C" {
 #endif
 
 /* mode 0: normal operation (default).
- * mode 1: in every bf16 hsa_active_attention launch that follows, each CTA
+ * mode 1: in every bf16 hsa_active_attention (and hsa_active_attention_prefix,
+ *         hsa_packed_attention) launch that follows, each CTA
  *         never loads its first value tile, so the bounded wait for it runs
  *         out; the call then reports HSA_ERR_TIMEOUT through
  *         hsa_get_device_error and its output is unspecified.

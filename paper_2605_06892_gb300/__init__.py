@@ -29,6 +29,7 @@ __all__ = [
     "hsa_cached_euler", "hsa_cached_euler_l1rel",
     "HSA_E4M3", "hsa_kv_quant_scatter", "hsa_kv_dequant_gather",
     "hsa_paged_attention", "hsa_paged_attention_workspace_bytes",
+    "hsa_packed_attention", "hsa_packed_attention_workspace_bytes",
     "hsa_get_device_error", "hsa_launch_count", "hsa_test_inject_attention_stall",
     "hsa_test_f32_cluster",
 ]
@@ -52,6 +53,7 @@ class HsaError(RuntimeError):
 
 _c_int, _c_p, _c_sz, _c_f, _c_d = (ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t,
                                    ctypes.c_float, ctypes.c_double)
+_c_ll = ctypes.c_longlong
 _SIGS = {
     "hsa_status_string": ([_c_int], ctypes.c_char_p),
     "hsa_version": ([], _c_int),
@@ -91,6 +93,9 @@ _SIGS = {
     "hsa_paged_attention": ([_c_p, _c_int, _c_int, _c_int] + [_c_p] * 4 + [_c_int] * 5 +
                             [_c_p, _c_int, _c_p, _c_f, _c_p, _c_p, _c_sz, _c_p], _c_int),
     "hsa_paged_attention_workspace_bytes": ([_c_int] * 5, _c_sz),
+    "hsa_packed_attention": ([_c_p, _c_ll, _c_p, _c_ll, _c_p, _c_ll, _c_p, _c_p] + [_c_int] * 7 +
+                             [_c_f, _c_p, _c_int, _c_p, _c_sz, _c_p], _c_int),
+    "hsa_packed_attention_workspace_bytes": ([_c_int] * 3, _c_sz),
     "hsa_get_device_error": ([_c_p], _c_int),
     "hsa_launch_count": ([], ctypes.c_ulonglong),
     "hsa_test_inject_attention_stall": ([_c_int], _c_int),
@@ -456,6 +461,44 @@ def hsa_paged_attention(q, k_pages, v_pages, page_table, seq_lens, out, k_scale=
         _want("seq_lens", seq_lens, torch.int32, B), float(scale),
         _want("out", out, torch.bfloat16, B, n_new, Hq, D), where, size, _stream(stream)),
         "hsa_paged_attention")
+
+
+def hsa_packed_attention_workspace_bytes(Hq: int, Hkv: int, D: int) -> int:
+    return lib().hsa_packed_attention_workspace_bytes(Hq, Hkv, D)
+
+
+def _token_rows(name, t, H, D):
+    """Address and row stride of bf16 token rows [tokens, H, D] on the current device whose
+    heads lie together; rows may lie apart, as in a fused projection's output."""
+    tokens = t.shape[0]
+    near = t[:0] if tokens == 0 else t[0]
+    if tuple(t.shape) != (tokens, H, D) or (tokens and not near.is_contiguous()):
+        raise ValueError(f"{name} is not rows of {H} heads x {D} that lie together")
+    _want(name, near if tokens else t, torch.bfloat16, *((H, D) if tokens else t.shape))
+    row = t.stride(0) if tokens > 1 else H * D
+    return (t.data_ptr() if tokens else None), row
+
+
+def hsa_packed_attention(q, k, v, cu_q, cu_k, out, mask: int = 0, scale: float = 0.0, workspace=None,
+                         stream=None) -> None:
+    """out [total_q, Hq, D] = attention of packed sequences: queries q[cu_q[b]:cu_q[b+1]] of
+    [total_q, Hq, D] over k, v[cu_k[b]:cu_k[b+1]] of [total_k, Hkv, D], bf16; mask 0: none,
+    F: causal by frames of F tokens (1: causal).  The rows of q, k and v may be slices of a
+    wider tensor.  workspace (optional): uint8 device tensor of
+    hsa_packed_attention_workspace_bytes(Hq, Hkv, D) bytes."""
+    total_q, Hq, D = q.shape
+    total_k, Hkv, _ = k.shape
+    (qp, q_row), (kp, k_row) = _token_rows("q", q, Hq, D), _token_rows("k", k, Hkv, D)
+    if v.shape[0] != total_k:
+        raise ValueError("v holds another number of rows than k")
+    vp, v_row = _token_rows("v", v, Hkv, D)
+    where, size = _scratch(workspace)
+    batch = cu_q.numel() - 1
+    _check(lib().hsa_packed_attention(
+        qp, q_row, kp, k_row, vp, v_row, _want("cu_q", cu_q, torch.int32, batch + 1),
+        _want("cu_k", cu_k, torch.int32, batch + 1), batch, total_q, total_k, Hq, Hkv, D, mask,
+        float(scale), _want("out", out, torch.bfloat16, total_q, Hq, D), HSA_BF16, where, size,
+        _stream(stream)), "hsa_packed_attention")
 
 
 def hsa_get_device_error(stream=None) -> int:

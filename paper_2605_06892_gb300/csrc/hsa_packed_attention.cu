@@ -1,0 +1,665 @@
+// Attention over whole prompts: several sequences packed one behind the other, query
+// heads in groups that share a K/V head, bidirectional or causal by frames of F tokens
+// (F = 1: plainly causal).  Query i of a sequence of Lq queries and Lk keys stands at
+// p = i + Lk - Lq and sees the keys below
+//   limit_i = Lk, or min(Lk, (floor(p / F) + 1) F) with a mask (none where that is <= 0).
+// 4 D FLOPs per query head and visible pair: bound by the tensor pipe.
+//
+// The pipeline of a CTA (256 query rows in two Q tiles, 128-key tiles through a TMA ring,
+// scores and O in TMEM, named-barrier hand-offs) is the active attention's (hsa_tc.cuh,
+// hsa_attention.cu).  What differs:
+//  - Rows.  A unit's rows are (token, head of the group) pairs, row R = i G + g of a
+//    sequence and K/V head.  One pass over the keys serves the whole group: K and V are
+//    read 1/G as often, short sequences fill the 256 rows G times sooner, and the rows of
+//    a unit span only 256 / G tokens, so fewer of its key tiles cross the mask's edge.
+//  - Units.  The lengths are on the device, so every block works out its own unit from
+//    them: sequence by sequence, head by head, each head's query blocks from the last
+//    (under a mask the longest) to the first, so that a head's K/V are read by blocks that
+//    run together and the last units to start are short.
+//  - Mask.  A unit's key tiles end at its last row's limit; a row's own limit is applied
+//    to its scores in the tiles that some row of its warp does not see whole.
+//  - Few units.  With a workspace the units of the last, partly filled wave (all of them
+//    where there are fewer units than SMs) are cut along the keys and joined afterwards;
+//    under a mask only the latter, since the last units to start are short already.
+//  - Rows without keys come out as zeros.
+//  - Values that a row does not see must not reach it by 0 * NaN.  The rows of V behind a
+//    sequence's end are zeroed in shared memory before they are multiplied.  Under a mask,
+//    a row whose result is not finite looks through the values it should not have met in
+//    its unit's tiles; if one of those is not finite the row is formed again without them
+//    on the CUDA cores.
+#include <algorithm>
+#include <atomic>
+#include <cmath>
+
+#include "hsa_internal.cuh"
+#include "hsa_ptx.cuh"
+#include "hsa_tc.cuh"
+
+namespace hsa {
+namespace {
+
+constexpr int kUnitRows = kQT * kBM;
+constexpr float kLowest = -3.0e38f;   // running maximum of a row that has seen no key
+
+struct PackedArgs {
+  const __nv_bfloat16 *q, *k, *v;
+  __nv_bfloat16 *out;
+  const int32_t *cu_q, *cu_k;
+  unsigned *err;
+  int batch, total_q, total_k, Hq, Hkv, G, mask;
+  long long q_row, k_row, v_row;   // elements from a token to the next
+  float scale_log2;
+  int sms, split;                  // split: the workspace is there
+  int inject_stall;                // test hook (hsa_test.h)
+  float *ws_o, *ws_ml;             // [piece][kUnitRows][D], [piece][kUnitRows][2]
+};
+
+struct Sequence {
+  int q0, lq, k0, lk;
+};
+
+// Sequence b's rows and keys; ends that run backwards or past the tensors are moved
+// inside and reported.
+__device__ __forceinline__ Sequence sequence(const PackedArgs &a, int b) {
+  const int q0 = __ldg(a.cu_q + b), q1 = __ldg(a.cu_q + b + 1);
+  const int k0 = __ldg(a.cu_k + b), k1 = __ldg(a.cu_k + b + 1);
+  Sequence s;
+  s.q0 = min(max(q0, 0), a.total_q);
+  s.k0 = min(max(k0, 0), a.total_k);
+  const int qe = min(max(q1, s.q0), a.total_q), ke = min(max(k1, s.k0), a.total_k);
+  if (s.q0 != q0 || s.k0 != k0 || qe != q1 || ke != k1) set_error(a.err, kErrIndex);
+  s.lq = qe - s.q0;
+  s.lk = ke - s.k0;
+  return s;
+}
+
+__device__ __forceinline__ int query_blocks(const PackedArgs &a, const Sequence &s) {
+  return (int)(((long long)s.lq * a.G + kUnitRows - 1) / kUnitRows);
+}
+
+// Keys that query i of a sequence sees.
+__device__ __forceinline__ int key_limit(const PackedArgs &a, const Sequence &s, int i) {
+  if (!a.mask) return s.lk;
+  const int p = i + s.lk - s.lq;
+  if (p < 0) return 0;
+  return (int)min((long long)s.lk, ((long long)(p / a.mask) + 1) * a.mask);
+}
+
+// What all blocks of a launch share: units, how many of them whole, pieces of the others.
+struct Split {
+  int units, n_whole, pieces;
+};
+
+// One unit and this block's part of its key tiles.
+struct Unit {
+  Sequence seq;
+  int head, row0;        // row0: its first row among the sequence's lq G
+  int parts;             // pieces that it is cut into; 1: whole
+  int tiles;             // key tiles of the whole unit
+};
+
+// Called by whole warps (any number of them, each for itself).
+__device__ __forceinline__ Split split_of(const PackedArgs &a) {
+  const int lane = threadIdx.x & 31;
+  Split s;
+  int mine = 0;
+  for (int b = lane; b < a.batch; b += 32) mine += query_blocks(a, sequence(a, b));
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+  s.units = mine * a.Hkv;
+  s.n_whole = s.units;
+  s.pieces = 1;
+  const int rem = s.units < a.sms ? s.units : a.mask ? 0 : s.units % a.sms;
+  if (!a.split || rem == 0) return s;
+  // The rem units in P pieces take ceil(rem P / sms) waves of 1/P unit, and each piece
+  // 0.005 unit more for its start, its partial rows and their join; at most two waves.
+  const int most = 2 * a.sms / rem;
+  float best = 1.005f;
+  int best_p = 1;
+  for (int p0 = 2; p0 <= most; p0 += 32) {
+    const int p = p0 + lane;
+    float cost = p <= most ? (float)((rem * p + a.sms - 1) / a.sms) / p + 0.005f * p : INFINITY;
+    int at = p;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const float c = __shfl_xor_sync(0xffffffffu, cost, o);
+      const int x = __shfl_xor_sync(0xffffffffu, at, o);
+      if (c < cost || (c == cost && x < at)) cost = c, at = x;
+    }
+    if (cost < best) best = cost, best_p = at;
+  }
+  if (best_p > 1) {
+    s.n_whole = s.units - rem;
+    s.pieces = best_p;
+  }
+  return s;
+}
+
+__device__ __forceinline__ Unit unit_of(const PackedArgs &a, const Split &s, int unit) {
+  const int lane = threadIdx.x & 31;
+  Unit u = {};
+  long long before = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += 32) {
+    Sequence seq = {};
+    int blocks = 0;
+    if (b0 + lane < a.batch) {
+      seq = sequence(a, b0 + lane);
+      blocks = query_blocks(a, seq);
+    }
+    const long long n = (long long)blocks * a.Hkv;
+    long long end = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long x = __shfl_up_sync(0xffffffffu, end, o);
+      if (lane >= o) end += x;
+    }
+    end += before;
+    const unsigned here = __ballot_sync(0xffffffffu, unit >= end - n && unit < end);
+    if (here) {
+      const int src = __ffs(here) - 1;
+      u.seq.q0 = __shfl_sync(0xffffffffu, seq.q0, src);
+      u.seq.lq = __shfl_sync(0xffffffffu, seq.lq, src);
+      u.seq.k0 = __shfl_sync(0xffffffffu, seq.k0, src);
+      u.seq.lk = __shfl_sync(0xffffffffu, seq.lk, src);
+      blocks = __shfl_sync(0xffffffffu, blocks, src);
+      const int at = (int)(unit - __shfl_sync(0xffffffffu, end - n, src));
+      u.head = at / blocks;
+      u.row0 = (blocks - 1 - at % blocks) * kUnitRows;
+      break;
+    }
+    before = __shfl_sync(0xffffffffu, end, 31);
+  }
+  const long long rows = (long long)u.seq.lq * a.G;
+  const int last = (int)(min(rows, (long long)u.row0 + kUnitRows) - 1);
+  u.tiles = (key_limit(a, u.seq, last / a.G) + kBN - 1) / kBN;
+  // four key tiles a piece at least: shorter ones cost more than they save
+  u.parts = unit < s.n_whole ? 1 : max(1, min(s.pieces, u.tiles / 4));
+  return u;
+}
+
+// Address of output row R of a unit's sequence.
+template <int D>
+__device__ __forceinline__ __nv_bfloat16 *out_row(const PackedArgs &a, const Unit &u, int R) {
+  const int i = R / a.G;
+  return a.out + ((size_t)(u.seq.q0 + i) * a.Hq + (size_t)u.head * a.G + (R - i * a.G)) * D;
+}
+
+// Forms this warp's rows again whose O took in a masked value that is not finite: O = sum
+// over the row's own keys [k0, min(limit, k1)) of 2^(c s - m) v, m and the sum being right
+// already.  Rare and slow; out of line so that it costs the usual path no registers.
+template <int D>
+__device__ __noinline__ void form_again(const PackedArgs &a, const Unit &u, uint32_t tO,
+                                        const uint8_t *q_tile, int row, int limit, int k0, int k1,
+                                        float m, bool valid) {
+  const __nv_bfloat16 *K = a.k + (size_t)u.seq.k0 * a.k_row + (size_t)u.head * D;
+  const __nv_bfloat16 *V = a.v + (size_t)u.seq.k0 * a.v_row + (size_t)u.head * D;
+  bool bad = false;
+  if (valid)
+    for (int j = max(limit, k0); j < k1 && !bad; ++j)
+      for (int d = 0; d < D; d += 8) {
+        const uint4 w = __ldg(reinterpret_cast<const uint4 *>(V + (size_t)j * a.v_row + d));
+        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+        for (int i = 0; i < 4; ++i)
+          bad |= (x[i] & 0x7f80u) == 0x7f80u || (x[i] & 0x7f800000u) == 0x7f800000u;
+      }
+  const int end = bad ? min(limit, k1) : 0;
+  const int most = __reduce_max_sync(0xffffffffu, end);
+  if (!__any_sync(0xffffffffu, bad)) return;
+  for (int c = 0; c < D / 32; ++c) {
+    float acc[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) acc[i] = 0.f;
+    for (int j = k0; j < most; ++j) {
+      float s = 0.f;
+      for (int v = 0; v < D / 8; ++v) {
+        const uint4 qw = *reinterpret_cast<const uint4 *>(q_tile + (v >> 3) * (kBM * 128) + row * 128 +
+                                                          (((v & 7) ^ (row & 7)) << 4));
+        const uint4 kw = __ldg(reinterpret_cast<const uint4 *>(K + (size_t)j * a.k_row) + v);
+        const uint32_t x[4] = {qw.x, qw.y, qw.z, qw.w}, y[4] = {kw.x, kw.y, kw.z, kw.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s = fmaf(__uint_as_float(x[i] << 16), __uint_as_float(y[i] << 16), s);
+          s = fmaf(__uint_as_float(x[i] & 0xffff0000u), __uint_as_float(y[i] & 0xffff0000u), s);
+        }
+      }
+      const float p = fast_exp2(fmaf(s, a.scale_log2, -m));
+      if (j < end) {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const uint4 w = __ldg(reinterpret_cast<const uint4 *>(V + (size_t)j * a.v_row + 32 * c) + v);
+          const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            acc[8 * v + 2 * i] = fmaf(p, __uint_as_float(x[i] << 16), acc[8 * v + 2 * i]);
+            acc[8 * v + 2 * i + 1] = fmaf(p, __uint_as_float(x[i] & 0xffff0000u), acc[8 * v + 2 * i + 1]);
+          }
+        }
+      }
+    }
+    __syncwarp();
+    uint32_t o[32];
+    tmem_ld32(tO + 32 * c, o);
+    tmem_wait_ld();
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      if (bad) o[i] = __float_as_uint(acc[i]);
+    tmem_st32(tO + 32 * c, o);
+    tmem_wait_st();
+  }
+}
+
+// Whether any of a row's D sums in TMEM is not finite.
+template <int D>
+__device__ __forceinline__ bool row_not_finite(uint32_t tO) {
+  bool bad = false;
+#pragma unroll
+  for (int c = 0; c < D / 16; ++c) {
+    uint32_t o[16];
+    tmem_ld16(tO + 16 * c, o);
+    tmem_wait_ld();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) bad |= (o[i] & 0x7f800000u) == 0x7f800000u;
+  }
+  return bad;
+}
+
+// Stores a warp's 32 rows (r0 ..) of a unit or a piece by way of `stage`, 32 D floats of
+// the warp's own (see the active attention's store: neighbouring lanes store neighbouring
+// vectors).
+template <int D>
+__device__ __forceinline__ void store_rows(const PackedArgs &a, const Unit &u, int piece, int r0, int lane,
+                                           uint32_t tO, float m_run, float l_run, uint8_t *stage) {
+  uint4 *st = reinterpret_cast<uint4 *>(stage);
+  if (piece >= 0) {
+    constexpr int kV = D / 4;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) {
+      uint32_t o[32];
+      tmem_ld32(tO + 32 * c, o);
+      tmem_wait_ld();
+#pragma unroll
+      for (int v = 0; v < 8; ++v)
+        st[lane * kV + (8 * c + (v ^ (lane & 7)))] =
+            make_uint4(o[4 * v], o[4 * v + 1], o[4 * v + 2], o[4 * v + 3]);
+    }
+    __syncwarp();
+    uint4 *dst = reinterpret_cast<uint4 *>(a.ws_o) + ((size_t)piece * kUnitRows + r0) * kV;
+#pragma unroll 8
+    for (int i = 0; i < kV; ++i) {
+      const int e = 32 * i + lane, row = e / kV, v = e % kV;
+      dst[e] = st[row * kV + ((v & ~7) | ((v & 7) ^ (row & 7)))];
+    }
+    reinterpret_cast<float2 *>(a.ws_ml)[(size_t)piece * kUnitRows + r0 + lane] = make_float2(m_run, l_run);
+    return;
+  }
+  const float inv = l_run > 0.f ? 1.f / l_run : l_run == 0.f ? 0.f : l_run;   // no keys: zeros
+  constexpr int kV = D / 8;
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c) {
+    uint32_t o[32];
+    tmem_ld32(tO + 32 * c, o);
+    tmem_wait_ld();
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      uint32_t pk[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        pk[i] = pack_bf16(__uint_as_float(o[8 * v + 2 * i]) * inv,
+                          __uint_as_float(o[8 * v + 2 * i + 1]) * inv);
+      const int x = 4 * c + v;
+      st[lane * kV + ((x & ~7) | ((x & 7) ^ (lane & 7)))] = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+    }
+  }
+  __syncwarp();
+  const int rows = (int)min((long long)u.seq.lq * a.G - u.row0, (long long)kUnitRows);
+#pragma unroll
+  for (int i = 0; i < kV; ++i) {
+    const int e = 32 * i + lane, row = e / kV, v = e % kV;
+    const uint4 x = st[row * kV + ((v & ~7) | ((v & 7) ^ (row & 7)))];
+    if (r0 + row < rows)
+      *reinterpret_cast<uint4 *>(out_row<D>(a, u, u.row0 + r0 + row) + 8 * v) = x;
+  }
+}
+
+template <int D>
+__global__ void __launch_bounds__(kTcThreads, 1)
+packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                        const PackedArgs a) {
+  using C = TcCfg<D>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                            ~(uintptr_t)1023);
+  uint8_t *sQ = sm;
+  uint8_t *sKV = sm + kQT * C::kTileBytes;
+  __shared__ __align__(8) uint64_t bar_full[C::kStages], bar_empty[C::kStages];
+  __shared__ __align__(8) uint64_t bar_s[kQT * C::kSBars], bar_o;
+  __shared__ uint32_t tmem_base_sh;
+  __shared__ volatile int abort_flag;
+  const TcPipe pipe = {bar_full, bar_empty, bar_s, &bar_o, &abort_flag, a.err};
+
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);
+  const int lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < C::kStages; ++s) {
+      mbar_init(&bar_full[s], 1);
+      mbar_init(&bar_empty[s], 1);
+    }
+    for (int t = 0; t < kQT * C::kSBars; ++t) mbar_init(&bar_s[t], 1);
+    mbar_init(&bar_o, 1);
+    abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  pdl_wait();
+
+  // ---- this block's unit and key tiles; every warp works them out for itself
+  const Split sp = split_of(a);
+  int id = blockIdx.x, part = 0, piece = -1;
+  if (id >= sp.n_whole) {
+    piece = id - sp.n_whole;
+    id = sp.n_whole + piece / sp.pieces;
+    part = piece % sp.pieces;
+  }
+  if (id >= sp.units) return;
+  const Unit u = unit_of(a, sp, id);
+  if (part >= u.parts) return;
+  if (u.parts == 1) piece = -1;
+  const int j0 = (int)((long long)u.tiles * part / u.parts);
+  const int nT = (int)((long long)u.tiles * (part + 1) / u.parts) - j0;
+  const int rows = (int)min((long long)u.seq.lq * a.G - u.row0, (long long)kUnitRows);
+  if (nT == 0) {   // no row has keys
+    for (int i = threadIdx.x; i < rows * (D / 8); i += kTcThreads)
+      *reinterpret_cast<uint4 *>(out_row<D>(a, u, u.row0 + i / (D / 8)) + 8 * (i % (D / 8))) =
+          make_uint4(0u, 0u, 0u, 0u);
+    return;
+  }
+
+  auto load_kv = [&](int L) {
+    const int slot = L % C::kStages;
+    mbar_expect_tx(&bar_full[slot], C::kTileBytes);
+    uint8_t *dst = sKV + slot * C::kTileBytes;
+    const int y = u.seq.k0 + (j0 + (L >> 1)) * kBN;
+#pragma unroll
+    for (int c = 0; c < C::kChunks; ++c)
+      tma_load_2d(dst + c * (kBN * 128), (L & 1) ? &tm_v : &tm_k, &bar_full[slot], u.head * D + c * 64, y);
+  };
+  const int withheld = a.inject_stall == 1 ? 1 : -1;
+  const int n_pre = min(3, 2 * nT);
+  // TMEM after the wait and before the trigger, as in the active attention; the blocks of
+  // the last wave let the next kernel start.
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
+                     smem_addr(&tmem_base_sh)),
+                 "r"(kTmemCols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    if (blockIdx.x + (unsigned)a.sms >= gridDim.x) pdl_trigger();
+  }
+  if (threadIdx.x == 0)
+    for (int L = 0; L < n_pre; ++L)
+      if (L != withheld) load_kv(L);
+
+  // ---- query rows into the two swizzled Q tiles
+  {
+    constexpr int kVecPerRow = D / 8;
+    constexpr int kVecs = kUnitRows * kVecPerRow;
+    constexpr int kPer = (kVecs + kTcThreads - 1) / kTcThreads;
+    uint4 v[kPer];
+#pragma unroll
+    for (int x = 0; x < kPer; ++x) {
+      const int i = threadIdx.x + x * kTcThreads, r = i / kVecPerRow;
+      v[x] = make_uint4(0u, 0u, 0u, 0u);
+      if (r < rows) {
+        const int R = u.row0 + r, tok = R / a.G;
+        const uint4 *p = reinterpret_cast<const uint4 *>(
+                             a.q + (size_t)(u.seq.q0 + tok) * a.q_row +
+                             ((size_t)u.head * a.G + (R - tok * a.G)) * D) + i % kVecPerRow;
+        asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                     : "=r"(v[x].x), "=r"(v[x].y), "=r"(v[x].z), "=r"(v[x].w)
+                     : "l"(p));
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < kPer; ++x) {
+      const int i = threadIdx.x + x * kTcThreads;
+      if (i < kVecs) {
+        const int row = i / kVecPerRow, c = i % kVecPerRow;
+        const int t = row / kBM, rr = row % kBM;
+        *reinterpret_cast<uint4 *>(sQ + t * C::kTileBytes + (c >> 3) * (kBM * 128) + rr * 128 +
+                                   (((c & 7) ^ (rr & 7)) << 4)) = v[x];
+      }
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_base_sh, 0);
+
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsLow));
+    if (warp == 0) {
+      tc_produce<D>(pipe, lane, nT, n_pre, withheld, load_kv);
+    } else if (warp == 1) {
+      tc_issue<D>(pipe, tmem, smem_addr(sQ), smem_addr(sKV), nT);
+    } else if (warp == 2) {
+      // V rows behind the sequence's last key (another sequence's, or what lies behind
+      // the last) become zeros before the issuer hears of the tile.
+      tc_watch_kv<D>(pipe, lane, nT, [&](int j) {
+        const int have = u.seq.lk - (j0 + j) * kBN;
+        if (have >= kBN) return;
+        uint8_t *tile = sKV + ((2 * j + 1) % C::kStages) * C::kTileBytes;
+        for (int i = have * 8 + lane; i < kBN * 8; i += 32)
+#pragma unroll
+          for (int c = 0; c < C::kChunks; ++c)
+            *reinterpret_cast<uint4 *>(tile + c * (kBN * 128) + 16 * i) = make_uint4(0u, 0u, 0u, 0u);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+      });
+    } else {
+      tc_watch_s<D>(pipe, nT);
+    }
+    fence_before();
+    named_barrier_sync(kBarTeardown, kTcThreads);
+    if (warp == 1) {
+      fence_after();
+      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem),
+                   "r"(kTmemCols)
+                   : "memory");
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsHigh));
+    const int t = (warp - 4) >> 2;
+    const int wq = warp & 3;
+    const uint32_t lane_off = (uint32_t)(wq * 32) << 16;
+    const uint32_t tO = tmem + lane_off + C::kOCol0 + D * t;
+    const float sl2 = a.scale_log2;
+    float m_run = kLowest, l_run = 0.f;
+    // Keys that this thread's row sees; rows past the sequence's last take no mask.  The
+    // warp's first row sees fewest.
+    const int r = t * kBM + wq * 32 + lane;
+    const int limit = r < rows ? key_limit(a, u.seq, (u.row0 + r) / a.G) : u.seq.lk;
+    const int all_see = __shfl_sync(0xffffffffu, limit, 0);
+    for (int j = 0; j < nT; ++j) {
+      named_barrier_sync(kBarS0 + t, kMeetS);
+      fence_after();
+      const int valid = limit - (j0 + j) * kBN;
+      const uint32_t tSj = tmem + lane_off + 128 * (C::kThreeS ? (2 * j + t) % 3 : t);
+      auto o_idle = [&]() -> bool {   // as in the active attention
+        if constexpr (!C::kThreeS) return true;
+        uint64_t *b = t == 0 ? &bar_s[2 + (j & 1)] : &bar_s[(j + 1) & 1];
+        const uint32_t par = t == 0 ? (j >> 1) & 1 : ((j + 1) >> 1) & 1;
+        const bool idle = __all_sync(0xffffffffu, mbar_wait(b, par, &abort_flag, a.err));
+        fence_after();
+        return idle;
+      };
+      if (all_see - (j0 + j) * kBN >= kBN)
+        softmax_tile<D, false>(tSj, tO, kBN, j == 0, sl2, m_run, l_run, o_idle);
+      else
+        softmax_tile<D, true>(tSj, tO, valid, j == 0, sl2, m_run, l_run, o_idle);
+      tmem_wait_st();
+      fence_before();
+      named_barrier_sync(kBarP0 + t, kMeetP);
+    }
+    bool ok = __all_sync(0xffffffffu, mbar_wait(&bar_o, 0, &abort_flag, a.err));
+    ok = !__any_sync(0xffffffffu, abort_flag != 0) && ok;
+    if (ok) {
+      fence_after();
+      if (a.mask && __any_sync(0xffffffffu, row_not_finite<D>(tO)))
+        form_again<D>(a, u, tO, sQ + t * C::kTileBytes, wq * 32 + lane, limit, j0 * kBN,
+                      min(u.seq.lk, (j0 + nT) * kBN), m_run, r < rows);
+      store_rows<D>(a, u, piece, t * kBM + wq * 32, lane, tO, m_run, l_run,
+                    sKV + (warp - 4) * (32 * D * 4));
+    }
+    fence_before();
+    named_barrier_sync(kBarTeardown, kTcThreads);
+  }
+}
+
+// Joins the pieces of the units that were cut.  D/4 lanes per row, four dimensions each;
+// the blocks take the cut units' rows in turn.
+constexpr int kJoinThreads = 256;
+
+template <int D>
+__global__ void __launch_bounds__(kJoinThreads)
+packed_join_kernel(const PackedArgs a) {
+  pdl_wait();
+  pdl_trigger();
+  constexpr int kL = D / 4, kPer = kJoinThreads / kL;   // rows per block and turn
+  const Split sp = split_of(a);
+  const int n = (sp.units - sp.n_whole) * (kUnitRows / kPer);
+  const int sub = threadIdx.x % kL;
+  for (int i = blockIdx.x; i < n; i += gridDim.x) {
+    const int tail = i / (kUnitRows / kPer);
+    const int r = i % (kUnitRows / kPer) * kPer + threadIdx.x / kL;
+    const Unit u = unit_of(a, sp, sp.n_whole + tail);
+    if (u.parts == 1) continue;
+    const size_t at = (size_t)tail * sp.pieces * kUnitRows + r;
+    const float2 *ml = reinterpret_cast<const float2 *>(a.ws_ml) + at;
+    const float4 *o = reinterpret_cast<const float4 *>(a.ws_o) + at * kL + sub;
+    float M = kLowest;
+    for (int p = 0; p < u.parts; ++p) M = fmaxf(M, ml[(size_t)p * kUnitRows].x);
+    float L = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int p = 0; p < u.parts; ++p) {
+      const float2 v = ml[(size_t)p * kUnitRows];
+      const float4 x = o[(size_t)p * kUnitRows * kL];
+      const float w = fast_exp2(v.x - M);
+      L = fmaf(w, v.y, L);
+      acc.x = fmaf(w, x.x, acc.x);
+      acc.y = fmaf(w, x.y, acc.y);
+      acc.z = fmaf(w, x.z, acc.z);
+      acc.w = fmaf(w, x.w, acc.w);
+    }
+    if ((long long)u.row0 + r < (long long)u.seq.lq * a.G) {
+      const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;
+      reinterpret_cast<uint2 *>(out_row<D>(a, u, u.row0 + r))[sub] =
+          make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+    }
+  }
+}
+
+// -------------------------------------------------------------- host side
+
+template <int D>
+int launch(PackedArgs &a, const void *any, cudaStream_t stream) {
+  using C = TcCfg<D>;
+  auto kernel = packed_attention_kernel<D>;
+  static std::atomic<int> configured[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return HSA_ERR_CUDA;
+  if (!configured[dev].load()) {
+    // the register hand-over assumes exactly kLaunchRegs registers at launch
+    cudaFuncAttributes fa;
+    if (cudaFuncGetAttributes(&fa, kernel) != cudaSuccess) return HSA_ERR_CUDA;
+    if (fa.numRegs != kLaunchRegs || fa.maxThreadsPerBlock < kTcThreads) return HSA_ERR_UNSUPPORTED;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) !=
+        cudaSuccess)
+      return HSA_ERR_CUDA;
+    configured[dev].store(1);
+  }
+  CUtensorMap mk, mv;
+  // without keys no tile is loaded: any valid map serves
+  const int keys = std::max(a.total_k, 1);
+  if (!make_kv_map(&mk, a.total_k ? a.k : any, keys, a.Hkv * D, a.total_k ? a.k_row : (long long)a.Hkv * D) ||
+      !make_kv_map(&mv, a.total_k ? a.v : any, keys, a.Hkv * D, a.total_k ? a.v_row : (long long)a.Hkv * D))
+    return HSA_ERR_CUDA;
+  // Every sequence has at most one partly filled block; pieces come on top.
+  const long long units = ((long long)a.total_q * a.G / kUnitRows + a.batch) * a.Hkv;
+  const long long grid = units + (a.split ? 2 * a.sms : 0);
+  if (grid > 0x7fffffffLL) return HSA_ERR_UNSUPPORTED;
+  count_launches(a.split ? 2 : 1);
+  launch_pdl(kernel, dim3((unsigned)grid), dim3(kTcThreads), C::kSmem, stream, mk, mv, a);
+  if (cudaGetLastError() != cudaSuccess) return HSA_ERR_CUDA;
+  if (a.split)
+    launch_pdl(packed_join_kernel<D>, dim3((unsigned)(8 * a.sms)), dim3(kJoinThreads), 0, stream, a);
+  return launch_status();
+}
+
+size_t workspace_bytes(int D) {
+  return 2 * (size_t)sm_count() * kUnitRows * ((size_t)D * 4 + 8) + 512;
+}
+
+}  // namespace
+}  // namespace hsa
+
+using namespace hsa;
+
+extern "C" size_t hsa_packed_attention_workspace_bytes(int Hq, int Hkv, int D) {
+  if (Hq <= 0 || Hkv <= 0 || Hq % Hkv || (D != 64 && D != 128)) return 0;
+  return workspace_bytes(D);
+}
+
+extern "C" int hsa_packed_attention(const void *q, long long q_row, const void *k, long long k_row,
+                                    const void *v, long long v_row, const int32_t *cu_q,
+                                    const int32_t *cu_k, int batch, int total_q, int total_k, int Hq,
+                                    int Hkv, int D, int mask, float scale, void *out, hsa_dtype dtype,
+                                    void *workspace, size_t workspace_size, hsa_stream_t stream) {
+  if (batch < 0 || total_q < 0 || total_k < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv || mask < 0)
+    return HSA_ERR_INVALID_ARG;
+  if (dtype != HSA_BF16 && dtype != HSA_F32) return HSA_ERR_INVALID_ARG;
+  if (dtype == HSA_F32 || (D != 64 && D != 128) || (long long)Hq * D > (1LL << 24))
+    return HSA_ERR_UNSUPPORTED;
+  if (total_k > 0x7fffff00 || (long long)total_q * (Hq / Hkv) > 0x7fffff00LL) return HSA_ERR_UNSUPPORTED;
+  if (q_row < (long long)Hq * D || k_row < (long long)Hkv * D || v_row < (long long)Hkv * D ||
+      (q_row & 7) || (k_row & 7) || (v_row & 7) || q_row > (1LL << 31) || k_row > (1LL << 31) ||
+      v_row > (1LL << 31))
+    return HSA_ERR_INVALID_ARG;
+  if (batch == 0 || total_q == 0) return HSA_OK;
+  if (!q || !out || !cu_q || !cu_k || !aligned16(q) || !aligned16(out)) return HSA_ERR_INVALID_ARG;
+  if (total_k > 0 && (!k || !v || !aligned16(k) || !aligned16(v))) return HSA_ERR_INVALID_ARG;
+  PackedArgs a;
+  a.sms = sm_count();
+  a.split = 0;
+  a.ws_o = a.ws_ml = nullptr;
+  if (workspace) {
+    if (workspace_size < workspace_bytes(D) || !aligned16(workspace)) return HSA_ERR_WORKSPACE;
+    a.split = 1;
+    a.ws_o = static_cast<float *>(workspace);
+    a.ws_ml = a.ws_o + 2 * (size_t)a.sms * kUnitRows * D;
+  }
+  if (!(scale > 0.f) || !std::isfinite(scale)) scale = 1.f / std::sqrt((float)D);
+  a.q = static_cast<const __nv_bfloat16 *>(q);
+  a.k = static_cast<const __nv_bfloat16 *>(k);
+  a.v = static_cast<const __nv_bfloat16 *>(v);
+  a.out = static_cast<__nv_bfloat16 *>(out);
+  a.cu_q = cu_q;
+  a.cu_k = cu_k;
+  a.err = device_error_word();
+  if (!a.err) return HSA_ERR_CUDA;
+  a.batch = batch;
+  a.total_q = total_q;
+  a.total_k = total_k;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.G = Hq / Hkv;
+  a.mask = mask;
+  a.q_row = q_row;
+  a.k_row = k_row;
+  a.v_row = v_row;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  a.inject_stall = attention_stall();
+  cudaStream_t s = (cudaStream_t)stream;
+  return D == 128 ? launch<128>(a, q, s) : launch<64>(a, q, s);
+}

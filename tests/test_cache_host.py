@@ -125,3 +125,39 @@ def test_binding_refuses_what_c_cannot_see(hsa, monkeypatch):
         hsa.hsa_paged_attention(q, pages, pages, t, n, q)
     with pytest.raises(TypeError):
         hsa.hsa_paged_attention(q.float(), pages, pages, t, n, q)
+
+
+def _packed(hsa, q=P, qr=512, k=P, kr=128, v=P, vr=128, cq=P, ck=P, B=2, tq=10, tk=10, Hq=8, Hkv=2, D=64, mask=1,
+            out=P, dt=0, ws=None, size=0):
+    return hsa.lib().hsa_packed_attention(q, qr, k, kr, v, vr, cq, ck, B, tq, tk, Hq, Hkv, D, mask, 0.0, out, dt,
+                                          ws, size, None)
+
+
+def test_packed_attention_refusals(hsa):
+    c0 = hsa.hsa_launch_count()
+    assert _packed(hsa, B=0, q=None) == 0 and _packed(hsa, tq=0, q=None, out=None) == 0
+    for bad in (dict(B=-1), dict(tq=-1), dict(tk=-1), dict(Hq=0), dict(Hkv=0), dict(Hq=7), dict(mask=-1),
+                dict(dt=2), dict(q=None), dict(k=None), dict(v=None), dict(out=None), dict(cq=None),
+                dict(ck=None), dict(q=ODD), dict(k=ODD), dict(v=ODD), dict(out=ODD), dict(qr=504),
+                dict(qr=516), dict(kr=120), dict(kr=132), dict(vr=64), dict(vr=1 << 32)):
+        assert _packed(hsa, **bad) == -1, bad
+    for bad in (dict(dt=1), dict(D=96, qr=768, kr=192, vr=192), dict(tk=2 ** 31 - 1), dict(tq=1 << 30),
+                dict(Hq=1 << 19, qr=1 << 25)):
+        assert _packed(hsa, **bad) == -4, bad
+    for bad in (dict(ws=ODD, size=1 << 30), dict(ws=P, size=1000)):
+        assert _packed(hsa, **bad) == -9, bad
+    assert hsa.hsa_launch_count() == c0
+    size = hsa.hsa_packed_attention_workspace_bytes
+    assert size(8, 2, 128) > size(8, 2, 64) > 0 and size(8, 3, 64) == 0 and size(8, 2, 96) == 0
+
+
+def test_packed_binding_refuses_what_c_cannot_see(hsa, monkeypatch):
+    monkeypatch.setattr(hsa, "lib", lambda: None)
+    q, k = torch.zeros((4, 2, 64), dtype=torch.bfloat16), torch.zeros((4, 1, 64), dtype=torch.bfloat16)
+    cu = torch.tensor([0, 4], dtype=torch.int32)
+    with pytest.raises(ValueError, match="CUDA"):
+        hsa.hsa_packed_attention(q, k, k, cu, cu, q)
+    with pytest.raises(TypeError):
+        hsa.hsa_packed_attention(q.float(), k, k, cu, cu, q)
+    with pytest.raises(ValueError, match="lie together"):
+        hsa.hsa_packed_attention(torch.zeros((4, 64, 2), dtype=torch.bfloat16).transpose(1, 2), k, k, cu, cu, q)
