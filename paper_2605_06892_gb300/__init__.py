@@ -174,31 +174,33 @@ def _dtype_code(t: torch.Tensor) -> int:
     raise TypeError(f"unsupported dtype {t.dtype}")
 
 
-def _want(name, t, dtype, *shape, optional=False):
-    """Refuses a tensor that is not a contiguous device tensor of the current device with
-    this dtype (or one of a tuple) and shape (None: any size); returns its address.  What
-    C cannot see of a tensor is checked here."""
-    if t is None:
-        if optional:
-            return None
-        raise TypeError(f"{name} is missing")
-    if t.dtype is not dtype and not (isinstance(dtype, tuple) and t.dtype in dtype):
+def _want(name, t, dtype, shape, device):
+    """The address of a tensor that has this dtype and shape, lies on this device and is
+    contiguous; any other is refused.  What C cannot see of a tensor is checked here."""
+    if (t.dtype is dtype and t.shape == shape and t.get_device() == device
+            and t.is_contiguous()):
+        return t.data_ptr()
+    if t.dtype is not dtype:
         raise TypeError(f"{name} has dtype {t.dtype}, not {dtype}")
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+    if t.get_device() != device or device < 0:
         raise ValueError(f"{name} is on {t.device}, not on the current CUDA device")
-    if t.dim() != len(shape) or any(w is not None and n != w for n, w in zip(t.shape, shape)):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, not "
-                         f"{tuple('any' if w is None else w for w in shape)}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} is not contiguous")
-    return t.data_ptr()
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    raise ValueError(f"{name} is not contiguous")
 
 
-def _scratch(t):
+def _device() -> int:
+    """The current CUDA device; -1, which no tensor is on, where there is none."""
+    if _current_device and torch.cuda.is_initialized():
+        return _current_device()
+    return torch.cuda.current_device() if torch.cuda.is_available() else -2
+
+
+def _scratch(t, device):
     """Address and bytes of a workspace (None: none)."""
     if t is None:
         return None, 0
-    return _want("workspace", t.view(-1), t.dtype, None), t.numel() * t.element_size()
+    return _want("workspace", t, t.dtype, t.shape, device), t.numel() * t.element_size()
 
 
 # ---------------------------------------------------------- host helpers
@@ -384,54 +386,65 @@ def hsa_cached_euler_l1rel(x, v_cache, v_fresh, pos, dsigma: float, stat, weight
 
 # ------------------------------------------------ 8-bit cache, paged attention
 
-_CODES = (torch.float8_e4m3fn, torch.uint8)
-_FLOATS = (torch.bfloat16, torch.float32)
+def _codes_of(k_cache):
+    """dtype of an 8-bit cache's code tensors."""
+    dt = k_cache.dtype
+    if dt is not torch.float8_e4m3fn and dt is not torch.uint8:
+        raise TypeError(f"the cache's codes have dtype {dt}, not float8_e4m3fn or uint8")
+    return dt
 
 
 def hsa_kv_quant_scatter(k_cache, v_cache, k_scale, v_scale, k_fresh, v_fresh, idx, n_active: int,
                          table=None, table_idx=None, stream=None) -> None:
-    """Fresh rows [n, H, D] (bf16 or fp32) into rows idx of an 8-bit cache: codes [N, H, D]
-    (float8_e4m3fn or uint8) and scale bytes [N, H] (uint8); a cache in pages [P, page, H, D]
-    with scales [P, page, H] counts as P * page rows.  table: K is rotated first (bf16), by
-    the table's rows table_idx (idx where that is None)."""
-    H, D = k_cache.shape[-2:]
-    lead = k_cache.shape[:-2]
-    N = lead.numel()
-    dt = k_fresh.dtype
-    if idx.dim() != 1 or not 0 <= n_active <= min(idx.numel(), k_fresh.shape[0]):
+    """Fresh rows [>= n_active, H, D] (bf16 or fp32) into rows idx of an 8-bit cache: codes
+    [N, H, D] (float8_e4m3fn or uint8) and scale bytes [N, H] (uint8); a cache in pages [P,
+    page, H, D] with scales [P, page, H] counts as P * page rows.  table: K is rotated first
+    (bf16), by the table's rows table_idx (idx where that is None)."""
+    dev, code = _device(), _codes_of(k_cache)
+    size, fresh = k_cache.shape, k_fresh.shape
+    H, D = size[-2:]
+    if n_active < 0 or idx.numel() < n_active or fresh[0] < n_active:
         raise ValueError("idx or k_fresh holds fewer than n_active rows")
-    rows = k_fresh.shape[0]
-    ids = None
+    if fresh[1:] != size[-2:]:
+        raise ValueError(f"k_fresh has shape {tuple(fresh)}, not rows of {H} heads x {D}")
+    tp = ip = None
+    rows = 0
+    if table is not None:
+        rows = table.shape[0]
+        tp = _want("table", table, torch.float32, (rows, D // 2, 2), dev)
     if table_idx is not None:
-        ids = _want("table_idx", table_idx, torch.int32, None)
         if table_idx.numel() < n_active:
             raise ValueError("table_idx holds fewer than n_active rows")
+        ip = _want("table_idx", table_idx, torch.int32, table_idx.shape, dev)
     _check(lib().hsa_kv_quant_scatter(
-        _want("k_cache", k_cache, _CODES, *lead, H, D), _want("v_cache", v_cache, _CODES, *lead, H, D),
-        _want("k_scale", k_scale, torch.uint8, *lead, H),
-        _want("v_scale", v_scale, torch.uint8, *lead, H),
-        _want("k_fresh", k_fresh, _FLOATS, rows, H, D), _want("v_fresh", v_fresh, dt, rows, H, D),
-        _want("idx", idx, torch.int32, None), n_active, N, H, D, _dtype_code(k_fresh),
-        _want("table", table, torch.float32, None, D // 2, 2, optional=True), ids,
-        0 if table is None else table.shape[0], _stream(stream)), "hsa_kv_quant_scatter")
+        _want("k_cache", k_cache, code, size, dev), _want("v_cache", v_cache, code, size, dev),
+        _want("k_scale", k_scale, torch.uint8, size[:-1], dev),
+        _want("v_scale", v_scale, torch.uint8, size[:-1], dev),
+        _want("k_fresh", k_fresh, k_fresh.dtype, fresh, dev),
+        _want("v_fresh", v_fresh, k_fresh.dtype, fresh, dev),
+        _want("idx", idx, torch.int32, idx.shape, dev), n_active, k_scale.numel() // max(H, 1), H, D,
+        _dtype_code(k_fresh), tp, ip, rows, _stream(stream)), "hsa_kv_quant_scatter")
 
 
 def hsa_kv_dequant_gather(k_cache, v_cache, k_scale, v_scale, idx, n: int, k_out, v_out,
                           stream=None) -> None:
     """k_out[:n], v_out[:n] ([>= n, H, D], bf16 or fp32) <- rows idx[:n] of an 8-bit cache
     (idx None: rows 0 .. n-1); the cache as for hsa_kv_quant_scatter."""
-    H, D = k_cache.shape[-2:]
-    lead = k_cache.shape[:-2]
-    if not 0 <= n <= k_out.shape[0] or (idx is not None and n > idx.numel()):
+    dev, code = _device(), _codes_of(k_cache)
+    size, out = k_cache.shape, k_out.shape
+    H, D = size[-2:]
+    if n < 0 or out[0] < n or (idx is not None and idx.numel() < n):
         raise ValueError("idx or k_out holds fewer than n rows")
-    rows = k_out.shape[0]
+    if out[1:] != size[-2:]:
+        raise ValueError(f"k_out has shape {tuple(out)}, not rows of {H} heads x {D}")
     _check(lib().hsa_kv_dequant_gather(
-        _want("k_cache", k_cache, _CODES, *lead, H, D), _want("v_cache", v_cache, _CODES, *lead, H, D),
-        _want("k_scale", k_scale, torch.uint8, *lead, H),
-        _want("v_scale", v_scale, torch.uint8, *lead, H),
-        _want("idx", idx, torch.int32, None, optional=True), n, lead.numel(), H, D,
-        _want("k_out", k_out, _FLOATS, rows, H, D), _want("v_out", v_out, k_out.dtype, rows, H, D),
-        _dtype_code(k_out), _stream(stream)), "hsa_kv_dequant_gather")
+        _want("k_cache", k_cache, code, size, dev), _want("v_cache", v_cache, code, size, dev),
+        _want("k_scale", k_scale, torch.uint8, size[:-1], dev),
+        _want("v_scale", v_scale, torch.uint8, size[:-1], dev),
+        None if idx is None else _want("idx", idx, torch.int32, idx.shape, dev), n,
+        k_scale.numel() // max(H, 1), H, D, _want("k_out", k_out, k_out.dtype, out, dev),
+        _want("v_out", v_out, k_out.dtype, out, dev), _dtype_code(k_out), _stream(stream)),
+        "hsa_kv_dequant_gather")
 
 
 def hsa_paged_attention_workspace_bytes(batch: int, n_new: int, Hq: int, Hkv: int, D: int) -> int:
@@ -445,21 +458,29 @@ def hsa_paged_attention(q, k_pages, v_pages, page_table, seq_lens, out, k_scale=
     max_pages]; bf16 pages, or 8-bit ones (float8_e4m3fn or uint8) with their scale bytes
     [n_pages, page, Hkv].  workspace: uint8 device tensor of at least
     hsa_paged_attention_workspace_bytes(...) bytes."""
-    B, n_new, Hq, D = q.shape
-    n_pages, page, Hkv, _ = k_pages.shape
-    f8 = k_scale is not None
-    kind = _CODES if f8 else torch.bfloat16
-    where, size = _scratch(workspace)
+    dev = _device()
+    size, pool = q.shape, k_pages.shape
+    B, n_new, Hq, D = size
+    n_pages, page, Hkv = pool[:3]
+    if pool[3] != D or page_table.shape[0] != B:
+        raise ValueError("q, k_pages and page_table disagree on the batch or the head dimension")
+    cols = page_table.shape[1]
+    ks = vs = None
+    if k_scale is None and v_scale is None:
+        kind, code = torch.bfloat16, HSA_BF16
+    else:
+        if k_scale is None or v_scale is None:
+            raise TypeError("an 8-bit cache has both k_scale and v_scale")
+        kind, code = _codes_of(k_pages), HSA_E4M3
+        ks = _want("k_scale", k_scale, torch.uint8, pool[:3], dev)
+        vs = _want("v_scale", v_scale, torch.uint8, pool[:3], dev)
+    where, room = _scratch(workspace, dev)
     _check(lib().hsa_paged_attention(
-        _want("q", q, torch.bfloat16, B, n_new, Hq, D), B, n_new, Hq,
-        _want("k_pages", k_pages, kind, n_pages, page, Hkv, D),
-        _want("v_pages", v_pages, kind, n_pages, page, Hkv, D),
-        _want("k_scale", k_scale, torch.uint8, n_pages, page, Hkv, optional=True),
-        _want("v_scale", v_scale, torch.uint8, n_pages, page, Hkv, optional=not f8),
-        n_pages, page, Hkv, D, HSA_E4M3 if f8 else HSA_BF16,
-        _want("page_table", page_table, torch.int32, B, None), page_table.shape[1],
-        _want("seq_lens", seq_lens, torch.int32, B), float(scale),
-        _want("out", out, torch.bfloat16, B, n_new, Hq, D), where, size, _stream(stream)),
+        _want("q", q, torch.bfloat16, size, dev), B, n_new, Hq,
+        _want("k_pages", k_pages, kind, pool, dev), _want("v_pages", v_pages, kind, pool, dev), ks, vs,
+        n_pages, page, Hkv, D, code, _want("page_table", page_table, torch.int32, (B, cols), dev), cols,
+        _want("seq_lens", seq_lens, torch.int32, (B,), dev), float(scale),
+        _want("out", out, torch.bfloat16, size, dev), where, room, _stream(stream)),
         "hsa_paged_attention")
 
 
@@ -467,16 +488,17 @@ def hsa_packed_attention_workspace_bytes(Hq: int, Hkv: int, D: int) -> int:
     return lib().hsa_packed_attention_workspace_bytes(Hq, Hkv, D)
 
 
-def _token_rows(name, t, H, D):
-    """Address and row stride of bf16 token rows [tokens, H, D] on the current device whose
-    heads lie together; rows may lie apart, as in a fused projection's output."""
+def _token_rows(name, t, H, D, device):
+    """Address and row stride of bf16 token rows [tokens, H, D] on the device whose heads
+    lie together; the rows may lie apart, as in a fused projection's output."""
     tokens = t.shape[0]
-    near = t[:0] if tokens == 0 else t[0]
-    if tuple(t.shape) != (tokens, H, D) or (tokens and not near.is_contiguous()):
+    if t.is_contiguous() or tokens == 0:
+        return _want(name, t, torch.bfloat16, (tokens, H, D), device) if tokens else None, H * D
+    row, head, one = t.stride()
+    if one != 1 or head != D:
         raise ValueError(f"{name} is not rows of {H} heads x {D} that lie together")
-    _want(name, near if tokens else t, torch.bfloat16, *((H, D) if tokens else t.shape))
-    row = t.stride(0) if tokens > 1 else H * D
-    return (t.data_ptr() if tokens else None), row
+    _want(name, t[0], torch.bfloat16, (H, D), device)
+    return t.data_ptr(), row
 
 
 def hsa_packed_attention(q, k, v, cu_q, cu_k, out, mask: int = 0, scale: float = 0.0, workspace=None,
@@ -486,18 +508,21 @@ def hsa_packed_attention(q, k, v, cu_q, cu_k, out, mask: int = 0, scale: float =
     F: causal by frames of F tokens (1: causal).  The rows of q, k and v may be slices of a
     wider tensor.  workspace (optional): uint8 device tensor of
     hsa_packed_attention_workspace_bytes(Hq, Hkv, D) bytes."""
-    total_q, Hq, D = q.shape
-    total_k, Hkv, _ = k.shape
-    (qp, q_row), (kp, k_row) = _token_rows("q", q, Hq, D), _token_rows("k", k, Hkv, D)
-    if v.shape[0] != total_k:
-        raise ValueError("v holds another number of rows than k")
-    vp, v_row = _token_rows("v", v, Hkv, D)
-    where, size = _scratch(workspace)
+    dev = _device()
+    size = q.shape
+    total_q, Hq, D = size
+    total_k, Hkv = k.shape[:2]
+    (qp, q_row), (kp, k_row) = _token_rows("q", q, Hq, D, dev), _token_rows("k", k, Hkv, D, dev)
+    if v.shape != k.shape:
+        raise ValueError("v has another shape than k")
+    vp, v_row = _token_rows("v", v, Hkv, D, dev)
+    where, room = _scratch(workspace, dev)
+    ends = cu_q.shape
     batch = cu_q.numel() - 1
     _check(lib().hsa_packed_attention(
-        qp, q_row, kp, k_row, vp, v_row, _want("cu_q", cu_q, torch.int32, batch + 1),
-        _want("cu_k", cu_k, torch.int32, batch + 1), batch, total_q, total_k, Hq, Hkv, D, mask,
-        float(scale), _want("out", out, torch.bfloat16, total_q, Hq, D), HSA_BF16, where, size,
+        qp, q_row, kp, k_row, vp, v_row, _want("cu_q", cu_q, torch.int32, (batch + 1,), dev),
+        _want("cu_k", cu_k, torch.int32, ends, dev), batch, total_q, total_k, Hq, Hkv, D, mask,
+        float(scale), _want("out", out, torch.bfloat16, size, dev), HSA_BF16, where, room,
         _stream(stream)), "hsa_packed_attention")
 
 

@@ -97,6 +97,21 @@ int launch_attention_f32(const void *q, const int32_t *q_idx, int n_active, cons
 // The mode of the attention's test hook (hsa_test.h).
 int attention_stall();
 
+// n / d for n < 2^31 by one high multiplication: q = (umulhi(n, mul) + n) >> shift with
+// shift = ceil(log2 d), mul = floor(2^32 (2^shift - d) / d) + 1.
+struct Divider {
+  unsigned d, mul, shift;
+};
+inline Divider make_divider(unsigned d) {
+  Divider v{d, 0, 0};
+  while ((1ull << v.shift) < d) ++v.shift;
+  v.mul = (unsigned)((((1ull << v.shift) - d) << 32) / d + 1);
+  return v;
+}
+__device__ __forceinline__ unsigned quotient(unsigned n, const Divider &v) {
+  return (__umulhi(n, v.mul) + n) >> v.shift;
+}
+
 // Number of lanes that cooperate on one row of `vecs` 16-byte vectors:
 // a power of two, at most 32.
 inline int lanes_per_row(long long vecs) {

@@ -25,21 +25,6 @@ constexpr int kThreads = 256;
 constexpr int kMaxD = 256;             // 32 lanes of 8 elements
 constexpr unsigned kLeastScale = 27;   // e >= -100: every value is a normal fp32 and bf16
 
-// n / d for n < 2^31 by one high multiplication: q = (umulhi(n, mul) + n) >> shift with
-// shift = ceil(log2 d), mul = floor(2^32 (2^shift - d) / d) + 1.
-struct Divider {
-  unsigned d, mul, shift;
-};
-Divider make_divider(unsigned d) {
-  Divider v{d, 0, 0};
-  while ((1ull << v.shift) < d) ++v.shift;
-  v.mul = (unsigned)((((1ull << v.shift) - d) << 32) / d + 1);
-  return v;
-}
-__device__ __forceinline__ unsigned quotient(unsigned n, const Divider &v) {
-  return (__umulhi(n, v.mul) + n) >> v.shift;
-}
-
 __device__ __forceinline__ uint4 ld_stream(const void *p) {
   uint4 v;
   asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"

@@ -38,6 +38,8 @@
 namespace hsa {
 namespace {
 
+struct Cuts;
+
 constexpr int kUnitRows = kQT * kBM;
 constexpr float kLowest = -3.0e38f;   // running maximum of a row that has seen no key
 
@@ -46,12 +48,15 @@ struct PackedArgs {
   __nv_bfloat16 *out;
   const int32_t *cu_q, *cu_k;
   unsigned *err;
-  int batch, total_q, total_k, Hq, Hkv, G, mask;
+  int batch, total_q, total_k, Hq, Hkv, mask;
+  Divider group, frame;            // by G = Hq / Hkv and by the mask
   long long q_row, k_row, v_row;   // elements from a token to the next
   float scale_log2;
-  int sms, split;                  // split: the workspace is there
+  int sms, most;                   // most: pieces that a cut may make, 0: none
+  int bound;                       // units that the host allowed for
   int inject_stall;                // test hook (hsa_test.h)
   float *ws_o, *ws_ml;             // [piece][kUnitRows][D], [piece][kUnitRows][2]
+  Cuts *cuts;                      // what the join reads
 };
 
 struct Sequence {
@@ -74,7 +79,7 @@ __device__ __forceinline__ Sequence sequence(const PackedArgs &a, int b) {
 }
 
 __device__ __forceinline__ int query_blocks(const PackedArgs &a, const Sequence &s) {
-  return (int)(((long long)s.lq * a.G + kUnitRows - 1) / kUnitRows);
+  return (int)(((long long)s.lq * a.group.d + kUnitRows - 1) / kUnitRows);
 }
 
 // Keys that query i of a sequence sees.
@@ -82,113 +87,198 @@ __device__ __forceinline__ int key_limit(const PackedArgs &a, const Sequence &s,
   if (!a.mask) return s.lk;
   const int p = i + s.lk - s.lq;
   if (p < 0) return 0;
-  return (int)min((long long)s.lk, ((long long)(p / a.mask) + 1) * a.mask);
+  return (int)min((long long)s.lk, ((long long)quotient(p, a.frame) + 1) * a.mask);
 }
 
-// What all blocks of a launch share: units, how many of them whole, pieces of the others.
-struct Split {
-  int units, n_whole, pieces;
+// What all blocks of a launch share.  Units below n_whole are whole.  The others are cut:
+// all of them (n_whole = 0) into parts of `longest` key tiles of their sequence, or, with
+// longest = 0, the last units into `pieces` each.
+struct Plan {
+  int units, n_whole, pieces, longest;
 };
 
-// One unit and this block's part of its key tiles.
+// One unit, or one part of one.
 struct Unit {
   Sequence seq;
   int head, row0;        // row0: its first row among the sequence's lq G
-  int parts;             // pieces that it is cut into; 1: whole
   int tiles;             // key tiles of the whole unit
+  int part, parts;       // parts = 1: whole
+  int slot;              // of its first part in the workspace
+  int cut;               // its place among the cut units, or -1
 };
 
-// Called by whole warps (any number of them, each for itself).
-__device__ __forceinline__ Split split_of(const PackedArgs &a) {
-  const int lane = threadIdx.x & 31;
-  Split s;
-  int mine = 0;
-  for (int b = lane; b < a.batch; b += 32) mine += query_blocks(a, sequence(a, b));
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
-  s.units = mine * a.Hkv;
-  s.n_whole = s.units;
-  s.pieces = 1;
-  const int rem = s.units < a.sms ? s.units : a.mask ? 0 : s.units % a.sms;
-  if (!a.split || rem == 0) return s;
-  // The rem units in P pieces take ceil(rem P / sms) waves of 1/P unit, and each piece
-  // 0.005 unit more for its start, its partial rows and their join; at most two waves.
-  const int most = 2 * a.sms / rem;
-  float best = 1.005f;
-  int best_p = 1;
-  for (int p0 = 2; p0 <= most; p0 += 32) {
-    const int p = p0 + lane;
-    float cost = p <= most ? (float)((rem * p + a.sms - 1) / a.sms) / p + 0.005f * p : INFINITY;
-    int at = p;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const float c = __shfl_xor_sync(0xffffffffu, cost, o);
-      const int x = __shfl_xor_sync(0xffffffffu, at, o);
-      if (c < cost || (c == cost && x < at)) cost = c, at = x;
-    }
-    if (cost < best) best = cost, best_p = at;
-  }
-  if (best_p > 1) {
-    s.n_whole = s.units - rem;
-    s.pieces = best_p;
-  }
-  return s;
+constexpr int kLeastTiles = 4;   // per part: shorter ones cost more than they save
+
+__device__ __forceinline__ int parts_of(const Sequence &s, int longest) {
+  const int tiles = (s.lk + kBN - 1) / kBN;
+  return longest && tiles > longest ? (tiles + longest - 1) / longest : 1;
 }
 
-__device__ __forceinline__ Unit unit_of(const PackedArgs &a, const Split &s, int unit) {
+// The unit and part of block `id`; false: it has none.  Called by whole warps, each for
+// itself: lane l holds sequence l, and where there are more than 32 the later ones are
+// read again by each pass over them.
+__device__ __forceinline__ bool unit_of(const PackedArgs &a, int id, Plan &p, Unit &u) {
   const int lane = threadIdx.x & 31;
-  Unit u = {};
-  long long before = 0;
+  Sequence first = {};
+  if (lane < a.batch) first = sequence(a, lane);
+  const int first_blocks = query_blocks(a, first);
+  // f(sequence, its query blocks) for this lane's sequences
+  auto each = [&](auto &&f) {
+    f(first, first_blocks);
+    for (int b = lane + 32; b < a.batch; b += 32) {
+      const Sequence s = sequence(a, b);
+      f(s, query_blocks(a, s));
+    }
+  };
+  int mine = 0;
+  each([&](const Sequence &, int blocks) { mine += blocks; });
+  p.units = __reduce_add_sync(0xffffffffu, mine) * a.Hkv;
+  p.n_whole = p.units;
+  p.pieces = 1;
+  p.longest = 0;
+  const bool may = a.most && p.units > 0 && p.units <= a.bound;   // more: offsets that overlap
+  if (may && p.units < a.sms) {
+    // Fewer units than SMs: the shortest part length that makes no more parts than SMs, or
+    // than two waves of them; a part costs its tiles and about 5 tiles' time more.
+    int far = 0;
+    unsigned work = 0;   // < 2^24 tiles of fewer units than SMs
+    each([&](const Sequence &s, int blocks) {
+      const int tiles = (s.lk + kBN - 1) / kBN;
+      if (blocks) far = max(far, tiles);
+      work += (unsigned)blocks * tiles;
+    });
+    far = __reduce_max_sync(0xffffffffu, far);
+    work = __reduce_add_sync(0xffffffffu, work) * a.Hkv;
+    auto shortest = [&](int most) {
+      // n parts of L tiles: work / L <= n < work / L + units
+      int lo = max(kLeastTiles, (int)(work / most));
+      int hi = most > p.units ? min(far, (int)(work / (most - p.units)) + 1) : far;
+      hi = max(hi, lo);
+      while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        int n = 0;
+        each([&](const Sequence &s, int blocks) { n += blocks * parts_of(s, mid); });
+        if (__reduce_add_sync(0xffffffffu, n) * a.Hkv <= most) hi = mid;
+        else lo = mid + 1;
+      }
+      return lo;
+    };
+    int len = shortest(a.sms);
+    if (a.most > a.sms) {
+      const int two = shortest(2 * a.sms);
+      if (2 * (two + 5) < len + 5) len = two;
+    }
+    if (len < far) {
+      p.n_whole = 0;
+      p.longest = len;
+    }
+  } else if (may && a.most >= 2 * a.sms && !a.mask && p.units % a.sms) {
+    // More units than SMs: under a mask the last ones to start are short already.  Without,
+    // the rem units of the last wave in P pieces each take ceil(rem P / sms) waves of 1/P
+    // unit, and each piece 0.005 unit more; at most two waves.
+    const int rem = p.units % a.sms;
+    float best = 1.005f;
+    for (int p0 = 2; p0 <= 2 * a.sms / rem; p0 += 32) {
+      const int n = p0 + lane;
+      float cost =
+          n <= 2 * a.sms / rem ? (float)((rem * n + a.sms - 1) / a.sms) / n + 0.005f * n : INFINITY;
+      int at = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const float c = __shfl_xor_sync(0xffffffffu, cost, o);
+        const int x = __shfl_xor_sync(0xffffffffu, at, o);
+        if (c < cost || (c == cost && x < at)) cost = c, at = x;
+      }
+      if (cost < best) best = cost, p.pieces = at;
+    }
+    if (p.pieces > 1) p.n_whole = p.units - rem;
+  }
+  // ---- this block's place: `id` counts units, or with `longest` parts
+  u.part = u.slot = 0;
+  u.cut = -1;
+  int pieces = 1;
+  if (!p.longest && id >= p.n_whole) {
+    const int i = id - p.n_whole;
+    pieces = p.pieces;
+    u.cut = i / pieces;
+    u.part = i - u.cut * pieces;
+    u.slot = u.cut * pieces;
+    id = p.n_whole + u.cut;
+    if (id >= p.units) return false;
+  }
+  int before = 0, units = 0;
   for (int b0 = 0; b0 < a.batch; b0 += 32) {
-    Sequence seq = {};
-    int blocks = 0;
-    if (b0 + lane < a.batch) {
-      seq = sequence(a, b0 + lane);
+    Sequence seq = first;
+    int blocks = first_blocks;
+    if (b0) {
+      seq = {};
+      if (b0 + lane < a.batch) seq = sequence(a, b0 + lane);
       blocks = query_blocks(a, seq);
     }
-    const long long n = (long long)blocks * a.Hkv;
-    long long end = n;
+    const int parts = parts_of(seq, p.longest);
+    const int w = blocks * a.Hkv * parts;
+    int end = w;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const long long x = __shfl_up_sync(0xffffffffu, end, o);
+      const int x = __shfl_up_sync(0xffffffffu, end, o);
       if (lane >= o) end += x;
     }
     end += before;
-    const unsigned here = __ballot_sync(0xffffffffu, unit >= end - n && unit < end);
+    const unsigned here = __ballot_sync(0xffffffffu, id >= end - w && id < end);
     if (here) {
       const int src = __ffs(here) - 1;
       u.seq.q0 = __shfl_sync(0xffffffffu, seq.q0, src);
       u.seq.lq = __shfl_sync(0xffffffffu, seq.lq, src);
       u.seq.k0 = __shfl_sync(0xffffffffu, seq.k0, src);
       u.seq.lk = __shfl_sync(0xffffffffu, seq.lk, src);
+      int at = id - __shfl_sync(0xffffffffu, end - w, src);
+      if (p.longest) {
+        pieces = __shfl_sync(0xffffffffu, parts, src);
+        units += __reduce_add_sync(0xffffffffu, lane < src ? blocks * a.Hkv : 0);
+        const int x = at / pieces;
+        u.part = at - x * pieces;
+        u.slot = id - u.part;
+        u.cut = units + x;
+        at = x;
+      }
       blocks = __shfl_sync(0xffffffffu, blocks, src);
-      const int at = (int)(unit - __shfl_sync(0xffffffffu, end - n, src));
       u.head = at / blocks;
-      u.row0 = (blocks - 1 - at % blocks) * kUnitRows;
-      break;
+      u.row0 = (blocks - 1 - (at - u.head * blocks)) * kUnitRows;
+      const long long rows = (long long)u.seq.lq * a.group.d;
+      const int last = (int)(min(rows, (long long)u.row0 + kUnitRows) - 1);
+      u.tiles = (key_limit(a, u.seq, quotient(last, a.group)) + kBN - 1) / kBN;
+      u.parts = max(1, min(pieces, u.tiles / kLeastTiles));
+      return u.part < u.parts;
     }
     before = __shfl_sync(0xffffffffu, end, 31);
+    if (p.longest) units += __reduce_add_sync(0xffffffffu, blocks * a.Hkv);
   }
-  const long long rows = (long long)u.seq.lq * a.G;
-  const int last = (int)(min(rows, (long long)u.row0 + kUnitRows) - 1);
-  u.tiles = (key_limit(a, u.seq, last / a.G) + kBN - 1) / kBN;
-  // four key tiles a piece at least: shorter ones cost more than they save
-  u.parts = unit < s.n_whole ? 1 : max(1, min(s.pieces, u.tiles / 4));
-  return u;
+  return false;
 }
 
-// Address of output row R of a unit's sequence.
+// What the join has to know, written by the kernel before it: how many units were cut, and
+// of each its first part's slot and parts, its rows and where they go.
+struct CutUnit {
+  int parts, slot, rows, row0, q0, head, pad[2];
+};
+struct Cuts {
+  int n, pad[7];
+  CutUnit unit[1];   // one per SM at most
+};
+
+// Address of output row R of a K/V head and the sequence whose first row is q0.
 template <int D>
-__device__ __forceinline__ __nv_bfloat16 *out_row(const PackedArgs &a, const Unit &u, int R) {
-  const int i = R / a.G;
-  return a.out + ((size_t)(u.seq.q0 + i) * a.Hq + (size_t)u.head * a.G + (R - i * a.G)) * D;
+__device__ __forceinline__ __nv_bfloat16 *out_row(const PackedArgs &a, int q0, int head, int R) {
+  const int i = quotient(R, a.group);
+  return a.out + ((size_t)(q0 + i) * a.Hq + head * (int)a.group.d + (R - i * (int)a.group.d)) * D;
 }
 
 // Forms this warp's rows again whose O took in a masked value that is not finite: O = sum
 // over the row's own keys [k0, min(limit, k1)) of 2^(c s - m) v, m and the sum being right
-// already.  Rare and slow; out of line so that it costs the usual path no registers.
+// already.  Rare and slow; out of line so that it costs the usual path no registers.  False:
+// no row needed it.
 template <int D>
-__device__ __noinline__ void form_again(const PackedArgs &a, const Unit &u, uint32_t tO,
+__device__ __noinline__ bool form_again(const PackedArgs &a, const Unit &u, uint32_t tO,
                                         const uint8_t *q_tile, int row, int limit, int k0, int k1,
                                         float m, bool valid) {
   const __nv_bfloat16 *K = a.k + (size_t)u.seq.k0 * a.k_row + (size_t)u.head * D;
@@ -204,7 +294,7 @@ __device__ __noinline__ void form_again(const PackedArgs &a, const Unit &u, uint
       }
   const int end = bad ? min(limit, k1) : 0;
   const int most = __reduce_max_sync(0xffffffffu, end);
-  if (!__any_sync(0xffffffffu, bad)) return;
+  if (!__any_sync(0xffffffffu, bad)) return false;
   for (int c = 0; c < D / 32; ++c) {
     float acc[32];
 #pragma unroll
@@ -246,42 +336,36 @@ __device__ __noinline__ void form_again(const PackedArgs &a, const Unit &u, uint
     tmem_st32(tO + 32 * c, o);
     tmem_wait_st();
   }
-}
-
-// Whether any of a row's D sums in TMEM is not finite.
-template <int D>
-__device__ __forceinline__ bool row_not_finite(uint32_t tO) {
-  bool bad = false;
-#pragma unroll
-  for (int c = 0; c < D / 16; ++c) {
-    uint32_t o[16];
-    tmem_ld16(tO + 16 * c, o);
-    tmem_wait_ld();
-#pragma unroll
-    for (int i = 0; i < 16; ++i) bad |= (o[i] & 0x7f800000u) == 0x7f800000u;
-  }
-  return bad;
+  return true;
 }
 
 // Stores a warp's 32 rows (r0 ..) of a unit or a piece by way of `stage`, 32 D floats of
 // the warp's own (see the active attention's store: neighbouring lanes store neighbouring
-// vectors).
-template <int D>
+// vectors).  again() is called once if a row's sums are not all finite and may change them.
+template <int D, typename Again>
 __device__ __forceinline__ void store_rows(const PackedArgs &a, const Unit &u, int piece, int r0, int lane,
-                                           uint32_t tO, float m_run, float l_run, uint8_t *stage) {
+                                           uint32_t tO, float m_run, float l_run, uint8_t *stage,
+                                           Again &&again) {
   uint4 *st = reinterpret_cast<uint4 *>(stage);
   if (piece >= 0) {
     constexpr int kV = D / 4;
+    auto put = [&]() {
+      float worst[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int c = 0; c < D / 32; ++c) {
-      uint32_t o[32];
-      tmem_ld32(tO + 32 * c, o);
-      tmem_wait_ld();
+      for (int c = 0; c < D / 32; ++c) {
+        uint32_t o[32];
+        tmem_ld32(tO + 32 * c, o);
+        tmem_wait_ld();
 #pragma unroll
-      for (int v = 0; v < 8; ++v)
-        st[lane * kV + (8 * c + (v ^ (lane & 7)))] =
-            make_uint4(o[4 * v], o[4 * v + 1], o[4 * v + 2], o[4 * v + 3]);
-    }
+        for (int v = 0; v < 8; ++v)
+          st[lane * kV + (8 * c + (v ^ (lane & 7)))] =
+              make_uint4(o[4 * v], o[4 * v + 1], o[4 * v + 2], o[4 * v + 3]);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) worst[i & 3] = fmaf(__uint_as_float(o[i]), 0.f, worst[i & 3]);
+      }
+      return (worst[0] + worst[1]) + (worst[2] + worst[3]);   // NaN where a sum is not finite
+    };
+    if (__any_sync(0xffffffffu, put() != 0.f) && again()) put();
     __syncwarp();
     uint4 *dst = reinterpret_cast<uint4 *>(a.ws_o) + ((size_t)piece * kUnitRows + r0) * kV;
 #pragma unroll 8
@@ -294,30 +378,37 @@ __device__ __forceinline__ void store_rows(const PackedArgs &a, const Unit &u, i
   }
   const float inv = l_run > 0.f ? 1.f / l_run : l_run == 0.f ? 0.f : l_run;   // no keys: zeros
   constexpr int kV = D / 8;
+  auto put = [&]() {
+    float worst[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int c = 0; c < D / 32; ++c) {
-    uint32_t o[32];
-    tmem_ld32(tO + 32 * c, o);
-    tmem_wait_ld();
+    for (int c = 0; c < D / 32; ++c) {
+      uint32_t o[32];
+      tmem_ld32(tO + 32 * c, o);
+      tmem_wait_ld();
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      uint32_t pk[4];
+      for (int v = 0; v < 4; ++v) {
+        uint32_t pk[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        pk[i] = pack_bf16(__uint_as_float(o[8 * v + 2 * i]) * inv,
-                          __uint_as_float(o[8 * v + 2 * i + 1]) * inv);
-      const int x = 4 * c + v;
-      st[lane * kV + ((x & ~7) | ((x & 7) ^ (lane & 7)))] = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+        for (int i = 0; i < 4; ++i)
+          pk[i] = pack_bf16(__uint_as_float(o[8 * v + 2 * i]) * inv,
+                            __uint_as_float(o[8 * v + 2 * i + 1]) * inv);
+        const int x = 4 * c + v;
+        st[lane * kV + ((x & ~7) | ((x & 7) ^ (lane & 7)))] = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+      }
+#pragma unroll
+      for (int i = 0; i < 32; ++i) worst[i & 3] = fmaf(__uint_as_float(o[i]), 0.f, worst[i & 3]);
     }
-  }
+    return (worst[0] + worst[1]) + (worst[2] + worst[3]);
+  };
+  if (__any_sync(0xffffffffu, put() != 0.f) && again()) put();
   __syncwarp();
-  const int rows = (int)min((long long)u.seq.lq * a.G - u.row0, (long long)kUnitRows);
+  const int rows = (int)min((long long)u.seq.lq * a.group.d - u.row0, (long long)kUnitRows);
 #pragma unroll
   for (int i = 0; i < kV; ++i) {
     const int e = 32 * i + lane, row = e / kV, v = e % kV;
     const uint4 x = st[row * kV + ((v & ~7) | ((v & 7) ^ (row & 7)))];
     if (r0 + row < rows)
-      *reinterpret_cast<uint4 *>(out_row<D>(a, u, u.row0 + r0 + row) + 8 * v) = x;
+      *reinterpret_cast<uint4 *>(out_row<D>(a, u.seq.q0, u.head, u.row0 + r0 + row) + 8 * v) = x;
   }
 }
 
@@ -353,23 +444,20 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
   pdl_wait();
 
   // ---- this block's unit and key tiles; every warp works them out for itself
-  const Split sp = split_of(a);
-  int id = blockIdx.x, part = 0, piece = -1;
-  if (id >= sp.n_whole) {
-    piece = id - sp.n_whole;
-    id = sp.n_whole + piece / sp.pieces;
-    part = piece % sp.pieces;
-  }
-  if (id >= sp.units) return;
-  const Unit u = unit_of(a, sp, id);
-  if (part >= u.parts) return;
-  if (u.parts == 1) piece = -1;
-  const int j0 = (int)((long long)u.tiles * part / u.parts);
-  const int nT = (int)((long long)u.tiles * (part + 1) / u.parts) - j0;
-  const int rows = (int)min((long long)u.seq.lq * a.G - u.row0, (long long)kUnitRows);
+  Plan plan;
+  Unit u;
+  const bool busy = unit_of(a, blockIdx.x, plan, u);
+  if (a.most && blockIdx.x == 0 && threadIdx.x == 0) a.cuts->n = plan.units - plan.n_whole;
+  if (!busy) return;
+  const int piece = u.parts > 1 ? u.slot + u.part : -1;
+  const int j0 = (int)((long long)u.tiles * u.part / u.parts);
+  const int nT = (int)((long long)u.tiles * (u.part + 1) / u.parts) - j0;
+  const int rows = (int)min((long long)u.seq.lq * a.group.d - u.row0, (long long)kUnitRows);
+  if (u.cut >= 0 && u.part == 0 && threadIdx.x == 0)
+    a.cuts->unit[u.cut] = {u.parts, u.slot, rows, u.row0, u.seq.q0, u.head, {0, 0}};
   if (nT == 0) {   // no row has keys
     for (int i = threadIdx.x; i < rows * (D / 8); i += kTcThreads)
-      *reinterpret_cast<uint4 *>(out_row<D>(a, u, u.row0 + i / (D / 8)) + 8 * (i % (D / 8))) =
+      *reinterpret_cast<uint4 *>(out_row<D>(a, u.seq.q0, u.head, u.row0 + i / (D / 8)) + 8 * (i % (D / 8))) =
           make_uint4(0u, 0u, 0u, 0u);
     return;
   }
@@ -404,20 +492,24 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
     constexpr int kVecPerRow = D / 8;
     constexpr int kVecs = kUnitRows * kVecPerRow;
     constexpr int kPer = (kVecs + kTcThreads - 1) / kTcThreads;
+    const int G = a.group.d;
+    // the addresses first, then all loads together
+    const uint4 *src[kPer];
+#pragma unroll
+    for (int x = 0; x < kPer; ++x) {
+      const int i = threadIdx.x + x * kTcThreads, R = u.row0 + i / kVecPerRow;
+      const int tok = quotient(R, a.group);
+      src[x] = reinterpret_cast<const uint4 *>(a.q + (size_t)(u.seq.q0 + tok) * a.q_row +
+                                               (u.head * G + (R - tok * G)) * D) + i % kVecPerRow;
+    }
     uint4 v[kPer];
 #pragma unroll
     for (int x = 0; x < kPer; ++x) {
-      const int i = threadIdx.x + x * kTcThreads, r = i / kVecPerRow;
       v[x] = make_uint4(0u, 0u, 0u, 0u);
-      if (r < rows) {
-        const int R = u.row0 + r, tok = R / a.G;
-        const uint4 *p = reinterpret_cast<const uint4 *>(
-                             a.q + (size_t)(u.seq.q0 + tok) * a.q_row +
-                             ((size_t)u.head * a.G + (R - tok * a.G)) * D) + i % kVecPerRow;
+      if ((threadIdx.x + x * kTcThreads) / kVecPerRow < rows)
         asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
                      : "=r"(v[x].x), "=r"(v[x].y), "=r"(v[x].z), "=r"(v[x].w)
-                     : "l"(p));
-      }
+                     : "l"(src[x]));
     }
 #pragma unroll
     for (int x = 0; x < kPer; ++x) {
@@ -478,7 +570,7 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
     // Keys that this thread's row sees; rows past the sequence's last take no mask.  The
     // warp's first row sees fewest.
     const int r = t * kBM + wq * 32 + lane;
-    const int limit = r < rows ? key_limit(a, u.seq, (u.row0 + r) / a.G) : u.seq.lk;
+    const int limit = r < rows ? key_limit(a, u.seq, quotient(u.row0 + r, a.group)) : u.seq.lk;
     const int all_see = __shfl_sync(0xffffffffu, limit, 0);
     for (int j = 0; j < nT; ++j) {
       named_barrier_sync(kBarS0 + t, kMeetS);
@@ -505,57 +597,107 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
     ok = !__any_sync(0xffffffffu, abort_flag != 0) && ok;
     if (ok) {
       fence_after();
-      if (a.mask && __any_sync(0xffffffffu, row_not_finite<D>(tO)))
-        form_again<D>(a, u, tO, sQ + t * C::kTileBytes, wq * 32 + lane, limit, j0 * kBN,
-                      min(u.seq.lk, (j0 + nT) * kBN), m_run, r < rows);
       store_rows<D>(a, u, piece, t * kBM + wq * 32, lane, tO, m_run, l_run,
-                    sKV + (warp - 4) * (32 * D * 4));
+                    sKV + (warp - 4) * (32 * D * 4), [&]() {
+                      return a.mask && form_again<D>(a, u, tO, sQ + t * C::kTileBytes, wq * 32 + lane,
+                                                     limit, j0 * kBN, min(u.seq.lk, (j0 + nT) * kBN),
+                                                     m_run, r < rows);
+                    });
     }
     fence_before();
     named_barrier_sync(kBarTeardown, kTcThreads);
   }
 }
 
-// Joins the pieces of the units that were cut.  D/4 lanes per row, four dimensions each;
-// the blocks take the cut units' rows in turn.
+// Joins the parts of the units that were cut.  A row takes D/4 lanes, four dimensions
+// each, and where there are many parts all lane groups of the block share a row: bound by
+// the round trips to L2, each group loads four parts at once.  The blocks divide the cut
+// units' rows into runs.
 constexpr int kJoinThreads = 256;
 
 template <int D>
 __global__ void __launch_bounds__(kJoinThreads)
 packed_join_kernel(const PackedArgs a) {
+  constexpr int kL = D / 4, kGroups = kJoinThreads / kL;
+  __shared__ float4 sh_o[kJoinThreads];
+  __shared__ float2 sh_ml[kGroups];
   pdl_wait();
   pdl_trigger();
-  constexpr int kL = D / 4, kPer = kJoinThreads / kL;   // rows per block and turn
-  const Split sp = split_of(a);
-  const int n = (sp.units - sp.n_whole) * (kUnitRows / kPer);
-  const int sub = threadIdx.x % kL;
-  for (int i = blockIdx.x; i < n; i += gridDim.x) {
-    const int tail = i / (kUnitRows / kPer);
-    const int r = i % (kUnitRows / kPer) * kPer + threadIdx.x / kL;
-    const Unit u = unit_of(a, sp, sp.n_whole + tail);
-    if (u.parts == 1) continue;
-    const size_t at = (size_t)tail * sp.pieces * kUnitRows + r;
-    const float2 *ml = reinterpret_cast<const float2 *>(a.ws_ml) + at;
-    const float4 *o = reinterpret_cast<const float4 *>(a.ws_o) + at * kL + sub;
-    float M = kLowest;
-    for (int p = 0; p < u.parts; ++p) M = fmaxf(M, ml[(size_t)p * kUnitRows].x);
-    float L = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int p = 0; p < u.parts; ++p) {
-      const float2 v = ml[(size_t)p * kUnitRows];
-      const float4 x = o[(size_t)p * kUnitRows * kL];
-      const float w = fast_exp2(v.x - M);
-      L = fmaf(w, v.y, L);
-      acc.x = fmaf(w, x.x, acc.x);
-      acc.y = fmaf(w, x.y, acc.y);
-      acc.z = fmaf(w, x.z, acc.z);
-      acc.w = fmaf(w, x.w, acc.w);
-    }
-    if ((long long)u.row0 + r < (long long)u.seq.lq * a.G) {
-      const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;
-      reinterpret_cast<uint2 *>(out_row<D>(a, u, u.row0 + r))[sub] =
-          make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+  const int n = a.cuts->n * kUnitRows;
+  const int i0 = (int)((long long)n * blockIdx.x / gridDim.x), i1 = (int)((long long)n * (blockIdx.x + 1) / gridDim.x);
+  const int sub = threadIdx.x % kL, group = threadIdx.x / kL;
+  for (int i = i0; i < i1;) {
+    const int tail = i / kUnitRows, end = min(i1, (tail + 1) * kUnitRows);
+    const CutUnit u = a.cuts->unit[tail];
+    int r = i - tail * kUnitRows;
+    const int r1 = u.parts > 1 ? min(end - tail * kUnitRows, u.rows) : 0;
+    i = end;
+    const bool wide = u.parts > 8;                 // the block's groups share a row
+    for (; r < r1; r += wide ? 1 : kGroups) {
+      const int row = wide ? r : r + group;
+      float M = kLowest, L = 0.f;
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (row < r1) {
+        const size_t at = (size_t)u.slot * kUnitRows + row;
+        const float2 *ml = reinterpret_cast<const float2 *>(a.ws_ml) + at;
+        const float4 *o = reinterpret_cast<const float4 *>(a.ws_o) + at * kL + sub;
+        const int step = wide ? kGroups : 1;
+        for (int p0 = wide ? group : 0; p0 < u.parts; p0 += 4 * step) {
+          float2 w[4];
+          float4 x[4];
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const int p = p0 + y * step;
+            w[y] = make_float2(kLowest, 0.f);
+            x[y] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (p < u.parts) {
+              w[y] = ml[(size_t)p * kUnitRows];
+              x[y] = o[(size_t)p * kUnitRows * kL];
+            }
+          }
+          const float to = fmaxf(fmaxf(fmaxf(w[0].x, w[1].x), fmaxf(w[2].x, w[3].x)), M);
+          const float f0 = fast_exp2(M - to);
+          M = to;
+          L *= f0, acc.x *= f0, acc.y *= f0, acc.z *= f0, acc.w *= f0;
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const float f = fast_exp2(w[y].x - M);
+            L = fmaf(f, w[y].y, L);
+            acc.x = fmaf(f, x[y].x, acc.x);
+            acc.y = fmaf(f, x[y].y, acc.y);
+            acc.z = fmaf(f, x[y].z, acc.z);
+            acc.w = fmaf(f, x[y].w, acc.w);
+          }
+        }
+      }
+      if (wide) {                                  // the same in the whole block
+        sh_o[threadIdx.x] = acc;
+        if (sub == 0) sh_ml[group] = make_float2(M, L);
+        __syncthreads();
+        if (group == 0) {
+#pragma unroll
+          for (int y = 0; y < kGroups; ++y) M = fmaxf(M, sh_ml[y].x);
+          L = 0.f;
+          acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+          for (int y = 0; y < kGroups; ++y) {
+            const float2 w = sh_ml[y];
+            const float4 x = sh_o[y * kL + sub];
+            const float f = fast_exp2(w.x - M);
+            L = fmaf(f, w.y, L);
+            acc.x = fmaf(f, x.x, acc.x);
+            acc.y = fmaf(f, x.y, acc.y);
+            acc.z = fmaf(f, x.z, acc.z);
+            acc.w = fmaf(f, x.w, acc.w);
+          }
+        }
+        __syncthreads();
+      }
+      if (row < r1 && (!wide || group == 0)) {
+        const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;
+        reinterpret_cast<uint2 *>(out_row<D>(a, u.q0, u.head, u.row0 + row))[sub] =
+            make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+      }
     }
   }
 }
@@ -585,20 +727,28 @@ int launch(PackedArgs &a, const void *any, cudaStream_t stream) {
   if (!make_kv_map(&mk, a.total_k ? a.k : any, keys, a.Hkv * D, a.total_k ? a.k_row : (long long)a.Hkv * D) ||
       !make_kv_map(&mv, a.total_k ? a.v : any, keys, a.Hkv * D, a.total_k ? a.v_row : (long long)a.Hkv * D))
     return HSA_ERR_CUDA;
-  // Every sequence has at most one partly filled block; pieces come on top.
-  const long long units = ((long long)a.total_q * a.G / kUnitRows + a.batch) * a.Hkv;
-  const long long grid = units + (a.split ? 2 * a.sms : 0);
+  // Units at most: every sequence has at most one partly filled block.  How many there are
+  // is on the device, so the grid holds what a cut may make of them: a block too many costs
+  // about a microsecond of an SM.  Fewer units than SMs become at most sms parts, or 2 sms
+  // where they are too many for a part each; without a mask pieces of the last wave's
+  // units come on top of the others.  Too few keys for two parts: no cut, no join.
+  const long long units = ((long long)a.total_q * a.group.d / kUnitRows + a.batch) * a.Hkv;
+  if (a.total_k < 2 * kLeastTiles * kBN - kBN + 1) a.most = 0;
+  if (a.most) a.most = 2 * units <= a.sms ? a.sms : 2 * a.sms;
+  const long long grid = a.mask || units < a.sms ? std::max<long long>(units, a.most) : units + a.most;
   if (grid > 0x7fffffffLL) return HSA_ERR_UNSUPPORTED;
-  count_launches(a.split ? 2 : 1);
+  a.bound = (int)units;
+  count_launches(a.most ? 2 : 1);
   launch_pdl(kernel, dim3((unsigned)grid), dim3(kTcThreads), C::kSmem, stream, mk, mv, a);
   if (cudaGetLastError() != cudaSuccess) return HSA_ERR_CUDA;
-  if (a.split)
+  if (a.most)
     launch_pdl(packed_join_kernel<D>, dim3((unsigned)(8 * a.sms)), dim3(kJoinThreads), 0, stream, a);
   return launch_status();
 }
 
 size_t workspace_bytes(int D) {
-  return 2 * (size_t)sm_count() * kUnitRows * ((size_t)D * 4 + 8) + 512;
+  return 2 * (size_t)sm_count() * kUnitRows * ((size_t)D * 4 + 8) +
+         ((size_t)sm_count() + 1) * sizeof(CutUnit);
 }
 
 }  // namespace
@@ -631,13 +781,15 @@ extern "C" int hsa_packed_attention(const void *q, long long q_row, const void *
   if (total_k > 0 && (!k || !v || !aligned16(k) || !aligned16(v))) return HSA_ERR_INVALID_ARG;
   PackedArgs a;
   a.sms = sm_count();
-  a.split = 0;
+  a.most = 0;
   a.ws_o = a.ws_ml = nullptr;
+  a.cuts = nullptr;
   if (workspace) {
     if (workspace_size < workspace_bytes(D) || !aligned16(workspace)) return HSA_ERR_WORKSPACE;
-    a.split = 1;
+    a.most = 1;
     a.ws_o = static_cast<float *>(workspace);
     a.ws_ml = a.ws_o + 2 * (size_t)a.sms * kUnitRows * D;
+    a.cuts = reinterpret_cast<Cuts *>(a.ws_ml + 2 * (size_t)a.sms * kUnitRows * 2);
   }
   if (!(scale > 0.f) || !std::isfinite(scale)) scale = 1.f / std::sqrt((float)D);
   a.q = static_cast<const __nv_bfloat16 *>(q);
@@ -653,7 +805,8 @@ extern "C" int hsa_packed_attention(const void *q, long long q_row, const void *
   a.total_k = total_k;
   a.Hq = Hq;
   a.Hkv = Hkv;
-  a.G = Hq / Hkv;
+  a.group = make_divider((unsigned)(Hq / Hkv));
+  a.frame = make_divider((unsigned)std::max(mask, 1));
   a.mask = mask;
   a.q_row = q_row;
   a.k_row = k_row;
