@@ -114,8 +114,7 @@ __device__ __forceinline__ int parts_of(const Sequence &s, int longest) {
   return longest && tiles > longest ? (tiles + longest - 1) / longest : 1;
 }
 
-// The unit and part of block `id`; false: it has none.  Called by whole warps, each for
-// itself: lane l holds sequence l, and where there are more than 32 the later ones are
+// The unit and part of block `id`; false: it has none.  Called by a whole warp: lane l holds sequence l, and where there are more than 32 the later ones are
 // read again by each pass over them.
 __device__ __forceinline__ bool unit_of(const PackedArgs &a, int id, Plan &p, Unit &u) {
   const int lane = threadIdx.x & 31;
@@ -402,13 +401,18 @@ __device__ __forceinline__ void store_rows(const PackedArgs &a, const Unit &u, i
   };
   if (__any_sync(0xffffffffu, put() != 0.f) && again()) put();
   __syncwarp();
-  const int rows = (int)min((long long)u.seq.lq * a.group.d - u.row0, (long long)kUnitRows);
+  // a lane works out the place of its own row, from the unit's first, in vectors
+  const int rows = (int)min((long long)u.seq.lq * a.group.d - u.row0, (long long)kUnitRows) - r0;
+  const int tok0 = quotient(u.row0, a.group), R = u.row0 + r0 + lane, tok = quotient(R, a.group);
+  const int place = ((tok - tok0) * a.Hq + R - tok * (int)a.group.d) * (D / 8);
+  uint4 *base = reinterpret_cast<uint4 *>(a.out) +
+                ((size_t)(u.seq.q0 + tok0) * a.Hq + u.head * (int)a.group.d) * (D / 8);
 #pragma unroll
   for (int i = 0; i < kV; ++i) {
     const int e = 32 * i + lane, row = e / kV, v = e % kV;
+    const int at = __shfl_sync(0xffffffffu, place, row);
     const uint4 x = st[row * kV + ((v & ~7) | ((v & 7) ^ (row & 7)))];
-    if (r0 + row < rows)
-      *reinterpret_cast<uint4 *>(out_row<D>(a, u.seq.q0, u.head, u.row0 + r0 + row) + 8 * v) = x;
+    if (row < rows) base[at + v] = x;
   }
 }
 
@@ -426,10 +430,15 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
   __shared__ __align__(8) uint64_t bar_s[kQT * C::kSBars], bar_o;
   __shared__ uint32_t tmem_base_sh;
   __shared__ volatile int abort_flag;
+  __shared__ Unit unit_sh;
   const TcPipe pipe = {bar_full, bar_empty, bar_s, &bar_o, &abort_flag, a.err};
 
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);
   const int lane = threadIdx.x & 31;
+  if (threadIdx.x == 32) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_k) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_v) : "memory");
+  }
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::kStages; ++s) {
       mbar_init(&bar_full[s], 1);
@@ -443,12 +452,21 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
   }
   pdl_wait();
 
-  // ---- this block's unit and key tiles; every warp works them out for itself
-  Plan plan;
-  Unit u;
-  const bool busy = unit_of(a, blockIdx.x, plan, u);
-  if (a.most && blockIdx.x == 0 && threadIdx.x == 0) a.cuts->n = plan.units - plan.n_whole;
-  if (!busy) return;
+  // ---- this block's unit and key tiles, worked out by one warp: twelve at once would take
+  // each other's issue slots
+  if (warp == 1) {
+    Plan plan;
+    Unit mine;
+    const bool busy = unit_of(a, blockIdx.x, plan, mine);
+    if (lane == 0) {
+      if (a.most && blockIdx.x == 0) a.cuts->n = plan.units - plan.n_whole;
+      if (!busy) mine.parts = 0;
+      unit_sh = mine;
+    }
+  }
+  __syncthreads();
+  const Unit u = unit_sh;
+  if (u.parts == 0) return;
   const int piece = u.parts > 1 ? u.slot + u.part : -1;
   const int j0 = (int)((long long)u.tiles * u.part / u.parts);
   const int nT = (int)((long long)u.tiles * (u.part + 1) / u.parts) - j0;
@@ -483,10 +501,6 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     if (blockIdx.x + (unsigned)a.sms >= gridDim.x) pdl_trigger();
   }
-  if (threadIdx.x == 0)
-    for (int L = 0; L < n_pre; ++L)
-      if (L != withheld) load_kv(L);
-
   // ---- query rows into the two swizzled Q tiles
   {
     constexpr int kVecPerRow = D / 8;
@@ -511,6 +525,10 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
                      : "=r"(v[x].x), "=r"(v[x].y), "=r"(v[x].z), "=r"(v[x].w)
                      : "l"(src[x]));
     }
+    // the first key tiles are requested while the rows are on their way
+    if (threadIdx.x == 0)
+      for (int L = 0; L < n_pre; ++L)
+        if (L != withheld) load_kv(L);
 #pragma unroll
     for (int x = 0; x < kPer; ++x) {
       const int i = threadIdx.x + x * kTcThreads;

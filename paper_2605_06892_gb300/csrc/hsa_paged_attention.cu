@@ -3,21 +3,23 @@
 // with k, v of the head that h's group shares.  A few FLOPs per byte of cache, so what
 // bounds it is reading the cache once.
 //
-// Work split.  A unit is (sequence, K/V head, 16 query rows); its rows are the group's
-// heads of all new tokens, row r = i G + g, so that one pass over the keys serves the
-// whole group.  The units' key tiles, laid end to end, are cut into equal runs, one per
-// CTA and as many CTAs as are resident: sequences of any mix of lengths keep every SM
-// busy to the end.  A run that holds a whole unit stores its rows; the others leave
-// (M, l, O) in the workspace and the join kernel merges them.
+// Work split.  A unit is (sequence, K/V head, up to 8 kNR query rows); its rows are the
+// group's heads of all new tokens, row r = i G + g, so that one pass over the keys serves
+// the whole group.  The units' key tiles, laid end to end, are cut into equal runs, one per
+// CTA and as many CTAs as are resident: sequences of any mix of lengths keep every SM busy
+// to the end.  A run that holds a whole unit stores its rows; the others leave (M, l, O) in
+// the workspace and the join kernel merges them.
 //
 // In a CTA each of four warps takes its own kKW keys of a tile, with its own running
 // maximum, its own ring of cp.async stages and no CTA barrier until the unit's end; the
-// ring runs on across units.  The products are m16n8k16 MMAs: 16 rows are all there is,
-// an eighth of the 128-row tile of the tcgen05 form, and the tensor pipe idles most of
-// the time at these rows (the attention over whole prompts uses tcgen05).  The fragments
-// come straight from 16-byte shared loads: the order of the head's dimensions inside a
-// product and of the keys inside a tile is free, so each lane multiplies what lies
-// together (column orders below), without transposing loads.
+// ring runs on across units.  The products are m16n8k16 MMAs with the keys (and the head's
+// dimensions) as the 16 rows and the query rows as the 8 columns: S^T = K Q^T and O^T = V^T
+// P^T.  Eight rows are what one token of a group has, a sixteenth of the 128-row tile of
+// the tcgen05 form, so nothing is computed for rows that are not there; more rows take kNR
+// column blocks that share the K and V fragments.  The fragments come straight from 16-byte
+// shared loads: the order of the head's dimensions inside a product and of the keys inside
+// a tile is free, so each lane multiplies what lies together (column orders below), without
+// transposing loads; P^T is transposed on its way by movmatrix.
 //
 // 8-bit cache.  A key's e4m3 codes are exact in fp16, and so is a bf16 query row after
 // scaling by a power of two (its values below 2^-39 of the largest aside), so the
@@ -41,7 +43,7 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
-constexpr int kRows = 16;             // query rows of a unit
+constexpr int kMostRows = 32;         // query rows of a unit at most
 constexpr int kMaxPerSm = 4;          // CTAs per SM that the workspace is sized for
 constexpr float kLowest = -3.0e38f;   // running maximum before the first key
 constexpr float kPShift = 14.f;       // fp16 probabilities are 2^(u - M + 14)
@@ -80,6 +82,13 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint3
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// An 8 x 8 block of 16-bit values, a pair per lane, transposed.
+__device__ __forceinline__ uint32_t transposed(uint32_t w) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(w));
+  return r;
+}
+
 // 16 bytes into shared memory, zeros where !ok.
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool ok) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0)
@@ -105,8 +114,9 @@ __device__ __forceinline__ uint32_t word(const uint4 &v, int i) {
   return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w;
 }
 
-template <int D, bool kF8>
+template <int D, bool kF8, int kNR>
 struct Cfg {
+  static constexpr int kRows = 8 * kNR;                        // query rows of a unit
   static constexpr int kRowBytes = D * (kF8 ? 1 : 2);
   static constexpr int kChunks = kRowBytes / 16;               // 16-byte chunks per row
   static constexpr int kKW = kRowBytes == 256 ? 16 : 32;       // keys per warp and tile
@@ -119,9 +129,9 @@ struct Cfg {
   static constexpr int kSmem = kWarps * kStages * kStage + kMergeO;
 };
 
-// The key (row of an 8-key block) of MMA column n.  A lane quad's 16-byte loads of K
-// (keys of columns 2x, 2x+1; four chunks) and of V (keys of columns 0, 2, 4, 6 or 1, 3,
-// 5, 7; two chunks) then fall into distinct banks under the swizzles below.
+// The key (row of an 8-key block) of MMA index n.  The 16-byte loads of K (a quarter-warp:
+// keys of n = 2x, 2x+1; four chunks) and of V (keys of n = 0, 2, 4, 6 or 1, 3, 5, 7; two
+// chunks) then fall into distinct banks under the swizzles below.
 template <int kChunks>
 __device__ __forceinline__ int key_of(int n) {
   return kChunks == 4 ? n ^ ((n >> 1) & 1) : (n >> 1) | ((n & 1) << 2);
@@ -135,7 +145,14 @@ __device__ __forceinline__ int v_chunk(int c, int row) {
   return kChunks == 4 ? c ^ (((row >> 2) & 1) << 1) : c ^ ((row & 3) << 1);
 }
 
+// What the join has to know of a unit that several blocks shared, from the block that
+// ended it: how many, the first, and that one's slot; parts = 0: that block ended none.
+struct CutUnit {
+  int parts, first, slot, b, unit, pad[3];
+};
+
 struct Args {
+  CutUnit *cuts;                   // [blocks]
   const __nv_bfloat16 *q;
   const uint8_t *k, *v;            // pages [n_pages][page][Hkv][D]
   const uint8_t *ks, *vs;          // [n_pages][page][Hkv]
@@ -143,7 +160,8 @@ struct Args {
   __nv_bfloat16 *out;
   float *ws;
   unsigned *err;
-  int batch, n_new, Hq, Hkv, G, rows, row_tiles;   // rows = n_new G
+  int batch, n_new, Hq, Hkv, rows, row_tiles;   // rows = n_new G
+  Divider group;                                // by G = Hq / Hkv
   int n_pages, page_log2, max_pages;
   float scale_log2;
 };
@@ -173,11 +191,10 @@ __device__ __forceinline__ int length(const Args &a, int b) {
 }
 
 // Sums the sequences' tiles over the block: `before` is what comes before this thread's
-// own run of sequences [b0, b1), `total` all of them.  kN threads; two barriers.
-template <int kN>
+// own run of sequences [b0, b1), `total` all of them.
 __device__ __forceinline__ void scan_tiles(const Args &a, int tile, int &b0, int &b1, long long &before,
                                            long long &mine, long long &total, long long *sh) {
-  const int per = (a.batch + kN - 1) / kN;
+  const int per = (a.batch + kThreads - 1) / kThreads;
   b0 = min(a.batch, (int)threadIdx.x * per);
   b1 = min(a.batch, b0 + per);
   mine = 0;
@@ -195,11 +212,10 @@ __device__ __forceinline__ void scan_tiles(const Args &a, int tile, int &b0, int
   before = x - mine;
   total = 0;
 #pragma unroll
-  for (int w = 0; w < kN / 32; ++w) {
+  for (int w = 0; w < kWarps; ++w) {
     if (w < warp) before += sh[w];
     total += sh[w];
   }
-  __syncthreads();
 }
 
 // A place in the row of key tiles.
@@ -218,11 +234,23 @@ __device__ __forceinline__ void step(const Args &a, Cursor &c, int tile) {
   } while (c.tiles == 0);
 }
 
-template <int D, bool kF8>
+// Zeros for the rows of sequences without keys; the blocks share the sequences out.
+template <int D>
+__device__ __forceinline__ void clear_empty(const Args &a) {
+  for (int b = blockIdx.x; b < a.batch; b += gridDim.x) {
+    if (length(a, b) != 0) continue;
+    const long long n = (long long)a.n_new * a.Hq * (D / 8);
+    uint4 *dst = reinterpret_cast<uint4 *>(a.out) + b * n;
+    for (long long i = threadIdx.x; i < n; i += kThreads) dst[i] = make_uint4(0u, 0u, 0u, 0u);
+  }
+}
+
+template <int D, bool kF8, int kNR>
 __global__ void __launch_bounds__(kThreads)
 paged_attention_kernel(const Args a) {
-  using C = Cfg<D, kF8>;
-  constexpr int kCh = C::kChunks, kNB = C::kKW / 16, kSteps = D / 16, kNT = D / 8;
+  using C = Cfg<D, kF8, kNR>;
+  constexpr int kCh = C::kChunks, kNB = C::kKW / 16, kSteps = D / 16, kNT = D / 8, kMT = D / 16;
+  constexpr int kRows = C::kRows;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ long long sh_sum[kWarps];
   __shared__ int sh_b;
@@ -239,9 +267,13 @@ paged_attention_kernel(const Args a) {
   {
     int b0, b1;
     long long before, mine;
-    scan_tiles<kThreads>(a, C::kTile, b0, b1, before, mine, plan.total, sh_sum);
+    scan_tiles(a, C::kTile, b0, b1, before, mine, plan.total, sh_sum);
     plan.ctas = (int)min((long long)gridDim.x, plan.total);
-    if ((int)blockIdx.x >= plan.ctas) return;
+    if ((int)blockIdx.x >= plan.ctas) {
+      if (threadIdx.x == 0) a.cuts[blockIdx.x].parts = 0;
+      clear_empty<D>(a);
+      return;
+    }
     const long long at = first_tile(plan, blockIdx.x);
     if (at >= before && at < before + mine) {
       const long long per_tile = (long long)a.Hkv * a.row_tiles;
@@ -263,7 +295,8 @@ paged_attention_kernel(const Args a) {
   cur.len = length(a, cur.b);
   cur.tiles = (cur.len + C::kTile - 1) / C::kTile;
   cur.unit = (int)(sh_off / cur.tiles);
-  cur.tile = (int)(sh_off % cur.tiles);
+  cur.tile = (int)(sh_off - (long long)cur.unit * cur.tiles);
+  CutUnit cut = {};
 
   // ---- the ring: `ahead` is the next tile to load; the page of this lane's key in it is
   // read one tile before its use
@@ -327,63 +360,62 @@ paged_attention_kernel(const Args a) {
     if (loaded >= 0) load_tile();
     else commit();
 
-  // ---- per unit state
-  uint32_t qf[kSteps][4];
-  float o[kNT][4], m[2], l[2], c2[2];
-  int limit[2];          // keys that rows g and g + 8 see
+  // ---- per unit state; column block x of the MMAs holds rows 8 x .. 8 x + 7, and this
+  // lane row 8 x + g of Q^T and P^T, rows 8 x + 2 t + j of S^T and O^T
+  uint32_t qf[kSteps][kNR][2];
+  float o[kMT][kNR][4], m[kNR][2], l[kNR][2], c2[kNR][2];
+  int limit[kNR][2];     // keys that rows 8 x + 2 t + j see
   int unit_tile0 = 0;    // the unit's tile that this run of it starts with
-  bool fresh = true;
-  bool first_unit = true;
+  bool fresh = true, first_unit = true;
 
   for (int it = 0; it < n_tiles; ++it) {
     if (fresh) {
       fresh = false;
       unit_tile0 = cur.tile;
-      const int h = cur.unit / a.row_tiles, r0 = (cur.unit % a.row_tiles) * kRows;
-      float big[2] = {0.f, 0.f};
+      const int h = cur.unit / a.row_tiles, r0 = (cur.unit - h * a.row_tiles) * kRows;
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s) {
-        // dimensions of K = 16 step s that this lane's K fragments hold
-        const int d = kF8 ? 16 * (t + 4 * (s / 4)) + 4 * (s % 4) : 8 * (t + 4 * (s / 2)) + 4 * (s % 2);
+      for (int x = 0; x < kNR; ++x) {
+        const int r = r0 + 8 * x + g, i = quotient(r, a.group);
+        const uint2 *src = reinterpret_cast<const uint2 *>(
+            a.q + ((size_t)((size_t)cur.b * a.n_new + i) * a.Hq + h * (int)a.group.d + (r - i * (int)a.group.d)) * D);
+        float big = 0.f;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int r = r0 + g + 8 * e;
+        for (int s = 0; s < kSteps; ++s) {
+          // dimensions of K = 16 step s that this lane's fragments hold
+          const int d = kF8 ? 16 * (t + 4 * (s / 4)) + 4 * (s % 4) : 8 * (t + 4 * (s / 2)) + 4 * (s % 2);
           uint2 w = make_uint2(0u, 0u);
-          if (r < a.rows) {
-            const int i = r / a.G, head = h * a.G + r % a.G;
-            w = __ldg(reinterpret_cast<const uint2 *>(
-                a.q + ((size_t)((size_t)cur.b * a.n_new + i) * a.Hq + head) * D + d));
-          }
-          qf[s][e] = w.x;
-          qf[s][2 + e] = w.y;
+          if (r < a.rows) w = __ldg(src + d / 4);
+          qf[s][x][0] = w.x;
+          qf[s][x][1] = w.y;
           if (kF8)
-            big[e] = fmaxf(fmaxf(big[e], fmaxf(fabsf(lo_bf16(w.x)), fabsf(hi_bf16(w.x)))),
-                           fmaxf(fabsf(lo_bf16(w.y)), fabsf(hi_bf16(w.y))));
+            big = fmaxf(fmaxf(big, fmaxf(fabsf(lo_bf16(w.x)), fabsf(hi_bf16(w.x)))),
+                        fmaxf(fabsf(lo_bf16(w.y)), fabsf(hi_bf16(w.y))));
         }
-      }
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int r = r0 + g + 8 * e;
-        limit[e] = r < a.rows ? cur.len - a.n_new + r / a.G + 1 : 0;
-        m[e] = kLowest;
-        l[e] = 0.f;
-        c2[e] = a.scale_log2;
+        float scale = a.scale_log2;
         if (kF8) {
           // the row times 2^(14 - E), its largest magnitude in [2^14, 2^15)
-          big[e] = fmaxf(big[e], __shfl_xor_sync(0xffffffffu, big[e], 1));
-          big[e] = fmaxf(big[e], __shfl_xor_sync(0xffffffffu, big[e], 2));
-          const unsigned E = max(__float_as_uint(big[e]) >> 23, 20u);   // biased
+          big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
+          big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
+          const unsigned E = max(__float_as_uint(big) >> 23, 20u);   // biased
           const float f = __uint_as_float((268u - E) << 23);
-          c2[e] *= __uint_as_float((E - 14u) << 23);
+          scale *= __uint_as_float((E - 14u) << 23);
 #pragma unroll
-          for (int s = 0; s < kSteps; ++s) {
-            qf[s][e] = pack_f16(lo_bf16(qf[s][e]) * f, hi_bf16(qf[s][e]) * f);
-            qf[s][2 + e] = pack_f16(lo_bf16(qf[s][2 + e]) * f, hi_bf16(qf[s][2 + e]) * f);
-          }
+          for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+              qf[s][x][y] = pack_f16(lo_bf16(qf[s][x][y]) * f, hi_bf16(qf[s][x][y]) * f);
         }
-      }
 #pragma unroll
-      for (int n = 0; n < kNT; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
+        for (int j = 0; j < 2; ++j) {
+          const int rc = r0 + 8 * x + 2 * t + j;
+          limit[x][j] = rc < a.rows ? cur.len - a.n_new + (int)quotient(rc, a.group) + 1 : 0;
+          c2[x][j] = kF8 ? __shfl_sync(0xffffffffu, scale, 4 * (2 * t + j)) : scale;
+          m[x][j] = kLowest;
+          l[x][j] = 0.f;
+        }
+#pragma unroll
+        for (int n = 0; n < kMT; ++n) o[n][x][0] = o[n][x][1] = o[n][x][2] = o[n][x][3] = 0.f;
+      }
     }
 
     wait_all_but<C::kStages - 2>();
@@ -397,122 +429,136 @@ paged_attention_kernel(const Args a) {
       const uint32_t sv = sk + C::kHalf;
       const float2 *scales = reinterpret_cast<const float2 *>(ring + (it % C::kStages) * C::kStage +
                                                               2 * C::kHalf);
-      // ---- scores: column n of block q is key 8 q + key_of(n)
-      float s[2 * kNB][4];
+      // ---- scores: MMA row n (n + 8) of block b is key 16 b + key_of(n) (+ 8)
+      float s[kNB][kNR][4];
 #pragma unroll
-      for (int q = 0; q < 2 * kNB; ++q) {
-        s[q][0] = s[q][1] = s[q][2] = s[q][3] = 0.f;
-        const int row = 8 * q + key_of<kCh>(g);
+      for (int b = 0; b < kNB; ++b) {
+#pragma unroll
+        for (int x = 0; x < kNR; ++x) s[b][x][0] = s[b][x][1] = s[b][x][2] = s[b][x][3] = 0.f;
+        const int row = 16 * b + key_of<kCh>(g);
 #pragma unroll
         for (int i = 0; i < kCh / 4; ++i) {
-          const uint4 w = lds128(sk + row * C::kRowBytes + 16 * k_chunk<kCh>(t + 4 * i, row));
-          if (kF8) {
+          const uint32_t at = 16 * k_chunk<kCh>(t + 4 * i, row);   // the same for row + 8
+          const uint4 w0 = lds128(sk + row * C::kRowBytes + at);
+          const uint4 w1 = lds128(sk + (row + 8) * C::kRowBytes + at);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              mma<true>(s[q], qf[(4 * i + e) % kSteps], f16x2_of_e4m3x2(word(w, e)),
-                        f16x2_of_e4m3x2(word(w, e) >> 16));
-          } else {
-            mma<false>(s[q], qf[(2 * i) % kSteps], w.x, w.y);
-            mma<false>(s[q], qf[(2 * i + 1) % kSteps], w.z, w.w);
+          for (int e = 0; e < (kF8 ? 4 : 2); ++e) {
+            const int step = (kF8 ? 4 : 2) * i + e;
+            uint32_t k[4];
+            if (kF8) {
+              k[0] = f16x2_of_e4m3x2(word(w0, e)), k[2] = f16x2_of_e4m3x2(word(w0, e) >> 16);
+              k[1] = f16x2_of_e4m3x2(word(w1, e)), k[3] = f16x2_of_e4m3x2(word(w1, e) >> 16);
+            } else {
+              k[0] = word(w0, 2 * e), k[2] = word(w0, 2 * e + 1);
+              k[1] = word(w1, 2 * e), k[3] = word(w1, 2 * e + 1);
+            }
+#pragma unroll
+            for (int x = 0; x < kNR; ++x) mma<kF8>(s[b][x], k, qf[step][x][0], qf[step][x][1]);
           }
         }
       }
       // ---- log2 units, the mask, the running maximum
-      float vinv[2 * kNB][2], mx[2] = {m[0], m[1]};
+      float vinv[kNB][2], mx[kNR][2];
       const bool ragged = key0 + C::kKW > cur.len - a.n_new + 1;
 #pragma unroll
-      for (int q = 0; q < 2 * kNB; ++q) {
+      for (int x = 0; x < kNR; ++x) mx[x][0] = m[x][0], mx[x][1] = m[x][1];
+#pragma unroll
+      for (int b = 0; b < kNB; ++b)
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
-          const int row = 8 * q + key_of<kCh>(2 * t + n);
+          const int row = 16 * b + 8 * n + key_of<kCh>(g);
           float kf = 1.f, ve = 0.f;
           if (kF8) {
             const float2 f = scales[row];
-            kf = f.x, ve = f.y, vinv[q][n] = fast_exp2(-ve);
+            kf = f.x, ve = f.y, vinv[b][n] = fast_exp2(-ve);
           }
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            float &x = s[q][2 * e + n];
-            x = kF8 ? fmaf(x * kf, c2[e], ve) : x * c2[e];
-            if (ragged && key0 + row >= limit[e]) x = -INFINITY;
-            mx[e] = fmaxf(mx[e], x);
+          for (int x = 0; x < kNR; ++x)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              float &y = s[b][x][2 * n + j];
+              y = kF8 ? fmaf(y * kf, c2[x][j], ve) : y * c2[x][j];
+              if (ragged && key0 + row >= limit[x][j]) y = -INFINITY;
+              mx[x][j] = fmaxf(mx[x][j], y);
+            }
+        }
+      bool moved = false;
+#pragma unroll
+      for (int x = 0; x < kNR; ++x)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1)
+            mx[x][j] = fmaxf(mx[x][j], __shfl_xor_sync(0xffffffffu, mx[x][j], d));
+          moved |= mx[x][j] != m[x][j];
+        }
+      if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+        for (int x = 0; x < kNR; ++x)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const float f = fast_exp2(m[x][j] - mx[x][j]);
+            m[x][j] = mx[x][j];
+            l[x][j] *= f;
+#pragma unroll
+            for (int n = 0; n < kMT; ++n) o[n][x][j] *= f, o[n][x][2 + j] *= f;
           }
-        }
       }
+      // ---- probabilities, as the 16 x 8 B operand of O^T += V^T P^T
+      uint32_t p[kNB][kNR][2];
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 1));
-        mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 2));
-      }
-      if (__any_sync(0xffffffffu, mx[0] != m[0] || mx[1] != m[1])) {
+      for (int b = 0; b < kNB; ++b)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float f = fast_exp2(m[e] - mx[e]);
-          m[e] = mx[e];
-          l[e] *= f;
-#pragma unroll
-          for (int n = 0; n < kNT; ++n) o[n][2 * e] *= f, o[n][2 * e + 1] *= f;
-        }
-      }
-      // ---- probabilities, in place
-      const float shift[2] = {kF8 ? m[0] - kPShift : m[0], kF8 ? m[1] - kPShift : m[1]};
-#pragma unroll
-      for (int q = 0; q < 2 * kNB; ++q)
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
+        for (int x = 0; x < kNR; ++x)
 #pragma unroll
           for (int n = 0; n < 2; ++n) {
-            float &x = s[q][2 * e + n];
-            x = fast_exp2(x - shift[e]);
-            l[e] = kF8 ? fmaf(x, vinv[q][n], l[e]) : l[e] + x;
+            float y[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              y[j] = fast_exp2(s[b][x][2 * n + j] - (kF8 ? m[x][j] - kPShift : m[x][j]));
+              l[x][j] = kF8 ? fmaf(y[j], vinv[b][n], l[x][j]) : l[x][j] + y[j];
+            }
+            p[b][x][n] = transposed(kF8 ? pack_f16(y[0], y[1]) : pack_bf16(y[0], y[1]));
           }
-      // ---- O += P V, 16 keys at a time
+      // ---- O^T += V^T P^T, 16 keys at a time
 #pragma unroll
-      for (int blk = 0; blk < kNB; ++blk) {
-        uint32_t p[4];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          p[e] = kF8 ? pack_f16(s[2 * blk][2 * e], s[2 * blk][2 * e + 1])
-                     : pack_bf16(s[2 * blk][2 * e], s[2 * blk][2 * e + 1]);
-          p[2 + e] = kF8 ? pack_f16(s[2 * blk + 1][2 * e], s[2 * blk + 1][2 * e + 1])
-                         : pack_bf16(s[2 * blk + 1][2 * e], s[2 * blk + 1][2 * e + 1]);
-        }
-        // This lane's V rows: the keys of MMA rows 2t, 2t+1, 2t+8, 2t+9.  vf[n] holds
-        // dimension E g + n (+ 64 for n >= 8 in bf16) of them, E = kNT or 8.
+      for (int b = 0; b < kNB; ++b) {
+        // This lane's V rows: the keys of MMA indices 2t, 2t+1 (+ 8).  vf[n][hi] holds their
+        // values of dimension E g + n (bf16: + 56 for n >= 8), E = kNT in 8 bits, else 8.
         uint32_t vf[kNT][2];
 #pragma unroll
         for (int hi = 0; hi < 2; ++hi) {
-          const int ra = 16 * blk + 8 * hi + key_of<kCh>(2 * t);
-          const int rb = 16 * blk + 8 * hi + key_of<kCh>(2 * t + 1);
+          const int ra = 16 * b + 8 * hi + key_of<kCh>(2 * t);
+          const int rb = 16 * b + 8 * hi + key_of<kCh>(2 * t + 1);
           const uint32_t pa = sv + ra * C::kRowBytes, pb = sv + rb * C::kRowBytes;
           if (kF8) {
             uint32_t wa[4] = {0, 0, 0, 0}, wb[4] = {0, 0, 0, 0};
             if (D == 128) {
-              const uint4 x = lds128(pa + 16 * v_chunk<kCh>(g, ra)), y = lds128(pb + 16 * v_chunk<kCh>(g, rb));
-              wa[0] = x.x, wa[1] = x.y, wa[2] = x.z, wa[3] = x.w;
-              wb[0] = y.x, wb[1] = y.y, wb[2] = y.z, wb[3] = y.w;
+              const uint4 y = lds128(pa + 16 * v_chunk<kCh>(g, ra)), z = lds128(pb + 16 * v_chunk<kCh>(g, rb));
+              wa[0] = y.x, wa[1] = y.y, wa[2] = y.z, wa[3] = y.w;
+              wb[0] = z.x, wb[1] = z.y, wb[2] = z.z, wb[3] = z.w;
             } else {
-              const uint2 x = lds64(pa + 16 * v_chunk<kCh>(g >> 1, ra) + 8 * (g & 1));
-              const uint2 y = lds64(pb + 16 * v_chunk<kCh>(g >> 1, rb) + 8 * (g & 1));
-              wa[0] = x.x, wa[1] = x.y, wb[0] = y.x, wb[1] = y.y;
+              const uint2 y = lds64(pa + 16 * v_chunk<kCh>(g >> 1, ra) + 8 * (g & 1));
+              const uint2 z = lds64(pb + 16 * v_chunk<kCh>(g >> 1, rb) + 8 * (g & 1));
+              wa[0] = y.x, wa[1] = y.y, wb[0] = z.x, wb[1] = z.y;
             }
 #pragma unroll
             for (int w = 0; w < kNT / 4; ++w) {
-              const uint32_t u = __byte_perm(wa[w], wb[w], 0x5140), v = __byte_perm(wa[w], wb[w], 0x7362);
-              vf[4 * w][hi] = f16x2_of_e4m3x2(u);
-              vf[4 * w + 1][hi] = f16x2_of_e4m3x2(u >> 16);
-              vf[4 * w + 2][hi] = f16x2_of_e4m3x2(v);
-              vf[4 * w + 3][hi] = f16x2_of_e4m3x2(v >> 16);
+              const uint32_t y = __byte_perm(wa[w], wb[w], 0x5140), z = __byte_perm(wa[w], wb[w], 0x7362);
+              vf[4 * w][hi] = f16x2_of_e4m3x2(y);
+              vf[4 * w + 1][hi] = f16x2_of_e4m3x2(y >> 16);
+              vf[4 * w + 2][hi] = f16x2_of_e4m3x2(z);
+              vf[4 * w + 3][hi] = f16x2_of_e4m3x2(z >> 16);
             }
           } else {
 #pragma unroll
             for (int half = 0; half < kNT / 8; ++half) {
-              const uint4 x = lds128(pa + 16 * v_chunk<kCh>(g + 8 * half, ra));
-              const uint4 y = lds128(pb + 16 * v_chunk<kCh>(g + 8 * half, rb));
+              const uint4 y = lds128(pa + 16 * v_chunk<kCh>(g + 8 * half, ra));
+              const uint4 z = lds128(pb + 16 * v_chunk<kCh>(g + 8 * half, rb));
 #pragma unroll
               for (int w = 0; w < 4; ++w) {
-                vf[8 * half + 2 * w][hi] = __byte_perm(word(x, w), word(y, w), 0x5410);
-                vf[8 * half + 2 * w + 1][hi] = __byte_perm(word(x, w), word(y, w), 0x7632);
+                vf[8 * half + 2 * w][hi] = __byte_perm(word(y, w), word(z, w), 0x5410);
+                vf[8 * half + 2 * w + 1][hi] = __byte_perm(word(y, w), word(z, w), 0x7632);
               }
             }
           }
@@ -533,37 +579,39 @@ paged_attention_kernel(const Args a) {
         }
         if (!apart) {
 #pragma unroll
-          for (int n = 0; n < kNT; ++n) mma<kF8>(o[n], p, vf[n][0], vf[n][1]);
+          for (int n = 0; n < kMT; ++n) {
+            const uint32_t v[4] = {vf[2 * n][0], vf[2 * n + 1][0], vf[2 * n][1], vf[2 * n + 1][1]};
+#pragma unroll
+            for (int x = 0; x < kNR; ++x) mma<kF8>(o[n][x], v, p[b][x][0], p[b][x][1]);
+          }
         } else {
           const int r0 = (cur.unit % a.row_tiles) * kRows;
-          const int i1 = (min(a.rows, r0 + kRows) - 1) / a.G;
-          for (int i = r0 / a.G; i <= i1; ++i) {
+          const int i1 = (min(a.rows, r0 + kRows) - 1) / (int)a.group.d;
+          for (int i = r0 / (int)a.group.d; i <= i1; ++i) {
             const int lim = cur.len - a.n_new + i + 1;
-            uint32_t pi[4];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const bool mine = limit[e] == lim && r0 + g + 8 * e < a.rows;
-              pi[e] = mine ? p[e] : 0u;
-              pi[2 + e] = mine ? p[2 + e] : 0u;
-            }
             uint32_t keep[2];
 #pragma unroll
             for (int hi = 0; hi < 2; ++hi) {
-              const int k = key0 + 16 * blk + 8 * hi;
+              const int k = key0 + 16 * b + 8 * hi;
               keep[hi] = (k + key_of<kCh>(2 * t) < lim ? 0xffffu : 0u) |
                          (k + key_of<kCh>(2 * t + 1) < lim ? 0xffff0000u : 0u);
             }
-            // rows of the other tokens take nothing, not 0 * NaN: their sums stand aside
+            // the other tokens' sums stand aside: they take nothing, not 0 * NaN
 #pragma unroll
-            for (int n = 0; n < kNT; ++n) {
-              float x[4] = {0.f, 0.f, 0.f, 0.f};
-              mma<kF8>(x, pi, vf[n][0] & keep[0], vf[n][1] & keep[1]);
+            for (int n = 0; n < kMT; ++n) {
+              const uint32_t v[4] = {vf[2 * n][0] & keep[0], vf[2 * n + 1][0] & keep[0],
+                                     vf[2 * n][1] & keep[1], vf[2 * n + 1][1] & keep[1]};
 #pragma unroll
-              for (int e = 0; e < 2; ++e)
-                if (limit[e] == lim && r0 + g + 8 * e < a.rows) {
-                  o[n][2 * e] += x[2 * e];
-                  o[n][2 * e + 1] += x[2 * e + 1];
-                }
+              for (int x = 0; x < kNR; ++x) {
+                float y[4] = {0.f, 0.f, 0.f, 0.f};
+                mma<kF8>(y, v, p[b][x][0], p[b][x][1]);
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                  if (limit[x][j] == lim && r0 + 8 * x + 2 * t + j < a.rows) {
+                    o[n][x][j] += y[j];
+                    o[n][x][2 + j] += y[2 + j];
+                  }
+              }
             }
           }
         }
@@ -573,99 +621,115 @@ paged_attention_kernel(const Args a) {
     const bool unit_done = cur.tile + 1 == cur.tiles;
     if (unit_done || it + 1 == n_tiles) {
       // ---- the unit's end, or the run's: the four warps' parts become one in warp 0
-      const int r0 = (cur.unit % a.row_tiles) * kRows, h = cur.unit / a.row_tiles;
+      const int h = cur.unit / a.row_tiles, r0 = (cur.unit - h * a.row_tiles) * kRows;
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        l[e] += __shfl_xor_sync(0xffffffffu, l[e], 1);
-        l[e] += __shfl_xor_sync(0xffffffffu, l[e], 2);
-        if (t == 0) {
-          sh_m[warp][g + 8 * e] = m[e];
-          sh_l[warp][g + 8 * e] = l[e];
+      for (int x = 0; x < kNR; ++x)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) l[x][j] += __shfl_xor_sync(0xffffffffu, l[x][j], d);
+          if (g == 0) {
+            sh_m[warp][8 * x + 2 * t + j] = m[x][j];
+            sh_l[warp][8 * x + 2 * t + j] = l[x][j];
+          }
         }
-      }
       __syncthreads();
-      float M[2], sum[2];
+      float M[kNR][2], sum[kNR][2];
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        M[e] = sh_m[0][g + 8 * e];
+      for (int x = 0; x < kNR; ++x)
 #pragma unroll
-        for (int w = 1; w < kWarps; ++w) M[e] = fmaxf(M[e], sh_m[w][g + 8 * e]);
-        sum[e] = 0.f;
+        for (int j = 0; j < 2; ++j) {
+          const int r = 8 * x + 2 * t + j;
+          M[x][j] = sh_m[0][r];
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w)
-          sum[e] += sh_l[w][g + 8 * e] * fast_exp2(sh_m[w][g + 8 * e] - M[e]);
-        const float f = fast_exp2(m[e] - M[e]);
+          for (int w = 1; w < kWarps; ++w) M[x][j] = fmaxf(M[x][j], sh_m[w][r]);
+          sum[x][j] = 0.f;
 #pragma unroll
-        for (int n = 0; n < kNT; ++n) o[n][2 * e] *= f, o[n][2 * e + 1] *= f;
-      }
-      // lane-major: each lane adds the same lane's sums of another warp; the buffer holds
-      // one warp's O, or halves of two
-      auto at = [&](int n) { return reinterpret_cast<float4 *>(merge) + n * 32 + lane; };
+          for (int w = 0; w < kWarps; ++w) sum[x][j] += sh_l[w][r] * fast_exp2(sh_m[w][r] - M[x][j]);
+          const float f = fast_exp2(m[x][j] - M[x][j]);
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const int base = (warp & 1) * (kNT / 2);
+          for (int n = 0; n < kMT; ++n) o[n][x][j] *= f, o[n][x][2 + j] *= f;
+        }
+      // lane-major: each lane adds the same lane's sums of another warp, by way of a buffer
+      // of one warp's O
+      auto at = [&](int n, int x) { return reinterpret_cast<float4 *>(merge) + (n * kNR + x) * 32 + lane; };
+      auto put = [&](int n, int to) {
+#pragma unroll
+        for (int x = 0; x < kNR; ++x) *at(to, x) = make_float4(o[n][x][0], o[n][x][1], o[n][x][2], o[n][x][3]);
+      };
+      auto add = [&](int n, int from) {
+#pragma unroll
+        for (int x = 0; x < kNR; ++x) {
+          const float4 z = *at(from, x);
+          o[n][x][0] += z.x, o[n][x][1] += z.y, o[n][x][2] += z.z, o[n][x][3] += z.w;
+        }
+      };
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {   // warp 2 to 0 and 3 to 1, in halves
         if (warp >= 2) {
 #pragma unroll
-          for (int n = 0; n < kNT / 2; ++n) {
-            const float(&x)[4] = o[half * (kNT / 2) + n];
-            *at(base + n) = make_float4(x[0], x[1], x[2], x[3]);
-          }
+          for (int n = 0; n < kMT / 2; ++n) put(half * (kMT / 2) + n, (warp & 1) * (kMT / 2) + n);
         }
         __syncthreads();
         if (warp < 2) {
 #pragma unroll
-          for (int n = 0; n < kNT / 2; ++n) {
-            const float4 x = *at(base + n);
-            float(&y)[4] = o[half * (kNT / 2) + n];
-            y[0] += x.x, y[1] += x.y, y[2] += x.z, y[3] += x.w;
-          }
+          for (int n = 0; n < kMT / 2; ++n) add(half * (kMT / 2) + n, warp * (kMT / 2) + n);
         }
         __syncthreads();
       }
       if (warp == 1) {
 #pragma unroll
-        for (int n = 0; n < kNT; ++n) *at(n) = make_float4(o[n][0], o[n][1], o[n][2], o[n][3]);
+        for (int n = 0; n < kMT; ++n) put(n, n);
       }
       __syncthreads();
       if (warp == 0) {
 #pragma unroll
-        for (int n = 0; n < kNT; ++n) {
-          const float4 x = *at(n);
-          o[n][0] += x.x, o[n][1] += x.y, o[n][2] += x.z, o[n][3] += x.w;
-        }
+        for (int n = 0; n < kMT; ++n) add(n, n);
+      }
+      if (warp == 0) {
         const bool whole = unit_tile0 == 0 && unit_done;
         float *part = a.ws + (size_t)(2 * blockIdx.x + (first_unit ? 0 : 1)) * (kRows * (D + 2));
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int rr = g + 8 * e, r = r0 + rr;
-          if (r >= a.rows) continue;
-          const float inv = sum[e] > 0.f ? 1.f / sum[e] : sum[e] == 0.f ? 0.f : sum[e];
-          __nv_bfloat16 *dst = a.out + ((size_t)((size_t)cur.b * a.n_new + r / a.G) * a.Hq + h * a.G + r % a.G) * D;
+        for (int x = 0; x < kNR; ++x)
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            // columns 2t + j of all n: neighbouring dimensions
+            const int rr = 8 * x + 2 * t + j, r = r0 + rr;
+            if (r >= a.rows) continue;
+            const float sm = sum[x][j], inv = sm > 0.f ? 1.f / sm : sm == 0.f ? 0.f : sm;
+            const int i = quotient(r, a.group);
+            __nv_bfloat16 *dst = a.out + ((size_t)((size_t)cur.b * a.n_new + i) * a.Hq + h * (int)a.group.d +
+                                          (r - i * (int)a.group.d)) * D;
+            // eight neighbouring dimensions from four MMA blocks
             constexpr int kE = kF8 ? kNT : 8;
 #pragma unroll
-            for (int n0 = 0; n0 < kNT; n0 += 8) {
-              const int d = kE * (2 * t + j) + (kE == 8 ? 8 * n0 : n0);
+            for (int n = 0; n < kMT; n += 4) {
+              const int d = kE * g + (kE == 8 ? 16 * n : 2 * n);
               if (whole) {
                 uint4 w;
-                w.x = pack_bf16(o[n0][2 * e + j] * inv, o[n0 + 1][2 * e + j] * inv);
-                w.y = pack_bf16(o[n0 + 2][2 * e + j] * inv, o[n0 + 3][2 * e + j] * inv);
-                w.z = pack_bf16(o[n0 + 4][2 * e + j] * inv, o[n0 + 5][2 * e + j] * inv);
-                w.w = pack_bf16(o[n0 + 6][2 * e + j] * inv, o[n0 + 7][2 * e + j] * inv);
+                w.x = pack_bf16(o[n][x][j] * inv, o[n][x][2 + j] * inv);
+                w.y = pack_bf16(o[n + 1][x][j] * inv, o[n + 1][x][2 + j] * inv);
+                w.z = pack_bf16(o[n + 2][x][j] * inv, o[n + 2][x][2 + j] * inv);
+                w.w = pack_bf16(o[n + 3][x][j] * inv, o[n + 3][x][2 + j] * inv);
                 *reinterpret_cast<uint4 *>(dst + d) = w;
               } else {
                 float4 *f = reinterpret_cast<float4 *>(part + rr * D + d);
-                f[0] = make_float4(o[n0][2 * e + j], o[n0 + 1][2 * e + j], o[n0 + 2][2 * e + j], o[n0 + 3][2 * e + j]);
-                f[1] = make_float4(o[n0 + 4][2 * e + j], o[n0 + 5][2 * e + j], o[n0 + 6][2 * e + j], o[n0 + 7][2 * e + j]);
+                f[0] = make_float4(o[n][x][j], o[n][x][2 + j], o[n + 1][x][j], o[n + 1][x][2 + j]);
+                f[1] = make_float4(o[n + 2][x][j], o[n + 2][x][2 + j], o[n + 3][x][j], o[n + 3][x][2 + j]);
               }
             }
+            if (!whole && g == 0) {
+              part[kRows * D + 2 * rr] = M[x][j];
+              part[kRows * D + 2 * rr + 1] = sm;
+            }
           }
-          if (!whole && t == 0) {
-            part[kRows * D + 2 * rr] = M[e];
-            part[kRows * D + 2 * rr + 1] = sum[e];
-          }
+        if (unit_done && !whole) {   // a run ends one such unit at most: its first
+          const long long t0 = first_tile(plan, blockIdx.x) - unit_tile0;
+          const int c0 = cta_of(plan, t0);
+          cut.parts = blockIdx.x - c0 + 1;
+          cut.first = c0;
+          cut.slot = first_tile(plan, c0) == t0 ? 2 * c0 : 2 * c0 + 1;
+          cut.b = cur.b;
+          cut.unit = cur.unit;
         }
       }
       first_unit = false;
@@ -674,103 +738,95 @@ paged_attention_kernel(const Args a) {
     if (it + 1 < n_tiles) step(a, cur, C::kTile);
   }
   wait_all_but<0>();
+  if (threadIdx.x == 0) a.cuts[blockIdx.x] = cut;
+  clear_empty<D>(a);
 }
 
-// Joins the parts of each output row whose unit several blocks shared, and stores zeros
-// for sequences without keys.  One block per (sequence, K/V head, row); a warp takes
-// every eighth part, D/4 lanes a part's four-dimension vectors.
+// Joins a row's parts where several blocks shared its unit: one block for each block of
+// the kernel before and each row, and most of them find that theirs ended no such unit.
+// A part takes D/4 lanes, four dimensions each; bound by the round trips to L2, so each
+// lane group loads four parts at once, and statistics with sums.
 constexpr int kJoinThreads = 256;
-constexpr int kJoinWarps = kJoinThreads / 32;
 
-template <int D>
+template <int D, int kNR>
 __global__ void __launch_bounds__(kJoinThreads)
-paged_join_kernel(const Args a, int tile, int grid) {
-  __shared__ long long sh_sum[kJoinWarps];
-  __shared__ long long sh_before;
-  __shared__ float sh_red[kJoinWarps];
+paged_join_kernel(const Args a) {
+  constexpr int kRows = 8 * kNR, kL = D / 4, kGroups = kJoinThreads / kL;
   __shared__ float4 sh_o[kJoinThreads];
-  __shared__ float sh_l[kJoinThreads / (D / 4)];
+  __shared__ float2 sh_ml[kGroups];
   pdl_wait();
   pdl_trigger();
-  const int r = blockIdx.x % a.rows, h = blockIdx.x / a.rows % a.Hkv;
-  const int b = blockIdx.x / a.rows / a.Hkv;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  Plan plan;
-  {
-    int b0, b1;
-    long long before, mine;
-    scan_tiles<kJoinThreads>(a, tile, b0, b1, before, mine, plan.total, sh_sum);
-    if (b >= b0 && b < b1) {
-      for (int x = b0; x < b; ++x)
-        before += (long long)((length(a, x) + tile - 1) / tile) * a.Hkv * a.row_tiles;
-      sh_before = before;
-    }
-    __syncthreads();
-  }
-  plan.ctas = (int)min((long long)grid, plan.total);
-  const int tiles = (length(a, b) + tile - 1) / tile;
-  __nv_bfloat16 *dst =
-      a.out + ((size_t)((size_t)b * a.n_new + r / a.G) * a.Hq + h * a.G + r % a.G) * D;
-  if (tiles == 0) {
-    if (threadIdx.x < D / 8) reinterpret_cast<uint4 *>(dst)[threadIdx.x] = make_uint4(0, 0, 0, 0);
-    return;
-  }
-  const long long t0 = sh_before + (long long)(h * a.row_tiles + r / kRows) * tiles;
-  const int c0 = cta_of(plan, t0), c1 = cta_of(plan, t0 + tiles - 1);
-  if (c0 == c1) return;   // stored by its block
-  const int parts = c1 - c0 + 1, rr = r % kRows;
-  const int slot0 = first_tile(plan, c0) == t0 ? 2 * c0 : 2 * c0 + 1;
-  auto part = [&](int p) {
-    return a.ws + (size_t)(p ? 2 * (c0 + p) : slot0) * (kRows * (D + 2));
-  };
-  float M = kLowest;
-  for (int p = threadIdx.x; p < parts; p += kJoinThreads) M = fmaxf(M, part(p)[kRows * D + 2 * rr]);
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-  if (lane == 0) sh_red[warp] = M;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kJoinWarps; ++w) M = fmaxf(M, sh_red[w]);
-  constexpr int kL = D / 4;                 // lanes per part
-  const int sub = threadIdx.x % kL, at = threadIdx.x / kL;
+  const CutUnit u = a.cuts[blockIdx.x];
+  if (u.parts == 0) return;
+  const int h = u.unit / a.row_tiles, rr = blockIdx.y, r = (u.unit - h * a.row_tiles) * kRows + rr;
+  if (r >= a.rows) return;
+  const int sub = threadIdx.x % kL, group = threadIdx.x / kL;
+  float M = kLowest, L = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  float sum = 0.f;
-#pragma unroll 4
-  for (int p = at; p < parts; p += kJoinThreads / kL) {
-    const float *w = part(p);
-    const float2 ml = *reinterpret_cast<const float2 *>(w + kRows * D + 2 * rr);
-    const float4 x = *reinterpret_cast<const float4 *>(w + rr * D + 4 * sub);
-    const float f = fast_exp2(ml.x - M);
-    sum = fmaf(f, ml.y, sum);
+  for (int p0 = group; p0 < u.parts; p0 += 4 * kGroups) {
+    float2 w[4];
+    float4 x[4];
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+      const int p = p0 + y * kGroups;
+      w[y] = make_float2(kLowest, 0.f);
+      x[y] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (p < u.parts) {
+        const float *part = a.ws + (size_t)(p ? 2 * (u.first + p) : u.slot) * (kRows * (D + 2));
+        w[y] = *reinterpret_cast<const float2 *>(part + kRows * D + 2 * rr);
+        x[y] = *reinterpret_cast<const float4 *>(part + rr * D + 4 * sub);
+      }
+    }
+    const float to = fmaxf(fmaxf(fmaxf(w[0].x, w[1].x), fmaxf(w[2].x, w[3].x)), M);
+    const float f0 = fast_exp2(M - to);
+    M = to;
+    L *= f0, acc.x *= f0, acc.y *= f0, acc.z *= f0, acc.w *= f0;
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+      const float f = fast_exp2(w[y].x - M);
+      L = fmaf(f, w[y].y, L);
+      acc.x = fmaf(f, x[y].x, acc.x);
+      acc.y = fmaf(f, x[y].y, acc.y);
+      acc.z = fmaf(f, x[y].z, acc.z);
+      acc.w = fmaf(f, x[y].w, acc.w);
+    }
+  }
+  sh_o[threadIdx.x] = acc;
+  if (sub == 0) sh_ml[group] = make_float2(M, L);
+  __syncthreads();
+  if (group) return;
+#pragma unroll
+  for (int y = 0; y < kGroups; ++y) M = fmaxf(M, sh_ml[y].x);
+  L = 0.f;
+  acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int y = 0; y < kGroups; ++y) {
+    const float2 w = sh_ml[y];
+    const float4 x = sh_o[y * kL + sub];
+    const float f = fast_exp2(w.x - M);
+    L = fmaf(f, w.y, L);
     acc.x = fmaf(f, x.x, acc.x);
     acc.y = fmaf(f, x.y, acc.y);
     acc.z = fmaf(f, x.z, acc.z);
     acc.w = fmaf(f, x.w, acc.w);
   }
-  sh_o[threadIdx.x] = acc;
-  if (sub == 0) sh_l[at] = sum;
-  __syncthreads();
-  if (threadIdx.x < kL) {
-    float total = 0.f;
-    acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int i = 0; i < kJoinThreads / kL; ++i) {
-      const float4 x = sh_o[i * kL + threadIdx.x];
-      acc.x += x.x, acc.y += x.y, acc.z += x.z, acc.w += x.w;
-      total += sh_l[i];
-    }
-    const float inv = total > 0.f ? 1.f / total : total == 0.f ? 0.f : total;
-    reinterpret_cast<uint2 *>(dst)[threadIdx.x] =
-        make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-  }
+  const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;
+  const int i = quotient(r, a.group);
+  reinterpret_cast<uint2 *>(a.out + ((size_t)((size_t)u.b * a.n_new + i) * a.Hq + h * (int)a.group.d +
+                                     (r - i * (int)a.group.d)) * D)[sub] =
+      make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
 }
 
 // -------------------------------------------------------------- host side
 
-template <int D, bool kF8>
-int launch(const Args &a, size_t ws_bytes, cudaStream_t stream) {
-  using C = Cfg<D, kF8>;
-  auto kernel = paged_attention_kernel<D, kF8>;
+size_t workspace_bytes(int D) {
+  return (size_t)sm_count() * kMaxPerSm * (sizeof(CutUnit) + 2 * kMostRows * ((size_t)D + 2) * 4);
+}
+
+template <int D, bool kF8, int kNR>
+int launch(Args &a, void *workspace, cudaStream_t stream) {
+  using C = Cfg<D, kF8, kNR>;
+  auto kernel = paged_attention_kernel<D, kF8, kNR>;
   static std::atomic<int> per_sm[64];
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return HSA_ERR_CUDA;
@@ -785,16 +841,31 @@ int launch(const Args &a, size_t ws_bytes, cudaStream_t stream) {
     nb = std::min(nb, kMaxPerSm);
     per_sm[dev].store(nb, std::memory_order_release);
   }
+  a.row_tiles = (a.rows + C::kRows - 1) / C::kRows;
   const long long units = (long long)a.batch * a.Hkv * a.row_tiles;
-  const long long most = units * ((((long long)a.max_pages << a.page_log2) + C::kTile - 1) / C::kTile);
-  const int grid = (int)std::min<long long>((long long)nb * sm_count(), std::max(1LL, most));
-  if ((size_t)grid * 2 * kRows * (D + 2) * 4 > ws_bytes) return HSA_ERR_WORKSPACE;
+  const long long tiles = (((long long)a.max_pages << a.page_log2) + C::kTile - 1) / C::kTile;
+  const int blocks = nb * sm_count();
+  const int grid = tiles == 0 ? std::min(a.batch, blocks)
+                              : units >= blocks || tiles >= blocks ? blocks
+                                                                   : (int)std::min<long long>(blocks, units * tiles);
+  a.cuts = static_cast<CutUnit *>(workspace);
+  a.ws = reinterpret_cast<float *>(a.cuts + (size_t)sm_count() * kMaxPerSm);
   count_launches(2);
   launch_pdl(kernel, dim3((unsigned)grid), dim3(kThreads), C::kSmem, stream, a);
   if (cudaGetLastError() != cudaSuccess) return HSA_ERR_CUDA;
-  launch_pdl(paged_join_kernel<D>, dim3((unsigned)(a.batch * a.Hkv * a.rows)), dim3(kJoinThreads), 0,
-             stream, a, (int)C::kTile, grid);
+  launch_pdl(paged_join_kernel<D, kNR>, dim3((unsigned)grid, (unsigned)std::min(a.rows, C::kRows)),
+             dim3(kJoinThreads), 0, stream, a);
   return launch_status();
+}
+
+// Column blocks of eight rows: as many as the rows need and a unit's sums fit in registers
+// (at D = 128 four blocks spill: 5 tokens of 8 heads against 43403 keys 155 us, two at a
+// time 92).  Rows beyond are further units, which read the keys again, from L2.
+template <int D, bool kF8>
+int launch_rows(Args &a, void *workspace, cudaStream_t stream) {
+  if constexpr (D == 64)
+    if (a.rows > 16) return launch<D, kF8, 4>(a, workspace, stream);
+  return a.rows <= 8 ? launch<D, kF8, 1>(a, workspace, stream) : launch<D, kF8, 2>(a, workspace, stream);
 }
 
 }  // namespace
@@ -804,7 +875,7 @@ using namespace hsa;
 
 extern "C" size_t hsa_paged_attention_workspace_bytes(int batch, int n_new, int Hq, int Hkv, int D) {
   if (batch <= 0 || n_new <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || (D != 64 && D != 128)) return 0;
-  return (size_t)sm_count() * kMaxPerSm * 2 * kRows * (D + 2) * 4;
+  return workspace_bytes(D);
 }
 
 extern "C" int hsa_paged_attention(const void *q, int batch, int n_new, int Hq, const void *k_pages,
@@ -812,7 +883,7 @@ extern "C" int hsa_paged_attention(const void *q, int batch, int n_new, int Hq, 
                                    const uint8_t *v_scale, int n_pages, int page_size, int Hkv, int D,
                                    hsa_dtype cache_dtype, const int32_t *page_table, int max_pages,
                                    const int32_t *seq_lens, float scale, void *out, void *workspace,
-                                   size_t workspace_bytes, hsa_stream_t stream) {
+                                   size_t size, hsa_stream_t stream) {
   if (batch < 0 || n_new < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv || n_pages < 0 || max_pages < 0 ||
       page_size < 1)
     return HSA_ERR_INVALID_ARG;
@@ -822,7 +893,7 @@ extern "C" int hsa_paged_attention(const void *q, int batch, int n_new, int Hq, 
     return HSA_ERR_UNSUPPORTED;
   const long long rows = (long long)n_new * (Hq / Hkv);
   if ((long long)n_pages * page_size > 0x7fffffffLL || (long long)max_pages * page_size > 0x7fffff00LL ||
-      Hq > 65535 || rows > 0x7fffffffLL || (long long)batch * Hkv * rows > 0x7fffffffLL)
+      Hq > 65535 || rows > 0x7fffffffLL || (long long)batch * Hkv * rows > 0x7fffff00LL)
     return HSA_ERR_UNSUPPORTED;
   if (batch == 0 || n_new == 0) return HSA_OK;
   if (!q || !out || !seq_lens || !aligned16(q) || !aligned16(out)) return HSA_ERR_INVALID_ARG;
@@ -831,7 +902,7 @@ extern "C" int hsa_paged_attention(const void *q, int batch, int n_new, int Hq, 
       (!k_pages || !v_pages || !page_table || (f8 && (!k_scale || !v_scale)) ||
        !aligned16(k_pages) || !aligned16(v_pages)))
     return HSA_ERR_INVALID_ARG;
-  if (!workspace || !aligned16(workspace)) return HSA_ERR_WORKSPACE;
+  if (!workspace || !aligned16(workspace) || size < workspace_bytes(D)) return HSA_ERR_WORKSPACE;
   if (!(scale > 0.f) || !std::isfinite(scale)) scale = 1.f / std::sqrt((float)D);
   Args a;
   a.q = static_cast<const __nv_bfloat16 *>(q);
@@ -842,22 +913,24 @@ extern "C" int hsa_paged_attention(const void *q, int batch, int n_new, int Hq, 
   a.table = page_table;
   a.lens = seq_lens;
   a.out = static_cast<__nv_bfloat16 *>(out);
-  a.ws = static_cast<float *>(workspace);
   a.err = device_error_word();
   if (!a.err) return HSA_ERR_CUDA;
   a.batch = batch;
   a.n_new = n_new;
   a.Hq = Hq;
   a.Hkv = Hkv;
-  a.G = Hq / Hkv;
+  a.group = make_divider((unsigned)(Hq / Hkv));
   a.rows = (int)rows;
-  a.row_tiles = (int)((rows + kRows - 1) / kRows);
+  a.row_tiles = 0;
+  a.cuts = nullptr;
+  a.ws = nullptr;
   a.n_pages = n_pages;
   a.max_pages = n_pages > 0 ? max_pages : 0;
   a.page_log2 = 0;
   while ((1 << a.page_log2) < page_size) ++a.page_log2;
   a.scale_log2 = scale * 1.4426950408889634f;
   cudaStream_t s = (cudaStream_t)stream;
-  if (f8) return D == 128 ? launch<128, true>(a, workspace_bytes, s) : launch<64, true>(a, workspace_bytes, s);
-  return D == 128 ? launch<128, false>(a, workspace_bytes, s) : launch<64, false>(a, workspace_bytes, s);
+  if (f8)
+    return D == 128 ? launch_rows<128, true>(a, workspace, s) : launch_rows<64, true>(a, workspace, s);
+  return D == 128 ? launch_rows<128, false>(a, workspace, s) : launch_rows<64, false>(a, workspace, s);
 }

@@ -84,7 +84,7 @@ def test_paged_attention_refusals(hsa):
     for bad in (dict(dt=1), dict(D=96), dict(page=48), dict(pages=1 << 27), dict(cols=1 << 27),
                 dict(Hq=65538, Hkv=2), dict(B=1 << 20, new=1 << 10)):
         assert _paged(hsa, **bad) == -4, bad
-    for bad in (dict(ws=None), dict(ws=ODD)):
+    for bad in (dict(ws=None), dict(ws=ODD), dict(size=1000)):
         assert _paged(hsa, **bad) == -9, bad
     assert hsa.hsa_launch_count() == c0
 
