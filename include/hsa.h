@@ -386,7 +386,8 @@ int hsa_kv_dequant_gather(const void *k_cache, const void *v_cache, const uint8_
  *   workspace    device, >= hsa_paged_attention_workspace_bytes(...) bytes, 16-byte
  *                aligned, overwritten; calls (and captured graphs) sharing one must
  *                not overlap on the GPU.  Its size depends on D and the device only.
- * D in {64, 128}; page_size a power of two; max_pages * page_size < 2^31 - 256.  A
+ * D in {64, 128}; page_size a power of two; max_pages * page_size < 2^31 - 256; batch *
+ * Hkv * ceil(rows / 8) * max_pages * page_size / 64 < 2^31 with rows = n_new * Hq / Hkv.  A
  * page id outside [0, n_pages) reads as rows of zeros (HSA_ERR_INDEX).  Two launches;
  * the result does not depend on what else runs.  A flat cache of N rows is a cache of
  * ceil(N / page_size) pages with the identity as its table. */

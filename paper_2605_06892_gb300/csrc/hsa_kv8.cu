@@ -9,10 +9,12 @@
 // the code, and code 2^e (four significant bits, 2^-109 to 1.75 2^127) is exact in bf16:
 // what is read back as bf16 is the cache's value, and the tensor cores can take it.
 //
-// Both kernels are bound by HBM: 3 bytes move per element of a bf16 tensor.  Lane c of a
-// group of L lanes (a power of two) holds elements 8c .. 8c+7 of a head's row, of K and
-// of V, so that a row's maximum takes log2(L) shuffles and all loads and stores are
-// coalesced vectors.
+// Both kernels are bound by HBM: 3 bytes move per element of a bf16 tensor.  The lanes of a
+// group (a power of two) hold vectors of eight elements of a head's row, of K and of V, so
+// that a row's maximum takes a few shuffles and all loads and stores are coalesced.  When
+// quantising, what is done per row and not per element would fill the issue slots, so a
+// lane holds two vectors, c and c + L (LTX-like layer, three quarters of the rows rotated
+// and in: 19.5 us with one vector a lane).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -22,7 +24,7 @@ namespace hsa {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMaxD = 256;             // 32 lanes of 8 elements
+constexpr int kMaxD = 256;             // 32 vectors of 8 elements
 constexpr unsigned kLeastScale = 27;   // e >= -100: every value is a normal fp32 and bf16
 
 __device__ __forceinline__ uint4 ld_stream(const void *p) {
@@ -87,56 +89,78 @@ __device__ __forceinline__ unsigned scale_byte(uint32_t bits) {
   return max(t, kLeastScale + 8u) - 8u;
 }
 
-// The codes of eight elements (all lanes of the row's group call it together) and the
-// row's scale byte.  `bad` is set where an element is not finite: its code is NaN and
-// the others go by the largest finite magnitude.  Finite magnitudes above 1.875 2^127
-// count as that, since the next code would stand for 2^128.
+// The largest magnitude's bits among eight elements.
 template <bool kF32>
-__device__ __forceinline__ uint2 quantise(const Eight<kF32> &v, int L, unsigned group, unsigned &scale,
-                                          bool &bad) {
-  constexpr uint32_t kTop = 0x7f700000u;   // 1.875 2^127
-  float x[8];
-  uint32_t m;
+__device__ __forceinline__ uint32_t largest(const Eight<kF32> &v) {
   if (kF32) {
-    m = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint4 &q = v.w[kF32 ? i / 4 : 0];
-      const uint32_t b = i % 4 == 0 ? q.x : i % 4 == 1 ? q.y : i % 4 == 2 ? q.z : q.w;
-      x[i] = __uint_as_float(b);
-      m = max(m, b & 0x7fffffffu);
-    }
-  } else {
-    const uint4 &q = v.w[0];
-    // magnitudes of bf16 are ordered as their bits: two at a time
-    const uint32_t m2 = __vmaxu2(__vmaxu2(q.x & 0x7fff7fffu, q.y & 0x7fff7fffu),
-                                 __vmaxu2(q.z & 0x7fff7fffu, q.w & 0x7fff7fffu));
-    m = max(m2 << 16, m2 & 0xffff0000u);
-    x[0] = lo_bf16(q.x), x[1] = hi_bf16(q.x), x[2] = lo_bf16(q.y), x[3] = hi_bf16(q.y);
-    x[4] = lo_bf16(q.z), x[5] = hi_bf16(q.z), x[6] = lo_bf16(q.w), x[7] = hi_bf16(q.w);
+    const uint4 &p = v.w[0], &q = v.w[kF32 ? 1 : 0];
+    constexpr uint32_t kM = 0x7fffffffu;
+    return max(max(max(p.x & kM, p.y & kM), max(p.z & kM, p.w & kM)),
+               max(max(q.x & kM, q.y & kM), max(q.z & kM, q.w & kM)));
   }
+  // magnitudes of bf16 are ordered as their bits: two at a time
+  const uint4 &q = v.w[0];
+  constexpr uint32_t kM = 0x7fff7fffu;
+  const uint32_t m = __vmaxu2(__vmaxu2(q.x & kM, q.y & kM), __vmaxu2(q.z & kM, q.w & kM));
+  return max(m << 16, m & 0xffff0000u);
+}
+template <bool kF32>
+__device__ __forceinline__ void unpack8(const Eight<kF32> &v, float (&x)[8]) {
+  const uint4 &p = v.w[0], &q = v.w[kF32 ? 1 : 0];
+  if (kF32) {
+    x[0] = __uint_as_float(p.x), x[1] = __uint_as_float(p.y), x[2] = __uint_as_float(p.z);
+    x[3] = __uint_as_float(p.w), x[4] = __uint_as_float(q.x), x[5] = __uint_as_float(q.y);
+    x[6] = __uint_as_float(q.z), x[7] = __uint_as_float(q.w);
+  } else {
+    x[0] = lo_bf16(p.x), x[1] = hi_bf16(p.x), x[2] = lo_bf16(p.y), x[3] = hi_bf16(p.y);
+    x[4] = lo_bf16(p.z), x[5] = hi_bf16(p.z), x[6] = lo_bf16(p.w), x[7] = hi_bf16(p.w);
+  }
+}
+
+constexpr uint32_t kTop = 0x7f700000u;   // 1.875 2^127: the next code would stand for 2^128
+
+// The codes of a row's eight elements, twice (all lanes of the row's group call it
+// together), and the row's scale byte.  `bad` is set where an element is not finite: its
+// code is NaN and the others go by the largest finite magnitude.  Finite magnitudes above
+// kTop count as that.
+template <bool kF32>
+__device__ __forceinline__ void quantise(const Eight<kF32> (&v)[2], int L, unsigned group, uint2 (&c)[2],
+                                         unsigned &scale, bool &bad) {
+  uint32_t m = max(largest(v[0]), largest(v[1]));
   for (int o = 1; o < L; o <<= 1) m = max(m, __shfl_xor_sync(group, m, o));
-  if (m > kTop) {   // rare; the same in all lanes of the group
+  const bool odd = m > kTop;             // rare; the same in all lanes of the group
+  if (odd) {
     m = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t b = __float_as_uint(x[i]) & 0x7fffffffu;
-      if (b >= 0x7f800000u) {
-        bad = true;
-        x[i] = __uint_as_float(0x7fffffffu);
-      } else {
-        if (b > kTop) x[i] = copysignf(__uint_as_float(kTop), x[i]);
-        m = max(m, min(b, kTop));
+    for (int y = 0; y < 2; ++y) {
+      float x[8];
+      unpack8(v[y], x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t b = __float_as_uint(x[i]) & 0x7fffffffu;
+        if (b >= 0x7f800000u) bad = true;
+        else m = max(m, min(b, kTop));
       }
     }
     for (int o = 1; o < L; o <<= 1) m = max(m, __shfl_xor_sync(group, m, o));
   }
   scale = scale_byte(m);
   const float f = __uint_as_float((254u - scale) << 23);   // 2^-e, a normal number
-  uint2 c;
-  c.x = codes2(x[0] * f, x[1] * f) | codes2(x[2] * f, x[3] * f) << 16;
-  c.y = codes2(x[4] * f, x[5] * f) | codes2(x[6] * f, x[7] * f) << 16;
-  return c;
+#pragma unroll
+  for (int y = 0; y < 2; ++y) {
+    float x[8];
+    unpack8(v[y], x);
+    if (odd) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t b = __float_as_uint(x[i]) & 0x7fffffffu;
+        if (b >= 0x7f800000u) x[i] = __uint_as_float(0x7fffffffu);
+        else if (b > kTop) x[i] = copysignf(__uint_as_float(kTop), x[i]);
+      }
+    }
+    c[y].x = codes2(x[0] * f, x[1] * f) | codes2(x[2] * f, x[3] * f) << 16;
+    c[y].y = codes2(x[4] * f, x[5] * f) | codes2(x[6] * f, x[7] * f) << 16;
+  }
 }
 
 struct QuantArgs {
@@ -150,68 +174,61 @@ struct QuantArgs {
   int N, D, table_rows, lpr_log2;
 };
 
-// One item is a (token, head) of the fresh rows, K and V; a lane group takes kU of them
-// at a time.
-template <bool kF32, bool kRope, int kU>
+// One item is a (token, head) of the fresh rows, K and V.
+template <bool kF32, bool kRope>
 __global__ void __launch_bounds__(kThreads)
 kv_quant_scatter_kernel(const QuantArgs a) {
   pdl_wait();
   const int L = 1 << a.lpr_log2, lane = threadIdx.x & 31, c = lane & (L - 1);
   const unsigned group = (L == 32 ? 0xffffffffu : ((1u << L) - 1)) << (lane & ~(L - 1));
-  const bool in = 8 * c < a.D;
+  const bool in[2] = {8 * c < a.D, 8 * (c + L) < a.D};
   const unsigned step = (gridDim.x * (unsigned)kThreads) >> a.lpr_log2;
   const unsigned first = (blockIdx.x * (unsigned)kThreads + threadIdx.x) >> a.lpr_log2;
-  for (unsigned long long i0 = first; i0 < a.items; i0 += (unsigned long long)step * kU) {
-    Eight<kF32> k[kU], v[kU];
-    int slot[kU], trow[kU];
+  for (unsigned long long i = first; i < a.items; i += step) {   // the same in all lanes of a group
+    const unsigned j = quotient((unsigned)i, a.heads), h = (unsigned)i - j * a.heads.d;
+    const int slot = __ldg(a.idx + j);
+    const int trow = !kRope ? 0 : a.tidx ? __ldg(a.tidx + j) : slot;
+    Eight<kF32> k[2] = {}, v[2] = {};
+    const size_t at = (size_t)i * a.D + 8 * c;
 #pragma unroll
-    for (int u = 0; u < kU; ++u) {
-      const unsigned long long i = i0 + (unsigned long long)u * step;
-      slot[u] = trow[u] = -1;
-      k[u] = v[u] = {};
-      if (i < a.items) {
-        const unsigned j = quotient((unsigned)i, a.heads);
-        slot[u] = __ldg(a.idx + j);
-        if (kRope) trow[u] = a.tidx ? __ldg(a.tidx + j) : slot[u];
-        if (in) {
-          const size_t at = (size_t)i * a.D + 8 * c;
-          k[u] = load8<kF32>(a.kf, at);
-          v[u] = load8<kF32>(a.vf, at);
-        }
+    for (int y = 0; y < 2; ++y)
+      if (in[y]) {
+        k[y] = load8<kF32>(a.kf, at + 8 * L * y);
+        v[y] = load8<kF32>(a.vf, at + 8 * L * y);
       }
+    if (slot < 0 || slot >= a.N || (kRope && (trow < 0 || trow >= a.table_rows))) {
+      set_error(a.err, kErrIndex);
+      continue;
     }
+    if (kRope) {
+      const float4 *t = reinterpret_cast<const float4 *>(a.table + (size_t)trow * a.D) + 2 * c;
 #pragma unroll
-    for (int u = 0; u < kU; ++u) {
-      const unsigned long long i = i0 + (unsigned long long)u * step;
-      if (i >= a.items) continue;                        // the same in all lanes of a group
-      if (slot[u] < 0 || slot[u] >= a.N || (kRope && (trow[u] < 0 || trow[u] >= a.table_rows))) {
-        set_error(a.err, kErrIndex);
-        continue;
+      for (int y = 0; y < 2; ++y)
+        if (in[y]) {
+          const float4 t0 = __ldg(t + 2 * L * y), t1 = __ldg(t + 2 * L * y + 1);
+          uint4 &w = k[y].w[0];
+          w.x = rotate2(w.x, t0.x, t0.y);
+          w.y = rotate2(w.y, t0.z, t0.w);
+          w.z = rotate2(w.z, t1.x, t1.y);
+          w.w = rotate2(w.w, t1.z, t1.w);
+        }
+    }
+    bool bad = false;
+    unsigned sk, sv;
+    uint2 ck[2], cv[2];
+    quantise<kF32>(k, L, group, ck, sk, bad);
+    quantise<kF32>(v, L, group, cv, sv, bad);
+    if (bad) set_error(a.err, kErrNonfinite);
+    const size_t row = (size_t)slot * a.heads.d + h, to = row * a.D + 8 * c;
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+      if (in[y]) {
+        *reinterpret_cast<uint2 *>(a.kc + to + 8 * L * y) = ck[y];
+        *reinterpret_cast<uint2 *>(a.vc + to + 8 * L * y) = cv[y];
       }
-      if (kRope && in) {
-        const float4 *t = reinterpret_cast<const float4 *>(a.table + (size_t)trow[u] * a.D) + 2 * c;
-        const float4 t0 = __ldg(t), t1 = __ldg(t + 1);
-        uint4 &w = k[u].w[0];
-        w.x = rotate2(w.x, t0.x, t0.y);
-        w.y = rotate2(w.y, t0.z, t0.w);
-        w.z = rotate2(w.z, t1.x, t1.y);
-        w.w = rotate2(w.w, t1.z, t1.w);
-      }
-      bool bad = false;
-      unsigned sk, sv;
-      const uint2 ck = quantise<kF32>(k[u], L, group, sk, bad);
-      const uint2 cv = quantise<kF32>(v[u], L, group, sv, bad);
-      if (bad) set_error(a.err, kErrNonfinite);
-      const unsigned h = (unsigned)i - quotient((unsigned)i, a.heads) * a.heads.d;
-      const size_t row = (size_t)slot[u] * a.heads.d + h;
-      if (in) {
-        *reinterpret_cast<uint2 *>(a.kc + row * a.D + 8 * c) = ck;
-        *reinterpret_cast<uint2 *>(a.vc + row * a.D + 8 * c) = cv;
-      }
-      if (c == 0) {
-        a.ks[row] = (uint8_t)sk;
-        a.vs[row] = (uint8_t)sv;
-      }
+    if (c == 0) {
+      a.ks[row] = (uint8_t)sk;
+      a.vs[row] = (uint8_t)sv;
     }
   }
 }
@@ -304,7 +321,7 @@ unsigned grid_for(unsigned items, int lpr_log2, int kU, int per_sm) {
   return (unsigned)(need < 1 ? 1 : need < cap ? need : cap);
 }
 
-constexpr int kU = 2;
+constexpr int kU = 2;        // items of a lane at a time, reading back
 constexpr int kBlocks = 32;
 
 // Sizes that both calls take; 1 where there is nothing to do.
@@ -353,12 +370,12 @@ extern "C" int hsa_kv_quant_scatter(void *k_cache, void *v_cache, uint8_t *k_sca
   a.N = N;
   a.D = D;
   a.table_rows = table_rows;
-  a.lpr_log2 = log2i(D / 8);
+  a.lpr_log2 = log2i((D / 8 + 1) / 2);
   count_launches(1);
-  launch_pdl(dtype == HSA_F32 ? kv_quant_scatter_kernel<true, false, kU>
-             : table          ? kv_quant_scatter_kernel<false, true, kU>
-                              : kv_quant_scatter_kernel<false, false, kU>,
-             dim3(grid_for(a.items, a.lpr_log2, kU, kBlocks)), dim3(kThreads), 0,
+  launch_pdl(dtype == HSA_F32 ? kv_quant_scatter_kernel<true, false>
+             : table          ? kv_quant_scatter_kernel<false, true>
+                              : kv_quant_scatter_kernel<false, false>,
+             dim3(grid_for(a.items, a.lpr_log2, 1, kBlocks)), dim3(kThreads), 0,
              (cudaStream_t)stream, a);
   return launch_status();
 }

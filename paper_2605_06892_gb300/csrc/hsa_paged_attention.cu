@@ -94,6 +94,9 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool ok) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0)
                : "memory");
 }
+__device__ __forceinline__ void copy4(uint32_t dst, const void *src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int n>
 __device__ __forceinline__ void wait_all_but() {
@@ -121,12 +124,13 @@ struct Cfg {
   static constexpr int kChunks = kRowBytes / 16;               // 16-byte chunks per row
   static constexpr int kKW = kRowBytes == 256 ? 16 : 32;       // keys per warp and tile
   static constexpr int kTile = kWarps * kKW;                   // keys per tile
-  static constexpr int kStages = kRowBytes == 64 ? 4 : 3;
+  static constexpr int kStages = 2;
+  static constexpr int kBlocks = kNR == 1 ? (D == 64 ? 4 : 3) : 2;   // per SM: registers
   static constexpr int kHalf = kKW * kRowBytes;                // K (or V) bytes of a stage
-  static constexpr int kScales = kF8 ? kKW * 8 : 0;            // (2^ks, vs) per key
+  static constexpr int kScales = kF8 ? kKW * 16 : 0;           // per key four words
   static constexpr int kStage = 2 * kHalf + kScales;
-  static constexpr int kMergeO = kRows * D * 4;                // O of one warp
-  static constexpr int kSmem = kWarps * kStages * kStage + kMergeO;
+  static constexpr int kQ = kRows * D * 2;                     // a unit's query rows
+  static constexpr int kSmem = kWarps * kStages * kStage + kStages * kQ;
 };
 
 // The key (row of an 8-key block) of MMA index n.  The 16-byte loads of K (a quarter-warp:
@@ -162,21 +166,29 @@ struct Args {
   unsigned *err;
   int batch, n_new, Hq, Hkv, rows, row_tiles;   // rows = n_new G
   Divider group;                                // by G = Hq / Hkv
-  int n_pages, page_log2, max_pages;
+  int n_pages, page_log2, max_pages, sms;
   float scale_log2;
 };
 
-// What every block of a launch derives from the lengths: the number of tiles, and this
-// tile's (or sequence's) place among them.
+// What every block of a launch derives from the lengths: the key tiles of all units, cut
+// into `ctas` runs of `base` or base + 1 tiles.  A tile per block up to one block per SM,
+// then at least two, which overlap (one token against 4001 keys of 8 heads 10.3 us, 11.7
+// with 456 blocks of one or two).
 struct Plan {
-  long long total;     // key tiles of all units
-  int ctas;            // blocks with work: min(gridDim, total)
+  int total, ctas, base, more;     // more: how many runs have one tile more, the first ones
 };
-__device__ __forceinline__ long long first_tile(const Plan &p, int cta) {
-  return (long long)cta * p.total / p.ctas;
+__device__ __forceinline__ Plan plan_of(int total, int grid, int sms) {
+  Plan p;
+  p.total = total;
+  p.ctas = max(1, min(grid, max(min(total, sms), total / 2)));
+  p.base = total / p.ctas;
+  p.more = total - p.base * p.ctas;
+  return p;
 }
-__device__ __forceinline__ int cta_of(const Plan &p, long long tile) {
-  return (int)(((tile + 1) * p.ctas - 1) / p.total);
+__device__ __forceinline__ int first_tile(const Plan &p, int cta) { return cta * p.base + min(cta, p.more); }
+__device__ __forceinline__ int cta_of(const Plan &p, int tile) {
+  const int longer = p.more * (p.base + 1);
+  return tile < longer ? tile / (p.base + 1) : p.more + (tile - longer) / p.base;
 }
 
 // len_b, checked: negative, or more than the table's pages hold.
@@ -188,34 +200,6 @@ __device__ __forceinline__ int length(const Args &a, int b) {
     return n < 0 ? 0 : (int)most;
   }
   return n;
-}
-
-// Sums the sequences' tiles over the block: `before` is what comes before this thread's
-// own run of sequences [b0, b1), `total` all of them.
-__device__ __forceinline__ void scan_tiles(const Args &a, int tile, int &b0, int &b1, long long &before,
-                                           long long &mine, long long &total, long long *sh) {
-  const int per = (a.batch + kThreads - 1) / kThreads;
-  b0 = min(a.batch, (int)threadIdx.x * per);
-  b1 = min(a.batch, b0 + per);
-  mine = 0;
-  for (int b = b0; b < b1; ++b) mine += (length(a, b) + tile - 1) / tile;
-  mine *= (long long)a.Hkv * a.row_tiles;
-  long long x = mine;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const long long y = __shfl_up_sync(0xffffffffu, x, o);
-    if (lane >= o) x += y;
-  }
-  if (lane == 31) sh[warp] = x;
-  __syncthreads();
-  before = x - mine;
-  total = 0;
-#pragma unroll
-  for (int w = 0; w < kWarps; ++w) {
-    if (w < warp) before += sh[w];
-    total += sh[w];
-  }
 }
 
 // A place in the row of key tiles.
@@ -246,42 +230,61 @@ __device__ __forceinline__ void clear_empty(const Args &a) {
 }
 
 template <int D, bool kF8, int kNR>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, (Cfg<D, kF8, kNR>::kBlocks))
 paged_attention_kernel(const Args a) {
   using C = Cfg<D, kF8, kNR>;
   constexpr int kCh = C::kChunks, kNB = C::kKW / 16, kSteps = D / 16, kNT = D / 8, kMT = D / 16;
   constexpr int kRows = C::kRows;
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ long long sh_sum[kWarps];
-  __shared__ int sh_b;
-  __shared__ long long sh_off;
+  __shared__ int sh_sum[kWarps], sh_at[3];
   __shared__ float sh_m[kWarps][kRows], sh_l[kWarps][kRows];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   uint8_t *ring = smem + warp * (C::kStages * C::kStage);
-  float *merge = reinterpret_cast<float *>(smem + kWarps * C::kStages * C::kStage);
   pdl_wait();
   pdl_trigger();   // the join's blocks wait beside this kernel's, which are all resident by then
 
-  // ---- this block's run of tiles
+  // ---- this block's run of tiles: thread x counts those of a run of sequences, and the
+  // one whose sequences the block's first tile falls into says where
   Plan plan;
   {
-    int b0, b1;
-    long long before, mine;
-    scan_tiles(a, C::kTile, b0, b1, before, mine, plan.total, sh_sum);
-    plan.ctas = (int)min((long long)gridDim.x, plan.total);
-    if ((int)blockIdx.x >= plan.ctas) {
+    const int per = (a.batch + kThreads - 1) / kThreads;
+    const int b0 = min(a.batch, (int)threadIdx.x * per), b1 = min(a.batch, b0 + per);
+    const int per_tile = a.Hkv * a.row_tiles;
+    int first_len = 0, mine = 0;
+    for (int b = b0; b < b1; ++b) {
+      const int n = length(a, b);
+      if (b == b0) first_len = n;
+      mine += (n + C::kTile - 1) / C::kTile * per_tile;
+    }
+    int end = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, end, o);
+      if (lane >= o) end += y;
+    }
+    if (lane == 31) sh_sum[warp] = end;
+    __syncthreads();
+    int total = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      if (w < warp) end += sh_sum[w];
+      total += sh_sum[w];
+    }
+    plan = plan_of(total, gridDim.x, a.sms);
+    if (total == 0 || (int)blockIdx.x >= plan.ctas) {
       if (threadIdx.x == 0) a.cuts[blockIdx.x].parts = 0;
       clear_empty<D>(a);
       return;
     }
-    const long long at = first_tile(plan, blockIdx.x);
-    if (at >= before && at < before + mine) {
-      const long long per_tile = (long long)a.Hkv * a.row_tiles;
-      for (int b = b0; b < b1; ++b) {
-        const long long n = (long long)((length(a, b) + C::kTile - 1) / C::kTile) * per_tile;
+    const int at = first_tile(plan, blockIdx.x);
+    if (at >= end - mine && at < end) {
+      int before = end - mine, len = first_len;
+      for (int b = b0;; len = length(a, ++b)) {
+        const int n = (len + C::kTile - 1) / C::kTile * per_tile;
         if (at < before + n) {
-          sh_b = b;
-          sh_off = at - before;
+          sh_at[0] = b;
+          sh_at[1] = len;
+          sh_at[2] = at - before;
           break;
         }
         before += n;
@@ -289,76 +292,113 @@ paged_attention_kernel(const Args a) {
     }
     __syncthreads();
   }
-  const int n_tiles = (int)(first_tile(plan, blockIdx.x + 1) - first_tile(plan, blockIdx.x));
+  const int n_tiles = first_tile(plan, blockIdx.x + 1) - first_tile(plan, blockIdx.x);
   Cursor cur;
-  cur.b = sh_b;
-  cur.len = length(a, cur.b);
+  cur.b = sh_at[0];
+  cur.len = sh_at[1];
   cur.tiles = (cur.len + C::kTile - 1) / C::kTile;
-  cur.unit = (int)(sh_off / cur.tiles);
-  cur.tile = (int)(sh_off - (long long)cur.unit * cur.tiles);
+  cur.unit = sh_at[2] / cur.tiles;
+  cur.tile = sh_at[2] - cur.unit * cur.tiles;
   CutUnit cut = {};
 
-  // ---- the ring: `ahead` is the next tile to load; the page of this lane's key in it is
-  // read one tile before its use
+  // ---- the ring: `ahead` is the next tile to load; the pages of this lane's keys in it are
+  // read one tile before their use, and looked at only then
   Cursor ahead = cur;
-  int loaded = 0;
+  int left = n_tiles;                       // tiles to load
+  uint32_t fill = 0;                        // where the next one goes: offset of its stage
+  constexpr int kPer = C::kKW > 32 ? 2 : 1; // keys that a lane looks up: krow + 32 x
+  constexpr int kStep = 32 / kCh;           // rows that a warp copies at a time
   const int krow = lane & (C::kKW - 1);
-  auto page_of = [&](const Cursor &c) -> int {
-    const int key = c.tile * C::kTile + warp * C::kKW + krow;
-    if (key >= c.len) return -1;
-    const int p = __ldg(a.table + (size_t)c.b * a.max_pages + (key >> a.page_log2));
-    if (p < 0 || p >= a.n_pages) {
-      set_error(a.err, kErrIndex);
-      return -1;
+  const uint32_t ring_s = smem_addr(ring);
+  const unsigned row_stride = a.Hkv * C::kRowBytes;
+  // this lane's chunk of rows lane / kCh + kStep i, in K's order and in V's; the swizzles
+  // repeat after eight rows
+  uint32_t to_k[kStep < 8 ? 8 / kStep : 1], to_v[kStep < 8 ? 8 / kStep : 1];
+#pragma unroll
+  for (int i = 0; i < (kStep < 8 ? 8 / kStep : 1); ++i) {
+    const int row = lane / kCh + kStep * i;
+    to_k[i] = row * C::kRowBytes + 16 * k_chunk<kCh>(lane % kCh, row);
+    to_v[i] = row * C::kRowBytes + 16 * v_chunk<kCh>(lane % kCh, row) + C::kHalf;
+  }
+  int page[kPer];
+  auto look_up = [&]() {
+#pragma unroll
+    for (int x = 0; x < kPer; ++x) {
+      const int key = ahead.tile * C::kTile + warp * C::kKW + krow + 32 * x;
+      page[x] = key < ahead.len
+                    ? __ldg(a.table + (size_t)ahead.b * a.max_pages + (key >> a.page_log2)) : -1;
     }
-    return p;
   };
-  int page = page_of(ahead);
-  unsigned ks_byte = 127, vs_byte = 127;   // of the tile loaded last, not yet in its stage
-  auto put_scales = [&]() {
-    if (kF8 && loaded > 0 && lane < C::kKW) {
-      *reinterpret_cast<float2 *>(ring + ((loaded - 1) % C::kStages) * C::kStage + 2 * C::kHalf +
-                                  8 * lane) =
-          make_float2(__uint_as_float(ks_byte ? ks_byte << 23 : 0x00400000u),
-                      (float)((int)vs_byte - 127));
-    }
-  };
+  look_up();
+  int q_fill = 0, q_now = 0;                // buffers of the next unit's rows, and of this one's
+  uint8_t *sq = smem + kWarps * C::kStages * C::kStage;
   auto load_tile = [&]() {
-    put_scales();
-    if (loaded < n_tiles) {
-      const int key = ahead.tile * C::kTile + warp * C::kKW + krow;
-      const int slot = page < 0 ? -1 : (page << a.page_log2) + (key & ((1 << a.page_log2) - 1));
+    if (left > 0) {
       const int h = ahead.unit / a.row_tiles;
-      const uint32_t dst = smem_addr(ring + (loaded % C::kStages) * C::kStage);
-      if (kF8) {
-        ks_byte = vs_byte = 127;
-        if (slot >= 0 && lane < C::kKW) {
-          ks_byte = a.ks[(size_t)slot * a.Hkv + h];
-          vs_byte = a.vs[(size_t)slot * a.Hkv + h];
+      if (ahead.tile == 0 || left == n_tiles) {
+        // The unit's query rows come with its first tile here, a chunk or more per thread:
+        // rows past the last are zeros.  Chunk c of row r lies at c ^ (r & 7).
+        const int r0 = (ahead.unit - h * a.row_tiles) * kRows;
+        const uint32_t to = smem_addr(sq + q_fill * C::kQ);
+#pragma unroll
+        for (int e0 = 0; e0 < kRows * (D / 8); e0 += kThreads) {
+          const int e = e0 + threadIdx.x, r = e / (D / 8), c = e % (D / 8);
+          if (kRows * (D / 8) % kThreads != 0 && e >= kRows * (D / 8)) break;
+          const bool ok = r0 + r < a.rows;
+          const int i = ok ? quotient(r0 + r, a.group) : 0, head = ok ? r0 + r - i * (int)a.group.d : 0;
+          copy16(to + r * (2 * D) + 16 * (c ^ (r & 7)),
+                 a.q + ((size_t)((size_t)ahead.b * a.n_new + i) * a.Hq + h * (int)a.group.d + head) * D + 8 * c, ok);
+        }
+        q_fill = q_fill + 1 == C::kStages ? 0 : q_fill + 1;
+      }
+      int slot[kPer];
+      unsigned have[kPer];                  // rows that there are
+#pragma unroll
+      for (int x = 0; x < kPer; ++x) {
+        const int key = ahead.tile * C::kTile + warp * C::kKW + krow + 32 * x;
+        const bool ok = page[x] >= 0 && page[x] < a.n_pages;
+        if (!ok && key < ahead.len) set_error(a.err, kErrIndex);
+        slot[x] = ok ? (page[x] << a.page_log2) + (key & ((1 << a.page_log2) - 1)) : 0;
+        have[x] = __ballot_sync(0xffffffffu, ok);
+        if (kF8 && lane < C::kKW) {
+          // The aligned words around the key's scale bytes, and the bytes' place in them:
+          // the bytes need not be waited for here.  A word that holds a byte of the scales
+          // can be read whole, whatever the other three are.  No page: a row of zeros,
+          // times one.
+          const size_t at = (size_t)slot[x] * a.Hkv + h;
+          const uintptr_t ks = (uintptr_t)(a.ks + at), vs = (uintptr_t)(a.vs + at);
+          uint32_t *to = reinterpret_cast<uint32_t *>(ring + fill + 2 * C::kHalf) + 4 * (lane + 32 * x);
+          if (ok) {
+            copy4(smem_addr(to), (const void *)(ks & ~(uintptr_t)3));
+            copy4(smem_addr(to + 1), (const void *)(vs & ~(uintptr_t)3));
+          } else {
+            to[0] = to[1] = 0x7f7f7f7fu;
+          }
+          to[2] = (uint32_t)(ks & 3) * 8 + ((uint32_t)(vs & 3) * 8 << 16);
         }
       }
+      const uint8_t *kb = a.k + (size_t)h * C::kRowBytes + 16 * (lane % kCh);
+      const uint8_t *vb = a.v + (size_t)h * C::kRowBytes + 16 * (lane % kCh);
 #pragma unroll
-      for (int i = 0; i < C::kKW * kCh / 32; ++i) {
-        const int e = 32 * i + lane, row = e / kCh, c = e % kCh;
-        const int s = __shfl_sync(0xffffffffu, slot, row);
-        const size_t at = ((size_t)max(s, 0) * a.Hkv + h) * C::kRowBytes + 16 * c;
-        copy16(dst + row * C::kRowBytes + 16 * k_chunk<kCh>(c, row), a.k + at, s >= 0);
-        copy16(dst + C::kHalf + row * C::kRowBytes + 16 * v_chunk<kCh>(c, row), a.v + at, s >= 0);
+      for (int i = 0; i < C::kKW / kStep; ++i) {
+        constexpr int kCycle = kStep < 8 ? 8 / kStep : 1;
+        const int row = lane / kCh + kStep * i;
+        const unsigned at = __shfl_sync(0xffffffffu, slot[kStep * i / 32], row & 31);
+        const bool ok = have[kStep * i / 32] >> (row & 31) & 1;
+        const uint32_t dst = ring_s + fill + (i / kCycle) * (kCycle * kStep * C::kRowBytes);
+        copy16(dst + to_k[i % kCycle], kb + (uint64_t)at * row_stride, ok);
+        copy16(dst + to_v[i % kCycle], vb + (uint64_t)at * row_stride, ok);
       }
-      ++loaded;
-      if (loaded < n_tiles) {
+      fill = fill + C::kStage == C::kStages * C::kStage ? 0 : fill + C::kStage;
+      if (--left > 0) {
         step(a, ahead, C::kTile);
-        page = page_of(ahead);
+        look_up();
       }
-    } else if (kF8) {
-      loaded = -1;   // the last tile's scales are in place
     }
     commit();
   };
 #pragma unroll
-  for (int s = 0; s < C::kStages - 1; ++s)
-    if (loaded >= 0) load_tile();
-    else commit();
+  for (int s = 0; s < C::kStages - 1; ++s) load_tile();
 
   // ---- per unit state; column block x of the MMAs holds rows 8 x .. 8 x + 7, and this
   // lane row 8 x + g of Q^T and P^T, rows 8 x + 2 t + j of S^T and O^T
@@ -367,24 +407,29 @@ paged_attention_kernel(const Args a) {
   int limit[kNR][2];     // keys that rows 8 x + 2 t + j see
   int unit_tile0 = 0;    // the unit's tile that this run of it starts with
   bool fresh = true, first_unit = true;
+  uint32_t now = 0;      // the stage of tile `it`
 
   for (int it = 0; it < n_tiles; ++it) {
+    wait_all_but<C::kStages - 2>();
+    if (fresh) __syncthreads();   // the query rows are every thread's copies
+    else __syncwarp();
+    load_tile();
+
     if (fresh) {
       fresh = false;
       unit_tile0 = cur.tile;
-      const int h = cur.unit / a.row_tiles, r0 = (cur.unit - h * a.row_tiles) * kRows;
+      const int r0 = (cur.unit % a.row_tiles) * kRows;
+      const uint32_t from = smem_addr(sq + q_now * C::kQ);
+      q_now = q_now + 1 == C::kStages ? 0 : q_now + 1;
 #pragma unroll
       for (int x = 0; x < kNR; ++x) {
-        const int r = r0 + 8 * x + g, i = quotient(r, a.group);
-        const uint2 *src = reinterpret_cast<const uint2 *>(
-            a.q + ((size_t)((size_t)cur.b * a.n_new + i) * a.Hq + h * (int)a.group.d + (r - i * (int)a.group.d)) * D);
+        const int r = 8 * x + g;
         float big = 0.f;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
           // dimensions of K = 16 step s that this lane's fragments hold
           const int d = kF8 ? 16 * (t + 4 * (s / 4)) + 4 * (s % 4) : 8 * (t + 4 * (s / 2)) + 4 * (s % 2);
-          uint2 w = make_uint2(0u, 0u);
-          if (r < a.rows) w = __ldg(src + d / 4);
+          const uint2 w = lds64(from + r * (2 * D) + 16 * ((d / 8) ^ (r & 7)) + (d & 4) * 2);
           qf[s][x][0] = w.x;
           qf[s][x][1] = w.y;
           if (kF8)
@@ -418,17 +463,22 @@ paged_attention_kernel(const Args a) {
       }
     }
 
-    wait_all_but<C::kStages - 2>();
-    __syncwarp();
-    if (loaded >= 0) load_tile();
-    else commit();
-
     const int key0 = cur.tile * C::kTile + warp * C::kKW;
     if (key0 < cur.len) {
-      const uint32_t sk = smem_addr(ring + (it % C::kStages) * C::kStage);
-      const uint32_t sv = sk + C::kHalf;
-      const float2 *scales = reinterpret_cast<const float2 *>(ring + (it % C::kStages) * C::kStage +
-                                                              2 * C::kHalf);
+      const uint32_t sk = ring_s + now, sv = sk + C::kHalf;
+      uint4 *scales = reinterpret_cast<uint4 *>(ring + now + 2 * C::kHalf);
+      if (kF8) {
+        // each lane makes 2^ks, vs and 2^-vs of its key's scale bytes (within [27, 247])
+#pragma unroll
+        for (int x = 0; x < kPer; ++x)
+          if (lane < C::kKW) {
+            const uint4 w = scales[lane + 32 * x];
+            const uint32_t ks = w.x >> (w.z & 0xffffu) & 255u, vs = w.y >> (w.z >> 16) & 255u;
+            scales[lane + 32 * x] =
+                make_uint4(ks << 23, __float_as_uint((float)((int)vs - 127)), (254u - vs) << 23, 0u);
+          }
+        __syncwarp();
+      }
       // ---- scores: MMA row n (n + 8) of block b is key 16 b + key_of(n) (+ 8)
       float s[kNB][kNR][4];
 #pragma unroll
@@ -469,8 +519,8 @@ paged_attention_kernel(const Args a) {
           const int row = 16 * b + 8 * n + key_of<kCh>(g);
           float kf = 1.f, ve = 0.f;
           if (kF8) {
-            const float2 f = scales[row];
-            kf = f.x, ve = f.y, vinv[b][n] = fast_exp2(-ve);
+            const uint4 w = scales[row];
+            kf = __uint_as_float(w.x), ve = __uint_as_float(w.y), vinv[b][n] = __uint_as_float(w.z);
           }
 #pragma unroll
           for (int x = 0; x < kNR; ++x)
@@ -478,10 +528,29 @@ paged_attention_kernel(const Args a) {
             for (int j = 0; j < 2; ++j) {
               float &y = s[b][x][2 * n + j];
               y = kF8 ? fmaf(y * kf, c2[x][j], ve) : y * c2[x][j];
-              if (ragged && key0 + row >= limit[x][j]) y = -INFINITY;
-              mx[x][j] = fmaxf(mx[x][j], y);
             }
         }
+      if (!ragged) {
+#pragma unroll
+        for (int b = 0; b < kNB; ++b)
+#pragma unroll
+          for (int x = 0; x < kNR; ++x)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) mx[x][j] = fmaxf(mx[x][j], fmaxf(s[b][x][j], s[b][x][2 + j]));
+      } else {
+#pragma unroll
+        for (int b = 0; b < kNB; ++b)
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int x = 0; x < kNR; ++x)
+#pragma unroll
+              for (int j = 0; j < 2; ++j) {
+                float &y = s[b][x][2 * n + j];
+                if (key0 + 16 * b + 8 * n + key_of<kCh>(g) >= limit[x][j]) y = -INFINITY;
+                mx[x][j] = fmaxf(mx[x][j], y);
+              }
+      }
       bool moved = false;
 #pragma unroll
       for (int x = 0; x < kNR; ++x)
@@ -620,7 +689,10 @@ paged_attention_kernel(const Args a) {
 
     const bool unit_done = cur.tile + 1 == cur.tiles;
     if (unit_done || it + 1 == n_tiles) {
-      // ---- the unit's end, or the run's: the four warps' parts become one in warp 0
+      // ---- the unit's end, or the run's: the four warps' parts become one.  Each leaves its
+      // sums in the stage that it has just read, lane by lane, and takes a quarter of the
+      // dimensions of all four.  The stage is filled again only after the barrier that
+      // starts the next unit.
       const int h = cur.unit / a.row_tiles, r0 = (cur.unit - h * a.row_tiles) * kRows;
 #pragma unroll
       for (int x = 0; x < kNR; ++x)
@@ -633,108 +705,95 @@ paged_attention_kernel(const Args a) {
             sh_l[warp][8 * x + 2 * t + j] = l[x][j];
           }
         }
-      __syncthreads();
-      float M[kNR][2], sum[kNR][2];
+      constexpr int kQuarter = kMT / kWarps;                // MMA blocks of 16 dimensions
+      constexpr int kFit = C::kStage / (kMT * 512);         // column blocks whose sums fit
+      constexpr int kAt = kFit < 1 ? 0 : kFit < kNR ? kFit : kNR;
+      static_assert(kAt > 0 && kNR % kAt == 0, "a stage takes the sums of a column block");
+      const bool whole = unit_tile0 == 0 && unit_done;
+      float *part = a.ws + (size_t)(2 * blockIdx.x + (first_unit ? 0 : 1)) * (kRows * (D + 2));
 #pragma unroll
-      for (int x = 0; x < kNR; ++x)
+      for (int x0 = 0; x0 < kNR; x0 += kAt) {
+        if (x0) __syncthreads();
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int r = 8 * x + 2 * t + j;
-          M[x][j] = sh_m[0][r];
+        for (int n = 0; n < kMT; ++n)
 #pragma unroll
-          for (int w = 1; w < kWarps; ++w) M[x][j] = fmaxf(M[x][j], sh_m[w][r]);
-          sum[x][j] = 0.f;
-#pragma unroll
-          for (int w = 0; w < kWarps; ++w) sum[x][j] += sh_l[w][r] * fast_exp2(sh_m[w][r] - M[x][j]);
-          const float f = fast_exp2(m[x][j] - M[x][j]);
-#pragma unroll
-          for (int n = 0; n < kMT; ++n) o[n][x][j] *= f, o[n][x][2 + j] *= f;
-        }
-      // lane-major: each lane adds the same lane's sums of another warp, by way of a buffer
-      // of one warp's O
-      auto at = [&](int n, int x) { return reinterpret_cast<float4 *>(merge) + (n * kNR + x) * 32 + lane; };
-      auto put = [&](int n, int to) {
-#pragma unroll
-        for (int x = 0; x < kNR; ++x) *at(to, x) = make_float4(o[n][x][0], o[n][x][1], o[n][x][2], o[n][x][3]);
-      };
-      auto add = [&](int n, int from) {
-#pragma unroll
-        for (int x = 0; x < kNR; ++x) {
-          const float4 z = *at(from, x);
-          o[n][x][0] += z.x, o[n][x][1] += z.y, o[n][x][2] += z.z, o[n][x][3] += z.w;
-        }
-      };
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {   // warp 2 to 0 and 3 to 1, in halves
-        if (warp >= 2) {
-#pragma unroll
-          for (int n = 0; n < kMT / 2; ++n) put(half * (kMT / 2) + n, (warp & 1) * (kMT / 2) + n);
-        }
+          for (int x = 0; x < kAt; ++x) {
+            const float(&y)[4] = o[n][x0 + x];
+            reinterpret_cast<float4 *>(ring + now)[(n * kAt + x) * 32 + lane] = make_float4(y[0], y[1], y[2], y[3]);
+          }
         __syncthreads();
-        if (warp < 2) {
 #pragma unroll
-          for (int n = 0; n < kMT / 2; ++n) add(half * (kMT / 2) + n, warp * (kMT / 2) + n);
-        }
-        __syncthreads();
-      }
-      if (warp == 1) {
+        for (int x = x0; x < x0 + kAt; ++x) {
+          float f[2][kWarps], M[2], sum[2];
 #pragma unroll
-        for (int n = 0; n < kMT; ++n) put(n, n);
-      }
-      __syncthreads();
-      if (warp == 0) {
+          for (int j = 0; j < 2; ++j) {
+            const int r = 8 * x + 2 * t + j;
+            M[j] = sh_m[0][r];
 #pragma unroll
-        for (int n = 0; n < kMT; ++n) add(n, n);
-      }
-      if (warp == 0) {
-        const bool whole = unit_tile0 == 0 && unit_done;
-        float *part = a.ws + (size_t)(2 * blockIdx.x + (first_unit ? 0 : 1)) * (kRows * (D + 2));
+            for (int w = 1; w < kWarps; ++w) M[j] = fmaxf(M[j], sh_m[w][r]);
+            sum[j] = 0.f;
 #pragma unroll
-        for (int x = 0; x < kNR; ++x)
+            for (int w = 0; w < kWarps; ++w) {
+              f[j][w] = fast_exp2(sh_m[w][r] - M[j]);
+              sum[j] = fmaf(sh_l[w][r], f[j][w], sum[j]);
+            }
+          }
+          float y[kQuarter][4];
+#pragma unroll
+          for (int n = 0; n < kQuarter; ++n) {
+            y[n][0] = y[n][1] = y[n][2] = y[n][3] = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+              const float4 z = reinterpret_cast<const float4 *>(
+                  smem + w * (C::kStages * C::kStage) + now)[((warp * kQuarter + n) * kAt + x - x0) * 32 + lane];
+              y[n][0] = fmaf(z.x, f[0][w], y[n][0]), y[n][1] = fmaf(z.y, f[1][w], y[n][1]);
+              y[n][2] = fmaf(z.z, f[0][w], y[n][2]), y[n][3] = fmaf(z.w, f[1][w], y[n][3]);
+            }
+          }
+          // block n holds dimensions E g + 2 n and the next (bf16: + 56 from n = 4 on)
+          constexpr int kE = kF8 ? kNT : 8;
+          const int n0 = warp * kQuarter, d = kE * g + (kE == 8 ? (n0 / 4) * 64 + 2 * (n0 % 4) : 2 * n0);
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             const int rr = 8 * x + 2 * t + j, r = r0 + rr;
             if (r >= a.rows) continue;
-            const float sm = sum[x][j], inv = sm > 0.f ? 1.f / sm : sm == 0.f ? 0.f : sm;
-            const int i = quotient(r, a.group);
-            __nv_bfloat16 *dst = a.out + ((size_t)((size_t)cur.b * a.n_new + i) * a.Hq + h * (int)a.group.d +
-                                          (r - i * (int)a.group.d)) * D;
-            // eight neighbouring dimensions from four MMA blocks
-            constexpr int kE = kF8 ? kNT : 8;
+            if (whole) {
+              const float inv = sum[j] > 0.f ? 1.f / sum[j] : sum[j] == 0.f ? 0.f : sum[j];
+              const int i = quotient(r, a.group);
+              __nv_bfloat16 *dst = a.out + ((size_t)((size_t)cur.b * a.n_new + i) * a.Hq +
+                                            h * (int)a.group.d + (r - i * (int)a.group.d)) * D + d;
+              uint32_t w[kQuarter];
 #pragma unroll
-            for (int n = 0; n < kMT; n += 4) {
-              const int d = kE * g + (kE == 8 ? 16 * n : 2 * n);
-              if (whole) {
-                uint4 w;
-                w.x = pack_bf16(o[n][x][j] * inv, o[n][x][2 + j] * inv);
-                w.y = pack_bf16(o[n + 1][x][j] * inv, o[n + 1][x][2 + j] * inv);
-                w.z = pack_bf16(o[n + 2][x][j] * inv, o[n + 2][x][2 + j] * inv);
-                w.w = pack_bf16(o[n + 3][x][j] * inv, o[n + 3][x][2 + j] * inv);
-                *reinterpret_cast<uint4 *>(dst + d) = w;
-              } else {
-                float4 *f = reinterpret_cast<float4 *>(part + rr * D + d);
-                f[0] = make_float4(o[n][x][j], o[n][x][2 + j], o[n + 1][x][j], o[n + 1][x][2 + j]);
-                f[1] = make_float4(o[n + 2][x][j], o[n + 2][x][2 + j], o[n + 3][x][j], o[n + 3][x][2 + j]);
+              for (int n = 0; n < kQuarter; ++n) w[n] = pack_bf16(y[n][j] * inv, y[n][2 + j] * inv);
+              if constexpr (kQuarter == 2)
+                *reinterpret_cast<uint2 *>(dst) = make_uint2(w[0], w[kQuarter - 1]);
+              else
+                *reinterpret_cast<uint32_t *>(dst) = w[0];
+            } else {
+#pragma unroll
+              for (int n = 0; n < kQuarter; ++n)
+                *reinterpret_cast<float2 *>(part + rr * D + d + 2 * n) = make_float2(y[n][j], y[n][2 + j]);
+              if (warp == 0 && g == 0) {
+                part[kRows * D + 2 * rr] = M[j];
+                part[kRows * D + 2 * rr + 1] = sum[j];
               }
             }
-            if (!whole && g == 0) {
-              part[kRows * D + 2 * rr] = M[x][j];
-              part[kRows * D + 2 * rr + 1] = sm;
-            }
           }
-        if (unit_done && !whole) {   // a run ends one such unit at most: its first
-          const long long t0 = first_tile(plan, blockIdx.x) - unit_tile0;
-          const int c0 = cta_of(plan, t0);
-          cut.parts = blockIdx.x - c0 + 1;
-          cut.first = c0;
-          cut.slot = first_tile(plan, c0) == t0 ? 2 * c0 : 2 * c0 + 1;
-          cut.b = cur.b;
-          cut.unit = cur.unit;
         }
+      }
+      if (unit_done && !whole) {   // a run ends one such unit at most: its first
+        const int t0 = first_tile(plan, blockIdx.x) - unit_tile0;
+        const int c0 = cta_of(plan, t0);
+        cut.parts = blockIdx.x - c0 + 1;
+        cut.first = c0;
+        cut.slot = first_tile(plan, c0) == t0 ? 2 * c0 : 2 * c0 + 1;
+        cut.b = cur.b;
+        cut.unit = cur.unit;
       }
       first_unit = false;
       fresh = true;
     }
+    now = now + C::kStage == C::kStages * C::kStage ? 0 : now + C::kStage;
     if (it + 1 < n_tiles) step(a, cur, C::kTile);
   }
   wait_all_but<0>();
@@ -832,8 +891,15 @@ int launch(Args &a, void *workspace, cudaStream_t stream) {
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return HSA_ERR_CUDA;
   int nb = per_sm[dev].load(std::memory_order_acquire);
   if (nb <= 0) {
+    // Both kernels ask for the same split between L1 and shared memory: a call that starts
+    // beside the join of the call before would otherwise find the join's, with room for
+    // half of its blocks, until the SM is empty (its blocks then start in two rounds).
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) !=
             cudaSuccess ||
+        cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout,
+                             cudaSharedmemCarveoutMaxShared) != cudaSuccess ||
+        cudaFuncSetAttribute(paged_join_kernel<D, kNR>, cudaFuncAttributePreferredSharedMemoryCarveout,
+                             cudaSharedmemCarveoutMaxShared) != cudaSuccess ||
         cudaOccupancyMaxActiveBlocksPerMultiprocessor(&nb, kernel, kThreads, C::kSmem) !=
             cudaSuccess ||
         nb < 1)
@@ -844,10 +910,9 @@ int launch(Args &a, void *workspace, cudaStream_t stream) {
   a.row_tiles = (a.rows + C::kRows - 1) / C::kRows;
   const long long units = (long long)a.batch * a.Hkv * a.row_tiles;
   const long long tiles = (((long long)a.max_pages << a.page_log2) + C::kTile - 1) / C::kTile;
+  if (units * tiles > 0x7fffffffLL) return HSA_ERR_UNSUPPORTED;   // tiles are counted in 32 bits
   const int blocks = nb * sm_count();
-  const int grid = tiles == 0 ? std::min(a.batch, blocks)
-                              : units >= blocks || tiles >= blocks ? blocks
-                                                                   : (int)std::min<long long>(blocks, units * tiles);
+  const int grid = (int)std::min<long long>(blocks, tiles ? units * tiles : a.batch);
   a.cuts = static_cast<CutUnit *>(workspace);
   a.ws = reinterpret_cast<float *>(a.cuts + (size_t)sm_count() * kMaxPerSm);
   count_launches(2);
@@ -926,6 +991,7 @@ extern "C" int hsa_paged_attention(const void *q, int batch, int n_new, int Hq, 
   a.ws = nullptr;
   a.n_pages = n_pages;
   a.max_pages = n_pages > 0 ? max_pages : 0;
+  a.sms = sm_count();
   a.page_log2 = 0;
   while ((1 << a.page_log2) < page_size) ++a.page_log2;
   a.scale_log2 = scale * 1.4426950408889634f;
