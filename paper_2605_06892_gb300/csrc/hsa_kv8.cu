@@ -119,16 +119,16 @@ __device__ __forceinline__ void unpack8(const Eight<kF32> &v, float (&x)[8]) {
 
 constexpr uint32_t kTop = 0x7f700000u;   // 1.875 2^127: the next code would stand for 2^128
 
-// The codes of a row's eight elements, twice (all lanes of the row's group call it
-// together), and the row's scale byte.  `bad` is set where an element is not finite: its
+// The codes of a row's eight elements, twice (all lanes of the warp call it together: a
+// shuffle over fewer costs a synchronisation of its own), and the row's scale byte.  `bad` is set where an element is not finite: its
 // code is NaN and the others go by the largest finite magnitude.  Finite magnitudes above
 // kTop count as that.
 template <bool kF32>
-__device__ __forceinline__ void quantise(const Eight<kF32> (&v)[2], int L, unsigned group, uint2 (&c)[2],
+__device__ __forceinline__ void quantise(const Eight<kF32> (&v)[2], int L, uint2 (&c)[2],
                                          unsigned &scale, bool &bad) {
   uint32_t m = max(largest(v[0]), largest(v[1]));
-  for (int o = 1; o < L; o <<= 1) m = max(m, __shfl_xor_sync(group, m, o));
-  const bool odd = m > kTop;             // rare; the same in all lanes of the group
+  for (int o = 1; o < L; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+  const bool odd = __any_sync(0xffffffffu, m > kTop);   // rare
   if (odd) {
     m = 0;
 #pragma unroll
@@ -142,7 +142,7 @@ __device__ __forceinline__ void quantise(const Eight<kF32> (&v)[2], int L, unsig
         else m = max(m, min(b, kTop));
       }
     }
-    for (int o = 1; o < L; o <<= 1) m = max(m, __shfl_xor_sync(group, m, o));
+    for (int o = 1; o < L; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
   }
   scale = scale_byte(m);
   const float f = __uint_as_float((254u - scale) << 23);   // 2^-e, a normal number
@@ -174,33 +174,40 @@ struct QuantArgs {
   int N, D, table_rows, lpr_log2;
 };
 
+// Blocks per SM, all resident at once: 6 hold more loads in flight than 5 (720p layer, a
+// quarter of the rows 116 -> 104 us), and a single wave of them beats 32 that follow one
+// another (LTX-like layer 13.7 -> 12.5).
+constexpr int kQuantBlocks = 6;
+
 // One item is a (token, head) of the fresh rows, K and V.
 template <bool kF32, bool kRope>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, kF32 ? 4 : kQuantBlocks)
 kv_quant_scatter_kernel(const QuantArgs a) {
   pdl_wait();
   const int L = 1 << a.lpr_log2, lane = threadIdx.x & 31, c = lane & (L - 1);
-  const unsigned group = (L == 32 ? 0xffffffffu : ((1u << L) - 1)) << (lane & ~(L - 1));
   const bool in[2] = {8 * c < a.D, 8 * (c + L) < a.D};
   const unsigned step = (gridDim.x * (unsigned)kThreads) >> a.lpr_log2;
   const unsigned first = (blockIdx.x * (unsigned)kThreads + threadIdx.x) >> a.lpr_log2;
-  for (unsigned long long i = first; i < a.items; i += step) {   // the same in all lanes of a group
+  // all lanes of a warp run as often as its first
+  for (unsigned long long i = first; i - (lane >> a.lpr_log2) < a.items; i += step) {
+    const bool there = i < a.items;
     const unsigned j = quotient((unsigned)i, a.heads), h = (unsigned)i - j * a.heads.d;
-    const int slot = __ldg(a.idx + j);
-    const int trow = !kRope ? 0 : a.tidx ? __ldg(a.tidx + j) : slot;
+    int slot = 0, trow = 0;
     Eight<kF32> k[2] = {}, v[2] = {};
-    const size_t at = (size_t)i * a.D + 8 * c;
+    if (there) {
+      slot = __ldg(a.idx + j);
+      trow = !kRope ? 0 : a.tidx ? __ldg(a.tidx + j) : slot;
+      const size_t at = (size_t)i * a.D + 8 * c;
 #pragma unroll
-    for (int y = 0; y < 2; ++y)
-      if (in[y]) {
-        k[y] = load8<kF32>(a.kf, at + 8 * L * y);
-        v[y] = load8<kF32>(a.vf, at + 8 * L * y);
-      }
-    if (slot < 0 || slot >= a.N || (kRope && (trow < 0 || trow >= a.table_rows))) {
-      set_error(a.err, kErrIndex);
-      continue;
+      for (int y = 0; y < 2; ++y)
+        if (in[y]) {
+          k[y] = load8<kF32>(a.kf, at + 8 * L * y);
+          v[y] = load8<kF32>(a.vf, at + 8 * L * y);
+        }
     }
-    if (kRope) {
+    const bool ok = there && slot >= 0 && slot < a.N && (!kRope || (trow >= 0 && trow < a.table_rows));
+    if (there && !ok) set_error(a.err, kErrIndex);
+    if (kRope && ok) {
       const float4 *t = reinterpret_cast<const float4 *>(a.table + (size_t)trow * a.D) + 2 * c;
 #pragma unroll
       for (int y = 0; y < 2; ++y)
@@ -216,8 +223,9 @@ kv_quant_scatter_kernel(const QuantArgs a) {
     bool bad = false;
     unsigned sk, sv;
     uint2 ck[2], cv[2];
-    quantise<kF32>(k, L, group, ck, sk, bad);
-    quantise<kF32>(v, L, group, cv, sv, bad);
+    quantise<kF32>(k, L, ck, sk, bad);
+    quantise<kF32>(v, L, cv, sv, bad);
+    if (!ok) continue;
     if (bad) set_error(a.err, kErrNonfinite);
     const size_t row = (size_t)slot * a.heads.d + h, to = row * a.D + 8 * c;
 #pragma unroll
@@ -375,7 +383,7 @@ extern "C" int hsa_kv_quant_scatter(void *k_cache, void *v_cache, uint8_t *k_sca
   launch_pdl(dtype == HSA_F32 ? kv_quant_scatter_kernel<true, false>
              : table          ? kv_quant_scatter_kernel<false, true>
                               : kv_quant_scatter_kernel<false, false>,
-             dim3(grid_for(a.items, a.lpr_log2, 1, kBlocks)), dim3(kThreads), 0,
+             dim3(grid_for(a.items, a.lpr_log2, 1, dtype == HSA_F32 ? 4 : kQuantBlocks)), dim3(kThreads), 0,
              (cudaStream_t)stream, a);
   return launch_status();
 }

@@ -468,8 +468,13 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
   const Unit u = unit_sh;
   if (u.parts == 0) return;
   const int piece = u.parts > 1 ? u.slot + u.part : -1;
-  const int j0 = (int)((long long)u.tiles * u.part / u.parts);
-  const int nT = (int)((long long)u.tiles * (u.part + 1) / u.parts) - j0;
+  int j0 = 0, nT = u.tiles;
+  if (u.parts > 1) {   // parts of one length, the first ones a tile longer
+    nT = u.tiles / u.parts;
+    const int more = u.tiles - nT * u.parts;
+    j0 = u.part * nT + min(u.part, more);
+    nT += u.part < more;
+  }
   const int rows = (int)min((long long)u.seq.lq * a.group.d - u.row0, (long long)kUnitRows);
   if (u.cut >= 0 && u.part == 0 && threadIdx.x == 0)
     a.cuts->unit[u.cut] = {u.parts, u.slot, rows, u.row0, u.seq.q0, u.head, {0, 0}};
