@@ -54,6 +54,7 @@ struct PackedArgs {
   float scale_log2;
   int sms, most;                   // most: pieces that a cut may make, 0: none
   int bound;                       // units that the host allowed for
+  int q_map;                       // the query rows come by TMA
   int inject_stall;                // test hook (hsa_test.h)
   float *ws_o, *ws_ml;             // [piece][kUnitRows][D], [piece][kUnitRows][2]
   Cuts *cuts;                      // what the join reads
@@ -62,6 +63,21 @@ struct PackedArgs {
 struct Sequence {
   int q0, lq, k0, lk;
 };
+
+// Bytes to come on a barrier's present phase, without an arrival.
+__device__ __forceinline__ void mbar_expect_tx_only(uint64_t *b, uint32_t bytes) {
+  asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(b)), "r"(bytes)
+               : "memory");
+}
+
+__device__ __forceinline__ void tma_load_3d(void *dst, const CUtensorMap *map, uint64_t *bar, int x, int y,
+                                            int z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_addr(dst)),
+      "l"(map), "r"(smem_addr(bar)), "r"(x), "r"(y), "r"(z)
+      : "memory");
+}
 
 // Sequence b's rows and keys; ends that run backwards or past the tensors are moved
 // inside and reported.
@@ -277,11 +293,13 @@ __device__ __forceinline__ __nv_bfloat16 *out_row(const PackedArgs &a, int q0, i
 // already.  Rare and slow; out of line so that it costs the usual path no registers.  False:
 // no row needed it.
 template <int D>
-__device__ __noinline__ bool form_again(const PackedArgs &a, const Unit &u, uint32_t tO,
-                                        const uint8_t *q_tile, int row, int limit, int k0, int k1,
-                                        float m, bool valid) {
+__device__ __noinline__ bool form_again(const PackedArgs &a, const Unit &u, uint32_t tO, int R, int limit,
+                                        int k0, int k1, float m, bool valid) {
   const __nv_bfloat16 *K = a.k + (size_t)u.seq.k0 * a.k_row + (size_t)u.head * D;
   const __nv_bfloat16 *V = a.v + (size_t)u.seq.k0 * a.v_row + (size_t)u.head * D;
+  const int tok = valid ? quotient(R, a.group) : 0;
+  const __nv_bfloat16 *Q = a.q + (size_t)(u.seq.q0 + tok) * a.q_row +
+                           (u.head * (int)a.group.d + (valid ? R - tok * (int)a.group.d : 0)) * D;
   bool bad = false;
   if (valid)
     for (int j = max(limit, k0); j < k1 && !bad; ++j)
@@ -301,8 +319,7 @@ __device__ __noinline__ bool form_again(const PackedArgs &a, const Unit &u, uint
     for (int j = k0; j < most; ++j) {
       float s = 0.f;
       for (int v = 0; v < D / 8; ++v) {
-        const uint4 qw = *reinterpret_cast<const uint4 *>(q_tile + (v >> 3) * (kBM * 128) + row * 128 +
-                                                          (((v & 7) ^ (row & 7)) << 4));
+        const uint4 qw = __ldg(reinterpret_cast<const uint4 *>(Q) + v);
         const uint4 kw = __ldg(reinterpret_cast<const uint4 *>(K + (size_t)j * a.k_row) + v);
         const uint32_t x[4] = {qw.x, qw.y, qw.z, qw.w}, y[4] = {kw.x, kw.y, kw.z, kw.w};
 #pragma unroll
@@ -419,7 +436,7 @@ __device__ __forceinline__ void store_rows(const PackedArgs &a, const Unit &u, i
 template <int D>
 __global__ void __launch_bounds__(kTcThreads, 1)
 packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
-                        const PackedArgs a) {
+                        const __grid_constant__ CUtensorMap tm_q, const PackedArgs a) {
   using C = TcCfg<D>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
@@ -438,6 +455,7 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
   if (threadIdx.x == 32) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_k) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_v) : "memory");
+    if (a.q_map) asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_q) : "memory");
   }
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::kStages; ++s) {
@@ -506,8 +524,24 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     if (blockIdx.x + (unsigned)a.sms >= gridDim.x) pdl_trigger();
   }
-  // ---- query rows into the two swizzled Q tiles
-  {
+  // ---- query rows into the two swizzled Q tiles.  Where G divides a tile's 128 rows a box
+  // of 128 / G tokens, G heads and 64 dimensions is a tile's column chunk as the MMA wants
+  // it, and arrives on the first K tile's barrier; rows past the sequence's last are another
+  // sequence's or zeros, and are never stored.  Else the threads load row by row.
+  if (a.q_map) {
+    if (threadIdx.x == 0) {
+      const int G = a.group.d, tok = u.seq.q0 + (int)quotient(u.row0, a.group);
+      mbar_expect_tx_only(&bar_full[0], kQT * C::kTileBytes);
+#pragma unroll
+      for (int t = 0; t < kQT; ++t)
+#pragma unroll
+        for (int c = 0; c < C::kChunks; ++c)
+          tma_load_3d(sQ + t * C::kTileBytes + c * (kBM * 128), &tm_q, &bar_full[0], c * 64, u.head * G,
+                      tok + t * (int)quotient(kBM, a.group));
+      for (int L = 0; L < n_pre; ++L)
+        if (L != withheld) load_kv(L);
+    }
+  } else {
     constexpr int kVecPerRow = D / 8;
     constexpr int kVecs = kUnitRows * kVecPerRow;
     constexpr int kPer = (kVecs + kTcThreads - 1) / kTcThreads;
@@ -622,9 +656,8 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
       fence_after();
       store_rows<D>(a, u, piece, t * kBM + wq * 32, lane, tO, m_run, l_run,
                     sKV + (warp - 4) * (32 * D * 4), [&]() {
-                      return a.mask && form_again<D>(a, u, tO, sQ + t * C::kTileBytes, wq * 32 + lane,
-                                                     limit, j0 * kBN, min(u.seq.lk, (j0 + nT) * kBN),
-                                                     m_run, r < rows);
+                      return a.mask && form_again<D>(a, u, tO, u.row0 + r, limit, j0 * kBN,
+                                                     min(u.seq.lk, (j0 + nT) * kBN), m_run, r < rows);
                     });
     }
     fence_before();
@@ -727,6 +760,21 @@ packed_join_kernel(const PackedArgs a) {
 
 // -------------------------------------------------------------- host side
 
+// 3-D map over N tokens of H heads x D bf16 values, the tokens `row` elements apart: boxes
+// of `tokens` x `heads` x 64 dimensions, 128-byte swizzle, tokens past N read as zero.
+bool make_rows_map(CUtensorMap *map, const void *base, int N, int H, int D, long long row, int heads,
+                   int tokens) {
+  auto enc = encode_fn();
+  if (!enc) return false;
+  const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)H, (cuuint64_t)N};
+  const cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)row * 2};
+  const cuuint32_t box[3] = {64, (cuuint32_t)heads, (cuuint32_t)tokens};
+  const cuuint32_t estride[3] = {1, 1, 1};
+  return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides, box,
+             estride, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int D>
 int launch(PackedArgs &a, const void *any, cudaStream_t stream) {
   using C = TcCfg<D>;
@@ -744,12 +792,17 @@ int launch(PackedArgs &a, const void *any, cudaStream_t stream) {
       return HSA_ERR_CUDA;
     configured[dev].store(1);
   }
-  CUtensorMap mk, mv;
+  CUtensorMap mk, mv, mq;
   // without keys no tile is loaded: any valid map serves
   const int keys = std::max(a.total_k, 1);
   if (!make_kv_map(&mk, a.total_k ? a.k : any, keys, a.Hkv * D, a.total_k ? a.k_row : (long long)a.Hkv * D) ||
       !make_kv_map(&mv, a.total_k ? a.v : any, keys, a.Hkv * D, a.total_k ? a.v_row : (long long)a.Hkv * D))
     return HSA_ERR_CUDA;
+  // A box of the query tensor [total_q, Hq, D] is a Q tile where G divides its rows.
+  const int G = (int)a.group.d;
+  a.q_map = kBM % G == 0;
+  if (a.q_map && !make_rows_map(&mq, a.q, a.total_q, a.Hq, D, a.q_row, G, kBM / G)) return HSA_ERR_CUDA;
+  if (!a.q_map) mq = mk;
   // Units at most: every sequence has at most one partly filled block.  How many there are
   // is on the device, so the grid holds what a cut may make of them: a block too many costs
   // about a microsecond of an SM.  Fewer units than SMs become at most sms parts, or 2 sms
@@ -762,7 +815,7 @@ int launch(PackedArgs &a, const void *any, cudaStream_t stream) {
   if (grid > 0x7fffffffLL) return HSA_ERR_UNSUPPORTED;
   a.bound = (int)units;
   count_launches(a.most ? 2 : 1);
-  launch_pdl(kernel, dim3((unsigned)grid), dim3(kTcThreads), C::kSmem, stream, mk, mv, a);
+  launch_pdl(kernel, dim3((unsigned)grid), dim3(kTcThreads), C::kSmem, stream, mk, mv, mq, a);
   if (cudaGetLastError() != cudaSuccess) return HSA_ERR_CUDA;
   if (a.most)
     launch_pdl(packed_join_kernel<D>, dim3((unsigned)(8 * a.sms)), dim3(kJoinThreads), 0, stream, a);
