@@ -122,6 +122,10 @@ struct Cfg {
   static constexpr int kRows = 8 * kNR;                        // query rows of a unit
   static constexpr int kRowBytes = D * (kF8 ? 1 : 2);
   static constexpr int kChunks = kRowBytes / 16;               // 16-byte chunks per row
+  // Four column blocks at D = 128 leave no registers for the query rows, which are then
+  // read from shared memory at each product.
+  static constexpr bool kLean = D == 128 && kNR == 4;
+  static_assert(!(kLean && kF8), "the rows in shared memory are bf16");
   static constexpr int kKW = kRowBytes == 256 ? 16 : 32;       // keys per warp and tile
   static constexpr int kTile = kWarps * kKW;                   // keys per tile
   static constexpr int kStages = 2;
@@ -147,6 +151,14 @@ __device__ __forceinline__ int k_chunk(int c, int row) {
 template <int kChunks>
 __device__ __forceinline__ int v_chunk(int c, int row) {
   return kChunks == 4 ? c ^ (((row >> 2) & 1) << 1) : c ^ ((row & 3) << 1);
+}
+
+// Where a query row's dimensions of K = 16 step s lie in shared memory that lane t of a
+// quad multiplies: those that its K fragments hold (chunk c of row r lies at c ^ (r & 7)).
+template <int D, bool kF8>
+__device__ __forceinline__ int query_place(int r, int s, int t) {
+  const int d = kF8 ? 16 * (t + 4 * (s / 4)) + 4 * (s % 4) : 8 * (t + 4 * (s / 2)) + 4 * (s % 2);
+  return r * (2 * D) + 16 * ((d / 8) ^ (r & 7)) + (d & 4) * 2;
 }
 
 // What the join has to know of a unit that several blocks shared, from the block that
@@ -402,9 +414,10 @@ paged_attention_kernel(const Args a) {
 
   // ---- per unit state; column block x of the MMAs holds rows 8 x .. 8 x + 7, and this
   // lane row 8 x + g of Q^T and P^T, rows 8 x + 2 t + j of S^T and O^T
-  uint32_t qf[kSteps][kNR][2];
-  float o[kMT][kNR][4], m[kNR][2], l[kNR][2], c2[kNR][2];
-  int limit[kNR][2];     // keys that rows 8 x + 2 t + j see
+  constexpr bool kLean = C::kLean;
+  uint32_t qf[kLean ? 1 : kSteps][kNR][2];
+  float o[kMT][kNR][4], m[kNR][2], l[kNR][2], c2[kF8 ? kNR : 1][2];
+  uint32_t sq_now = 0;   // kLean: the unit's rows
   int unit_tile0 = 0;    // the unit's tile that this run of it starts with
   bool fresh = true, first_unit = true;
   uint32_t now = 0;      // the stage of tile `it`
@@ -418,43 +431,44 @@ paged_attention_kernel(const Args a) {
     if (fresh) {
       fresh = false;
       unit_tile0 = cur.tile;
-      const int r0 = (cur.unit % a.row_tiles) * kRows;
       const uint32_t from = smem_addr(sq + q_now * C::kQ);
       q_now = q_now + 1 == C::kStages ? 0 : q_now + 1;
+      sq_now = from;
+      // 8 bits: a row times 2^(14 - E), its largest magnitude in [2^14, 2^15); `big` over the
+      // lanes that hold the row
+      auto scales_of = [&](float big, float &f) {
+        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
+        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
+        const unsigned E = max(__float_as_uint(big) >> 23, 20u);   // biased
+        f = __uint_as_float((268u - E) << 23);
+        return a.scale_log2 * __uint_as_float((E - 14u) << 23);
+      };
+      auto larger = [](float big, uint32_t w) { return fmaxf(big, fmaxf(fabsf(lo_bf16(w)), fabsf(hi_bf16(w)))); };
+      auto scaled = [](uint32_t w, float f) { return pack_f16(lo_bf16(w) * f, hi_bf16(w) * f); };
 #pragma unroll
       for (int x = 0; x < kNR; ++x) {
-        const int r = 8 * x + g;
-        float big = 0.f;
+        float scale = 0.f;
+        if constexpr (!kLean) {
+          const int r = 8 * x + g;
+          float big = 0.f, f;
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-          // dimensions of K = 16 step s that this lane's fragments hold
-          const int d = kF8 ? 16 * (t + 4 * (s / 4)) + 4 * (s % 4) : 8 * (t + 4 * (s / 2)) + 4 * (s % 2);
-          const uint2 w = lds64(from + r * (2 * D) + 16 * ((d / 8) ^ (r & 7)) + (d & 4) * 2);
-          qf[s][x][0] = w.x;
-          qf[s][x][1] = w.y;
-          if (kF8)
-            big = fmaxf(fmaxf(big, fmaxf(fabsf(lo_bf16(w.x)), fabsf(hi_bf16(w.x)))),
-                        fmaxf(fabsf(lo_bf16(w.y)), fabsf(hi_bf16(w.y))));
-        }
-        float scale = a.scale_log2;
-        if (kF8) {
-          // the row times 2^(14 - E), its largest magnitude in [2^14, 2^15)
-          big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
-          big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
-          const unsigned E = max(__float_as_uint(big) >> 23, 20u);   // biased
-          const float f = __uint_as_float((268u - E) << 23);
-          scale *= __uint_as_float((E - 14u) << 23);
+          for (int s = 0; s < kSteps; ++s) {
+            const uint2 w = lds64(from + query_place<D, kF8>(r, s, t));
+            qf[s][x][0] = w.x;
+            qf[s][x][1] = w.y;
+            if (kF8) big = larger(larger(big, w.x), w.y);
+          }
+          if (kF8) {
+            scale = scales_of(big, f);
 #pragma unroll
-          for (int s = 0; s < kSteps; ++s)
+            for (int s = 0; s < kSteps; ++s)
 #pragma unroll
-            for (int y = 0; y < 2; ++y)
-              qf[s][x][y] = pack_f16(lo_bf16(qf[s][x][y]) * f, hi_bf16(qf[s][x][y]) * f);
+              for (int y = 0; y < 2; ++y) qf[s][x][y] = scaled(qf[s][x][y], f);
+          }
         }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const int rc = r0 + 8 * x + 2 * t + j;
-          limit[x][j] = rc < a.rows ? cur.len - a.n_new + (int)quotient(rc, a.group) + 1 : 0;
-          c2[x][j] = kF8 ? __shfl_sync(0xffffffffu, scale, 4 * (2 * t + j)) : scale;
+          if (kF8) c2[kF8 ? x : 0][j] = __shfl_sync(0xffffffffu, scale, 4 * (2 * t + j));
           m[x][j] = kLowest;
           l[x][j] = 0.f;
         }
@@ -503,13 +517,25 @@ paged_attention_kernel(const Args a) {
               k[1] = word(w1, 2 * e), k[3] = word(w1, 2 * e + 1);
             }
 #pragma unroll
-            for (int x = 0; x < kNR; ++x) mma<kF8>(s[b][x], k, qf[step][x][0], qf[step][x][1]);
+            for (int x = 0; x < kNR; ++x) {
+              if constexpr (kLean) {
+                const uint2 w = lds64(sq_now + query_place<D, kF8>(8 * x + g, step, t));
+                mma<kF8>(s[b][x], k, w.x, w.y);
+              } else {
+                mma<kF8>(s[b][x], k, qf[step][x][0], qf[step][x][1]);
+              }
+            }
           }
         }
       }
       // ---- log2 units, the mask, the running maximum
       float vinv[kNB][2], mx[kNR][2];
       const bool ragged = key0 + C::kKW > cur.len - a.n_new + 1;
+      // keys that row 8 x + 2 t + j sees, where that matters
+      auto limit = [&](int x, int j) {
+        return cur.len - a.n_new + 1 +
+               (int)quotient((cur.unit % a.row_tiles) * kRows + 8 * x + 2 * t + j, a.group);
+      };
 #pragma unroll
       for (int x = 0; x < kNR; ++x) mx[x][0] = m[x][0], mx[x][1] = m[x][1];
 #pragma unroll
@@ -527,7 +553,7 @@ paged_attention_kernel(const Args a) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
               float &y = s[b][x][2 * n + j];
-              y = kF8 ? fmaf(y * kf, c2[x][j], ve) : y * c2[x][j];
+              y = kF8 ? fmaf(y * kf, c2[kF8 ? x : 0][j], ve) : y * a.scale_log2;
             }
         }
       if (!ragged) {
@@ -547,7 +573,7 @@ paged_attention_kernel(const Args a) {
 #pragma unroll
               for (int j = 0; j < 2; ++j) {
                 float &y = s[b][x][2 * n + j];
-                if (key0 + 16 * b + 8 * n + key_of<kCh>(g) >= limit[x][j]) y = -INFINITY;
+                if (key0 + 16 * b + 8 * n + key_of<kCh>(g) >= limit(x, j)) y = -INFINITY;
                 mx[x][j] = fmaxf(mx[x][j], y);
               }
       }
@@ -676,7 +702,7 @@ paged_attention_kernel(const Args a) {
                 mma<kF8>(y, v, p[b][x][0], p[b][x][1]);
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
-                  if (limit[x][j] == lim && r0 + 8 * x + 2 * t + j < a.rows) {
+                  if (limit(x, j) == lim && r0 + 8 * x + 2 * t + j < a.rows) {
                     o[n][x][j] += y[j];
                     o[n][x][2 + j] += y[2 + j];
                   }
@@ -923,14 +949,18 @@ int launch(Args &a, void *workspace, cudaStream_t stream) {
   return launch_status();
 }
 
-// Column blocks of eight rows: as many as the rows need and a unit's sums fit in registers
-// (at D = 128 four blocks spill: 5 tokens of 8 heads against 43403 keys 155 us, two at a
-// time 92).  Rows beyond are further units, which read the keys again, from L2.
+// Column blocks of eight rows per unit: one or two where the rows fit, else two or four.
+// Further units read the keys again, from L2, and by then the products bound the time: a
+// unit of four blocks takes 1.6 to 1.7 times one of two (4 sequences of 9000 to 30000 keys,
+// 8 K/V heads: 24 rows 48 against 57 us at D = 64, 82 against 99 at D = 128; 40 rows 77
+// against 75, 143 against 135).  8-bit keys at D = 128 leave it too few registers (24 rows
+// 84 against 73 us).
 template <int D, bool kF8>
 int launch_rows(Args &a, void *workspace, cudaStream_t stream) {
-  if constexpr (D == 64)
-    if (a.rows > 16) return launch<D, kF8, 4>(a, workspace, stream);
-  return a.rows <= 8 ? launch<D, kF8, 1>(a, workspace, stream) : launch<D, kF8, 2>(a, workspace, stream);
+  if (a.rows <= 8) return launch<D, kF8, 1>(a, workspace, stream);
+  if constexpr (!(kF8 && D == 128))
+    if (5 * ((a.rows + 31) / 32) < 3 * ((a.rows + 15) / 16)) return launch<D, kF8, 4>(a, workspace, stream);
+  return launch<D, kF8, 2>(a, workspace, stream);
 }
 
 }  // namespace

@@ -266,3 +266,33 @@ def test_same_result_in_any_company(hsa):
             pool.call(hsa, q, outs[1 + i], wss[i])
     torch.cuda.synchronize()
     assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+
+
+@pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Hq,new", [(17, 1), (31, 1), (33, 1), (8, 5), (3, 23)])
+def test_many_rows_per_head(hsa, Hq, new, D, f8):
+    """More than 16 rows of one K/V head, also more than a unit takes, over units of several
+    tiles, cut ones among them."""
+    _check(hsa, [2000, 129, new, 0, 40], new, Hq, 1, D, 32, f8, Hq + D)
+
+
+@pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+def test_nan_among_many_rows(hsa, D, f8):
+    """As above with a value that is not finite among the newest keys."""
+    new, Hq, n, at = 9, 4, 300, 296
+    pool = Pool([n], 16, 1, D, f8, 31)
+    j = int(pool.table[0, at // 16]), at % 16
+    pool.v[j[0], j[1], 0, 3] = 0x7f if f8 else float("inf")
+    q = torch.randn((1, new, Hq, D), generator=torch.Generator().manual_seed(32)).to(torch.bfloat16)
+    out = torch.empty((1, new, Hq, D), dtype=torch.bfloat16, device=DEV)
+    pool.call(hsa, q.to(DEV), out, _ws(hsa, 1, new, Hq, 1, D))
+    got = out[0].double().cpu()
+    want, tol = ref.attention(q[0].double(), *pool.keys[0], ref.limits(new, n, 1))
+    blind = at - (n - new)
+    assert ((got - want).abs()[:blind] <= tol[:blind]).all()
+    assert not got[blind:, :, 3].isfinite().any()
+    clean = [d for d in range(D) if d != 3]
+    assert ((got - want).abs()[blind:, :, clean] <= tol[blind:, :, clean]).all()
+    assert hsa.hsa_get_device_error() == 0
