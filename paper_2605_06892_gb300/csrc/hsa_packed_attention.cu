@@ -436,7 +436,7 @@ __device__ __forceinline__ void store_rows(const PackedArgs &a, const Unit &u, i
 template <int D>
 __global__ void __launch_bounds__(kTcThreads, 1)
 packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
-                        const __grid_constant__ CUtensorMap tm_q, const PackedArgs a) {
+                        const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ PackedArgs a) {
   using C = TcCfg<D>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
@@ -483,9 +483,10 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
     }
   }
   __syncthreads();
-  const Unit u = unit_sh;
+  // Read where it is needed: held in registers over the key loop it would spill, to an L1
+  // that the tiles have left no room in.
+  const Unit &u = unit_sh;
   if (u.parts == 0) return;
-  const int piece = u.parts > 1 ? u.slot + u.part : -1;
   int j0 = 0, nT = u.tiles;
   if (u.parts > 1) {   // parts of one length, the first ones a tile longer
     nT = u.tiles / u.parts;
@@ -503,14 +504,15 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
     return;
   }
 
+  const int key0 = u.seq.k0 + j0 * kBN, col0 = u.head * D;
   auto load_kv = [&](int L) {
     const int slot = L % C::kStages;
     mbar_expect_tx(&bar_full[slot], C::kTileBytes);
     uint8_t *dst = sKV + slot * C::kTileBytes;
-    const int y = u.seq.k0 + (j0 + (L >> 1)) * kBN;
+    const int y = key0 + (L >> 1) * kBN;
 #pragma unroll
     for (int c = 0; c < C::kChunks; ++c)
-      tma_load_2d(dst + c * (kBN * 128), (L & 1) ? &tm_v : &tm_k, &bar_full[slot], u.head * D + c * 64, y);
+      tma_load_2d(dst + c * (kBN * 128), (L & 1) ? &tm_v : &tm_k, &bar_full[slot], col0 + c * 64, y);
   };
   const int withheld = a.inject_stall == 1 ? 1 : -1;
   const int n_pre = min(3, 2 * nT);
@@ -594,8 +596,9 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
     } else if (warp == 2) {
       // V rows behind the sequence's last key (another sequence's, or what lies behind
       // the last) become zeros before the issuer hears of the tile.
+      const int keys = u.seq.lk - j0 * kBN;
       tc_watch_kv<D>(pipe, lane, nT, [&](int j) {
-        const int have = u.seq.lk - (j0 + j) * kBN;
+        const int have = keys - j * kBN;
         if (have >= kBN) return;
         uint8_t *tile = sKV + ((2 * j + 1) % C::kStages) * C::kTileBytes;
         for (int i = have * 8 + lane; i < kBN * 8; i += 32)
@@ -624,15 +627,15 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
     const uint32_t tO = tmem + lane_off + C::kOCol0 + D * t;
     const float sl2 = a.scale_log2;
     float m_run = kLowest, l_run = 0.f;
-    // Keys that this thread's row sees; rows past the sequence's last take no mask.  The
+    // Keys from tile j0 on that this thread's row sees; rows past the sequence's last take no mask.  The
     // warp's first row sees fewest.
     const int r = t * kBM + wq * 32 + lane;
-    const int limit = r < rows ? key_limit(a, u.seq, quotient(u.row0 + r, a.group)) : u.seq.lk;
+    const int limit = (r < rows ? key_limit(a, u.seq, quotient(u.row0 + r, a.group)) : u.seq.lk) - j0 * kBN;
     const int all_see = __shfl_sync(0xffffffffu, limit, 0);
     for (int j = 0; j < nT; ++j) {
       named_barrier_sync(kBarS0 + t, kMeetS);
       fence_after();
-      const int valid = limit - (j0 + j) * kBN;
+      const int valid = limit - j * kBN;
       const uint32_t tSj = tmem + lane_off + 128 * (C::kThreeS ? (2 * j + t) % 3 : t);
       auto o_idle = [&]() -> bool {   // as in the active attention
         if constexpr (!C::kThreeS) return true;
@@ -642,7 +645,7 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
         fence_after();
         return idle;
       };
-      if (all_see - (j0 + j) * kBN >= kBN)
+      if (all_see - j * kBN >= kBN)
         softmax_tile<D, false>(tSj, tO, kBN, j == 0, sl2, m_run, l_run, o_idle);
       else
         softmax_tile<D, true>(tSj, tO, valid, j == 0, sl2, m_run, l_run, o_idle);
@@ -654,9 +657,9 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
     ok = !__any_sync(0xffffffffu, abort_flag != 0) && ok;
     if (ok) {
       fence_after();
-      store_rows<D>(a, u, piece, t * kBM + wq * 32, lane, tO, m_run, l_run,
+      store_rows<D>(a, u, u.parts > 1 ? u.slot + u.part : -1, t * kBM + wq * 32, lane, tO, m_run, l_run,
                     sKV + (warp - 4) * (32 * D * 4), [&]() {
-                      return a.mask && form_again<D>(a, u, tO, u.row0 + r, limit, j0 * kBN,
+                      return a.mask && form_again<D>(a, u, tO, u.row0 + r, limit + j0 * kBN, j0 * kBN,
                                                      min(u.seq.lk, (j0 + nT) * kBN), m_run, r < rows);
                     });
     }
