@@ -375,8 +375,8 @@ int hsa_kv_dequant_gather(const void *k_cache, const void *v_cache, const uint8_
  *   q            device, bf16 [batch, n_new, Hq, D].
  *   k_pages,     device, [n_pages, page_size, Hkv, D] of cache_dtype: HSA_BF16, or
  *   v_pages      HSA_E4M3 as hsa_kv_quant_scatter writes it, with
- *   k_scale,     device, scales [n_pages, page_size, Hkv] (HSA_E4M3; else NULL).
- *   v_scale
+ *   k_scale,     device, scales [n_pages, page_size, Hkv] (HSA_E4M3; else NULL), any
+ *   v_scale      alignment; the aligned words of four bytes around those needed are read.
  *   page_table   device, int32 [batch, max_pages]: key j of sequence b is row
  *                j % page_size of page page_table[b, j / page_size].  Entries past a
  *                sequence's last page are not read, nor rows past its last key.

@@ -495,7 +495,7 @@ def _token_rows(name, t, H, D, device):
     if t.is_contiguous() or tokens == 0:
         return _want(name, t, torch.bfloat16, (tokens, H, D), device) if tokens else None, H * D
     row, head, one = t.stride()
-    if one != 1 or head != D:
+    if one != 1 or (head != D and H > 1):
         raise ValueError(f"{name} is not rows of {H} heads x {D} that lie together")
     _want(name, t[0], torch.bfloat16, (H, D), device)
     return t.data_ptr(), row

@@ -482,14 +482,14 @@ paged_attention_kernel(const Args a) {
       const uint32_t sk = ring_s + now, sv = sk + C::kHalf;
       uint4 *scales = reinterpret_cast<uint4 *>(ring + now + 2 * C::kHalf);
       if (kF8) {
-        // each lane makes 2^ks, vs and 2^-vs of its key's scale bytes (within [27, 247])
+        // each lane makes 2^ks and vs of its key's scale bytes (within [27, 247])
 #pragma unroll
         for (int x = 0; x < kPer; ++x)
           if (lane < C::kKW) {
             const uint4 w = scales[lane + 32 * x];
             const uint32_t ks = w.x >> (w.z & 0xffffu) & 255u, vs = w.y >> (w.z >> 16) & 255u;
             scales[lane + 32 * x] =
-                make_uint4(ks << 23, __float_as_uint((float)((int)vs - 127)), (254u - vs) << 23, 0u);
+                make_uint4(ks << 23, __float_as_uint((float)((int)vs - 127)), 0u, 0u);
           }
         __syncwarp();
       }
@@ -529,7 +529,7 @@ paged_attention_kernel(const Args a) {
         }
       }
       // ---- log2 units, the mask, the running maximum
-      float vinv[kNB][2], mx[kNR][2];
+      float ve[kNB][2], mx[kNR][2];   // s: u; u - ve: t
       const bool ragged = key0 + C::kKW > cur.len - a.n_new + 1;
       // keys that row 8 x + 2 t + j sees, where that matters
       auto limit = [&](int x, int j) {
@@ -543,17 +543,17 @@ paged_attention_kernel(const Args a) {
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
           const int row = 16 * b + 8 * n + key_of<kCh>(g);
-          float kf = 1.f, ve = 0.f;
+          float kf = 1.f;
           if (kF8) {
             const uint4 w = scales[row];
-            kf = __uint_as_float(w.x), ve = __uint_as_float(w.y), vinv[b][n] = __uint_as_float(w.z);
+            kf = __uint_as_float(w.x), ve[b][n] = __uint_as_float(w.y);
           }
 #pragma unroll
           for (int x = 0; x < kNR; ++x)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
               float &y = s[b][x][2 * n + j];
-              y = kF8 ? fmaf(y * kf, c2[kF8 ? x : 0][j], ve) : y * a.scale_log2;
+              y = kF8 ? fmaf(y * kf, c2[kF8 ? x : 0][j], ve[b][n]) : y * a.scale_log2;
             }
         }
       if (!ragged) {
@@ -610,8 +610,11 @@ paged_attention_kernel(const Args a) {
             float y[2];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-              y[j] = fast_exp2(s[b][x][2 * n + j] - (kF8 ? m[x][j] - kPShift : m[x][j]));
-              l[x][j] = kF8 ? fmaf(y[j], vinv[b][n], l[x][j]) : l[x][j] + y[j];
+              // 8 bits: 2^(t - M) by itself, not 2^(u - M) times 2^-vs: the first may be far
+              // below the least number where the second is not
+              const float z = s[b][x][2 * n + j] - (kF8 ? m[x][j] - kPShift : m[x][j]);
+              y[j] = fast_exp2(z);
+              l[x][j] += kF8 ? fast_exp2(z - ve[b][n]) : y[j];
             }
             p[b][x][n] = transposed(kF8 ? pack_f16(y[0], y[1]) : pack_bf16(y[0], y[1]));
           }

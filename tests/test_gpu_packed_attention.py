@@ -307,3 +307,16 @@ def test_prompts_then_tokens(hsa, f8):
                                       p_step=2.0 ** -11 if f8 else 2.0 ** -8)
             assert ((one[b].double().cpu() - want).abs() <= tol).all()
     assert hsa.hsa_get_device_error() == 0
+
+
+def test_rows_of_one_head_in_a_wider_tensor(hsa):
+    """One head's rows as a slice whose head dimension has any stride."""
+    x = torch.randn((50, 3 * 64), generator=torch.Generator().manual_seed(5)).to(torch.bfloat16)
+    xd = x.to(DEV)
+
+    def part(t, i):
+        return t.as_strided((50, 1, 64), (192, 7, 1), 64 * i)
+    cu = _cum([50])
+    out = torch.empty((50, 1, 64), dtype=torch.bfloat16, device=DEV)
+    hsa.hsa_packed_attention(*(part(xd, i) for i in range(3)), cu.to(DEV), cu.to(DEV), out, mask=1)
+    _compare(out.cpu(), *(part(x, i) for i in range(3)), cu, cu, [(50, 50)], 1)

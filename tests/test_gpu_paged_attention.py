@@ -296,3 +296,24 @@ def test_nan_among_many_rows(hsa, D, f8):
     clean = [d for d in range(D) if d != 3]
     assert ((got - want).abs()[blind:, :, clean] <= tol[blind:, :, clean]).all()
     assert hsa.hsa_get_device_error() == 0
+
+
+def test_values_over_the_whole_range(hsa):
+    """8-bit values of one sequence from 2^-100 to 2^100: the weights of keys whose values
+    are tiny count in the sum all the same, zeros among them."""
+    D, n, Hq = 64, 96, 4
+    pool = Pool([n], 16, 1, D, True, 41)
+    g = torch.Generator().manual_seed(42)
+    v = torch.randn((n, 1, D), generator=g) * torch.exp2((torch.arange(n) % 3 * 100.0 - 100.0))[:, None, None]
+    v[::7] = 0.0
+    code, scale, _ = ref.quantise_rows(v.to(torch.bfloat16).double().numpy())
+    at = torch.tensor([int(pool.table[0, j // 16]) for j in range(n)]), torch.arange(n) % 16
+    pool.v[at], pool.vs[at] = torch.from_numpy(code.astype(np.uint8)), torch.from_numpy(scale)
+    held = torch.from_numpy(ref.values(code, scale))
+    ws = _ws(hsa, 1, 1, Hq, 1, D)
+    q = torch.randn((1, 1, Hq, D), generator=g).to(torch.bfloat16)
+    out = torch.empty((1, 1, Hq, D), dtype=torch.bfloat16, device=DEV)
+    pool.call(hsa, q.to(DEV), out, ws)
+    want, tol = ref.attention(q[0].double(), pool.keys[0][0], held, [n], p_step=2.0 ** -11)
+    assert ((out[0].double().cpu() - want).abs() <= tol).all()
+    assert hsa.hsa_get_device_error() == 0
