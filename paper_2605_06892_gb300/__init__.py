@@ -12,6 +12,7 @@ Device tensors must be contiguous and live on the current CUDA device.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 
 import torch
@@ -394,57 +395,63 @@ def _codes_of(k_cache):
     return dt
 
 
+def _rows_of(name, t, size, n):
+    """Refuses fewer than n rows, or rows of other sizes than a cache of this shape has."""
+    shape = t.shape
+    if len(shape) != 3 or shape[1] != size[-2] or shape[2] != size[-1] or not 0 <= n <= shape[0]:
+        raise ValueError(f"{name} has shape {tuple(shape)}, not {n} or more rows of {size[-2]} heads x "
+                         f"{size[-1]}")
+    return shape
+
+
+def _ids(name, t, n, device):
+    """Address of at least n indices."""
+    if t.numel() < n:
+        raise ValueError(f"{name} holds fewer than {n} indices")
+    return _want(name, t, torch.int32, t.shape, device)
+
+
 def hsa_kv_quant_scatter(k_cache, v_cache, k_scale, v_scale, k_fresh, v_fresh, idx, n_active: int,
                          table=None, table_idx=None, stream=None) -> None:
     """Fresh rows [>= n_active, H, D] (bf16 or fp32) into rows idx of an 8-bit cache: codes
     [N, H, D] (float8_e4m3fn or uint8) and scale bytes [N, H] (uint8); a cache in pages [P,
     page, H, D] with scales [P, page, H] counts as P * page rows.  table: K is rotated first
     (bf16), by the table's rows table_idx (idx where that is None)."""
-    dev, code = _device(), _codes_of(k_cache)
-    size, fresh = k_cache.shape, k_fresh.shape
-    H, D = size[-2:]
-    if n_active < 0 or idx.numel() < n_active or fresh[0] < n_active:
-        raise ValueError("idx or k_fresh holds fewer than n_active rows")
-    if fresh[1:] != size[-2:]:
-        raise ValueError(f"k_fresh has shape {tuple(fresh)}, not rows of {H} heads x {D}")
+    dev, code, size, dt = _device(), _codes_of(k_cache), k_cache.shape, k_fresh.dtype
+    fresh = _rows_of("k_fresh", k_fresh, size, n_active)
+    *lead, H, D = size
+    scales = (*lead, H)
     tp = ip = None
     rows = 0
     if table is not None:
         rows = table.shape[0]
         tp = _want("table", table, torch.float32, (rows, D // 2, 2), dev)
     if table_idx is not None:
-        if table_idx.numel() < n_active:
-            raise ValueError("table_idx holds fewer than n_active rows")
-        ip = _want("table_idx", table_idx, torch.int32, table_idx.shape, dev)
+        ip = _ids("table_idx", table_idx, n_active, dev)
     _check(lib().hsa_kv_quant_scatter(
         _want("k_cache", k_cache, code, size, dev), _want("v_cache", v_cache, code, size, dev),
-        _want("k_scale", k_scale, torch.uint8, size[:-1], dev),
-        _want("v_scale", v_scale, torch.uint8, size[:-1], dev),
-        _want("k_fresh", k_fresh, k_fresh.dtype, fresh, dev),
-        _want("v_fresh", v_fresh, k_fresh.dtype, fresh, dev),
-        _want("idx", idx, torch.int32, idx.shape, dev), n_active, k_scale.numel() // max(H, 1), H, D,
-        _dtype_code(k_fresh), tp, ip, rows, _stream(stream)), "hsa_kv_quant_scatter")
+        _want("k_scale", k_scale, torch.uint8, scales, dev),
+        _want("v_scale", v_scale, torch.uint8, scales, dev),
+        _want("k_fresh", k_fresh, dt, fresh, dev), _want("v_fresh", v_fresh, dt, fresh, dev),
+        _ids("idx", idx, n_active, dev), n_active, math.prod(lead), H, D, _dtype_code(k_fresh), tp,
+        ip, rows, _stream(stream)), "hsa_kv_quant_scatter")
 
 
 def hsa_kv_dequant_gather(k_cache, v_cache, k_scale, v_scale, idx, n: int, k_out, v_out,
                           stream=None) -> None:
     """k_out[:n], v_out[:n] ([>= n, H, D], bf16 or fp32) <- rows idx[:n] of an 8-bit cache
     (idx None: rows 0 .. n-1); the cache as for hsa_kv_quant_scatter."""
-    dev, code = _device(), _codes_of(k_cache)
-    size, out = k_cache.shape, k_out.shape
-    H, D = size[-2:]
-    if n < 0 or out[0] < n or (idx is not None and idx.numel() < n):
-        raise ValueError("idx or k_out holds fewer than n rows")
-    if out[1:] != size[-2:]:
-        raise ValueError(f"k_out has shape {tuple(out)}, not rows of {H} heads x {D}")
+    dev, code, size, dt = _device(), _codes_of(k_cache), k_cache.shape, k_out.dtype
+    out = _rows_of("k_out", k_out, size, n)
+    *lead, H, D = size
+    scales = (*lead, H)
     _check(lib().hsa_kv_dequant_gather(
         _want("k_cache", k_cache, code, size, dev), _want("v_cache", v_cache, code, size, dev),
-        _want("k_scale", k_scale, torch.uint8, size[:-1], dev),
-        _want("v_scale", v_scale, torch.uint8, size[:-1], dev),
-        None if idx is None else _want("idx", idx, torch.int32, idx.shape, dev), n,
-        k_scale.numel() // max(H, 1), H, D, _want("k_out", k_out, k_out.dtype, out, dev),
-        _want("v_out", v_out, k_out.dtype, out, dev), _dtype_code(k_out), _stream(stream)),
-        "hsa_kv_dequant_gather")
+        _want("k_scale", k_scale, torch.uint8, scales, dev),
+        _want("v_scale", v_scale, torch.uint8, scales, dev),
+        None if idx is None else _ids("idx", idx, n, dev), n, math.prod(lead), H, D,
+        _want("k_out", k_out, dt, out, dev), _want("v_out", v_out, dt, out, dev),
+        _dtype_code(k_out), _stream(stream)), "hsa_kv_dequant_gather")
 
 
 def hsa_paged_attention_workspace_bytes(batch: int, n_new: int, Hq: int, Hkv: int, D: int) -> int:

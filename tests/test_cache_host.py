@@ -110,11 +110,13 @@ def test_binding_refuses_what_c_cannot_see(hsa, monkeypatch):
     x, i = torch.zeros((3, 2, 64), dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int32)
     with pytest.raises(ValueError, match="CUDA"):
         hsa.hsa_kv_quant_scatter(c, c, s, s, x, x, i, 3)
-    with pytest.raises(ValueError, match="n_active"):
+    with pytest.raises(ValueError, match="4 or more rows"):
         hsa.hsa_kv_quant_scatter(c, c, s, s, x, x, i, 4)
+    with pytest.raises(ValueError, match="rows of 2 heads x 64"):
+        hsa.hsa_kv_quant_scatter(c, c, s, s, x.view(3, 4, 32), x, i, 3)
     with pytest.raises(TypeError):
         hsa.hsa_kv_quant_scatter(c.float(), c, s, s, x, x, i, 3)
-    with pytest.raises(ValueError, match="n rows"):
+    with pytest.raises(ValueError, match="4 or more rows"):
         hsa.hsa_kv_dequant_gather(c, c, s, s, None, 4, x, x)
     with pytest.raises(ValueError, match="CUDA"):
         hsa.hsa_kv_dequant_gather(c, c, s, s, i, 3, x, x)
