@@ -123,7 +123,10 @@ struct Unit {
   int cut;               // its place among the cut units, or -1
 };
 
-constexpr int kLeastTiles = 4;   // per part: shorter ones cost more than they save
+// A part of a cut unit has four key tiles at least (two are no faster: 26 tokens after 19095
+// 25.3 against 25.9 us, eight slower, 28.5), and the join costs what seven tiles take: 64
+// tokens after 900, eight tiles, take 15.1 us whole and 18.5 in two.
+constexpr int kLeastTiles = 4, kJoinTiles = 7;
 
 __device__ __forceinline__ int parts_of(const Sequence &s, int longest) {
   const int tiles = (s.lk + kBN - 1) / kBN;
@@ -151,18 +154,20 @@ __device__ __forceinline__ bool unit_of(const PackedArgs &a, int id, Plan &p, Un
   p.n_whole = p.units;
   p.pieces = 1;
   p.longest = 0;
+  auto longest = [&]() {   // key tiles of a unit at most
+    int keys = 0;
+    each([&](const Sequence &s, int blocks) {
+      if (blocks) keys = max(keys, s.lk);
+    });
+    return (__reduce_max_sync(0xffffffffu, keys) + kBN - 1) / kBN;
+  };
   const bool may = a.most && p.units > 0 && p.units <= a.bound;   // more: offsets that overlap
   if (may && p.units < a.sms) {
     // Fewer units than SMs: the shortest part length that makes no more parts than SMs, or
     // than two waves of them; a part costs its tiles and about 5 tiles' time more.
-    int far = 0;
     unsigned work = 0;   // < 2^24 tiles of fewer units than SMs
-    each([&](const Sequence &s, int blocks) {
-      const int tiles = (s.lk + kBN - 1) / kBN;
-      if (blocks) far = max(far, tiles);
-      work += (unsigned)blocks * tiles;
-    });
-    far = __reduce_max_sync(0xffffffffu, far);
+    each([&](const Sequence &s, int blocks) { work += (unsigned)blocks * ((s.lk + kBN - 1) / kBN); });
+    const int far = longest();
     work = __reduce_add_sync(0xffffffffu, work) * a.Hkv;
     auto shortest = [&](int most) {
       // n parts of L tiles: work / L <= n < work / L + units
@@ -183,7 +188,7 @@ __device__ __forceinline__ bool unit_of(const PackedArgs &a, int id, Plan &p, Un
       const int two = shortest(2 * a.sms);
       if (2 * (two + 5) < len + 5) len = two;
     }
-    if (len < far) {
+    if (len + kJoinTiles < far) {
       p.n_whole = 0;
       p.longest = len;
     }
@@ -206,7 +211,8 @@ __device__ __forceinline__ bool unit_of(const PackedArgs &a, int id, Plan &p, Un
       }
       if (cost < best) best = cost, p.pieces = at;
     }
-    if (p.pieces > 1) p.n_whole = p.units - rem;
+    if (p.pieces > 1 && (1.f - best) * longest() > kJoinTiles) p.n_whole = p.units - rem;
+    else p.pieces = 1;
   }
   // ---- this block's place: `id` counts units, or with `longest` parts
   u.part = u.slot = 0;
@@ -810,9 +816,9 @@ int launch(PackedArgs &a, const void *any, cudaStream_t stream) {
   // is on the device, so the grid holds what a cut may make of them: a block too many costs
   // about a microsecond of an SM.  Fewer units than SMs become at most sms parts, or 2 sms
   // where they are too many for a part each; without a mask pieces of the last wave's
-  // units come on top of the others.  Too few keys for two parts: no cut, no join.
+  // units come on top of the others.  Too few keys for a cut to pay: no join.
   const long long units = ((long long)a.total_q * a.group.d / kUnitRows + a.batch) * a.Hkv;
-  if (a.total_k < 2 * kLeastTiles * kBN - kBN + 1) a.most = 0;
+  if (a.total_k <= (kLeastTiles + kJoinTiles) * kBN) a.most = 0;
   if (a.most) a.most = 2 * units <= a.sms ? a.sms : 2 * a.sms;
   const long long grid = a.mask || units < a.sms ? std::max<long long>(units, a.most) : units + a.most;
   if (grid > 0x7fffffffLL) return HSA_ERR_UNSUPPORTED;
