@@ -133,8 +133,9 @@ __device__ __forceinline__ int parts_of(const Sequence &s, int longest) {
   return longest && tiles > longest ? (tiles + longest - 1) / longest : 1;
 }
 
-// The unit and part of block `id`; false: it has none.  Called by a whole warp: lane l holds sequence l, and where there are more than 32 the later ones are
-// read again by each pass over them.
+// The unit and part of block `id`; false: it has none.  Called by a whole warp: lane l
+// holds sequence l, and where there are more than 32 the later ones are read again by each
+// pass over them.
 __device__ __forceinline__ bool unit_of(const PackedArgs &a, int id, Plan &p, Unit &u) {
   const int lane = threadIdx.x & 31;
   Sequence first = {};

@@ -318,7 +318,6 @@ paged_attention_kernel(const Args a) {
   Cursor ahead = cur;
   int left = n_tiles;                       // tiles to load
   uint32_t fill = 0;                        // where the next one goes: offset of its stage
-  constexpr int kPer = C::kKW > 32 ? 2 : 1; // keys that a lane looks up: krow + 32 x
   constexpr int kStep = 32 / kCh;           // rows that a warp copies at a time
   const int krow = lane & (C::kKW - 1);
   const uint32_t ring_s = smem_addr(ring);
@@ -332,14 +331,10 @@ paged_attention_kernel(const Args a) {
     to_k[i] = row * C::kRowBytes + 16 * k_chunk<kCh>(lane % kCh, row);
     to_v[i] = row * C::kRowBytes + 16 * v_chunk<kCh>(lane % kCh, row) + C::kHalf;
   }
-  int page[kPer];
+  int page;
   auto look_up = [&]() {
-#pragma unroll
-    for (int x = 0; x < kPer; ++x) {
-      const int key = ahead.tile * C::kTile + warp * C::kKW + krow + 32 * x;
-      page[x] = key < ahead.len
-                    ? __ldg(a.table + (size_t)ahead.b * a.max_pages + (key >> a.page_log2)) : -1;
-    }
+    const int key = ahead.tile * C::kTile + warp * C::kKW + krow;
+    page = key < ahead.len ? __ldg(a.table + (size_t)ahead.b * a.max_pages + (key >> a.page_log2)) : -1;
   };
   look_up();
   int q_fill = 0, q_now = 0;                // buffers of the next unit's rows, and of this one's
@@ -363,31 +358,25 @@ paged_attention_kernel(const Args a) {
         }
         q_fill = q_fill + 1 == C::kStages ? 0 : q_fill + 1;
       }
-      int slot[kPer];
-      unsigned have[kPer];                  // rows that there are
-#pragma unroll
-      for (int x = 0; x < kPer; ++x) {
-        const int key = ahead.tile * C::kTile + warp * C::kKW + krow + 32 * x;
-        const bool ok = page[x] >= 0 && page[x] < a.n_pages;
-        if (!ok && key < ahead.len) set_error(a.err, kErrIndex);
-        slot[x] = ok ? (page[x] << a.page_log2) + (key & ((1 << a.page_log2) - 1)) : 0;
-        have[x] = __ballot_sync(0xffffffffu, ok);
-        if (kF8 && lane < C::kKW) {
-          // The aligned words around the key's scale bytes, and the bytes' place in them:
-          // the bytes need not be waited for here.  A word that holds a byte of the scales
-          // can be read whole, whatever the other three are.  No page: a row of zeros,
-          // times one.
-          const size_t at = (size_t)slot[x] * a.Hkv + h;
-          const uintptr_t ks = (uintptr_t)(a.ks + at), vs = (uintptr_t)(a.vs + at);
-          uint32_t *to = reinterpret_cast<uint32_t *>(ring + fill + 2 * C::kHalf) + 4 * (lane + 32 * x);
-          if (ok) {
-            copy4(smem_addr(to), (const void *)(ks & ~(uintptr_t)3));
-            copy4(smem_addr(to + 1), (const void *)(vs & ~(uintptr_t)3));
-          } else {
-            to[0] = to[1] = 0x7f7f7f7fu;
-          }
-          to[2] = (uint32_t)(ks & 3) * 8 + ((uint32_t)(vs & 3) * 8 << 16);
+      const int key = ahead.tile * C::kTile + warp * C::kKW + krow;
+      const bool ok = page >= 0 && page < a.n_pages;
+      if (!ok && key < ahead.len) set_error(a.err, kErrIndex);
+      const int slot = ok ? (page << a.page_log2) + (key & ((1 << a.page_log2) - 1)) : 0;
+      const unsigned have = __ballot_sync(0xffffffffu, ok);   // rows that there are
+      if (kF8 && lane < C::kKW) {
+        // The aligned words around the key's scale bytes, and the bytes' place in them: the
+        // bytes need not be waited for here.  A word that holds a byte of the scales can be
+        // read whole, whatever the other three are.  No page: a row of zeros, times one.
+        const size_t at = (size_t)slot * a.Hkv + h;
+        const uintptr_t ks = (uintptr_t)(a.ks + at), vs = (uintptr_t)(a.vs + at);
+        uint32_t *to = reinterpret_cast<uint32_t *>(ring + fill + 2 * C::kHalf) + 4 * lane;
+        if (ok) {
+          copy4(smem_addr(to), (const void *)(ks & ~(uintptr_t)3));
+          copy4(smem_addr(to + 1), (const void *)(vs & ~(uintptr_t)3));
+        } else {
+          to[0] = to[1] = 0x7f7f7f7fu;
         }
+        to[2] = (uint32_t)(ks & 3) * 8 + ((uint32_t)(vs & 3) * 8 << 16);
       }
       const uint8_t *kb = a.k + (size_t)h * C::kRowBytes + 16 * (lane % kCh);
       const uint8_t *vb = a.v + (size_t)h * C::kRowBytes + 16 * (lane % kCh);
@@ -395,11 +384,11 @@ paged_attention_kernel(const Args a) {
       for (int i = 0; i < C::kKW / kStep; ++i) {
         constexpr int kCycle = kStep < 8 ? 8 / kStep : 1;
         const int row = lane / kCh + kStep * i;
-        const unsigned at = __shfl_sync(0xffffffffu, slot[kStep * i / 32], row & 31);
-        const bool ok = have[kStep * i / 32] >> (row & 31) & 1;
+        const unsigned at = __shfl_sync(0xffffffffu, slot, row);
+        const bool there = have >> row & 1;
         const uint32_t dst = ring_s + fill + (i / kCycle) * (kCycle * kStep * C::kRowBytes);
-        copy16(dst + to_k[i % kCycle], kb + (uint64_t)at * row_stride, ok);
-        copy16(dst + to_v[i % kCycle], vb + (uint64_t)at * row_stride, ok);
+        copy16(dst + to_k[i % kCycle], kb + (uint64_t)at * row_stride, there);
+        copy16(dst + to_v[i % kCycle], vb + (uint64_t)at * row_stride, there);
       }
       fill = fill + C::kStage == C::kStages * C::kStage ? 0 : fill + C::kStage;
       if (--left > 0) {
@@ -483,14 +472,11 @@ paged_attention_kernel(const Args a) {
       uint4 *scales = reinterpret_cast<uint4 *>(ring + now + 2 * C::kHalf);
       if (kF8) {
         // each lane makes 2^ks and vs of its key's scale bytes (within [27, 247])
-#pragma unroll
-        for (int x = 0; x < kPer; ++x)
-          if (lane < C::kKW) {
-            const uint4 w = scales[lane + 32 * x];
-            const uint32_t ks = w.x >> (w.z & 0xffffu) & 255u, vs = w.y >> (w.z >> 16) & 255u;
-            scales[lane + 32 * x] =
-                make_uint4(ks << 23, __float_as_uint((float)((int)vs - 127)), 0u, 0u);
-          }
+        if (lane < C::kKW) {
+          const uint4 w = scales[lane];
+          const uint32_t ks = w.x >> (w.z & 0xffffu) & 255u, vs = w.y >> (w.z >> 16) & 255u;
+          scales[lane] = make_uint4(ks << 23, __float_as_uint((float)((int)vs - 127)), 0u, 0u);
+        }
         __syncwarp();
       }
       // ---- scores: MMA row n (n + 8) of block b is key 16 b + key_of(n) (+ 8)
@@ -734,6 +720,7 @@ paged_attention_kernel(const Args a) {
             sh_l[warp][8 * x + 2 * t + j] = l[x][j];
           }
         }
+      __syncwarp();   // every lane has read the stage
       constexpr int kQuarter = kMT / kWarps;                // MMA blocks of 16 dimensions
       constexpr int kFit = C::kStage / (kMT * 512);         // column blocks whose sums fit
       constexpr int kAt = kFit < 1 ? 0 : kFit < kNR ? kFit : kNR;
