@@ -175,19 +175,22 @@ def _dtype_code(t: torch.Tensor) -> int:
     raise TypeError(f"unsupported dtype {t.dtype}")
 
 
-def _want(name, t, dtype, shape, device):
-    """The address of a tensor that has this dtype and shape, lies on this device and is
-    contiguous; any other is refused.  What C cannot see of a tensor is checked here."""
-    if (t.dtype is dtype and t.shape == shape and t.get_device() == device
-            and t.is_contiguous()):
+def _place(name, t, dtype, device):
+    """The address of a contiguous tensor of this dtype on this device; any other is
+    refused.  What C cannot see of a tensor is checked here; sizes are compared apart."""
+    if t.dtype is dtype and t.get_device() == device and t.is_contiguous():
         return t.data_ptr()
     if t.dtype is not dtype:
         raise TypeError(f"{name} has dtype {t.dtype}, not {dtype}")
-    if t.get_device() != device or device < 0:
+    if t.get_device() != device:
         raise ValueError(f"{name} is on {t.device}, not on the current CUDA device")
+    raise ValueError(f"{name} is not contiguous")
+
+
+def _sized(name, t, shape):
+    """Refuses a tensor of another shape."""
     if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
-    raise ValueError(f"{name} is not contiguous")
 
 
 def _device() -> int:
@@ -201,7 +204,7 @@ def _scratch(t, device):
     """Address and bytes of a workspace (None: none)."""
     if t is None:
         return None, 0
-    return _want("workspace", t, t.dtype, t.shape, device), t.numel() * t.element_size()
+    return _place("workspace", t, t.dtype, device), t.numel() * t.element_size()
 
 
 # ---------------------------------------------------------- host helpers
@@ -387,14 +390,6 @@ def hsa_cached_euler_l1rel(x, v_cache, v_fresh, pos, dsigma: float, stat, weight
 
 # ------------------------------------------------ 8-bit cache, paged attention
 
-def _codes_of(k_cache):
-    """dtype of an 8-bit cache's code tensors."""
-    dt = k_cache.dtype
-    if dt is not torch.float8_e4m3fn and dt is not torch.uint8:
-        raise TypeError(f"the cache's codes have dtype {dt}, not float8_e4m3fn or uint8")
-    return dt
-
-
 def _rows_of(name, t, size, n):
     """Refuses fewer than n rows, or rows of other sizes than a cache of this shape has."""
     shape = t.shape
@@ -408,7 +403,22 @@ def _ids(name, t, n, device):
     """Address of at least n indices."""
     if t.numel() < n:
         raise ValueError(f"{name} holds fewer than {n} indices")
-    return _want(name, t, torch.int32, t.shape, device)
+    return _place(name, t, torch.int32, device)
+
+
+def _cache8(k_cache, v_cache, k_scale, v_scale, size, device):
+    """Addresses of an 8-bit cache's four tensors, its rows, heads and dimensions."""
+    code = k_cache.dtype
+    if code is not torch.float8_e4m3fn and code is not torch.uint8:
+        raise TypeError(f"the cache's codes have dtype {code}, not float8_e4m3fn or uint8")
+    *lead, H, D = size
+    scales = (*lead, H)
+    _sized("v_cache", v_cache, size)
+    _sized("k_scale", k_scale, scales)
+    _sized("v_scale", v_scale, scales)
+    return (_place("k_cache", k_cache, code, device), _place("v_cache", v_cache, code, device),
+            _place("k_scale", k_scale, torch.uint8, device),
+            _place("v_scale", v_scale, torch.uint8, device), math.prod(lead), H, D)
 
 
 def hsa_kv_quant_scatter(k_cache, v_cache, k_scale, v_scale, k_fresh, v_fresh, idx, n_active: int,
@@ -417,41 +427,34 @@ def hsa_kv_quant_scatter(k_cache, v_cache, k_scale, v_scale, k_fresh, v_fresh, i
     [N, H, D] (float8_e4m3fn or uint8) and scale bytes [N, H] (uint8); a cache in pages [P,
     page, H, D] with scales [P, page, H] counts as P * page rows.  table: K is rotated first
     (bf16), by the table's rows table_idx (idx where that is None)."""
-    dev, code, size, dt = _device(), _codes_of(k_cache), k_cache.shape, k_fresh.dtype
-    fresh = _rows_of("k_fresh", k_fresh, size, n_active)
-    *lead, H, D = size
-    scales = (*lead, H)
+    dev, size, dt = _device(), k_cache.shape, k_fresh.dtype
+    _sized("v_fresh", v_fresh, _rows_of("k_fresh", k_fresh, size, n_active))
+    if table is not None:
+        _sized("table", table, (table.shape[0], size[-1] // 2, 2))
+    kc, vc, ks, vs, N, H, D = _cache8(k_cache, v_cache, k_scale, v_scale, size, dev)
     tp = ip = None
     rows = 0
     if table is not None:
-        rows = table.shape[0]
-        tp = _want("table", table, torch.float32, (rows, D // 2, 2), dev)
+        rows, tp = table.shape[0], _place("table", table, torch.float32, dev)
     if table_idx is not None:
         ip = _ids("table_idx", table_idx, n_active, dev)
     _check(lib().hsa_kv_quant_scatter(
-        _want("k_cache", k_cache, code, size, dev), _want("v_cache", v_cache, code, size, dev),
-        _want("k_scale", k_scale, torch.uint8, scales, dev),
-        _want("v_scale", v_scale, torch.uint8, scales, dev),
-        _want("k_fresh", k_fresh, dt, fresh, dev), _want("v_fresh", v_fresh, dt, fresh, dev),
-        _ids("idx", idx, n_active, dev), n_active, math.prod(lead), H, D, _dtype_code(k_fresh), tp,
-        ip, rows, _stream(stream)), "hsa_kv_quant_scatter")
+        kc, vc, ks, vs, _place("k_fresh", k_fresh, dt, dev), _place("v_fresh", v_fresh, dt, dev),
+        _ids("idx", idx, n_active, dev), n_active, N, H, D, _dtype_code(k_fresh), tp, ip, rows,
+        _stream(stream)), "hsa_kv_quant_scatter")
 
 
 def hsa_kv_dequant_gather(k_cache, v_cache, k_scale, v_scale, idx, n: int, k_out, v_out,
                           stream=None) -> None:
     """k_out[:n], v_out[:n] ([>= n, H, D], bf16 or fp32) <- rows idx[:n] of an 8-bit cache
     (idx None: rows 0 .. n-1); the cache as for hsa_kv_quant_scatter."""
-    dev, code, size, dt = _device(), _codes_of(k_cache), k_cache.shape, k_out.dtype
-    out = _rows_of("k_out", k_out, size, n)
-    *lead, H, D = size
-    scales = (*lead, H)
+    dev, size, dt = _device(), k_cache.shape, k_out.dtype
+    _sized("v_out", v_out, _rows_of("k_out", k_out, size, n))
+    kc, vc, ks, vs, N, H, D = _cache8(k_cache, v_cache, k_scale, v_scale, size, dev)
     _check(lib().hsa_kv_dequant_gather(
-        _want("k_cache", k_cache, code, size, dev), _want("v_cache", v_cache, code, size, dev),
-        _want("k_scale", k_scale, torch.uint8, scales, dev),
-        _want("v_scale", v_scale, torch.uint8, scales, dev),
-        None if idx is None else _ids("idx", idx, n, dev), n, math.prod(lead), H, D,
-        _want("k_out", k_out, dt, out, dev), _want("v_out", v_out, dt, out, dev),
-        _dtype_code(k_out), _stream(stream)), "hsa_kv_dequant_gather")
+        kc, vc, ks, vs, None if idx is None else _ids("idx", idx, n, dev), n, N, H, D,
+        _place("k_out", k_out, dt, dev), _place("v_out", v_out, dt, dev), _dtype_code(k_out),
+        _stream(stream)), "hsa_kv_dequant_gather")
 
 
 def hsa_paged_attention_workspace_bytes(batch: int, n_new: int, Hq: int, Hkv: int, D: int) -> int:
@@ -465,29 +468,30 @@ def hsa_paged_attention(q, k_pages, v_pages, page_table, seq_lens, out, k_scale=
     max_pages]; bf16 pages, or 8-bit ones (float8_e4m3fn or uint8) with their scale bytes
     [n_pages, page, Hkv].  workspace: uint8 device tensor of at least
     hsa_paged_attention_workspace_bytes(...) bytes."""
-    dev = _device()
-    size, pool = q.shape, k_pages.shape
+    dev, size, pool = _device(), q.shape, k_pages.shape
     B, n_new, Hq, D = size
-    n_pages, page, Hkv = pool[:3]
-    if pool[3] != D or page_table.shape[0] != B:
-        raise ValueError("q, k_pages and page_table disagree on the batch or the head dimension")
-    cols = page_table.shape[1]
-    ks = vs = None
+    n_pages, page, Hkv, Dk = pool
+    batch, cols = page_table.shape
+    if Dk != D or batch != B or seq_lens.shape != (B,):
+        raise ValueError("q, k_pages, page_table and seq_lens disagree on the batch or the head "
+                         "dimension")
+    _sized("out", out, size)
+    qp = _place("q", q, torch.bfloat16, dev)
     if k_scale is None and v_scale is None:
-        kind, code = torch.bfloat16, HSA_BF16
+        _sized("v_pages", v_pages, pool)
+        kp, vp, ks, vs, code = (_place("k_pages", k_pages, torch.bfloat16, dev),
+                                _place("v_pages", v_pages, torch.bfloat16, dev), None, None, HSA_BF16)
+    elif k_scale is None or v_scale is None:
+        raise TypeError("an 8-bit cache has both k_scale and v_scale")
     else:
-        if k_scale is None or v_scale is None:
-            raise TypeError("an 8-bit cache has both k_scale and v_scale")
-        kind, code = _codes_of(k_pages), HSA_E4M3
-        ks = _want("k_scale", k_scale, torch.uint8, pool[:3], dev)
-        vs = _want("v_scale", v_scale, torch.uint8, pool[:3], dev)
+        kp, vp, ks, vs, *_ = _cache8(k_pages, v_pages, k_scale, v_scale, pool, dev)
+        code = HSA_E4M3
     where, room = _scratch(workspace, dev)
     _check(lib().hsa_paged_attention(
-        _want("q", q, torch.bfloat16, size, dev), B, n_new, Hq,
-        _want("k_pages", k_pages, kind, pool, dev), _want("v_pages", v_pages, kind, pool, dev), ks, vs,
-        n_pages, page, Hkv, D, code, _want("page_table", page_table, torch.int32, (B, cols), dev), cols,
-        _want("seq_lens", seq_lens, torch.int32, (B,), dev), float(scale),
-        _want("out", out, torch.bfloat16, size, dev), where, room, _stream(stream)),
+        qp, B, n_new, Hq, kp, vp, ks, vs, n_pages, page, Hkv, D,
+        code, _place("page_table", page_table, torch.int32, dev), cols,
+        _place("seq_lens", seq_lens, torch.int32, dev), float(scale),
+        _place("out", out, torch.bfloat16, dev), where, room, _stream(stream)),
         "hsa_paged_attention")
 
 
@@ -495,16 +499,17 @@ def hsa_packed_attention_workspace_bytes(Hq: int, Hkv: int, D: int) -> int:
     return lib().hsa_packed_attention_workspace_bytes(Hq, Hkv, D)
 
 
-def _token_rows(name, t, H, D, device):
-    """Address and row stride of bf16 token rows [tokens, H, D] on the device whose heads
-    lie together; the rows may lie apart, as in a fused projection's output."""
-    tokens = t.shape[0]
-    if t.is_contiguous() or tokens == 0:
-        return _want(name, t, torch.bfloat16, (tokens, H, D), device) if tokens else None, H * D
+def _token_rows(name, t, device):
+    """Address of bf16 token rows [tokens, H, D] on the device whose heads lie together, and
+    the elements from a row to the next: the rows may lie apart, as in a fused projection's
+    output."""
+    tokens, H, D = t.shape
+    if t.is_contiguous():
+        return _place(name, t, torch.bfloat16, device), H * D
     row, head, one = t.stride()
     if one != 1 or (head != D and H > 1):
         raise ValueError(f"{name} is not rows of {H} heads x {D} that lie together")
-    _want(name, t[0], torch.bfloat16, (H, D), device)
+    _place(name, t[0], torch.bfloat16, device)
     return t.data_ptr(), row
 
 
@@ -515,21 +520,22 @@ def hsa_packed_attention(q, k, v, cu_q, cu_k, out, mask: int = 0, scale: float =
     F: causal by frames of F tokens (1: causal).  The rows of q, k and v may be slices of a
     wider tensor.  workspace (optional): uint8 device tensor of
     hsa_packed_attention_workspace_bytes(Hq, Hkv, D) bytes."""
-    dev = _device()
-    size = q.shape
+    dev, size, keys, ends = _device(), q.shape, k.shape, cu_q.shape
     total_q, Hq, D = size
-    total_k, Hkv = k.shape[:2]
-    (qp, q_row), (kp, k_row) = _token_rows("q", q, Hq, D, dev), _token_rows("k", k, Hkv, D, dev)
-    if v.shape != k.shape:
-        raise ValueError("v has another shape than k")
-    vp, v_row = _token_rows("v", v, Hkv, D, dev)
+    total_k, Hkv, Dk = keys
+    if Dk != D or len(ends) != 1:
+        raise ValueError("q and k disagree on the head dimension, or cu_q is not a vector")
+    _sized("v", v, keys)
+    _sized("cu_k", cu_k, ends)
+    _sized("out", out, size)
+    qp, q_row = _token_rows("q", q, dev)
+    kp, k_row = _token_rows("k", k, dev)
+    vp, v_row = _token_rows("v", v, dev)
     where, room = _scratch(workspace, dev)
-    ends = cu_q.shape
-    batch = cu_q.numel() - 1
     _check(lib().hsa_packed_attention(
-        qp, q_row, kp, k_row, vp, v_row, _want("cu_q", cu_q, torch.int32, (batch + 1,), dev),
-        _want("cu_k", cu_k, torch.int32, ends, dev), batch, total_q, total_k, Hq, Hkv, D, mask,
-        float(scale), _want("out", out, torch.bfloat16, size, dev), HSA_BF16, where, room,
+        qp, q_row, kp, k_row, vp, v_row, _place("cu_q", cu_q, torch.int32, dev),
+        _place("cu_k", cu_k, torch.int32, dev), ends[0] - 1, total_q, total_k, Hq, Hkv, D, mask,
+        float(scale), _place("out", out, torch.bfloat16, dev), HSA_BF16, where, room,
         _stream(stream)), "hsa_packed_attention")
 
 

@@ -163,3 +163,30 @@ def test_packed_binding_refuses_what_c_cannot_see(hsa, monkeypatch):
         hsa.hsa_packed_attention(q.float(), k, k, cu, cu, q)
     with pytest.raises(ValueError, match="lie together"):
         hsa.hsa_packed_attention(torch.zeros((4, 64, 2), dtype=torch.bfloat16).transpose(1, 2), k, k, cu, cu, q)
+
+
+def test_binding_names_what_is_wrong(hsa, monkeypatch):
+    """Shapes that do not go together are refused by name."""
+    monkeypatch.setattr(hsa, "lib", lambda: None)
+    c, s = torch.zeros((4, 2, 64), dtype=torch.uint8), torch.zeros((4, 2), dtype=torch.uint8)
+    x, i = torch.zeros((3, 2, 64), dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int32)
+    for name, args in (("v_fresh", (c, c, s, s, x, x[:2], i, 2)), ("v_cache", (c, c[:3], s, s, x, x, i, 2)),
+                       ("k_scale", (c, c, s[:3], s, x, x, i, 2)), ("v_scale", (c, c, s, s[:, :1], x, x, i, 2))):
+        with pytest.raises(ValueError, match=name):
+            hsa.hsa_kv_quant_scatter(*args)
+    with pytest.raises(ValueError, match="table"):
+        hsa.hsa_kv_quant_scatter(c, c, s, s, x, x, i, 2, table=torch.zeros((4, 16, 2)))
+    with pytest.raises(ValueError, match="v_out"):
+        hsa.hsa_kv_dequant_gather(c, c, s, s, None, 2, x, x[:1])
+    q, pages = torch.zeros((1, 1, 4, 64), dtype=torch.bfloat16), torch.zeros((2, 16, 2, 64), dtype=torch.bfloat16)
+    t, n = torch.zeros((1, 2), dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    with pytest.raises(ValueError, match="batch"):
+        hsa.hsa_paged_attention(q, pages, pages, t, n.repeat(2), q)
+    with pytest.raises(ValueError, match="out"):
+        hsa.hsa_paged_attention(q, pages, pages, t, n, q[:, :, :2])
+    k, cu = torch.zeros((4, 1, 64), dtype=torch.bfloat16), torch.tensor([0, 4], dtype=torch.int32)
+    p = torch.zeros((4, 2, 64), dtype=torch.bfloat16)
+    for name, args in (("v has", (p, k, k[:3], cu, cu, p)), ("cu_k", (p, k, k, cu, cu[:1], p)),
+                       ("out", (p, k, k, cu, cu, p[:3])), ("head", (p, k[:, :, :32], k, cu, cu, p))):
+        with pytest.raises(ValueError, match=name):
+            hsa.hsa_packed_attention(*args)
