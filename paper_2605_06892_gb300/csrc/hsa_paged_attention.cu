@@ -820,13 +820,13 @@ paged_attention_kernel(const Args a) {
 // Joins a row's parts where several blocks shared its unit: one block for each block of
 // the kernel before and each row, and most of them find that theirs ended no such unit.
 // A part takes D/4 lanes, four dimensions each; bound by the round trips to L2, so each
-// lane group loads four parts at once, and statistics with sums.
+// lane group loads eight parts at once, and statistics with sums.
 constexpr int kJoinThreads = 256;
 
 template <int D, int kNR>
 __global__ void __launch_bounds__(kJoinThreads)
 paged_join_kernel(const Args a) {
-  constexpr int kRows = 8 * kNR, kL = D / 4, kGroups = kJoinThreads / kL;
+  constexpr int kRows = 8 * kNR, kL = D / 4, kGroups = kJoinThreads / kL, kAtOnce = 8;
   __shared__ float4 sh_o[kJoinThreads];
   __shared__ float2 sh_ml[kGroups];
   pdl_wait();
@@ -838,11 +838,11 @@ paged_join_kernel(const Args a) {
   const int sub = threadIdx.x % kL, group = threadIdx.x / kL;
   float M = kLowest, L = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int p0 = group; p0 < u.parts; p0 += 4 * kGroups) {
-    float2 w[4];
-    float4 x[4];
+  for (int p0 = group; p0 < u.parts; p0 += kAtOnce * kGroups) {
+    float2 w[kAtOnce];
+    float4 x[kAtOnce];
 #pragma unroll
-    for (int y = 0; y < 4; ++y) {
+    for (int y = 0; y < kAtOnce; ++y) {
       const int p = p0 + y * kGroups;
       w[y] = make_float2(kLowest, 0.f);
       x[y] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -852,12 +852,14 @@ paged_join_kernel(const Args a) {
         x[y] = *reinterpret_cast<const float4 *>(part + rr * D + 4 * sub);
       }
     }
-    const float to = fmaxf(fmaxf(fmaxf(w[0].x, w[1].x), fmaxf(w[2].x, w[3].x)), M);
+    float to = M;
+#pragma unroll
+    for (int y = 0; y < kAtOnce; ++y) to = fmaxf(to, w[y].x);
     const float f0 = fast_exp2(M - to);
     M = to;
     L *= f0, acc.x *= f0, acc.y *= f0, acc.z *= f0, acc.w *= f0;
 #pragma unroll
-    for (int y = 0; y < 4; ++y) {
+    for (int y = 0; y < kAtOnce; ++y) {
       const float f = fast_exp2(w[y].x - M);
       L = fmaf(f, w[y].y, L);
       acc.x = fmaf(f, x[y].x, acc.x);
