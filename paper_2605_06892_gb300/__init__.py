@@ -394,8 +394,8 @@ def _rows_of(name, t, size, n):
     """Refuses fewer than n rows, or rows of other sizes than a cache of this shape has."""
     shape = t.shape
     if len(shape) != 3 or shape[1] != size[-2] or shape[2] != size[-1] or not 0 <= n <= shape[0]:
-        raise ValueError(f"{name} has shape {tuple(shape)}, not {n} or more rows of {size[-2]} heads x "
-                         f"{size[-1]}")
+        raise ValueError(f"{name} has shape {tuple(shape)}, not {n} or more rows of {size[-2]} "
+                         f"heads x {size[-1]}")
     return shape
 
 
@@ -479,8 +479,9 @@ def hsa_paged_attention(q, k_pages, v_pages, page_table, seq_lens, out, k_scale=
     qp = _place("q", q, torch.bfloat16, dev)
     if k_scale is None and v_scale is None:
         _sized("v_pages", v_pages, pool)
-        kp, vp, ks, vs, code = (_place("k_pages", k_pages, torch.bfloat16, dev),
-                                _place("v_pages", v_pages, torch.bfloat16, dev), None, None, HSA_BF16)
+        kp = _place("k_pages", k_pages, torch.bfloat16, dev)
+        vp = _place("v_pages", v_pages, torch.bfloat16, dev)
+        ks, vs, code = None, None, HSA_BF16
     elif k_scale is None or v_scale is None:
         raise TypeError("an 8-bit cache has both k_scale and v_scale")
     else:
@@ -513,8 +514,8 @@ def _token_rows(name, t, device):
     return t.data_ptr(), row
 
 
-def hsa_packed_attention(q, k, v, cu_q, cu_k, out, mask: int = 0, scale: float = 0.0, workspace=None,
-                         stream=None) -> None:
+def hsa_packed_attention(q, k, v, cu_q, cu_k, out, mask: int = 0, scale: float = 0.0,
+                         workspace=None, stream=None) -> None:
     """out [total_q, Hq, D] = attention of packed sequences: queries q[cu_q[b]:cu_q[b+1]] of
     [total_q, Hq, D] over k, v[cu_k[b]:cu_k[b+1]] of [total_k, Hkv, D], bf16; mask 0: none,
     F: causal by frames of F tokens (1: causal).  The rows of q, k and v may be slices of a

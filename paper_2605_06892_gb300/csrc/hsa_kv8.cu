@@ -120,9 +120,9 @@ __device__ __forceinline__ void unpack8(const Eight<kF32> &v, float (&x)[8]) {
 constexpr uint32_t kTop = 0x7f700000u;   // 1.875 2^127: the next code would stand for 2^128
 
 // The codes of a row's eight elements, twice (all lanes of the warp call it together: a
-// shuffle over fewer costs a synchronisation of its own), and the row's scale byte.  `bad` is set where an element is not finite: its
-// code is NaN and the others go by the largest finite magnitude.  Finite magnitudes above
-// kTop count as that.
+// shuffle over fewer costs a synchronisation of its own), and the row's scale byte.  `bad` is set
+// where an element is not finite: its code is NaN and the others go by the largest finite
+// magnitude.  Finite magnitudes above kTop count as that.
 template <bool kF32>
 __device__ __forceinline__ void quantise(const Eight<kF32> (&v)[2], int L, uint2 (&c)[2],
                                          unsigned &scale, bool &bad) {
@@ -205,7 +205,8 @@ kv_quant_scatter_kernel(const QuantArgs a) {
           v[y] = load8<kF32>(a.vf, at + 8 * L * y);
         }
     }
-    const bool ok = there && slot >= 0 && slot < a.N && (!kRope || (trow >= 0 && trow < a.table_rows));
+    const bool ok = there && slot >= 0 && slot < a.N &&
+                    (!kRope || (trow >= 0 && trow < a.table_rows));
     if (there && !ok) set_error(a.err, kErrIndex);
     if (kRope && ok) {
       const float4 *t = reinterpret_cast<const float4 *>(a.table + (size_t)trow * a.D) + 2 * c;
@@ -383,8 +384,8 @@ extern "C" int hsa_kv_quant_scatter(void *k_cache, void *v_cache, uint8_t *k_sca
   launch_pdl(dtype == HSA_F32 ? kv_quant_scatter_kernel<true, false>
              : table          ? kv_quant_scatter_kernel<false, true>
                               : kv_quant_scatter_kernel<false, false>,
-             dim3(grid_for(a.items, a.lpr_log2, 1, dtype == HSA_F32 ? 4 : kQuantBlocks)), dim3(kThreads), 0,
-             (cudaStream_t)stream, a);
+             dim3(grid_for(a.items, a.lpr_log2, 1, dtype == HSA_F32 ? 4 : kQuantBlocks)),
+             dim3(kThreads), 0, (cudaStream_t)stream, a);
   return launch_status();
 }
 
@@ -415,7 +416,8 @@ extern "C" int hsa_kv_dequant_gather(const void *k_cache, const void *v_cache,
   a.D = D;
   a.lpr_log2 = log2i(D / 8);
   count_launches(1);
-  launch_pdl(dtype == HSA_F32 ? kv_dequant_gather_kernel<true, kU> : kv_dequant_gather_kernel<false, kU>,
+  launch_pdl(dtype == HSA_F32 ? kv_dequant_gather_kernel<true, kU>
+                              : kv_dequant_gather_kernel<false, kU>,
              dim3(grid_for(a.items, a.lpr_log2, kU, kBlocks)), dim3(kThreads), 0,
              (cudaStream_t)stream, a);
   return launch_status();

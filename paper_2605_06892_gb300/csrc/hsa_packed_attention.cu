@@ -66,12 +66,13 @@ struct Sequence {
 
 // Bytes to come on a barrier's present phase, without an arrival.
 __device__ __forceinline__ void mbar_expect_tx_only(uint64_t *b, uint32_t bytes) {
-  asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(b)), "r"(bytes)
+  asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(b)),
+               "r"(bytes)
                : "memory");
 }
 
-__device__ __forceinline__ void tma_load_3d(void *dst, const CUtensorMap *map, uint64_t *bar, int x, int y,
-                                            int z) {
+__device__ __forceinline__ void tma_load_3d(void *dst, const CUtensorMap *map, uint64_t *bar,
+                                            int x, int y, int z) {
   asm volatile(
       "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes"
       " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_addr(dst)),
@@ -167,7 +168,9 @@ __device__ __forceinline__ bool unit_of(const PackedArgs &a, int id, Plan &p, Un
     // Fewer units than SMs: the shortest part length that makes no more parts than SMs, or
     // than two waves of them; a part costs its tiles and about 5 tiles' time more.
     unsigned work = 0;   // < 2^24 tiles of fewer units than SMs
-    each([&](const Sequence &s, int blocks) { work += (unsigned)blocks * ((s.lk + kBN - 1) / kBN); });
+    each([&](const Sequence &s, int blocks) {
+      work += (unsigned)blocks * ((s.lk + kBN - 1) / kBN);
+    });
     const int far = longest();
     work = __reduce_add_sync(0xffffffffu, work) * a.Hkv;
     auto shortest = [&](int most) {
@@ -300,8 +303,8 @@ __device__ __forceinline__ __nv_bfloat16 *out_row(const PackedArgs &a, int q0, i
 // already.  Rare and slow; out of line so that it costs the usual path no registers.  False:
 // no row needed it.
 template <int D>
-__device__ __noinline__ bool form_again(const PackedArgs &a, const Unit &u, uint32_t tO, int R, int limit,
-                                        int k0, int k1, float m, bool valid) {
+__device__ __noinline__ bool form_again(const PackedArgs &a, const Unit &u, uint32_t tO, int R,
+                                        int limit, int k0, int k1, float m, bool valid) {
   const __nv_bfloat16 *K = a.k + (size_t)u.seq.k0 * a.k_row + (size_t)u.head * D;
   const __nv_bfloat16 *V = a.v + (size_t)u.seq.k0 * a.v_row + (size_t)u.head * D;
   const int tok = valid ? quotient(R, a.group) : 0;
@@ -339,12 +342,14 @@ __device__ __noinline__ bool form_again(const PackedArgs &a, const Unit &u, uint
       if (j < end) {
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-          const uint4 w = __ldg(reinterpret_cast<const uint4 *>(V + (size_t)j * a.v_row + 32 * c) + v);
+          const uint4 w = __ldg(reinterpret_cast<const uint4 *>(V + (size_t)j * a.v_row +
+                                                                32 * c) + v);
           const uint32_t x[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             acc[8 * v + 2 * i] = fmaf(p, __uint_as_float(x[i] << 16), acc[8 * v + 2 * i]);
-            acc[8 * v + 2 * i + 1] = fmaf(p, __uint_as_float(x[i] & 0xffff0000u), acc[8 * v + 2 * i + 1]);
+            acc[8 * v + 2 * i + 1] = fmaf(p, __uint_as_float(x[i] & 0xffff0000u),
+                                          acc[8 * v + 2 * i + 1]);
           }
         }
       }
@@ -366,9 +371,9 @@ __device__ __noinline__ bool form_again(const PackedArgs &a, const Unit &u, uint
 // the warp's own (see the active attention's store: neighbouring lanes store neighbouring
 // vectors).  again() is called once if a row's sums are not all finite and may change them.
 template <int D, typename Again>
-__device__ __forceinline__ void store_rows(const PackedArgs &a, const Unit &u, int piece, int r0, int lane,
-                                           uint32_t tO, float m_run, float l_run, uint8_t *stage,
-                                           Again &&again) {
+__device__ __forceinline__ void store_rows(const PackedArgs &a, const Unit &u, int piece, int r0,
+                                           int lane, uint32_t tO, float m_run, float l_run,
+                                           uint8_t *stage, Again &&again) {
   uint4 *st = reinterpret_cast<uint4 *>(stage);
   if (piece >= 0) {
     constexpr int kV = D / 4;
@@ -396,7 +401,8 @@ __device__ __forceinline__ void store_rows(const PackedArgs &a, const Unit &u, i
       const int e = 32 * i + lane, row = e / kV, v = e % kV;
       dst[e] = st[row * kV + ((v & ~7) | ((v & 7) ^ (row & 7)))];
     }
-    reinterpret_cast<float2 *>(a.ws_ml)[(size_t)piece * kUnitRows + r0 + lane] = make_float2(m_run, l_run);
+    reinterpret_cast<float2 *>(a.ws_ml)[(size_t)piece * kUnitRows + r0 + lane] =
+        make_float2(m_run, l_run);
     return;
   }
   const float inv = l_run > 0.f ? 1.f / l_run : l_run == 0.f ? 0.f : l_run;   // no keys: zeros
@@ -416,7 +422,8 @@ __device__ __forceinline__ void store_rows(const PackedArgs &a, const Unit &u, i
           pk[i] = pack_bf16(__uint_as_float(o[8 * v + 2 * i]) * inv,
                             __uint_as_float(o[8 * v + 2 * i + 1]) * inv);
         const int x = 4 * c + v;
-        st[lane * kV + ((x & ~7) | ((x & 7) ^ (lane & 7)))] = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+        st[lane * kV + ((x & ~7) | ((x & 7) ^ (lane & 7)))] =
+            make_uint4(pk[0], pk[1], pk[2], pk[3]);
       }
 #pragma unroll
       for (int i = 0; i < 32; ++i) worst[i & 3] = fmaf(__uint_as_float(o[i]), 0.f, worst[i & 3]);
@@ -442,8 +449,10 @@ __device__ __forceinline__ void store_rows(const PackedArgs &a, const Unit &u, i
 
 template <int D>
 __global__ void __launch_bounds__(kTcThreads, 1)
-packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
-                        const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ PackedArgs a) {
+packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k,
+                        const __grid_constant__ CUtensorMap tm_v,
+                        const __grid_constant__ CUtensorMap tm_q,
+                        const __grid_constant__ PackedArgs a) {
   using C = TcCfg<D>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
@@ -506,7 +515,8 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
     a.cuts->unit[u.cut] = {u.parts, u.slot, rows, u.row0, u.seq.q0, u.head, {0, 0}};
   if (nT == 0) {   // no row has keys
     for (int i = threadIdx.x; i < rows * (D / 8); i += kTcThreads)
-      *reinterpret_cast<uint4 *>(out_row<D>(a, u.seq.q0, u.head, u.row0 + i / (D / 8)) + 8 * (i % (D / 8))) =
+      *reinterpret_cast<uint4 *>(out_row<D>(a, u.seq.q0, u.head, u.row0 + i / (D / 8)) +
+                                 8 * (i % (D / 8))) =
           make_uint4(0u, 0u, 0u, 0u);
     return;
   }
@@ -519,7 +529,8 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
     const int y = key0 + (L >> 1) * kBN;
 #pragma unroll
     for (int c = 0; c < C::kChunks; ++c)
-      tma_load_2d(dst + c * (kBN * 128), (L & 1) ? &tm_v : &tm_k, &bar_full[slot], col0 + c * 64, y);
+      tma_load_2d(dst + c * (kBN * 128), (L & 1) ? &tm_v : &tm_k, &bar_full[slot], col0 + c * 64,
+                  y);
   };
   const int withheld = a.inject_stall == 1 ? 1 : -1;
   const int n_pre = min(3, 2 * nT);
@@ -545,8 +556,8 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
       for (int t = 0; t < kQT; ++t)
 #pragma unroll
         for (int c = 0; c < C::kChunks; ++c)
-          tma_load_3d(sQ + t * C::kTileBytes + c * (kBM * 128), &tm_q, &bar_full[0], c * 64, u.head * G,
-                      tok + t * (int)quotient(kBM, a.group));
+          tma_load_3d(sQ + t * C::kTileBytes + c * (kBM * 128), &tm_q, &bar_full[0], c * 64,
+                      u.head * G, tok + t * (int)quotient(kBM, a.group));
       for (int L = 0; L < n_pre; ++L)
         if (L != withheld) load_kv(L);
     }
@@ -611,7 +622,8 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
         for (int i = have * 8 + lane; i < kBN * 8; i += 32)
 #pragma unroll
           for (int c = 0; c < C::kChunks; ++c)
-            *reinterpret_cast<uint4 *>(tile + c * (kBN * 128) + 16 * i) = make_uint4(0u, 0u, 0u, 0u);
+            *reinterpret_cast<uint4 *>(tile + c * (kBN * 128) + 16 * i) =
+                make_uint4(0u, 0u, 0u, 0u);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
       });
@@ -634,10 +646,11 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
     const uint32_t tO = tmem + lane_off + C::kOCol0 + D * t;
     const float sl2 = a.scale_log2;
     float m_run = kLowest, l_run = 0.f;
-    // Keys from tile j0 on that this thread's row sees; rows past the sequence's last take no mask.  The
-    // warp's first row sees fewest.
+    // Keys from tile j0 on that this thread's row sees; rows past the sequence's last take no
+    // mask.  The warp's first row sees fewest.
     const int r = t * kBM + wq * 32 + lane;
-    const int limit = (r < rows ? key_limit(a, u.seq, quotient(u.row0 + r, a.group)) : u.seq.lk) - j0 * kBN;
+    const int seen = r < rows ? key_limit(a, u.seq, quotient(u.row0 + r, a.group)) : u.seq.lk;
+    const int limit = seen - j0 * kBN;
     const int all_see = __shfl_sync(0xffffffffu, limit, 0);
     for (int j = 0; j < nT; ++j) {
       named_barrier_sync(kBarS0 + t, kMeetS);
@@ -664,10 +677,11 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
     ok = !__any_sync(0xffffffffu, abort_flag != 0) && ok;
     if (ok) {
       fence_after();
-      store_rows<D>(a, u, u.parts > 1 ? u.slot + u.part : -1, t * kBM + wq * 32, lane, tO, m_run, l_run,
-                    sKV + (warp - 4) * (32 * D * 4), [&]() {
-                      return a.mask && form_again<D>(a, u, tO, u.row0 + r, limit + j0 * kBN, j0 * kBN,
-                                                     min(u.seq.lk, (j0 + nT) * kBN), m_run, r < rows);
+      store_rows<D>(a, u, u.parts > 1 ? u.slot + u.part : -1, t * kBM + wq * 32, lane, tO, m_run,
+                    l_run, sKV + (warp - 4) * (32 * D * 4), [&]() {
+                      return a.mask && form_again<D>(a, u, tO, u.row0 + r, limit + j0 * kBN,
+                                                     j0 * kBN, min(u.seq.lk, (j0 + nT) * kBN),
+                                                     m_run, r < rows);
                     });
     }
     fence_before();
@@ -690,7 +704,8 @@ packed_join_kernel(const PackedArgs a) {
   pdl_wait();
   pdl_trigger();
   const int n = a.cuts->n * kUnitRows;
-  const int i0 = (int)((long long)n * blockIdx.x / gridDim.x), i1 = (int)((long long)n * (blockIdx.x + 1) / gridDim.x);
+  const int i0 = (int)((long long)n * blockIdx.x / gridDim.x);
+  const int i1 = (int)((long long)n * (blockIdx.x + 1) / gridDim.x);
   const int sub = threadIdx.x % kL, group = threadIdx.x / kL;
   for (int i = i0; i < i1;) {
     const int tail = i / kUnitRows, end = min(i1, (tail + 1) * kUnitRows);
@@ -772,8 +787,8 @@ packed_join_kernel(const PackedArgs a) {
 
 // 3-D map over N tokens of H heads x D bf16 values, the tokens `row` elements apart: boxes
 // of `tokens` x `heads` x 64 dimensions, 128-byte swizzle, tokens past N read as zero.
-bool make_rows_map(CUtensorMap *map, const void *base, int N, int H, int D, long long row, int heads,
-                   int tokens) {
+bool make_rows_map(CUtensorMap *map, const void *base, int N, int H, int D, long long row,
+                   int heads, int tokens) {
   auto enc = encode_fn();
   if (!enc) return false;
   const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)H, (cuuint64_t)N};
@@ -805,13 +820,16 @@ int launch(PackedArgs &a, const void *any, cudaStream_t stream) {
   CUtensorMap mk, mv, mq;
   // without keys no tile is loaded: any valid map serves
   const int keys = std::max(a.total_k, 1);
-  if (!make_kv_map(&mk, a.total_k ? a.k : any, keys, a.Hkv * D, a.total_k ? a.k_row : (long long)a.Hkv * D) ||
-      !make_kv_map(&mv, a.total_k ? a.v : any, keys, a.Hkv * D, a.total_k ? a.v_row : (long long)a.Hkv * D))
+  if (!make_kv_map(&mk, a.total_k ? a.k : any, keys, a.Hkv * D,
+                   a.total_k ? a.k_row : (long long)a.Hkv * D) ||
+      !make_kv_map(&mv, a.total_k ? a.v : any, keys, a.Hkv * D,
+                   a.total_k ? a.v_row : (long long)a.Hkv * D))
     return HSA_ERR_CUDA;
   // A box of the query tensor [total_q, Hq, D] is a Q tile where G divides its rows.
   const int G = (int)a.group.d;
   a.q_map = kBM % G == 0;
-  if (a.q_map && !make_rows_map(&mq, a.q, a.total_q, a.Hq, D, a.q_row, G, kBM / G)) return HSA_ERR_CUDA;
+  if (a.q_map && !make_rows_map(&mq, a.q, a.total_q, a.Hq, D, a.q_row, G, kBM / G))
+    return HSA_ERR_CUDA;
   if (!a.q_map) mq = mk;
   // Units at most: every sequence has at most one partly filled block.  How many there are
   // is on the device, so the grid holds what a cut may make of them: a block too many costs
@@ -821,14 +839,16 @@ int launch(PackedArgs &a, const void *any, cudaStream_t stream) {
   const long long units = ((long long)a.total_q * a.group.d / kUnitRows + a.batch) * a.Hkv;
   if (a.total_k <= (kLeastTiles + kJoinTiles) * kBN) a.most = 0;
   if (a.most) a.most = 2 * units <= a.sms ? a.sms : 2 * a.sms;
-  const long long grid = a.mask || units < a.sms ? std::max<long long>(units, a.most) : units + a.most;
+  const long long grid =
+      a.mask || units < a.sms ? std::max<long long>(units, a.most) : units + a.most;
   if (grid > 0x7fffffffLL) return HSA_ERR_UNSUPPORTED;
   a.bound = (int)units;
   count_launches(a.most ? 2 : 1);
   launch_pdl(kernel, dim3((unsigned)grid), dim3(kTcThreads), C::kSmem, stream, mk, mv, mq, a);
   if (cudaGetLastError() != cudaSuccess) return HSA_ERR_CUDA;
   if (a.most)
-    launch_pdl(packed_join_kernel<D>, dim3((unsigned)(8 * a.sms)), dim3(kJoinThreads), 0, stream, a);
+    launch_pdl(packed_join_kernel<D>, dim3((unsigned)(8 * a.sms)), dim3(kJoinThreads), 0, stream,
+               a);
   return launch_status();
 }
 
@@ -849,15 +869,17 @@ extern "C" size_t hsa_packed_attention_workspace_bytes(int Hq, int Hkv, int D) {
 
 extern "C" int hsa_packed_attention(const void *q, long long q_row, const void *k, long long k_row,
                                     const void *v, long long v_row, const int32_t *cu_q,
-                                    const int32_t *cu_k, int batch, int total_q, int total_k, int Hq,
-                                    int Hkv, int D, int mask, float scale, void *out, hsa_dtype dtype,
-                                    void *workspace, size_t workspace_size, hsa_stream_t stream) {
+                                    const int32_t *cu_k, int batch, int total_q, int total_k,
+                                    int Hq, int Hkv, int D, int mask, float scale, void *out,
+                                    hsa_dtype dtype, void *workspace, size_t workspace_size,
+                                    hsa_stream_t stream) {
   if (batch < 0 || total_q < 0 || total_k < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv || mask < 0)
     return HSA_ERR_INVALID_ARG;
   if (dtype != HSA_BF16 && dtype != HSA_F32) return HSA_ERR_INVALID_ARG;
   if (dtype == HSA_F32 || (D != 64 && D != 128) || (long long)Hq * D > (1LL << 24))
     return HSA_ERR_UNSUPPORTED;
-  if (total_k > 0x7fffff00 || (long long)total_q * (Hq / Hkv) > 0x7fffff00LL) return HSA_ERR_UNSUPPORTED;
+  if (total_k > 0x7fffff00 || (long long)total_q * (Hq / Hkv) > 0x7fffff00LL)
+    return HSA_ERR_UNSUPPORTED;
   if (q_row < (long long)Hq * D || k_row < (long long)Hkv * D || v_row < (long long)Hkv * D ||
       (q_row & 7) || (k_row & 7) || (v_row & 7) || q_row > (1LL << 31) || k_row > (1LL << 31) ||
       v_row > (1LL << 31))

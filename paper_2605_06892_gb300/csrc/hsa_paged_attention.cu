@@ -67,7 +67,8 @@ __device__ __forceinline__ uint32_t f16x2_of_e4m3x2(uint32_t codes16) {
 
 // d += a b, 16 rows x 8 columns x 16.
 template <bool kF16>
-__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0,
+                                    uint32_t b1) {
   if (kF16)
     asm volatile(
         "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
@@ -91,7 +92,8 @@ __device__ __forceinline__ uint32_t transposed(uint32_t w) {
 
 // 16 bytes into shared memory, zeros where !ok.
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool ok) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0)
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src),
+               "r"(ok ? 16 : 0)
                : "memory");
 }
 __device__ __forceinline__ void copy4(uint32_t dst, const void *src) {
@@ -197,7 +199,9 @@ __device__ __forceinline__ Plan plan_of(int total, int grid, int sms) {
   p.more = total - p.base * p.ctas;
   return p;
 }
-__device__ __forceinline__ int first_tile(const Plan &p, int cta) { return cta * p.base + min(cta, p.more); }
+__device__ __forceinline__ int first_tile(const Plan &p, int cta) {
+  return cta * p.base + min(cta, p.more);
+}
 __device__ __forceinline__ int cta_of(const Plan &p, int tile) {
   const int longer = p.more * (p.base + 1);
   return tile < longer ? tile / (p.base + 1) : p.more + (tile - longer) / p.base;
@@ -334,7 +338,9 @@ paged_attention_kernel(const Args a) {
   int page;
   auto look_up = [&]() {
     const int key = ahead.tile * C::kTile + warp * C::kKW + krow;
-    page = key < ahead.len ? __ldg(a.table + (size_t)ahead.b * a.max_pages + (key >> a.page_log2)) : -1;
+    page = -1;
+    if (key < ahead.len)
+      page = __ldg(a.table + (size_t)ahead.b * a.max_pages + (key >> a.page_log2));
   };
   look_up();
   int q_fill = 0, q_now = 0;                // buffers of the next unit's rows, and of this one's
@@ -352,9 +358,10 @@ paged_attention_kernel(const Args a) {
           const int e = e0 + threadIdx.x, r = e / (D / 8), c = e % (D / 8);
           if (kRows * (D / 8) % kThreads != 0 && e >= kRows * (D / 8)) break;
           const bool ok = r0 + r < a.rows;
-          const int i = ok ? quotient(r0 + r, a.group) : 0, head = ok ? r0 + r - i * (int)a.group.d : 0;
+          const int i = ok ? quotient(r0 + r, a.group) : 0;
+          const int head = h * (int)a.group.d + (ok ? r0 + r - i * (int)a.group.d : 0);
           copy16(to + r * (2 * D) + 16 * (c ^ (r & 7)),
-                 a.q + ((size_t)((size_t)ahead.b * a.n_new + i) * a.Hq + h * (int)a.group.d + head) * D + 8 * c, ok);
+                 a.q + (((size_t)ahead.b * a.n_new + i) * a.Hq + head) * D + 8 * c, ok);
         }
         q_fill = q_fill + 1 == C::kStages ? 0 : q_fill + 1;
       }
@@ -432,7 +439,9 @@ paged_attention_kernel(const Args a) {
         f = __uint_as_float((268u - E) << 23);
         return a.scale_log2 * __uint_as_float((E - 14u) << 23);
       };
-      auto larger = [](float big, uint32_t w) { return fmaxf(big, fmaxf(fabsf(lo_bf16(w)), fabsf(hi_bf16(w)))); };
+      auto larger = [](float big, uint32_t w) {
+        return fmaxf(big, fmaxf(fabsf(lo_bf16(w)), fabsf(hi_bf16(w))));
+      };
       auto scaled = [](uint32_t w, float f) { return pack_f16(lo_bf16(w) * f, hi_bf16(w) * f); };
 #pragma unroll
       for (int x = 0; x < kNR; ++x) {
@@ -548,7 +557,8 @@ paged_attention_kernel(const Args a) {
 #pragma unroll
           for (int x = 0; x < kNR; ++x)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) mx[x][j] = fmaxf(mx[x][j], fmaxf(s[b][x][j], s[b][x][2 + j]));
+            for (int j = 0; j < 2; ++j)
+              mx[x][j] = fmaxf(mx[x][j], fmaxf(s[b][x][j], s[b][x][2 + j]));
       } else {
 #pragma unroll
         for (int b = 0; b < kNB; ++b)
@@ -618,7 +628,8 @@ paged_attention_kernel(const Args a) {
           if (kF8) {
             uint32_t wa[4] = {0, 0, 0, 0}, wb[4] = {0, 0, 0, 0};
             if (D == 128) {
-              const uint4 y = lds128(pa + 16 * v_chunk<kCh>(g, ra)), z = lds128(pb + 16 * v_chunk<kCh>(g, rb));
+              const uint4 y = lds128(pa + 16 * v_chunk<kCh>(g, ra));
+              const uint4 z = lds128(pb + 16 * v_chunk<kCh>(g, rb));
               wa[0] = y.x, wa[1] = y.y, wa[2] = y.z, wa[3] = y.w;
               wb[0] = z.x, wb[1] = z.y, wb[2] = z.z, wb[3] = z.w;
             } else {
@@ -628,7 +639,8 @@ paged_attention_kernel(const Args a) {
             }
 #pragma unroll
             for (int w = 0; w < kNT / 4; ++w) {
-              const uint32_t y = __byte_perm(wa[w], wb[w], 0x5140), z = __byte_perm(wa[w], wb[w], 0x7362);
+              const uint32_t y = __byte_perm(wa[w], wb[w], 0x5140);
+              const uint32_t z = __byte_perm(wa[w], wb[w], 0x7362);
               vf[4 * w][hi] = f16x2_of_e4m3x2(y);
               vf[4 * w + 1][hi] = f16x2_of_e4m3x2(y >> 16);
               vf[4 * w + 2][hi] = f16x2_of_e4m3x2(z);
@@ -735,7 +747,8 @@ paged_attention_kernel(const Args a) {
 #pragma unroll
           for (int x = 0; x < kAt; ++x) {
             const float(&y)[4] = o[n][x0 + x];
-            reinterpret_cast<float4 *>(ring + now)[(n * kAt + x) * 32 + lane] = make_float4(y[0], y[1], y[2], y[3]);
+            reinterpret_cast<float4 *>(ring + now)[(n * kAt + x) * 32 + lane] =
+                make_float4(y[0], y[1], y[2], y[3]);
           }
         __syncthreads();
 #pragma unroll
@@ -760,15 +773,17 @@ paged_attention_kernel(const Args a) {
             y[n][0] = y[n][1] = y[n][2] = y[n][3] = 0.f;
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
-              const float4 z = reinterpret_cast<const float4 *>(
-                  smem + w * (C::kStages * C::kStage) + now)[((warp * kQuarter + n) * kAt + x - x0) * 32 + lane];
+              const float4 z =
+                  reinterpret_cast<const float4 *>(smem + w * (C::kStages * C::kStage) + now)
+                      [((warp * kQuarter + n) * kAt + x - x0) * 32 + lane];
               y[n][0] = fmaf(z.x, f[0][w], y[n][0]), y[n][1] = fmaf(z.y, f[1][w], y[n][1]);
               y[n][2] = fmaf(z.z, f[0][w], y[n][2]), y[n][3] = fmaf(z.w, f[1][w], y[n][3]);
             }
           }
           // block n holds dimensions E g + 2 n and the next (bf16: + 56 from n = 4 on)
           constexpr int kE = kF8 ? kNT : 8;
-          const int n0 = warp * kQuarter, d = kE * g + (kE == 8 ? (n0 / 4) * 64 + 2 * (n0 % 4) : 2 * n0);
+          const int n0 = warp * kQuarter;
+          const int d = kE * g + (kE == 8 ? (n0 / 4) * 64 + 2 * (n0 % 4) : 2 * n0);
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             const int rr = 8 * x + 2 * t + j, r = r0 + rr;
@@ -788,7 +803,8 @@ paged_attention_kernel(const Args a) {
             } else {
 #pragma unroll
               for (int n = 0; n < kQuarter; ++n)
-                *reinterpret_cast<float2 *>(part + rr * D + d + 2 * n) = make_float2(y[n][j], y[n][2 + j]);
+                *reinterpret_cast<float2 *>(part + rr * D + d + 2 * n) =
+                    make_float2(y[n][j], y[n][2 + j]);
               if (warp == 0 && g == 0) {
                 part[kRows * D + 2 * rr] = M[j];
                 part[kRows * D + 2 * rr + 1] = sum[j];
@@ -889,7 +905,8 @@ paged_join_kernel(const Args a) {
   }
   const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;
   const int i = quotient(r, a.group);
-  reinterpret_cast<uint2 *>(a.out + ((size_t)((size_t)u.b * a.n_new + i) * a.Hq + h * (int)a.group.d +
+  reinterpret_cast<uint2 *>(a.out + ((size_t)((size_t)u.b * a.n_new + i) * a.Hq +
+                                     h * (int)a.group.d +
                                      (r - i * (int)a.group.d)) * D)[sub] =
       make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
 }
@@ -916,7 +933,8 @@ int launch(Args &a, void *workspace, cudaStream_t stream) {
             cudaSuccess ||
         cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout,
                              cudaSharedmemCarveoutMaxShared) != cudaSuccess ||
-        cudaFuncSetAttribute(paged_join_kernel<D, kNR>, cudaFuncAttributePreferredSharedMemoryCarveout,
+        cudaFuncSetAttribute(paged_join_kernel<D, kNR>,
+                             cudaFuncAttributePreferredSharedMemoryCarveout,
                              cudaSharedmemCarveoutMaxShared) != cudaSuccess ||
         cudaOccupancyMaxActiveBlocksPerMultiprocessor(&nb, kernel, kThreads, C::kSmem) !=
             cudaSuccess ||
@@ -951,7 +969,8 @@ template <int D, bool kF8>
 int launch_rows(Args &a, void *workspace, cudaStream_t stream) {
   if (a.rows <= 8) return launch<D, kF8, 1>(a, workspace, stream);
   if constexpr (!(kF8 && D == 128))
-    if (5 * ((a.rows + 31) / 32) < 3 * ((a.rows + 15) / 16)) return launch<D, kF8, 4>(a, workspace, stream);
+    if (5 * ((a.rows + 31) / 32) < 3 * ((a.rows + 15) / 16))
+      return launch<D, kF8, 4>(a, workspace, stream);
   return launch<D, kF8, 2>(a, workspace, stream);
 }
 
@@ -960,16 +979,18 @@ int launch_rows(Args &a, void *workspace, cudaStream_t stream) {
 
 using namespace hsa;
 
-extern "C" size_t hsa_paged_attention_workspace_bytes(int batch, int n_new, int Hq, int Hkv, int D) {
-  if (batch <= 0 || n_new <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || (D != 64 && D != 128)) return 0;
+extern "C" size_t hsa_paged_attention_workspace_bytes(int batch, int n_new, int Hq, int Hkv,
+                                                      int D) {
+  if (batch <= 0 || n_new <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv) return 0;
+  if (D != 64 && D != 128) return 0;
   return workspace_bytes(D);
 }
 
 extern "C" int hsa_paged_attention(const void *q, int batch, int n_new, int Hq, const void *k_pages,
                                    const void *v_pages, const uint8_t *k_scale,
-                                   const uint8_t *v_scale, int n_pages, int page_size, int Hkv, int D,
-                                   hsa_dtype cache_dtype, const int32_t *page_table, int max_pages,
-                                   const int32_t *seq_lens, float scale, void *out, void *workspace,
+                                   const uint8_t *v_scale, int n_pages, int page_size, int Hkv,
+                                   int D, hsa_dtype cache_dtype, const int32_t *page_table,
+                                   int max_pages, const int32_t *seq_lens, float scale, void *out, void *workspace,
                                    size_t size, hsa_stream_t stream) {
   if (batch < 0 || n_new < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv || n_pages < 0 || max_pages < 0 ||
       page_size < 1)
@@ -979,7 +1000,8 @@ extern "C" int hsa_paged_attention(const void *q, int batch, int n_new, int Hq, 
   if (cache_dtype == HSA_F32 || (D != 64 && D != 128) || (page_size & (page_size - 1)))
     return HSA_ERR_UNSUPPORTED;
   const long long rows = (long long)n_new * (Hq / Hkv);
-  if ((long long)n_pages * page_size > 0x7fffffffLL || (long long)max_pages * page_size > 0x7fffff00LL ||
+  if ((long long)n_pages * page_size > 0x7fffffffLL ||
+      (long long)max_pages * page_size > 0x7fffff00LL ||
       Hq > 65535 || rows > 0x7fffffffLL || (long long)batch * Hkv * rows > 0x7fffff00LL)
     return HSA_ERR_UNSUPPORTED;
   if (batch == 0 || n_new == 0) return HSA_OK;
@@ -1019,6 +1041,8 @@ extern "C" int hsa_paged_attention(const void *q, int batch, int n_new, int Hq, 
   a.scale_log2 = scale * 1.4426950408889634f;
   cudaStream_t s = (cudaStream_t)stream;
   if (f8)
-    return D == 128 ? launch_rows<128, true>(a, workspace, s) : launch_rows<64, true>(a, workspace, s);
-  return D == 128 ? launch_rows<128, false>(a, workspace, s) : launch_rows<64, false>(a, workspace, s);
+    return D == 128 ? launch_rows<128, true>(a, workspace, s)
+                    : launch_rows<64, true>(a, workspace, s);
+  return D == 128 ? launch_rows<128, false>(a, workspace, s)
+                  : launch_rows<64, false>(a, workspace, s);
 }
