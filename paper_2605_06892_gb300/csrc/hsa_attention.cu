@@ -326,11 +326,11 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
     if (warp == 0) {
       tc_produce<D>(pipe, lane, nT, n_pre, withheld, load_kv);
     } else if (warp == 1) {
-      tc_issue<D>(pipe, tmem, smem_addr(sQ), smem_addr(sKV), nT);
+      tc_issue<D>(pipe, tmem, smem_addr(sQ), smem_addr(sKV), {0, 0, nT});
     } else if (warp == 2) {
-      tc_watch_kv<D>(pipe, lane, nT, [](int) {});
+      tc_watch_kv<D>(pipe, lane, {0, 0, nT}, [](int) {});
     } else if (warp == 3) {
-      tc_watch_s<D>(pipe, nT);
+      tc_watch_s<D>(pipe, {0, 0, nT});
     }
     fence_before();
     named_barrier_sync(kBarTeardown, kTcThreads);

@@ -12,10 +12,10 @@
 //    sequence and K/V head.  One pass over the keys serves the whole group: K and V are
 //    read 1/G as often, short sequences fill the 256 rows G times sooner, and the rows of
 //    a unit span only 256 / G tokens, so fewer of its key tiles cross the mask's edge.
-//  - Units.  The lengths are on the device, so every block works out its own unit from
-//    them: sequence by sequence, head by head, each head's query blocks from the last
-//    (under a mask the longest) to the first, so that a head's K/V are read by blocks that
-//    run together and the last units to start are short.
+//  - Units.  The lengths are on the device, so every block works out its units from them:
+//    sequence by sequence, head by head, each head's query blocks from the last (under a
+//    mask the longest) to the first, so that a head's K/V are read by blocks that run
+//    together and the last units to start are short.  A block goes on to further units.
 //  - Mask.  A unit's key tiles end at its last row's limit; a row's own limit is applied
 //    to its scores in the tiles that some row of its warp does not see whole.
 //  - Few units.  With a workspace the units of the last, partly filled wave (all of them
@@ -54,7 +54,7 @@ struct PackedArgs {
   float scale_log2;
   int sms, most;                   // most: pieces that a cut may make, 0: none
   int bound;                       // units that the host allowed for
-  int q_map;                       // the query rows come by TMA
+  int q_map, o_map;                // the query rows come, the output rows go by TMA
   int inject_stall;                // test hook (hsa_test.h)
   float *ws_o, *ws_ml;             // [piece][kUnitRows][D], [piece][kUnitRows][2]
   Cuts *cuts;                      // what the join reads
@@ -64,19 +64,20 @@ struct Sequence {
   int q0, lq, k0, lk;
 };
 
-// Bytes to come on a barrier's present phase, without an arrival.
-__device__ __forceinline__ void mbar_expect_tx_only(uint64_t *b, uint32_t bytes) {
-  asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(b)),
-               "r"(bytes)
-               : "memory");
-}
-
 __device__ __forceinline__ void tma_load_3d(void *dst, const CUtensorMap *map, uint64_t *bar,
                                             int x, int y, int z) {
   asm volatile(
       "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes"
       " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_addr(dst)),
       "l"(map), "r"(smem_addr(bar)), "r"(x), "r"(y), "r"(z)
+      : "memory");
+}
+
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap *map, const void *src, int x, int y,
+                                             int z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map),
+      "r"(smem_addr(src)), "r"(x), "r"(y), "r"(z)
       : "memory");
 }
 
@@ -117,9 +118,9 @@ struct Plan {
 // One unit, or one part of one.
 struct Unit {
   Sequence seq;
-  int head, row0;        // row0: its first row among the sequence's lq G
-  int tiles;             // key tiles of the whole unit
-  int part, parts;       // parts = 1: whole
+  int head, row0, rows;  // row0: its first row among the sequence's lq G
+  int j0, nT;            // key tiles: j0 .. j0 + nT - 1
+  int part, parts;       // parts = 1: whole; 0: there is no unit
   int slot;              // of its first part in the workspace
   int cut;               // its place among the cut units, or -1
 };
@@ -134,25 +135,39 @@ __device__ __forceinline__ int parts_of(const Sequence &s, int longest) {
   return longest && tiles > longest ? (tiles + longest - 1) / longest : 1;
 }
 
-// The unit and part of block `id`; false: it has none.  Called by a whole warp: lane l
-// holds sequence l, and where there are more than 32 the later ones are read again by each
-// pass over them.
-__device__ __forceinline__ bool unit_of(const PackedArgs &a, int id, Plan &p, Unit &u) {
+// The sequences b0 .. b0 + 31, one per lane, and how many units (with `longest` also parts)
+// come before them.  A block's ids rise, so it goes through the sequences once.
+struct Window {
+  Sequence seq;
+  int blocks, b0, ids, units;
+};
+__device__ __forceinline__ void look_at(const PackedArgs &a, Window &w, int b0, int ids,
+                                        int units) {
+  const int b = b0 + (threadIdx.x & 31);
+  w.seq = {};
+  if (b < a.batch) w.seq = sequence(a, b);
+  w.blocks = query_blocks(a, w.seq);
+  w.b0 = b0;
+  w.ids = ids;
+  w.units = units;
+}
+
+// The plan; called by a whole warp, `first` its window on the first sequences.
+__device__ __forceinline__ void plan_units(const PackedArgs &a, const Window &first, Plan &p) {
   const int lane = threadIdx.x & 31;
-  Sequence first = {};
-  if (lane < a.batch) first = sequence(a, lane);
-  const int first_blocks = query_blocks(a, first);
   // f(sequence, its query blocks) for this lane's sequences
   auto each = [&](auto &&f) {
-    f(first, first_blocks);
+    f(first.seq, first.blocks);
     for (int b = lane + 32; b < a.batch; b += 32) {
       const Sequence s = sequence(a, b);
       f(s, query_blocks(a, s));
     }
   };
-  int mine = 0;
-  each([&](const Sequence &, int blocks) { mine += blocks; });
-  p.units = __reduce_add_sync(0xffffffffu, mine) * a.Hkv;
+  // offsets that overlap may make more units than there are ids: those go without
+  unsigned mine = 0;
+  each([&](const Sequence &, int blocks) { mine = min(mine + blocks, 1u << 26); });
+  const long long units_all = (long long)__reduce_add_sync(0xffffffffu, mine) * a.Hkv;
+  p.units = (int)min(units_all, 0x7fffffffLL);
   p.n_whole = p.units;
   p.pieces = 1;
   p.longest = 0;
@@ -218,7 +233,13 @@ __device__ __forceinline__ bool unit_of(const PackedArgs &a, int id, Plan &p, Un
     if (p.pieces > 1 && (1.f - best) * longest() > kJoinTiles) p.n_whole = p.units - rem;
     else p.pieces = 1;
   }
-  // ---- this block's place: `id` counts units, or with `longest` parts
+}
+
+// The unit and part of block `id` (which counts units, or with `longest` parts); false: it
+// has none.  Called by a whole warp.
+__device__ __forceinline__ bool unit_of(const PackedArgs &a, int id, const Plan &p, Window &w,
+                                        Unit &u) {
+  const int lane = threadIdx.x & 31;
   u.part = u.slot = 0;
   u.cut = -1;
   int pieces = 1;
@@ -231,54 +252,53 @@ __device__ __forceinline__ bool unit_of(const PackedArgs &a, int id, Plan &p, Un
     id = p.n_whole + u.cut;
     if (id >= p.units) return false;
   }
-  int before = 0, units = 0;
-  for (int b0 = 0; b0 < a.batch; b0 += 32) {
-    Sequence seq = first;
-    int blocks = first_blocks;
-    if (b0) {
-      seq = {};
-      if (b0 + lane < a.batch) seq = sequence(a, b0 + lane);
-      blocks = query_blocks(a, seq);
-    }
-    const int parts = parts_of(seq, p.longest);
-    const int w = blocks * a.Hkv * parts;
-    int end = w;
+  if (id < w.ids) look_at(a, w, 0, 0, 0);   // ids that do not rise
+  while (true) {
+    const int parts = parts_of(w.seq, p.longest);
+    const int n = w.blocks * a.Hkv * parts;
+    int end = n;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int x = __shfl_up_sync(0xffffffffu, end, o);
       if (lane >= o) end += x;
     }
-    end += before;
-    const unsigned here = __ballot_sync(0xffffffffu, id >= end - w && id < end);
+    end += w.ids;
+    const unsigned here = __ballot_sync(0xffffffffu, id >= end - n && id < end);
     if (here) {
       const int src = __ffs(here) - 1;
-      u.seq.q0 = __shfl_sync(0xffffffffu, seq.q0, src);
-      u.seq.lq = __shfl_sync(0xffffffffu, seq.lq, src);
-      u.seq.k0 = __shfl_sync(0xffffffffu, seq.k0, src);
-      u.seq.lk = __shfl_sync(0xffffffffu, seq.lk, src);
-      int at = id - __shfl_sync(0xffffffffu, end - w, src);
+      u.seq.q0 = __shfl_sync(0xffffffffu, w.seq.q0, src);
+      u.seq.lq = __shfl_sync(0xffffffffu, w.seq.lq, src);
+      u.seq.k0 = __shfl_sync(0xffffffffu, w.seq.k0, src);
+      u.seq.lk = __shfl_sync(0xffffffffu, w.seq.lk, src);
+      int at = id - __shfl_sync(0xffffffffu, end - n, src);
       if (p.longest) {
         pieces = __shfl_sync(0xffffffffu, parts, src);
-        units += __reduce_add_sync(0xffffffffu, lane < src ? blocks * a.Hkv : 0);
+        const int before = __reduce_add_sync(0xffffffffu, lane < src ? w.blocks * a.Hkv : 0);
         const int x = at / pieces;
         u.part = at - x * pieces;
         u.slot = id - u.part;
-        u.cut = units + x;
+        u.cut = w.units + before + x;
         at = x;
       }
-      blocks = __shfl_sync(0xffffffffu, blocks, src);
+      const int blocks = __shfl_sync(0xffffffffu, w.blocks, src);
       u.head = at / blocks;
       u.row0 = (blocks - 1 - (at - u.head * blocks)) * kUnitRows;
       const long long rows = (long long)u.seq.lq * a.group.d;
-      const int last = (int)(min(rows, (long long)u.row0 + kUnitRows) - 1);
-      u.tiles = (key_limit(a, u.seq, quotient(last, a.group)) + kBN - 1) / kBN;
-      u.parts = max(1, min(pieces, u.tiles / kLeastTiles));
+      u.rows = (int)min(rows - u.row0, (long long)kUnitRows);
+      const int tiles =
+          (key_limit(a, u.seq, quotient(u.row0 + u.rows - 1, a.group)) + kBN - 1) / kBN;
+      u.parts = max(1, min(pieces, tiles / kLeastTiles));
+      // parts of one length, the first ones a tile longer
+      u.nT = tiles / u.parts;
+      const int more = tiles - u.nT * u.parts;
+      u.j0 = u.part * u.nT + min(u.part, more);
+      u.nT += u.part < more;
       return u.part < u.parts;
     }
-    before = __shfl_sync(0xffffffffu, end, 31);
-    if (p.longest) units += __reduce_add_sync(0xffffffffu, blocks * a.Hkv);
+    if (w.b0 + 32 >= a.batch) return false;
+    const int units = w.units + __reduce_add_sync(0xffffffffu, w.blocks * a.Hkv);
+    look_at(a, w, w.b0 + 32, __shfl_sync(0xffffffffu, end, 31), units);
   }
-  return false;
 }
 
 // What the join has to know, written by the kernel before it: how many units were cut, and
@@ -298,13 +318,15 @@ __device__ __forceinline__ __nv_bfloat16 *out_row(const PackedArgs &a, int q0, i
   return a.out + ((size_t)(q0 + i) * a.Hq + head * (int)a.group.d + (R - i * (int)a.group.d)) * D;
 }
 
-// Forms this warp's rows again whose O took in a masked value that is not finite: O = sum
-// over the row's own keys [k0, min(limit, k1)) of 2^(c s - m) v, m and the sum being right
-// already.  Rare and slow; out of line so that it costs the usual path no registers.  False:
-// no row needed it.
+// Forms and stores those of this warp's rows again whose sums took in a masked value that
+// is not finite: sum over the row's own keys [k0, min(limit, k1)) of 2^(c s - m) v, m and l
+// being right already; piece: of the workspace, or -1: the row of the output.  Rare and slow;
+// out of line so that it costs the usual path no registers.
 template <int D>
-__device__ __noinline__ bool form_again(const PackedArgs &a, const Unit &u, uint32_t tO, int R,
-                                        int limit, int k0, int k1, float m, bool valid) {
+__device__ __noinline__ void form_again(const PackedArgs &a, const Unit &u, int piece, int r,
+                                        int limit, float m, float l) {
+  const int k0 = u.j0 * kBN, k1 = min(u.seq.lk, k0 + u.nT * kBN), R = u.row0 + r;
+  const bool valid = r < u.rows;
   const __nv_bfloat16 *K = a.k + (size_t)u.seq.k0 * a.k_row + (size_t)u.head * D;
   const __nv_bfloat16 *V = a.v + (size_t)u.seq.k0 * a.v_row + (size_t)u.head * D;
   const int tok = valid ? quotient(R, a.group) : 0;
@@ -321,7 +343,8 @@ __device__ __noinline__ bool form_again(const PackedArgs &a, const Unit &u, uint
       }
   const int end = bad ? min(limit, k1) : 0;
   const int most = __reduce_max_sync(0xffffffffu, end);
-  if (!__any_sync(0xffffffffu, bad)) return false;
+  if (!__any_sync(0xffffffffu, bad)) return;
+  const float f = piece >= 0 ? 1.f : l > 0.f ? 1.f / l : l;
   for (int c = 0; c < D / 32; ++c) {
     float acc[32];
 #pragma unroll
@@ -354,35 +377,46 @@ __device__ __noinline__ bool form_again(const PackedArgs &a, const Unit &u, uint
         }
       }
     }
-    __syncwarp();
-    uint32_t o[32];
-    tmem_ld32(tO + 32 * c, o);
-    tmem_wait_ld();
+    if (bad && piece >= 0) {
+      float4 *to =
+          reinterpret_cast<float4 *>(a.ws_o + ((size_t)piece * kUnitRows + r) * D + 32 * c);
 #pragma unroll
-    for (int i = 0; i < 32; ++i)
-      if (bad) o[i] = __float_as_uint(acc[i]);
-    tmem_st32(tO + 32 * c, o);
-    tmem_wait_st();
+      for (int v = 0; v < 8; ++v)
+        to[v] = make_float4(acc[4 * v], acc[4 * v + 1], acc[4 * v + 2], acc[4 * v + 3]);
+    } else if (bad) {
+      uint4 *to = reinterpret_cast<uint4 *>(out_row<D>(a, u.seq.q0, u.head, R) + 32 * c);
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        uint32_t pk[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          pk[i] = pack_bf16(acc[8 * v + 2 * i] * f, acc[8 * v + 2 * i + 1] * f);
+        to[v] = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+      }
+    }
   }
-  return true;
 }
 
-// Stores a warp's 32 rows (r0 ..) of a unit or a piece by way of `stage`, 32 D floats of
+// Stores a warp's 32 rows (r0 ..) of a unit or a piece by way of `stage`, 64 D bytes of
 // the warp's own (see the active attention's store: neighbouring lanes store neighbouring
-// vectors).  again() is called once if a row's sums are not all finite and may change them.
-template <int D, typename Again>
-__device__ __forceinline__ void store_rows(const PackedArgs &a, const Unit &u, int piece, int r0,
-                                           int lane, uint32_t tO, float m_run, float l_run,
-                                           uint8_t *stage, Again &&again) {
+// vectors).  True: the sums are not all finite.  `stage` is free again once lane 0 has
+// waited for its bulk copies' reads.  Where the 32 rows are whole tokens, all the sequence's,
+// TMA stores them as a box: by the lanes' own stores 128 dimensions took 4800 clocks.
+template <int D>
+__device__ __forceinline__ bool store_rows(const PackedArgs &a, const CUtensorMap *tm_o,
+                                           const Unit &u, int piece, int r0, int lane, uint32_t tO,
+                                           float m_run, float l_run, uint8_t *stage) {
   uint4 *st = reinterpret_cast<uint4 *>(stage);
+  constexpr int kV = D / 8;
   if (piece >= 0) {
-    constexpr int kV = D / 4;
-    auto put = [&]() {
-      float worst[4] = {0.f, 0.f, 0.f, 0.f};
+    float worst[4] = {0.f, 0.f, 0.f, 0.f};   // NaN where a sum is not finite
+    // fp32, half of the dimensions at a time
 #pragma unroll
-      for (int c = 0; c < D / 32; ++c) {
+    for (int half = 0; half < 2; ++half) {
+#pragma unroll
+      for (int c = 0; c < D / 64; ++c) {
         uint32_t o[32];
-        tmem_ld32(tO + 32 * c, o);
+        tmem_ld32(tO + half * (D / 2) + 32 * c, o);
         tmem_wait_ld();
 #pragma unroll
         for (int v = 0; v < 8; ++v)
@@ -391,49 +425,64 @@ __device__ __forceinline__ void store_rows(const PackedArgs &a, const Unit &u, i
 #pragma unroll
         for (int i = 0; i < 32; ++i) worst[i & 3] = fmaf(__uint_as_float(o[i]), 0.f, worst[i & 3]);
       }
-      return (worst[0] + worst[1]) + (worst[2] + worst[3]);   // NaN where a sum is not finite
-    };
-    if (__any_sync(0xffffffffu, put() != 0.f) && again()) put();
-    __syncwarp();
-    uint4 *dst = reinterpret_cast<uint4 *>(a.ws_o) + ((size_t)piece * kUnitRows + r0) * kV;
-#pragma unroll 8
-    for (int i = 0; i < kV; ++i) {
-      const int e = 32 * i + lane, row = e / kV, v = e % kV;
-      dst[e] = st[row * kV + ((v & ~7) | ((v & 7) ^ (row & 7)))];
+      __syncwarp();
+      uint4 *dst = reinterpret_cast<uint4 *>(a.ws_o) +
+                   ((size_t)piece * kUnitRows + r0) * (2 * kV) + half * kV;
+#pragma unroll
+      for (int i = 0; i < kV; ++i) {
+        const int e = 32 * i + lane, row = e / kV, v = e % kV;
+        dst[row * (2 * kV) + v] = st[row * kV + ((v & ~7) | ((v & 7) ^ (row & 7)))];
+      }
+      __syncwarp();
     }
     reinterpret_cast<float2 *>(a.ws_ml)[(size_t)piece * kUnitRows + r0 + lane] =
         make_float2(m_run, l_run);
-    return;
+    return __any_sync(0xffffffffu, (worst[0] + worst[1]) + (worst[2] + worst[3]) != 0.f) != 0;
   }
   const float inv = l_run > 0.f ? 1.f / l_run : l_run == 0.f ? 0.f : l_run;   // no keys: zeros
-  constexpr int kV = D / 8;
-  auto put = [&]() {
-    float worst[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int c = 0; c < D / 32; ++c) {
-      uint32_t o[32];
-      tmem_ld32(tO + 32 * c, o);
-      tmem_wait_ld();
-#pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        uint32_t pk[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          pk[i] = pack_bf16(__uint_as_float(o[8 * v + 2 * i]) * inv,
-                            __uint_as_float(o[8 * v + 2 * i + 1]) * inv);
-        const int x = 4 * c + v;
-        st[lane * kV + ((x & ~7) | ((x & 7) ^ (lane & 7)))] =
-            make_uint4(pk[0], pk[1], pk[2], pk[3]);
-      }
-#pragma unroll
-      for (int i = 0; i < 32; ++i) worst[i & 3] = fmaf(__uint_as_float(o[i]), 0.f, worst[i & 3]);
-    }
-    return (worst[0] + worst[1]) + (worst[2] + worst[3]);
+  const bool box = a.o_map && u.rows - r0 >= 32;
+  // vector x of this lane's row: in a box 64 dimensions of all rows lie together
+  auto place_of = [&](int x) {
+    const int y = (x & ~7) | ((x & 7) ^ (lane & 7));
+    return box ? (x >> 3) * 256 + lane * 8 + (y & 7) : lane * kV + y;
   };
-  if (__any_sync(0xffffffffu, put() != 0.f) && again()) put();
+  const uint64_t inv2 = pack2(__float_as_uint(inv), __float_as_uint(inv));
+  const uint64_t minus0 = 0x8000000080000000ull;
+  uint32_t odd2 = 0u;   // bf16 pair: NaN where a value is not finite
+#pragma unroll
+  for (int c = 0; c < D / 64; ++c) {
+    uint32_t o[64];
+    tmem_ld32(tO + 64 * c, *reinterpret_cast<uint32_t(*)[32]>(&o[0]));
+    tmem_ld32(tO + 64 * c + 32, *reinterpret_cast<uint32_t(*)[32]>(&o[32]));
+    tmem_wait_ld();
+#pragma unroll
+    for (int v = 0; v < 8; ++v) {
+      uint32_t pk[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint64_t x = fma2(pack2(o[8 * v + 2 * i], o[8 * v + 2 * i + 1]), inv2, minus0);
+        pk[i] = pack_bf16(lo_f(x), hi_f(x));
+        asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(odd2) : "r"(pk[i]), "r"(0u));
+      }
+      st[place_of(8 * c + v)] = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+    }
+  }
+  const bool odd = __any_sync(0xffffffffu, odd2 & 0x7fff7fffu) != 0;
+  if (box) {
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) {
+      const int tok = u.seq.q0 + (int)quotient(u.row0 + r0, a.group);
+#pragma unroll
+      for (int c = 0; c < D / 64; ++c)
+        tma_store_3d(tm_o, stage + c * 4096, c * 64, u.head * (int)a.group.d, tok);
+      asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
+    return odd;
+  }
   __syncwarp();
   // a lane works out the place of its own row, from the unit's first, in vectors
-  const int rows = (int)min((long long)u.seq.lq * a.group.d - u.row0, (long long)kUnitRows) - r0;
+  const int rows = u.rows - r0;
   const int tok0 = quotient(u.row0, a.group), R = u.row0 + r0 + lane, tok = quotient(R, a.group);
   const int place = ((tok - tok0) * a.Hq + R - tok * (int)a.group.d) * (D / 8);
   uint4 *base = reinterpret_cast<uint4 *>(a.out) +
@@ -445,13 +494,57 @@ __device__ __forceinline__ void store_rows(const PackedArgs &a, const Unit &u, i
     const uint4 x = st[row * kV + ((v & ~7) | ((v & 7) ^ (row & 7)))];
     if (row < rows) base[at + v] = x;
   }
+  return odd;
 }
 
-template <int D>
+// Asks for the id of a block that has not started, which then never does (cluster launch
+// control); by one thread.
+__device__ __forceinline__ void ask_block(uint4 *answer, uint64_t *bar) {
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the last answer was read
+  mbar_expect_tx(bar, 16);
+  asm volatile(
+      "clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128"
+      " [%0], [%1];" ::"r"(smem_addr(answer)), "r"(smem_addr(bar))
+      : "memory");
+}
+// The id once the answer is there, or -1 where no block is left: then it is not to be asked
+// again.
+__device__ __forceinline__ int block_of(const uint4 *answer) {
+  int id;
+  asm volatile(
+      "{\n .reg .pred p;\n .reg .b64 lo, hi;\n .reg .b128 h;\n .reg .b32 x;\n"
+      " ld.shared.v2.b64 {lo, hi}, [%1];\n mov.b128 h, {lo, hi};\n"
+      " clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, h;\n mov.b32 x, -1;\n"
+      " @p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 x, h;\n"
+      " mov.b32 %0, x;\n}\n"
+      : "=r"(id)
+      : "r"(smem_addr(answer))
+      : "memory");
+  return id;
+}
+
+// Named barriers of this kernel: the start of the block; the query rows of a unit are in
+// shared memory (softmax and issuing warps); the rows of Q tile t have left shared memory.
+constexpr int kBarStart = 7, kBarQ = 8, kBarStored = 9;   // kBarStored + t
+
+// A block that is one of more than there are SMs (kChain) takes one unit after another: its
+// own, then those of blocks that have not started yet (ask_block), so that the roles run on
+// from unit to unit and the tensor pipe does not wait through a block's end and the next
+// one's start.  Warp 0 works out the next unit while the present one's last tiles are
+// multiplied and loads its first tiles into the slots that fall free, its query rows as soon
+// as the last S no longer needs the present ones; its first S is computed beside the present
+// one's store.  Units are handed over through unit_sh: bar_unit says that unit n is there,
+// bar_taken that all other warps have read on to it and so are done with unit n - 1, whose
+// place unit n + 1 takes.  Against a block per unit: six prompts of 503 to 5200 tokens, 32
+// heads x 128 on 8, 309 -> 285 us; two of 16 frames of 384, 32 x 64, 280 -> 265; 64 prompts of
+// 200 tokens, 32 x 128 on 8, 130 -> 114; 1024 of 20, 920 -> 270, mostly since a block goes
+// through the sequences once.
+template <int D, bool kChain>
 __global__ void __launch_bounds__(kTcThreads, 1)
 packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k,
                         const __grid_constant__ CUtensorMap tm_v,
                         const __grid_constant__ CUtensorMap tm_q,
+                        const __grid_constant__ CUtensorMap tm_o,
                         const __grid_constant__ PackedArgs a) {
   using C = TcCfg<D>;
   extern __shared__ uint8_t smem_raw[];
@@ -460,11 +553,13 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k,
   uint8_t *sQ = sm;
   uint8_t *sKV = sm + kQT * C::kTileBytes;
   __shared__ __align__(8) uint64_t bar_full[C::kStages], bar_empty[C::kStages];
-  __shared__ __align__(8) uint64_t bar_s[kQT * C::kSBars], bar_o;
+  __shared__ __align__(8) uint64_t bar_s[kQT * C::kSBars], bar_o[kQT];
+  __shared__ __align__(8) uint64_t bar_unit, bar_taken, bar_q, bar_answer;
+  __shared__ __align__(16) uint4 answer;
   __shared__ uint32_t tmem_base_sh;
   __shared__ volatile int abort_flag;
-  __shared__ Unit unit_sh;
-  const TcPipe pipe = {bar_full, bar_empty, bar_s, &bar_o, &abort_flag, a.err};
+  __shared__ Unit unit_sh[2];
+  const TcPipe pipe = {bar_full, bar_empty, bar_s, bar_o, &abort_flag, a.err};
 
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);
   const int lane = threadIdx.x & 31;
@@ -472,6 +567,7 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k,
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_k) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_v) : "memory");
     if (a.q_map) asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_q) : "memory");
+    if (a.o_map) asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_o) : "memory");
   }
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::kStages; ++s) {
@@ -479,211 +575,322 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k,
       mbar_init(&bar_empty[s], 1);
     }
     for (int t = 0; t < kQT * C::kSBars; ++t) mbar_init(&bar_s[t], 1);
-    mbar_init(&bar_o, 1);
+    for (int t = 0; t < kQT; ++t) mbar_init(&bar_o[t], 1);
+    mbar_init(&bar_unit, 1);
+    mbar_init(&bar_taken, kTcThreads / 32 - 1);
+    mbar_init(&bar_q, 1);
+    mbar_init(&bar_answer, 1);
     abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
   pdl_wait();
 
-  // ---- this block's unit and key tiles, worked out by one warp: twelve at once would take
-  // each other's issue slots
-  if (warp == 1) {
-    Plan plan;
-    Unit mine;
-    const bool busy = unit_of(a, blockIdx.x, plan, mine);
-    if (lane == 0) {
-      if (a.most && blockIdx.x == 0) a.cuts->n = plan.units - plan.n_whole;
-      if (!busy) mine.parts = 0;
-      unit_sh = mine;
-    }
-  }
-  __syncthreads();
-  // Read where it is needed: held in registers over the key loop it would spill, to an L1
-  // that the tiles have left no room in.
-  const Unit &u = unit_sh;
-  if (u.parts == 0) return;
-  int j0 = 0, nT = u.tiles;
-  if (u.parts > 1) {   // parts of one length, the first ones a tile longer
-    nT = u.tiles / u.parts;
-    const int more = u.tiles - nT * u.parts;
-    j0 = u.part * nT + min(u.part, more);
-    nT += u.part < more;
-  }
-  const int rows = (int)min((long long)u.seq.lq * a.group.d - u.row0, (long long)kUnitRows);
-  if (u.cut >= 0 && u.part == 0 && threadIdx.x == 0)
-    a.cuts->unit[u.cut] = {u.parts, u.slot, rows, u.row0, u.seq.q0, u.head, {0, 0}};
-  if (nT == 0) {   // no row has keys
-    for (int i = threadIdx.x; i < rows * (D / 8); i += kTcThreads)
-      *reinterpret_cast<uint4 *>(out_row<D>(a, u.seq.q0, u.head, u.row0 + i / (D / 8)) +
-                                 8 * (i % (D / 8))) =
-          make_uint4(0u, 0u, 0u, 0u);
-    return;
-  }
-
-  const int key0 = u.seq.k0 + j0 * kBN, col0 = u.head * D;
-  auto load_kv = [&](int L) {
-    const int slot = L % C::kStages;
-    mbar_expect_tx(&bar_full[slot], C::kTileBytes);
-    uint8_t *dst = sKV + slot * C::kTileBytes;
-    const int y = key0 + (L >> 1) * kBN;
-#pragma unroll
-    for (int c = 0; c < C::kChunks; ++c)
-      tma_load_2d(dst + c * (kBN * 128), (L & 1) ? &tm_v : &tm_k, &bar_full[slot], col0 + c * 64,
-                  y);
+  // Unit n, once it is there; false: there is none.  All waits of warp 0 are bounded, so it
+  // comes, also after a failure.
+  auto take = [&](int n) {
+    if (!kChain) return n == 0 && unit_sh[0].parts > 0;
+    bool there = __all_sync(0xffffffffu, mbar_wait(&bar_unit, n & 1, &abort_flag, a.err, false));
+    there = there && unit_sh[n & 1].parts > 0;
+    __syncwarp();
+    if (there && lane == 0) mbar_arrive(&bar_taken);
+    return there;
   };
-  const int withheld = a.inject_stall == 1 ? 1 : -1;
-  const int n_pre = min(3, 2 * nT);
-  // TMEM after the wait and before the trigger, as in the active attention; the blocks of
-  // the last wave let the next kernel start.
-  if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
-                     smem_addr(&tmem_base_sh)),
-                 "r"(kTmemCols)
-                 : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    if (blockIdx.x + (unsigned)a.sms >= gridDim.x) pdl_trigger();
-  }
-  // ---- query rows into the two swizzled Q tiles.  Where G divides a tile's 128 rows a box
-  // of 128 / G tokens, G heads and 64 dimensions is a tile's column chunk as the MMA wants
-  // it, and arrives on the first K tile's barrier; rows past the sequence's last are another
-  // sequence's or zeros, and are never stored.  Else the threads load row by row.
-  if (a.q_map) {
-    if (threadIdx.x == 0) {
-      const int G = a.group.d, tok = u.seq.q0 + (int)quotient(u.row0, a.group);
-      mbar_expect_tx_only(&bar_full[0], kQT * C::kTileBytes);
-#pragma unroll
-      for (int t = 0; t < kQT; ++t)
-#pragma unroll
-        for (int c = 0; c < C::kChunks; ++c)
-          tma_load_3d(sQ + t * C::kTileBytes + c * (kBM * 128), &tm_q, &bar_full[0], c * 64,
-                      u.head * G, tok + t * (int)quotient(kBM, a.group));
-      for (int L = 0; L < n_pre; ++L)
-        if (L != withheld) load_kv(L);
-    }
-  } else {
-    constexpr int kVecPerRow = D / 8;
-    constexpr int kVecs = kUnitRows * kVecPerRow;
-    constexpr int kPer = (kVecs + kTcThreads - 1) / kTcThreads;
-    const int G = a.group.d;
-    // the addresses first, then all loads together
-    const uint4 *src[kPer];
-#pragma unroll
-    for (int x = 0; x < kPer; ++x) {
-      const int i = threadIdx.x + x * kTcThreads, R = u.row0 + i / kVecPerRow;
-      const int tok = quotient(R, a.group);
-      src[x] = reinterpret_cast<const uint4 *>(a.q + (size_t)(u.seq.q0 + tok) * a.q_row +
-                                               (u.head * G + (R - tok * G)) * D) + i % kVecPerRow;
-    }
-    uint4 v[kPer];
-#pragma unroll
-    for (int x = 0; x < kPer; ++x) {
-      v[x] = make_uint4(0u, 0u, 0u, 0u);
-      if ((threadIdx.x + x * kTcThreads) / kVecPerRow < rows)
-        asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
-                     : "=r"(v[x].x), "=r"(v[x].y), "=r"(v[x].z), "=r"(v[x].w)
-                     : "l"(src[x]));
-    }
-    // the first key tiles are requested while the rows are on their way
-    if (threadIdx.x == 0)
-      for (int L = 0; L < n_pre; ++L)
-        if (L != withheld) load_kv(L);
-#pragma unroll
-    for (int x = 0; x < kPer; ++x) {
-      const int i = threadIdx.x + x * kTcThreads;
-      if (i < kVecs) {
-        const int row = i / kVecPerRow, c = i % kVecPerRow;
-        const int t = row / kBM, rr = row % kBM;
-        *reinterpret_cast<uint4 *>(sQ + t * C::kTileBytes + (c >> 3) * (kBM * 128) + rr * 128 +
-                                   (((c & 7) ^ (rr & 7)) << 4)) = v[x];
-      }
-    }
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-  }
-  fence_before();
-  __syncthreads();
-  fence_after();
-  const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_base_sh, 0);
+  TcSpan w = {0, 0, 0};
+  int done = 0;   // units with keys so far
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsLow));
     if (warp == 0) {
-      tc_produce<D>(pipe, lane, nT, n_pre, withheld, load_kv);
-    } else if (warp == 1) {
-      tc_issue<D>(pipe, tmem, smem_addr(sQ), smem_addr(sKV), nT);
-    } else if (warp == 2) {
-      // V rows behind the sequence's last key (another sequence's, or what lies behind
-      // the last) become zeros before the issuer hears of the tile.
-      const int keys = u.seq.lk - j0 * kBN;
-      tc_watch_kv<D>(pipe, lane, nT, [&](int j) {
-        const int have = keys - j * kBN;
-        if (have >= kBN) return;
-        uint8_t *tile = sKV + ((2 * j + 1) % C::kStages) * C::kTileBytes;
-        for (int i = have * 8 + lane; i < kBN * 8; i += 32)
+      const int withheld = a.inject_stall == 1 ? 1 : -1;
+      int id = blockIdx.x, asked = 0, issued = 0;
+      bool live = true;
+      auto answered = [&]() -> int {   // the id that was asked for
+        const bool ok = __all_sync(
+            0xffffffffu, mbar_wait(&bar_answer, asked++ & 1, &abort_flag, a.err, false));
+        const int x = ok ? block_of(&answer) : -1;
+        return __shfl_sync(0xffffffffu, x, 0);
+      };
+      Window window;
+      look_at(a, window, 0, 0, 0);
+      Plan plan;
+      plan_units(a, window, plan);
+      // The unit of `id` or of a later block; parts = 0: there is none.
+      auto find = [&]() {
+        Unit u = {};
+        while (live && id >= 0) {
+          const bool busy = unit_of(a, id, plan, window, u);
+          if (lane == 0 && a.most) {
+            if (id == 0) a.cuts->n = plan.units - plan.n_whole;
+            if (busy && u.cut >= 0 && u.part == 0)
+              a.cuts->unit[u.cut] = {u.parts, u.slot, u.rows, u.row0, u.seq.q0, u.head, {0, 0}};
+          }
+          if (busy) break;
+          u.parts = 0;
+          if (!kChain) break;
+          if (lane == 0) ask_block(&answer, &bar_answer);
+          id = answered();
+        }
+        if (u.parts == 0) u.nT = 0;
+        return u;
+      };
+      auto publish = [&](int n, const Unit &u) {
+        if (n) mbar_wait(&bar_taken, (n - 1) & 1, &abort_flag, a.err, false);
+        __syncwarp();
+        if (lane == 0) {
+          unit_sh[n & 1] = u;
+          if (kChain) mbar_arrive(&bar_unit);
+        }
+        __syncwarp();
+      };
+      Unit u = find();
+      publish(0, u);
+      for (int n = 0;; ++n) {
+        w.nT = u.nT;
+        const int key0 = u.seq.k0 + u.j0 * kBN;
+        // The query rows: where G divides a tile's 128 rows a box of 128 / G tokens, G heads
+        // and 64 dimensions is a tile's column chunk as the MMA wants it, and arrives on the
+        // first K tile's barrier; rows past the sequence's last are another sequence's or
+        // zeros, and are never stored.  Else the softmax warps load row by row.
+        auto load_kv = [&](int L, int slot) {
+          mbar_expect_tx(&bar_full[slot],
+                         C::kTileBytes * (L == 0 && a.q_map ? 1 + kQT : 1));
+          uint8_t *dst = sKV + slot * C::kTileBytes;
 #pragma unroll
           for (int c = 0; c < C::kChunks; ++c)
-            *reinterpret_cast<uint4 *>(tile + c * (kBN * 128) + 16 * i) =
-                make_uint4(0u, 0u, 0u, 0u);
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            tma_load_2d(dst + c * (kBN * 128), (L & 1) ? &tm_v : &tm_k, &bar_full[slot],
+                        u.head * D + c * 64, key0 + (L >> 1) * kBN);
+        };
+        auto load_q = [&]() {
+          const int G = a.group.d, tok = u.seq.q0 + (int)quotient(u.row0, a.group);
+          uint64_t *bar = &bar_full[w.L % C::kStages];
+#pragma unroll
+          for (int t = 0; t < kQT; ++t)
+#pragma unroll
+            for (int c = 0; c < C::kChunks; ++c)
+              tma_load_3d(sQ + t * C::kTileBytes + c * (kBM * 128), &tm_q, bar, c * 64,
+                          u.head * G, tok + t * (int)quotient(kBM, a.group));
+        };
+        int from = min(2, 2 * w.nT);   // the next load
+        if (lane == 0 && w.nT) {
+          if (a.q_map && !done) load_q();   // K_0's barrier still waits for K_0
+          live = tc_load<D>(pipe, w, 0, from, withheld, issued, load_kv);
+          if (a.q_map && done && issued > w.L) {
+            // K_0 is on its way, so its barrier waits for the rows too: they are loaded even
+            // if the wait fails
+            live = mbar_wait(&bar_q, (done - 1) & 1, &abort_flag, a.err) && live;
+            load_q();
+          }
+        }
         __syncwarp();
-      });
+        if (n == 0) named_barrier_sync(kBarStart, kTcThreads);
+        if (u.parts == 0) break;
+        auto load_to = [&](int to) {
+          to = max(from, to);
+          if (lane == 0) live = live && tc_load<D>(pipe, w, from, to, withheld, issued, load_kv);
+          from = to;
+        };
+        if (!kChain) {
+          load_to(2 * w.nT);
+          break;
+        }
+        // The next id is asked for before the last loads, which wait for their slots, and
+        // not sooner: a block that took units ahead would leave others without at the end.
+        load_to(2 * w.nT - 3);
+        if (lane == 0) ask_block(&answer, &bar_answer);
+        load_to(2 * w.nT);
+        live = __shfl_sync(0xffffffffu, live, 0);
+        id = answered();
+        // No block is left: the next kernel may start.  TMEM is taken by now, as in the
+        // active attention.
+        if (id < 0) pdl_trigger();
+        const Unit next = find();
+        publish(n + 1, next);
+        if (w.nT) {
+          tc_pass<D>(w);
+          ++done;
+        }
+        u = next;
+      }
+      if (lane == 0) tc_drain<D>(pipe, issued, withheld);
+      __syncwarp();
     } else {
-      tc_watch_s<D>(pipe, nT);
+      if (warp == 1) {
+        // TMEM after the wait and before the trigger, as in the active attention
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
+                         smem_addr(&tmem_base_sh)),
+                     "r"(kTmemCols)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        if (!kChain) pdl_trigger();
+      }
+      fence_before();
+      named_barrier_sync(kBarStart, kTcThreads);
+      fence_after();
+      const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_base_sh, 0);
+      for (int n = 0; take(n); ++n) {
+        const Unit &u = unit_sh[n & 1];
+        w.nT = __shfl_sync(0xffffffffu, u.nT, 0);
+        if (w.nT == 0) continue;
+        if (warp == 1) {
+          if (!a.q_map) {
+            named_barrier_sync(kBarQ, 256 + 32);
+            fence_after();
+          }
+          tc_issue<D, true>(pipe, tmem, smem_addr(sQ), smem_addr(sKV), w);
+        } else if (warp == 2) {
+          // V rows behind the sequence's last key (another sequence's, or what lies behind
+          // the last) become zeros before the issuer hears of the tile.
+          const int keys = u.seq.lk - u.j0 * kBN;
+          tc_watch_kv<D, true>(pipe, lane, w, [&](int j) {
+            const int have = keys - j * kBN;
+            if (have >= kBN) return;
+            uint8_t *tile = sKV + ((w.L + 2 * j + 1) % C::kStages) * C::kTileBytes;
+            for (int i = have * 8 + lane; i < kBN * 8; i += 32)
+#pragma unroll
+              for (int c = 0; c < C::kChunks; ++c)
+                *reinterpret_cast<uint4 *>(tile + c * (kBN * 128) + 16 * i) =
+                    make_uint4(0u, 0u, 0u, 0u);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+          });
+        } else {
+          tc_watch_s<D>(pipe, w);
+          if (lane == 0) mbar_arrive(&bar_q);   // the last S has read the query rows
+        }
+        tc_pass<D>(w);
+        ++done;
+      }
+      // TMEM is quiet before it is freed, also after a failure
+      if (warp == 1 && done) mbar_wait(&bar_o[1], (done - 1) & 1, &abort_flag, a.err, false);
+      __syncwarp();
     }
     fence_before();
     named_barrier_sync(kBarTeardown, kTcThreads);
     if (warp == 1) {
       fence_after();
-      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem),
+      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base_sh),
                    "r"(kTmemCols)
                    : "memory");
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsHigh));
+    fence_before();
+    named_barrier_sync(kBarStart, kTcThreads);
+    fence_after();
+    const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_base_sh, 0);
     const int t = (warp - 4) >> 2;
     const int wq = warp & 3;
     const uint32_t lane_off = (uint32_t)(wq * 32) << 16;
     const uint32_t tO = tmem + lane_off + C::kOCol0 + D * t;
     const float sl2 = a.scale_log2;
-    float m_run = kLowest, l_run = 0.f;
-    // Keys from tile j0 on that this thread's row sees; rows past the sequence's last take no
-    // mask.  The warp's first row sees fewest.
-    const int r = t * kBM + wq * 32 + lane;
-    const int seen = r < rows ? key_limit(a, u.seq, quotient(u.row0 + r, a.group)) : u.seq.lk;
-    const int limit = seen - j0 * kBN;
-    const int all_see = __shfl_sync(0xffffffffu, limit, 0);
-    for (int j = 0; j < nT; ++j) {
-      named_barrier_sync(kBarS0 + t, kMeetS);
-      fence_after();
-      const int valid = limit - j * kBN;
-      const uint32_t tSj = tmem + lane_off + 128 * (C::kThreeS ? (2 * j + t) % 3 : t);
-      auto o_idle = [&]() -> bool {   // as in the active attention
-        if constexpr (!C::kThreeS) return true;
-        uint64_t *b = t == 0 ? &bar_s[2 + (j & 1)] : &bar_s[(j + 1) & 1];
-        const uint32_t par = t == 0 ? (j >> 1) & 1 : ((j + 1) >> 1) & 1;
-        const bool idle = __all_sync(0xffffffffu, mbar_wait(b, par, &abort_flag, a.err));
+    for (int n = 0; take(n); ++n) {
+      // Read where it is needed: held in registers over the key loop it would spill, to an
+      // L1 that the tiles have left no room in.
+      const Unit &u = unit_sh[n & 1];
+      w.nT = __shfl_sync(0xffffffffu, u.nT, 0);
+      if (w.nT == 0) {   // no row has keys
+        for (int i = threadIdx.x - 128; i < u.rows * (D / 8); i += 256)
+          *reinterpret_cast<uint4 *>(out_row<D>(a, u.seq.q0, u.head, u.row0 + i / (D / 8)) +
+                                     8 * (i % (D / 8))) =
+              make_uint4(0u, 0u, 0u, 0u);
+        continue;
+      }
+      if (!a.q_map) {
+        // These warps have stored the unit before, so its products are done.  The addresses
+        // first, then the loads together, in two halves.
+        constexpr int kVecPerRow = D / 8, kPer = kUnitRows * kVecPerRow / 256 / 2;
+        const int G = a.group.d;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const uint4 *src[kPer];
+          uint4 v[kPer];
+          const int i0 = threadIdx.x - 128 + half * (kPer * 256);
+#pragma unroll
+          for (int x = 0; x < kPer; ++x) {
+            const int i = i0 + x * 256, R = u.row0 + i / kVecPerRow, tok = quotient(R, a.group);
+            src[x] = reinterpret_cast<const uint4 *>(a.q + (size_t)(u.seq.q0 + tok) * a.q_row +
+                                                     (u.head * G + (R - tok * G)) * D) +
+                     i % kVecPerRow;
+          }
+#pragma unroll
+          for (int x = 0; x < kPer; ++x) {
+            v[x] = make_uint4(0u, 0u, 0u, 0u);
+            if ((i0 + x * 256) / kVecPerRow < u.rows)
+              asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                           : "=r"(v[x].x), "=r"(v[x].y), "=r"(v[x].z), "=r"(v[x].w)
+                           : "l"(src[x]));
+          }
+#pragma unroll
+          for (int x = 0; x < kPer; ++x) {
+            const int i = i0 + x * 256, row = i / kVecPerRow, c = i % kVecPerRow;
+            const int rr = row % kBM;
+            *reinterpret_cast<uint4 *>(sQ + (row / kBM) * C::kTileBytes + (c >> 3) * (kBM * 128) +
+                                       rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) = v[x];
+          }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        fence_before();
+        named_barrier_sync(kBarQ, 256 + 32);
+      }
+      float m_run = kLowest, l_run = 0.f;
+      // Keys from the next tile on that this thread's row sees; rows past the sequence's last
+      // take no mask.  The warp's first row sees fewest.
+      const int r = t * kBM + wq * 32 + lane;
+      int limit = (r < u.rows ? key_limit(a, u.seq, quotient(u.row0 + r, a.group)) : u.seq.lk) -
+                  u.j0 * kBN;
+      int all_see = __shfl_sync(0xffffffffu, limit, 0);
+      const int end = w.J + w.nT;
+      for (int j = w.J; j < end; ++j) {
+        named_barrier_sync(kBarS0 + t, kMeetS);
         fence_after();
-        return idle;
-      };
-      if (all_see - j * kBN >= kBN)
-        softmax_tile<D, false>(tSj, tO, kBN, j == 0, sl2, m_run, l_run, o_idle);
-      else
-        softmax_tile<D, true>(tSj, tO, valid, j == 0, sl2, m_run, l_run, o_idle);
-      tmem_wait_st();
-      fence_before();
-      named_barrier_sync(kBarP0 + t, kMeetP);
+        const uint32_t tSj = tmem + lane_off + 128 * (C::kThreeS ? (2 * j + t) % 3 : t);
+        auto o_idle = [&]() -> bool {   // as in the active attention
+          if constexpr (!C::kThreeS) return true;
+          uint64_t *b = t == 0 ? &bar_s[2 + (j & 1)] : &bar_s[(j + 1) & 1];
+          const uint32_t par = t == 0 ? (j >> 1) & 1 : ((j + 1) >> 1) & 1;
+          const bool idle = __all_sync(0xffffffffu, mbar_wait(b, par, &abort_flag, a.err));
+          fence_after();
+          return idle;
+        };
+        if (all_see >= kBN)
+          softmax_tile<D, false>(tSj, tO, kBN, j == w.J, sl2, m_run, l_run, o_idle);
+        else
+          softmax_tile<D, true>(tSj, tO, limit, j == w.J, sl2, m_run, l_run, o_idle);
+        limit -= kBN;
+        all_see -= kBN;
+        tmem_wait_st();
+        fence_before();
+        named_barrier_sync(kBarP0 + t, kMeetP);
+      }
+      bool ok = __all_sync(0xffffffffu, mbar_wait(&bar_o[t], done & 1, &abort_flag, a.err));
+      ok = !__any_sync(0xffffffffu, abort_flag != 0) && ok;
+      // by way of the unit's last K (t = 0) or V slot, which this group then gives back
+      const int slot = (w.L + 2 * w.nT - 2 + t) % C::kStages;
+      if (ok) {
+        fence_after();
+        const int piece = u.parts > 1 ? u.slot + u.part : -1;
+        const bool odd =
+            store_rows<D>(a, &tm_o, u, piece, t * kBM + wq * 32, lane, tO, m_run, l_run,
+                          sKV + slot * C::kTileBytes + wq * (C::kTileBytes / 4));
+        if (odd && a.mask) {
+          if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+          __syncwarp();
+          form_again<D>(a, u, piece, r, limit + (u.j0 + u.nT) * kBN, m_run, l_run);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        fence_before();
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        __syncwarp();
+      }
+      if (kChain) {
+        named_barrier_sync(kBarStored + t, kBM);
+        if (ok && wq == 0 && lane == 0) mbar_arrive(&bar_empty[slot]);
+      }
+      tc_pass<D>(w);
+      ++done;
     }
-    bool ok = __all_sync(0xffffffffu, mbar_wait(&bar_o, 0, &abort_flag, a.err));
-    ok = !__any_sync(0xffffffffu, abort_flag != 0) && ok;
-    if (ok) {
-      fence_after();
-      store_rows<D>(a, u, u.parts > 1 ? u.slot + u.part : -1, t * kBM + wq * 32, lane, tO, m_run,
-                    l_run, sKV + (warp - 4) * (32 * D * 4), [&]() {
-                      return a.mask && form_again<D>(a, u, tO, u.row0 + r, limit + j0 * kBN,
-                                                     j0 * kBN, min(u.seq.lk, (j0 + nT) * kBN),
-                                                     m_run, r < rows);
-                    });
-    }
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
     fence_before();
     named_barrier_sync(kBarTeardown, kTcThreads);
   }
@@ -800,24 +1007,28 @@ bool make_rows_map(CUtensorMap *map, const void *base, int N, int H, int D, long
              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+template <int D, bool kChain>
+int configure(int dev) {
+  static std::atomic<int> configured[64];
+  if (configured[dev].load()) return HSA_OK;
+  auto kernel = packed_attention_kernel<D, kChain>;
+  // the register hand-over assumes exactly kLaunchRegs registers at launch
+  cudaFuncAttributes fa;
+  if (cudaFuncGetAttributes(&fa, kernel) != cudaSuccess) return HSA_ERR_CUDA;
+  if (fa.numRegs != kLaunchRegs || fa.maxThreadsPerBlock < kTcThreads) return HSA_ERR_UNSUPPORTED;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, TcCfg<D>::kSmem) !=
+      cudaSuccess)
+    return HSA_ERR_CUDA;
+  configured[dev].store(1);
+  return HSA_OK;
+}
+
 template <int D>
 int launch(PackedArgs &a, const void *any, cudaStream_t stream) {
   using C = TcCfg<D>;
-  auto kernel = packed_attention_kernel<D>;
-  static std::atomic<int> configured[64];
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return HSA_ERR_CUDA;
-  if (!configured[dev].load()) {
-    // the register hand-over assumes exactly kLaunchRegs registers at launch
-    cudaFuncAttributes fa;
-    if (cudaFuncGetAttributes(&fa, kernel) != cudaSuccess) return HSA_ERR_CUDA;
-    if (fa.numRegs != kLaunchRegs || fa.maxThreadsPerBlock < kTcThreads) return HSA_ERR_UNSUPPORTED;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) !=
-        cudaSuccess)
-      return HSA_ERR_CUDA;
-    configured[dev].store(1);
-  }
-  CUtensorMap mk, mv, mq;
+  CUtensorMap mk, mv, mq, mo;
   // without keys no tile is loaded: any valid map serves
   const int keys = std::max(a.total_k, 1);
   if (!make_kv_map(&mk, a.total_k ? a.k : any, keys, a.Hkv * D,
@@ -831,6 +1042,12 @@ int launch(PackedArgs &a, const void *any, cudaStream_t stream) {
   if (a.q_map && !make_rows_map(&mq, a.q, a.total_q, a.Hq, D, a.q_row, G, kBM / G))
     return HSA_ERR_CUDA;
   if (!a.q_map) mq = mk;
+  // and a warp's 32 rows are a box of the output
+  a.o_map = 32 % G == 0;
+  if (a.o_map &&
+      !make_rows_map(&mo, a.out, a.total_q, a.Hq, D, (long long)a.Hq * D, G, 32 / G))
+    return HSA_ERR_CUDA;
+  if (!a.o_map) mo = mk;
   // Units at most: every sequence has at most one partly filled block.  How many there are
   // is on the device, so the grid holds what a cut may make of them: a block too many costs
   // about a microsecond of an SM.  Fewer units than SMs become at most sms parts, or 2 sms
@@ -843,8 +1060,13 @@ int launch(PackedArgs &a, const void *any, cudaStream_t stream) {
       a.mask || units < a.sms ? std::max<long long>(units, a.most) : units + a.most;
   if (grid > 0x7fffffffLL) return HSA_ERR_UNSUPPORTED;
   a.bound = (int)units;
+  const bool chain = grid > a.sms;
+  const int st = chain ? configure<D, true>(dev) : configure<D, false>(dev);
+  if (st != HSA_OK) return st;
   count_launches(a.most ? 2 : 1);
-  launch_pdl(kernel, dim3((unsigned)grid), dim3(kTcThreads), C::kSmem, stream, mk, mv, mq, a);
+  launch_pdl(chain ? packed_attention_kernel<D, true> : packed_attention_kernel<D, false>,
+             dim3((unsigned)grid), dim3(kTcThreads), C::kSmem, stream, mk, mv, mq, mo,
+             a);
   if (cudaGetLastError() != cudaSuccess) return HSA_ERR_CUDA;
   if (a.most)
     launch_pdl(packed_join_kernel<D>, dim3((unsigned)(8 * a.sms)), dim3(kJoinThreads), 0, stream,
@@ -878,7 +1100,8 @@ extern "C" int hsa_packed_attention(const void *q, long long q_row, const void *
   if (dtype != HSA_BF16 && dtype != HSA_F32) return HSA_ERR_INVALID_ARG;
   if (dtype == HSA_F32 || (D != 64 && D != 128) || (long long)Hq * D > (1LL << 24))
     return HSA_ERR_UNSUPPORTED;
-  if (total_k > 0x7fffff00 || (long long)total_q * (Hq / Hkv) > 0x7fffff00LL)
+  if (batch > 0x7fffff00 || total_k > 0x7fffff00 ||
+      (long long)total_q * (Hq / Hkv) > 0x7fffff00LL)
     return HSA_ERR_UNSUPPORTED;
   if (q_row < (long long)Hq * D || k_row < (long long)Hkv * D || v_row < (long long)Hkv * D ||
       (q_row & 7) || (k_row & 7) || (v_row & 7) || q_row > (1LL << 31) || k_row > (1LL << 31) ||

@@ -358,35 +358,63 @@ __device__ __forceinline__ void softmax_tile(uint32_t tS, uint32_t tO, int valid
 
 // ------------------------------------------------------------ warp roles
 
+// A unit's place in its CTA's pipeline: its nT key tiles are the tiles J .. of the S
+// barriers and buffers and fill the ring from load L on.  A CTA of one unit starts at 0
+// (constants, which cost nothing); in a chain of units each starts where the one before
+// ended.
+struct TcSpan {
+  int J, L, nT;
+};
+// Moves past a span: three S buffers close a chained one with a round of S barriers of its
+// own (see the issuer).
+template <int D>
+__device__ __forceinline__ void tc_pass(TcSpan &w) {
+  w.J += w.nT + TcCfg<D>::kThreeS;
+  w.L += 2 * w.nT;
+}
+
 // The barriers of a CTA's pipeline, in its shared memory.
 struct TcPipe {
   uint64_t *full, *empty;   // ring slots, kStages each
-  uint64_t *s, *o;          // kQT * kSBars; one
+  uint64_t *s, *o;          // kQT * kSBars; one, or in a chain one per Q tile
   volatile int *abort_flag;
   unsigned *err;
 };
 
-// TMA producer (one warp): key tiles n_pre/2 .. nT-1, K then V; load_kv(L) issues the
-// copy of tile L/2 (L even: K).  `withheld`: a load that a test leaves out, or -1.
+// TMA producer (one lane): loads [from, to) of a unit's 2 nT; load_kv(L, slot) issues the
+// copy of its tile L/2 (L even: K, odd: V).  `withheld`: a load that a test leaves out, or
+// -1.  False: a wait failed; `issued` is the load after the last one issued.
+template <int D, typename Load>
+__device__ __forceinline__ bool tc_load(const TcPipe &p, const TcSpan &w, int from, int to,
+                                        int withheld, int &issued, Load &&load_kv) {
+  using C = TcCfg<D>;
+  for (int L = from; L < to; ++L) {
+    const int slot = (w.L + L) % C::kStages, use = (w.L + L) / C::kStages;
+    if (use > 0 && !mbar_wait(&p.empty[slot], (use - 1) & 1, p.abort_flag, p.err)) return false;
+    if (w.L + L == withheld) continue;
+    load_kv(L, slot);
+    issued = w.L + L + 1;
+  }
+  return true;
+}
+// Every issued copy has landed before the CTA may exit.  A slot is only refilled once its
+// previous tile was consumed, so the copies in flight are among the last kStages issued.
+template <int D>
+__device__ __forceinline__ void tc_drain(const TcPipe &p, int issued, int withheld) {
+  using C = TcCfg<D>;
+  for (int L = issued > C::kStages ? issued - C::kStages : 0; L < issued; ++L)
+    if (L != withheld)
+      mbar_wait(&p.full[L % C::kStages], (L / C::kStages) & 1, p.abort_flag, p.err, false);
+}
+// The producer warp of a CTA of one unit, from load n_pre on; load_kv(L) finds the slot.
 template <int D, typename Load>
 __device__ __forceinline__ void tc_produce(const TcPipe &p, int lane, int nT, int n_pre,
                                            int withheld, Load &&load_kv) {
-  using C = TcCfg<D>;
   if (lane == 0) {
     int issued = n_pre;
-    for (int L = n_pre; L < 2 * nT; ++L) {
-      const int slot = L % C::kStages, use = L / C::kStages;
-      if (use > 0 && !mbar_wait(&p.empty[slot], (use - 1) & 1, p.abort_flag, p.err)) break;
-      if (L == withheld) continue;
-      load_kv(L);
-      issued = L + 1;
-    }
-    // Drain: every issued copy has landed before the CTA may exit.  A
-    // slot is only refilled once its previous tile was consumed, so the
-    // copies in flight are among the last kStages issued.
-    for (int L = issued > C::kStages ? issued - C::kStages : 0; L < issued; ++L)
-      if (L != withheld)
-        mbar_wait(&p.full[L % C::kStages], (L / C::kStages) & 1, p.abort_flag, p.err, false);
+    tc_load<D>(p, {0, 0, nT}, n_pre, 2 * nT, withheld, issued,
+               [&](int L, int) { load_kv(L); });
+    tc_drain<D>(p, issued, withheld);
   }
   __syncwarp();
 }
@@ -416,11 +444,15 @@ __device__ __forceinline__ void tc_produce(const TcPipe &p, int lane, int nT, in
 // tensor core waited for them: D = 64, whose MMAs are half as long, went
 // from 1269 to 1505 TFLOP/s (24 heads, N = 32760), the LTX layer from 980
 // to 1132.  D = 128 is bound by the MMAs (1990 -> 1995).
-template <int D>
+// kChain: more units may follow.  p.o[t] then tells the softmax warps of Q tile t that this
+// one's O_t is complete, and the barriers of three S buffers all complete once for the tile
+// after the last, so that their phases stay in step.
+template <int D, bool kChain = false>
 __device__ __forceinline__ void tc_issue(const TcPipe &p, uint32_t tmem, uint32_t q_base,
-                                         uint32_t kv_base, int nT) {
+                                         uint32_t kv_base, const TcSpan &w) {
   using C = TcCfg<D>;
   const uint32_t lead = elect_one();
+  const int nT = w.nT;
   constexpr uint32_t kIdS = idesc_bf16(kBM, kBN, 0);
   constexpr uint32_t kIdO = idesc_bf16(kBM, D, 1);
   // Descriptors differ only in their start-address field (bits 0-13,
@@ -432,7 +464,7 @@ __device__ __forceinline__ void tc_issue(const TcPipe &p, uint32_t tmem, uint32_
   // S_t = Q_t K^T: K = D in steps of 16 (32 bytes inside a 128-byte chunk).
   auto issue_s = [&](int t, int L) {
     const uint64_t dq = dq0 + t * kTile16;
-    const uint64_t dk = dk0 + (L % C::kStages) * kTile16;
+    const uint64_t dk = dk0 + ((w.L + L) % C::kStages) * kTile16;
     const uint32_t ts = tmem + 128 * t;
 #pragma unroll
     for (int k = 0; k < D / 16; ++k) {
@@ -442,7 +474,7 @@ __device__ __forceinline__ void tc_issue(const TcPipe &p, uint32_t tmem, uint32_
   };
   // O_t += P_t V: P in TMEM (bf16 pairs in the S_t columns), V MN-major.
   auto issue_o = [&](int t, int L, bool acc) {
-    const uint64_t dv = dv0 + (L % C::kStages) * kTile16;
+    const uint64_t dv = dv0 + ((w.L + L) % C::kStages) * kTile16;
     const uint32_t to = tmem + C::kOCol0 + D * t, tp = tmem + 128 * t;
 #pragma unroll
     for (int k = 0; k < kBN / 16; ++k)
@@ -467,6 +499,8 @@ __device__ __forceinline__ void tc_issue(const TcPipe &p, uint32_t tmem, uint32_
       if (more) {
         issue_s(0, Lk);
         mma_commit(&p.s[0], lead);
+      } else if (kChain) {
+        mma_commit(&p.o[0], lead);
       }
       p_ready(1);
       issue_o(1, Lv, j > 0);
@@ -485,18 +519,19 @@ __device__ __forceinline__ void tc_issue(const TcPipe &p, uint32_t tmem, uint32_
     // by two completions of the barrier it waits on.
     auto issue_s3 = [&](int t, int j) {
       const uint64_t dq = dq0 + t * kTile16;
-      const uint64_t dk = dk0 + ((2 * j) % C::kStages) * kTile16;
-      const uint32_t ts = tmem + 128 * ((2 * j + t) % 3);
+      const uint64_t dk = dk0 + ((w.L + 2 * j) % C::kStages) * kTile16;
+      const uint32_t ts = tmem + 128 * ((2 * (w.J + j) + t) % 3);
 #pragma unroll
       for (int k = 0; k < D / 16; ++k) {
         const uint32_t off = ((k >> 2) * (kBM * 128) + (k & 3) * 32) >> 4;
         mma_ss(ts, dq + off, dk + off, kIdS, k > 0, lead);
       }
-      mma_commit(&p.s[2 * t + (j & 1)], lead);
+      mma_commit(&p.s[2 * t + ((w.J + j) & 1)], lead);
     };
     auto issue_o3 = [&](int t, int j) {
-      const uint64_t dv = dv0 + ((2 * j + 1) % C::kStages) * kTile16;
-      const uint32_t to = tmem + C::kOCol0 + D * t, tp = tmem + 128 * ((2 * j + t) % 3);
+      const uint64_t dv = dv0 + ((w.L + 2 * j + 1) % C::kStages) * kTile16;
+      const uint32_t to = tmem + C::kOCol0 + D * t;
+      const uint32_t tp = tmem + 128 * ((2 * (w.J + j) + t) % 3);
 #pragma unroll
       for (int k = 0; k < kBN / 16; ++k)
         mma_ts(to, tp + 8 * k, dv + ((k * 2048) >> 4), kIdO, (j > 0 || k > 0) ? 1u : 0u, lead);
@@ -510,18 +545,23 @@ __device__ __forceinline__ void tc_issue(const TcPipe &p, uint32_t tmem, uint32_
       p_ready(0);                               // P_0(j); V_j and K_(j+1) landed
       issue_o3(0, j);
       if (j + 1 < nT) issue_s3(1, j + 1);
+      else if (kChain) mma_commit(&p.o[0], lead);
       p_ready(1);                               // P_1(j); K_(j+2) landed
       issue_o3(1, j);
       if (j + 2 < nT)
         issue_s3(0, j + 2);
       else if (j + 2 == nT)
-        mma_commit(&p.s[(j + 2) & 1], lead);  // O_1(j) done, for the last tile's rescale
+        mma_commit(&p.s[(w.J + j + 2) & 1], lead);  // O_1(j) done, for the last tile's rescale
+    }
+    if constexpr (kChain) {
+      if (nT == 1) mma_commit(&p.s[(w.J + 1) & 1], lead);
+      mma_commit(&p.s[2 + ((w.J + nT) & 1)], lead);
     }
   }
   // Completes once every MMA issued above has finished (also on abort), so
   // TMEM is quiet before it is freed.
-  mma_commit(p.o, lead);
-  mbar_wait(p.o, 0, p.abort_flag, p.err, false);
+  mma_commit(&p.o[kChain], lead);
+  if constexpr (!kChain) mbar_wait(p.o, 0, p.abort_flag, p.err, false);
   __syncwarp();
 }
 
@@ -538,17 +578,22 @@ __device__ __forceinline__ void tc_issue(const TcPipe &p, uint32_t tmem, uint32_
 // nothing back, so no slot is refilled while a copy into it may still be
 // in flight.
 // v_landed(j) is called once V_j is in its slot, before the issuer is told.
-template <int D, typename Landed>
-__device__ __forceinline__ void tc_watch_kv(const TcPipe &p, int lane, int nT, Landed &&v_landed) {
+// kChain: all slots are given back but the last K's and V's, which the softmax warps give
+// back when they have stored the unit's rows by way of them.
+template <int D, bool kChain = false, typename Landed>
+__device__ __forceinline__ void tc_watch_kv(const TcPipe &p, int lane, const TcSpan &w,
+                                            Landed &&v_landed) {
   using C = TcCfg<D>;
   bool live = true;
+  const int nT = w.nT;
   auto landed = [&](int L) {
+    const int at = w.L + L;
     if (live)
-      live = __all_sync(0xffffffffu, mbar_wait(&p.full[L % C::kStages],
-                                               (L / C::kStages) & 1, p.abort_flag, p.err));
+      live = __all_sync(0xffffffffu, mbar_wait(&p.full[at % C::kStages], (at / C::kStages) & 1,
+                                               p.abort_flag, p.err));
   };
   auto give_back = [&](int L) {
-    if (lane == 0) mbar_arrive(&p.empty[L % C::kStages]);
+    if (lane == 0) mbar_arrive(&p.empty[(w.L + L) % C::kStages]);
   };
   if constexpr (!C::kThreeS) {
     landed(0);
@@ -559,9 +604,9 @@ __device__ __forceinline__ void tc_watch_kv(const TcPipe &p, int lane, int nT, L
       if (j + 1 < nT) landed(2 * j + 2);       // K_(j+1)
       named_barrier_sync(kBarP0, kMeetP);
       if (live) {
-        live = __all_sync(0xffffffffu, mbar_wait(&p.s[1], j & 1, p.abort_flag, p.err));
+        live = __all_sync(0xffffffffu, mbar_wait(&p.s[1], (w.J + j) & 1, p.abort_flag, p.err));
         if (live) {
-          give_back(2 * j);                    // K_j
+          if (!kChain || j + 1 < nT) give_back(2 * j);   // K_j
           if (j > 0) give_back(2 * j - 1);     // V_(j-1)
         }
       }
@@ -581,11 +626,12 @@ __device__ __forceinline__ void tc_watch_kv(const TcPipe &p, int lane, int nT, L
       landed(2 * j + 1);                       // V_j
       if (live) v_landed(j);
       named_barrier_sync(kBarP0, kMeetP);
-      if (live && j + 1 < nT) {
-        live = __all_sync(0xffffffffu, mbar_wait(&p.s[(j + 1) & 1], ((j + 1) >> 1) & 1,
-                                                 p.abort_flag, p.err));
+      // chained: after the last tile, the barrier's extra round
+      if (live && (j + 1 < nT || (kChain && nT > 1))) {
+        const int i = w.J + j + 1;
+        live = __all_sync(0xffffffffu, mbar_wait(&p.s[i & 1], (i >> 1) & 1, p.abort_flag, p.err));
         if (live) {
-          give_back(2 * j);                    // K_j
+          if (!kChain || j + 1 < nT) give_back(2 * j);   // K_j
           if (j > 0) give_back(2 * j - 1);     // V_(j-1)
         }
       }
@@ -602,10 +648,10 @@ __device__ __forceinline__ void tc_watch_kv(const TcPipe &p, int lane, int nT, L
 // and meets the softmax group.  It meets even after a failed wait.  24 x
 // 64, N = 32760: 1508 -> 1595 TFLOP/s; D = 128 within its spread.
 template <int D>
-__device__ __forceinline__ void tc_watch_s(const TcPipe &p, int nT) {
+__device__ __forceinline__ void tc_watch_s(const TcPipe &p, const TcSpan &w) {
   using C = TcCfg<D>;
   bool live = true;
-  for (int j = 0; j < nT; ++j) {
+  for (int j = w.J; j < w.J + w.nT; ++j) {
 #pragma unroll
     for (int t = 0; t < kQT; ++t) {
       uint64_t *b = C::kThreeS ? &p.s[2 * t + (j & 1)] : &p.s[t];

@@ -320,3 +320,137 @@ def test_rows_of_one_head_in_a_wider_tensor(hsa):
     out = torch.empty((50, 1, 64), dtype=torch.bfloat16, device=DEV)
     hsa.hsa_packed_attention(*(part(xd, i) for i in range(3)), cu.to(DEV), cu.to(DEV), out, mask=1)
     _compare(out.cpu(), *(part(x, i) for i in range(3)), cu, cu, [(50, 50)], 1)
+
+
+# ---------- more blocks than SMs: a block takes several units, in an order that may differ
+
+def _mixed(seed, batch=40):
+    """Sequences of none to 300 queries: continued, plain, without keys, or of fewer keys than
+    queries (whose first rows see nothing under a mask)."""
+    g = torch.Generator().manual_seed(seed)
+    lens = []
+    for b in range(batch):
+        n = int(torch.randint(0, 60, (), generator=g)) + (250 if b % 13 == 5 else 0)
+        lens.append((n, (n, n + 200, 0, n // 3, n + 1)[b % 5]))
+    return lens
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("mask", [0, 1, 24])
+@pytest.mark.parametrize("G", [1, 3, 4, 64])
+def test_blocks_take_several_units(hsa, G, mask, D):
+    """The query rows come by TMA or (G = 3) by the warps, the output rows go by TMA in boxes
+    of 32 or (G = 3, 64, and the last rows) by the warps."""
+    _check(hsa, _mixed(30 + G), 6 * G, 6, D, mask, 31, lead=2, trail=40, rows=9 if G < 64 else 120)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("mask", [0, 1])
+def test_same_bits_whichever_block_takes_a_unit(hsa, mask, D):
+    lens = [(90 + 11 * (b % 7), 90 + 300 * (b % 3)) for b in range(60)]
+    (q, k, v), cu_q, cu_k = _data(lens, 8, 4, D, 32)
+    q, k, v, cu_q, cu_k = (t.to(DEV) for t in (q, k, v, cu_q, cu_k))
+    ws = torch.empty(hsa.hsa_packed_attention_workspace_bytes(8, 4, D), dtype=torch.uint8,
+                     device=DEV)
+    outs = [torch.full_like(q, 9.0) for _ in range(6)]
+    for out in outs:
+        hsa.hsa_packed_attention(q, k, v, cu_q, cu_k, out, mask=mask, workspace=ws)
+    assert hsa.hsa_get_device_error() == 0
+    assert all(torch.equal(outs[0], out) for out in outs[1:])
+    _compare(outs[0].cpu(), q.cpu(), k.cpu(), v.cpu(), cu_q, cu_k, lens, mask, rows=67)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("G", [2, 3])
+def test_nan_between_units_of_a_block(hsa, G, D):
+    """The last key of every third sequence holds NaN and infinity: rows that do not see it,
+    and the other sequences', have their usual results."""
+    Hkv, lens = 4, [(40 + 7 * (b % 5), 40 + 7 * (b % 5) + 130 * (b % 2)) for b in range(45)]
+    (q, k, v), cu_q, cu_k = _data(lens, G * Hkv, Hkv, D, 33)
+    v0, k0 = v.clone(), k.clone()
+    for b in range(0, 45, 3):
+        at = int(cu_k[b + 1]) - 1
+        v[at, :, 3], v[at, :, D - 1] = float("nan"), float("-inf")
+        k[at, :, 7] = float("inf")
+    out = torch.empty(q.shape, dtype=torch.bfloat16, device=DEV)
+    hsa.hsa_packed_attention(*(t.to(DEV) for t in (q, k, v, cu_q, cu_k)), out, mask=1)
+    assert hsa.hsa_get_device_error() == 0
+    got = out.cpu()
+    for b in range(0, 45, 3):
+        last = int(cu_q[b + 1]) - 1
+        assert got[last].isnan().any(-1).all()
+        one = (torch.tensor([0]), torch.tensor([0]))
+        lq, lk = lens[b]
+        first, key = int(cu_q[b]), int(cu_k[b])
+        # all rows but the last see none of it: a continued prompt one key shorter
+        _compare(got[first:], q[first:], k0[key:], v0[key:], *one, [(lq - 1, lk - 1)], 1, rows=5)
+    others = [b for b in range(45) if b % 3]
+    for b in others:
+        _compare(got[int(cu_q[b]):], q[int(cu_q[b]):], k0[int(cu_k[b]):], v0[int(cu_k[b]):],
+                 torch.tensor([0]), torch.tensor([0]), [lens[b]], 1, rows=9)
+
+
+def test_many_bad_offsets(hsa):
+    """Offsets that fall and overlap make more rows than there are: reported, and nothing is
+    written behind the output."""
+    n, batch = 700, 300
+    q, k, v = (torch.randn((n, H, 64), device=DEV).to(torch.bfloat16) for H in (4, 2, 2))
+    ws = torch.empty(hsa.hsa_packed_attention_workspace_bytes(4, 2, 64), dtype=torch.uint8,
+                     device=DEV)
+    guard = torch.full((n + 300, 4, 64), 9.0, dtype=torch.bfloat16, device=DEV)
+    bad = torch.tensor([n * (b % 2) for b in range(batch + 1)], dtype=torch.int32, device=DEV)
+    rising = torch.arange(batch + 1, dtype=torch.int32, device=DEV)
+    for cu_q, cu_k in ((bad, bad), (bad, rising), (rising, bad)):
+        for w in (None, ws):
+            hsa.hsa_packed_attention(q, k, v, cu_q, cu_k, guard[:n], mask=1, workspace=w)
+            assert hsa.hsa_get_device_error() == -6
+            assert (guard[n:] == 9.0).all()
+    _check(hsa, _mixed(3), 8, 4, 64, 1, 34, rows=7)
+
+
+def test_captured_call_of_many_blocks_follows_the_offsets(hsa):
+    """The grid is that of the buffers; the units of a replay are those of its offsets, from
+    none to more than there are SMs."""
+    Hq, Hkv, D, cap, batch = 8, 4, 128, 2200, 48
+    q, k, v = (torch.empty((cap, H, D), dtype=torch.bfloat16, device=DEV) for H in (Hq, Hkv, Hkv))
+    cu_q, cu_k = (torch.zeros(batch + 1, dtype=torch.int32, device=DEV) for _ in range(2))
+    out = torch.empty_like(q)
+    ws = torch.empty(hsa.hsa_packed_attention_workspace_bytes(Hq, Hkv, D), dtype=torch.uint8,
+                     device=DEV)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            hsa.hsa_packed_attention(q, k, v, cu_q, cu_k, out, mask=1, workspace=ws)
+        for i, lens in enumerate(([(45, 45)] * batch, [(0, 0)] * batch,
+                                  [(0, 0)] * 20 + [(30, 2100)] + [(0, 0)] * 27,
+                                  [(b, b) for b in range(batch)])):
+            data, cq, ck = _data(lens, Hq, Hkv, D, 40 + i)
+            for t, x in zip((q, k, v), data):
+                t.fill_(float("nan"))
+                t[:x.shape[0]] = x
+            cu_q.copy_(cq)
+            cu_k.copy_(ck)
+            out.fill_(9.0)
+            graph.replay()
+            side.synchronize()
+            _compare(out.cpu(), *data, cq, ck, lens, 1, rows=11)
+            assert (out[int(cq[-1]):] == 9.0).all()
+    assert hsa.hsa_get_device_error() == 0
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_wait_timeout_where_blocks_take_several_units(hsa, D):
+    """As test_wait_timeout_is_reported: the blocks give up after their bounded wait and take
+    no further unit."""
+    lens = [(40, 300)] * 45
+    (q, k, v), cu_q, cu_k = _data(lens, 8, 4, D, 35)
+    out = torch.empty(q.shape, dtype=torch.bfloat16, device=DEV)
+    hsa.hsa_test_inject_attention_stall(1)
+    try:
+        hsa.hsa_packed_attention(*(t.to(DEV) for t in (q, k, v, cu_q, cu_k)), out, mask=1)
+        assert hsa.hsa_get_device_error() == -7
+    finally:
+        hsa.hsa_test_inject_attention_stall(0)
+    _check(hsa, lens, 8, 4, D, 1, 35, rows=13)
