@@ -386,9 +386,9 @@ int hsa_kv_dequant_gather(const void *k_cache, const void *v_cache, const uint8_
  *   workspace    device, >= hsa_paged_attention_workspace_bytes(...) bytes, 16-byte
  *                aligned, overwritten; calls (and captured graphs) sharing one must
  *                not overlap on the GPU.  Its size depends on D and the device only.
- * D in {64, 128}; page_size a power of two; max_pages * page_size < 2^31 - 256; batch *
- * Hkv * ceil(rows / 8) * max_pages * page_size / 64 < 2^31 with rows = n_new * Hq / Hkv.  A
- * page id outside [0, n_pages) reads as rows of zeros (HSA_ERR_INDEX).  Two launches;
+ * D in {64, 128}; Hq < 2^16; page_size a power of two; max_pages * page_size < 2^31 - 256;
+ * batch * Hkv * ceil(rows / 8) * max_pages * page_size / 64 < 2^31 with rows = n_new * Hq /
+ * Hkv.  A page id outside [0, n_pages) reads as rows of zeros (HSA_ERR_INDEX).  Two launches;
  * the result does not depend on what else runs.  A flat cache of N rows is a cache of
  * ceil(N / page_size) pages with the identity as its table. */
 int hsa_paged_attention(const void *q, int batch, int n_new, int Hq, const void *k_pages,
@@ -424,7 +424,8 @@ size_t hsa_paged_attention_workspace_bytes(int batch, int n_new, int Hq, int Hkv
  *                calls with few rows and long keys be cut along the keys and joined (a
  *                second launch).  Overwritten; calls (and captured graphs) sharing one
  *                must not overlap on the GPU.  Its size depends on D and the device.
- * D in {64, 128}; pointers but cu_q and cu_k 16-byte aligned. */
+ * D in {64, 128}; pointers but cu_q and cu_k 16-byte aligned; Hq * D <= 2^24; batch,
+ * total_k, total_q * Hq / Hkv and Hkv * (total_q * Hq / Hkv / 256 + batch) < 2^31 - 1024. */
 int hsa_packed_attention(const void *q, long long q_row, const void *k, long long k_row,
                          const void *v, long long v_row, const int32_t *cu_q,
                          const int32_t *cu_k, int batch, int total_q, int total_k, int Hq,

@@ -56,7 +56,7 @@ struct PackedArgs {
   int bound;                       // units that the host allowed for
   int q_map, o_map;                // the query rows come, the output rows go by TMA
   int inject_stall;                // test hook (hsa_test.h)
-  float *ws_o, *ws_ml;             // [piece][kUnitRows][D], [piece][kUnitRows][2]
+  float *ws_o, *ws_ml;             // [piece][sum_place], [piece][kUnitRows][2]
   Cuts *cuts;                      // what the join reads
 };
 
@@ -78,6 +78,13 @@ __device__ __forceinline__ void tma_store_3d(const CUtensorMap *map, const void 
   asm volatile(
       "cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map),
       "r"(smem_addr(src)), "r"(x), "r"(y), "r"(z)
+      : "memory");
+}
+
+__device__ __forceinline__ void bulk_store(void *dst, const void *src, int bytes) {
+  asm volatile(
+      "cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;\n"
+      "cp.async.bulk.commit_group;" ::"l"(dst), "r"(smem_addr(src)), "r"(bytes)
       : "memory");
 }
 
@@ -202,14 +209,17 @@ __device__ __forceinline__ void plan_units(const PackedArgs &a, const Window &fi
       }
       return lo;
     };
-    int len = shortest(a.sms);
-    if (a.most > a.sms) {
-      const int two = shortest(2 * a.sms);
-      if (2 * (two + 5) < len + 5) len = two;
-    }
-    if (len + kJoinTiles < far) {
-      p.n_whole = 0;
-      p.longest = len;
+    // (no search where even parts of one length would not pay: each takes a microsecond)
+    if ((int)(work / a.sms) + kJoinTiles < far) {
+      int len = shortest(a.sms);
+      if (a.most > a.sms && 2 * ((int)(work / (2 * a.sms)) + 5) < len + 5) {
+        const int two = shortest(2 * a.sms);
+        if (2 * (two + 5) < len + 5) len = two;
+      }
+      if (len + kJoinTiles < far) {
+        p.n_whole = 0;
+        p.longest = len;
+      }
     }
   } else if (may && a.most >= 2 * a.sms && !a.mask && p.units % a.sms) {
     // More units than SMs: under a mask the last ones to start are short already.  Without,
@@ -318,6 +328,15 @@ __device__ __forceinline__ __nv_bfloat16 *out_row(const PackedArgs &a, int q0, i
   return a.out + ((size_t)(q0 + i) * a.Hq + head * (int)a.group.d + (R - i * (int)a.group.d)) * D;
 }
 
+// Where a piece's workspace holds the sums of dimensions 4 x .. 4 x + 3 of row r, in vectors:
+// half of the dimensions of 32 rows lie together, as they leave shared memory.
+template <int D>
+__device__ __forceinline__ int sum_place(int r, int x) {
+  constexpr int kV = D / 8;
+  const int y = x % kV;
+  return (((r >> 5) * 2 + x / kV) * 32 + (r & 31)) * kV + ((y & ~7) | ((y ^ r) & 7));
+}
+
 // Forms and stores those of this warp's rows again whose sums took in a masked value that
 // is not finite: sum over the row's own keys [k0, min(limit, k1)) of 2^(c s - m) v, m and l
 // being right already; piece: of the workspace, or -1: the row of the output.  Rare and slow;
@@ -378,11 +397,11 @@ __device__ __noinline__ void form_again(const PackedArgs &a, const Unit &u, int 
       }
     }
     if (bad && piece >= 0) {
-      float4 *to =
-          reinterpret_cast<float4 *>(a.ws_o + ((size_t)piece * kUnitRows + r) * D + 32 * c);
+      float4 *to = reinterpret_cast<float4 *>(a.ws_o) + (size_t)piece * (kUnitRows * D / 4);
 #pragma unroll
       for (int v = 0; v < 8; ++v)
-        to[v] = make_float4(acc[4 * v], acc[4 * v + 1], acc[4 * v + 2], acc[4 * v + 3]);
+        to[sum_place<D>(r, 8 * c + v)] =
+            make_float4(acc[4 * v], acc[4 * v + 1], acc[4 * v + 2], acc[4 * v + 3]);
     } else if (bad) {
       uint4 *to = reinterpret_cast<uint4 *>(out_row<D>(a, u.seq.q0, u.head, R) + 32 * c);
 #pragma unroll
@@ -425,13 +444,13 @@ __device__ __forceinline__ bool store_rows(const PackedArgs &a, const CUtensorMa
 #pragma unroll
         for (int i = 0; i < 32; ++i) worst[i & 3] = fmaf(__uint_as_float(o[i]), 0.f, worst[i & 3]);
       }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
-      uint4 *dst = reinterpret_cast<uint4 *>(a.ws_o) +
-                   ((size_t)piece * kUnitRows + r0) * (2 * kV) + half * kV;
-#pragma unroll
-      for (int i = 0; i < kV; ++i) {
-        const int e = 32 * i + lane, row = e / kV, v = e % kV;
-        dst[row * (2 * kV) + v] = st[row * kV + ((v & ~7) | ((v & 7) ^ (row & 7)))];
+      if (lane == 0) {
+        bulk_store(reinterpret_cast<uint4 *>(a.ws_o) + (size_t)piece * (kUnitRows * D / 4) +
+                       (r0 / 32 * 2 + half) * (32 * kV),
+                   st, 32 * kV * 16);
+        if (half == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
       }
       __syncwarp();
     }
@@ -527,7 +546,7 @@ __device__ __forceinline__ int block_of(const uint4 *answer) {
 // shared memory (softmax and issuing warps); the rows of Q tile t have left shared memory.
 constexpr int kBarStart = 7, kBarQ = 8, kBarStored = 9;   // kBarStored + t
 
-// A block that is one of more than there are SMs (kChain) takes one unit after another: its
+// A block that is one of more than two per SM (kChain) takes one unit after another: its
 // own, then those of blocks that have not started yet (ask_block), so that the roles run on
 // from unit to unit and the tensor pipe does not wait through a block's end and the next
 // one's start.  Warp 0 works out the next unit while the present one's last tiles are
@@ -536,8 +555,8 @@ constexpr int kBarStart = 7, kBarQ = 8, kBarStored = 9;   // kBarStored + t
 // one's store.  Units are handed over through unit_sh: bar_unit says that unit n is there,
 // bar_taken that all other warps have read on to it and so are done with unit n - 1, whose
 // place unit n + 1 takes.  Against a block per unit: six prompts of 503 to 5200 tokens, 32
-// heads x 128 on 8, 309 -> 285 us; two of 16 frames of 384, 32 x 64, 280 -> 265; 64 prompts of
-// 200 tokens, 32 x 128 on 8, 130 -> 114; 1024 of 20, 920 -> 270, mostly since a block goes
+// heads x 128 on 8, 311 -> 283 us; two of 16 frames of 384, 32 x 64, 277 -> 264; 64 prompts of
+// 200 tokens, 32 x 128 on 8, 130 -> 104; 1024 of 20, 920 -> 270, mostly since a block goes
 // through the sequences once.
 template <int D, bool kChain>
 __global__ void __launch_bounds__(kTcThreads, 1)
@@ -634,69 +653,75 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k,
         if (u.parts == 0) u.nT = 0;
         return u;
       };
-      auto publish = [&](int n, const Unit &u) {
-        if (n) mbar_wait(&bar_taken, (n - 1) & 1, &abort_flag, a.err, false);
-        __syncwarp();
+      auto publish = [&](int n, const Unit &u) {   // unit n - 1 has been taken by all warps
         if (lane == 0) {
           unit_sh[n & 1] = u;
           if (kChain) mbar_arrive(&bar_unit);
         }
         __syncwarp();
       };
-      Unit u = find();
-      publish(0, u);
-      for (int n = 0;; ++n) {
-        w.nT = u.nT;
-        const int key0 = u.seq.k0 + u.j0 * kBN;
-        // The query rows: where G divides a tile's 128 rows a box of 128 / G tokens, G heads
-        // and 64 dimensions is a tile's column chunk as the MMA wants it, and arrives on the
-        // first K tile's barrier; rows past the sequence's last are another sequence's or
-        // zeros, and are never stored.  Else the softmax warps load row by row.
-        auto load_kv = [&](int L, int slot) {
-          mbar_expect_tx(&bar_full[slot],
-                         C::kTileBytes * (L == 0 && a.q_map ? 1 + kQT : 1));
-          uint8_t *dst = sKV + slot * C::kTileBytes;
+      Unit u;
+      int from = 0;   // the unit's next load
+      // The query rows: where G divides a tile's 128 rows a box of 128 / G tokens, G heads
+      // and 64 dimensions is a tile's column chunk as the MMA wants it, and arrives on the
+      // first K tile's barrier; rows past the sequence's last are another sequence's or
+      // zeros, and are never stored.  Else the softmax warps load row by row.
+      auto load_kv = [&](int L, int slot) {
+        mbar_expect_tx(&bar_full[slot], C::kTileBytes * (L == 0 && a.q_map ? 1 + kQT : 1));
+        uint8_t *dst = sKV + slot * C::kTileBytes;
+#pragma unroll
+        for (int c = 0; c < C::kChunks; ++c)
+          tma_load_2d(dst + c * (kBN * 128), (L & 1) ? &tm_v : &tm_k, &bar_full[slot],
+                      u.head * D + c * 64, u.seq.k0 + (u.j0 + (L >> 1)) * kBN);
+      };
+      auto load_q = [&]() {
+        const int G = a.group.d, tok = u.seq.q0 + (int)quotient(u.row0, a.group);
+        uint64_t *bar = &bar_full[w.L % C::kStages];
+#pragma unroll
+        for (int t = 0; t < kQT; ++t)
 #pragma unroll
           for (int c = 0; c < C::kChunks; ++c)
-            tma_load_2d(dst + c * (kBN * 128), (L & 1) ? &tm_v : &tm_k, &bar_full[slot],
-                        u.head * D + c * 64, key0 + (L >> 1) * kBN);
-        };
-        auto load_q = [&]() {
-          const int G = a.group.d, tok = u.seq.q0 + (int)quotient(u.row0, a.group);
-          uint64_t *bar = &bar_full[w.L % C::kStages];
-#pragma unroll
-          for (int t = 0; t < kQT; ++t)
-#pragma unroll
-            for (int c = 0; c < C::kChunks; ++c)
-              tma_load_3d(sQ + t * C::kTileBytes + c * (kBM * 128), &tm_q, bar, c * 64,
-                          u.head * G, tok + t * (int)quotient(kBM, a.group));
-        };
-        int from = min(2, 2 * w.nT);   // the next load
-        if (lane == 0 && w.nT) {
-          if (a.q_map && !done) load_q();   // K_0's barrier still waits for K_0
-          live = tc_load<D>(pipe, w, 0, from, withheld, issued, load_kv);
-          if (a.q_map && done && issued > w.L) {
-            // K_0 is on its way, so its barrier waits for the rows too: they are loaded even
-            // if the wait fails
-            live = mbar_wait(&bar_q, (done - 1) & 1, &abort_flag, a.err) && live;
-            load_q();
-          }
+            tma_load_3d(sQ + t * C::kTileBytes + c * (kBM * 128), &tm_q, bar, c * 64, u.head * G,
+                        tok + t * (int)quotient(kBM, a.group));
+      };
+      auto load_to = [&](int to) {
+        to = max(from, min(to, 2 * w.nT));
+        if (lane == 0) live = live && tc_load<D>(pipe, w, from, to, withheld, issued, load_kv);
+        from = to;
+      };
+      // What the unit's first S needs, before the other warps hear of the unit.
+      auto begin = [&]() {
+        w.nT = u.nT;
+        from = 0;
+        if (!done) {
+          if (lane == 0 && a.q_map && w.nT) load_q();   // K_0's barrier still waits for K_0
+          load_to(3);
+          return;
         }
-        __syncwarp();
-        if (n == 0) named_barrier_sync(kBarStart, kTcThreads);
-        if (u.parts == 0) break;
-        auto load_to = [&](int to) {
-          to = max(from, to);
-          if (lane == 0) live = live && tc_load<D>(pipe, w, from, to, withheld, issued, load_kv);
-          from = to;
-        };
+        load_to(1);
+        // K_0 is on its way, so its barrier waits for the rows too: they are loaded even if
+        // the wait fails
+        if (lane == 0 && a.q_map && issued > w.L) {
+          live = mbar_wait(&bar_q, (done - 1) & 1, &abort_flag, a.err) && live;
+          load_q();
+        }
+      };
+      u = find();
+      begin();
+      publish(0, u);
+      named_barrier_sync(kBarStart, kTcThreads);
+      for (int n = 0; u.parts; ++n) {
         if (!kChain) {
           load_to(2 * w.nT);
           break;
         }
         // The next id is asked for before the last loads, which wait for their slots, and
-        // not sooner: a block that took units ahead would leave others without at the end.
-        load_to(2 * w.nT - 3);
+        // when the softmax warps have begun this unit: not sooner, since a block that took
+        // units ahead would leave others without at the end (64 prompts of 200 tokens, 32
+        // heads x 128 on 8: 114 -> 104 us).
+        load_to(max(3, 2 * w.nT - 3));
+        mbar_wait(&bar_taken, n & 1, &abort_flag, a.err, false);
+        __syncwarp();
         if (lane == 0) ask_block(&answer, &bar_answer);
         load_to(2 * w.nT);
         live = __shfl_sync(0xffffffffu, live, 0);
@@ -704,13 +729,13 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k,
         // No block is left: the next kernel may start.  TMEM is taken by now, as in the
         // active attention.
         if (id < 0) pdl_trigger();
-        const Unit next = find();
-        publish(n + 1, next);
         if (w.nT) {
           tc_pass<D>(w);
           ++done;
         }
-        u = next;
+        u = find();
+        if (u.parts) begin();
+        publish(n + 1, u);
       }
       if (lane == 0) tc_drain<D>(pipe, issued, withheld);
       __syncwarp();
@@ -928,7 +953,8 @@ packed_join_kernel(const PackedArgs a) {
       if (row < r1) {
         const size_t at = (size_t)u.slot * kUnitRows + row;
         const float2 *ml = reinterpret_cast<const float2 *>(a.ws_ml) + at;
-        const float4 *o = reinterpret_cast<const float4 *>(a.ws_o) + at * kL + sub;
+        const float4 *o = reinterpret_cast<const float4 *>(a.ws_o) +
+                          (size_t)u.slot * (kUnitRows * kL) + sum_place<D>(row, sub);
         const int step = wide ? kGroups : 1;
         for (int p0 = wide ? group : 0; p0 < u.parts; p0 += 4 * step) {
           float2 w[4];
@@ -1055,12 +1081,15 @@ int launch(PackedArgs &a, const void *any, cudaStream_t stream) {
   // units come on top of the others.  Too few keys for a cut to pay: no join.
   const long long units = ((long long)a.total_q * a.group.d / kUnitRows + a.batch) * a.Hkv;
   if (a.total_k <= (kLeastTiles + kJoinTiles) * kBN) a.most = 0;
-  if (a.most) a.most = 2 * units <= a.sms ? a.sms : 2 * a.sms;
+  if (a.most) a.most = 2 * units <= a.sms || (a.mask && units >= a.sms) ? a.sms : 2 * a.sms;
   const long long grid =
       a.mask || units < a.sms ? std::max<long long>(units, a.most) : units + a.most;
   if (grid > 0x7fffffffLL) return HSA_ERR_UNSUPPORTED;
   a.bound = (int)units;
-  const bool chain = grid > a.sms;
+  // Two waves of blocks of one unit are as fast as a chain of two units, and a block that
+  // takes no other starts 0.6 us sooner (two prompts of 3000 to 6000 tokens, 8 heads x 128 on
+  // 2: 78 against 79 us; 2000 tokens, 16 x 128 on 2: 30 against 32).
+  const bool chain = grid > 2LL * a.sms;
   const int st = chain ? configure<D, true>(dev) : configure<D, false>(dev);
   if (st != HSA_OK) return st;
   count_launches(a.most ? 2 : 1);

@@ -990,8 +990,8 @@ extern "C" int hsa_paged_attention(const void *q, int batch, int n_new, int Hq, 
                                    const void *v_pages, const uint8_t *k_scale,
                                    const uint8_t *v_scale, int n_pages, int page_size, int Hkv,
                                    int D, hsa_dtype cache_dtype, const int32_t *page_table,
-                                   int max_pages, const int32_t *seq_lens, float scale, void *out, void *workspace,
-                                   size_t size, hsa_stream_t stream) {
+                                   int max_pages, const int32_t *seq_lens, float scale, void *out,
+                                   void *workspace, size_t size, hsa_stream_t stream) {
   if (batch < 0 || n_new < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv || n_pages < 0 || max_pages < 0 ||
       page_size < 1)
     return HSA_ERR_INVALID_ARG;
