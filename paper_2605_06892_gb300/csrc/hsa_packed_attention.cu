@@ -26,7 +26,7 @@
 //    sequence's end are zeroed in shared memory before they are multiplied.  Under a mask,
 //    a row whose result is not finite looks through the values it should not have met in
 //    its unit's tiles; if one of those is not finite the row is formed again without them
-//    on the CUDA cores.
+//    on the CUDA cores, once the block has ended its units.
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -337,18 +337,20 @@ __device__ __forceinline__ int sum_place(int r, int x) {
   return (((r >> 5) * 2 + x / kV) * 32 + (r & 31)) * kV + ((y & ~7) | ((y ^ r) & 7));
 }
 
-// Forms and stores those of this warp's rows again whose sums took in a masked value that
-// is not finite: sum over the row's own keys [k0, min(limit, k1)) of 2^(c s - m) v, m and l
-// being right already; piece: of the workspace, or -1: the row of the output.  Rare and slow;
-// out of line so that it costs the usual path no registers.
+// Forms and stores those of this warp's rows again (r: this lane's) whose sums took in a
+// masked value that is not finite: the softmax over the row's own keys of the unit or piece,
+// on the CUDA cores, 32 keys at a time by way of `st`, 64 D bytes of the warp's own.  Rare and
+// slow (4 us a key); out of line so that it costs the usual path no registers.
 template <int D>
-__device__ __noinline__ void form_again(const PackedArgs &a, const Unit &u, int piece, int r,
-                                        int limit, float m, float l) {
+__device__ __noinline__ void form_again(const PackedArgs &a, const Unit &u, int r, uint4 *st) {
+  const int lane = threadIdx.x & 31;
+  const int piece = u.parts > 1 ? u.slot + u.part : -1;
   const int k0 = u.j0 * kBN, k1 = min(u.seq.lk, k0 + u.nT * kBN), R = u.row0 + r;
   const bool valid = r < u.rows;
   const __nv_bfloat16 *K = a.k + (size_t)u.seq.k0 * a.k_row + (size_t)u.head * D;
   const __nv_bfloat16 *V = a.v + (size_t)u.seq.k0 * a.v_row + (size_t)u.head * D;
   const int tok = valid ? quotient(R, a.group) : 0;
+  const int limit = valid ? key_limit(a, u.seq, tok) : 0;
   const __nv_bfloat16 *Q = a.q + (size_t)(u.seq.q0 + tok) * a.q_row +
                            (u.head * (int)a.group.d + (valid ? R - tok * (int)a.group.d : 0)) * D;
   bool bad = false;
@@ -363,35 +365,66 @@ __device__ __noinline__ void form_again(const PackedArgs &a, const Unit &u, int 
   const int end = bad ? min(limit, k1) : 0;
   const int most = __reduce_max_sync(0xffffffffu, end);
   if (!__any_sync(0xffffffffu, bad)) return;
-  const float f = piece >= 0 ? 1.f : l > 0.f ? 1.f / l : l;
+  uint4 q[D / 8];
+#pragma unroll
+  for (int v = 0; v < D / 8; ++v)
+    q[v] = bad ? __ldg(reinterpret_cast<const uint4 *>(Q) + v) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll 1
   for (int c = 0; c < D / 32; ++c) {
-    float acc[32];
+    float acc[32], m = kLowest, l = 0.f;
 #pragma unroll
     for (int i = 0; i < 32; ++i) acc[i] = 0.f;
-    for (int j = k0; j < most; ++j) {
-      float s = 0.f;
-      for (int v = 0; v < D / 8; ++v) {
-        const uint4 qw = __ldg(reinterpret_cast<const uint4 *>(Q) + v);
-        const uint4 kw = __ldg(reinterpret_cast<const uint4 *>(K + (size_t)j * a.k_row) + v);
-        const uint32_t x[4] = {qw.x, qw.y, qw.z, qw.w}, y[4] = {kw.x, kw.y, kw.z, kw.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          s = fmaf(__uint_as_float(x[i] << 16), __uint_as_float(y[i] << 16), s);
-          s = fmaf(__uint_as_float(x[i] & 0xffff0000u), __uint_as_float(y[i] & 0xffff0000u), s);
+#pragma unroll 1
+    for (int j0 = k0; j0 < most; j0 += 32) {
+      auto bring = [&](const __nv_bfloat16 *rows, long long row, int vectors) {
+        __syncwarp();
+        for (int e = lane; e < 32 * vectors; e += 32) {
+          const int j = j0 + e / vectors;
+          st[e] = j < most ? __ldg(reinterpret_cast<const uint4 *>(rows + (size_t)j * row) +
+                                   e % vectors)
+                           : make_uint4(0u, 0u, 0u, 0u);
         }
+        __syncwarp();
+      };
+      float p[32], top = m;
+      bring(K, a.k_row, D / 8);
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int v = 0; v < D / 8; ++v) {
+          const uint4 kw = st[i * (D / 8) + v];
+          const uint32_t x[4] = {q[v].x, q[v].y, q[v].z, q[v].w}, y[4] = {kw.x, kw.y, kw.z, kw.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            s[e] = fmaf(__uint_as_float(x[e] << 16), __uint_as_float(y[e] << 16), s[e]);
+            s[e] = fmaf(__uint_as_float(x[e] & 0xffff0000u), __uint_as_float(y[e] & 0xffff0000u),
+                        s[e]);
+          }
+        }
+        p[i] = ((s[0] + s[1]) + (s[2] + s[3])) * a.scale_log2;
+        if (j0 + i < end) top = fmaxf(top, p[i]);
       }
-      const float p = fast_exp2(fmaf(s, a.scale_log2, -m));
-      if (j < end) {
+      const float f = fast_exp2(m - top);
+      m = top;
+      l *= f;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) acc[i] *= f;
+      bring(V + 32 * c, a.v_row, 4);
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        if (j0 + i >= end) continue;
+        const float w = fast_exp2(p[i] - m);
+        l += w;
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-          const uint4 w = __ldg(reinterpret_cast<const uint4 *>(V + (size_t)j * a.v_row +
-                                                                32 * c) + v);
-          const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+          const uint4 x4 = st[i * 4 + v];
+          const uint32_t x[4] = {x4.x, x4.y, x4.z, x4.w};
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            acc[8 * v + 2 * i] = fmaf(p, __uint_as_float(x[i] << 16), acc[8 * v + 2 * i]);
-            acc[8 * v + 2 * i + 1] = fmaf(p, __uint_as_float(x[i] & 0xffff0000u),
-                                          acc[8 * v + 2 * i + 1]);
+          for (int e = 0; e < 4; ++e) {
+            acc[8 * v + 2 * e] = fmaf(w, __uint_as_float(x[e] << 16), acc[8 * v + 2 * e]);
+            acc[8 * v + 2 * e + 1] =
+                fmaf(w, __uint_as_float(x[e] & 0xffff0000u), acc[8 * v + 2 * e + 1]);
           }
         }
       }
@@ -402,7 +435,9 @@ __device__ __noinline__ void form_again(const PackedArgs &a, const Unit &u, int 
       for (int v = 0; v < 8; ++v)
         to[sum_place<D>(r, 8 * c + v)] =
             make_float4(acc[4 * v], acc[4 * v + 1], acc[4 * v + 2], acc[4 * v + 3]);
+      reinterpret_cast<float2 *>(a.ws_ml)[(size_t)piece * kUnitRows + r] = make_float2(m, l);
     } else if (bad) {
+      const float f = l > 0.f ? 1.f / l : l;
       uint4 *to = reinterpret_cast<uint4 *>(out_row<D>(a, u.seq.q0, u.head, R) + 32 * c);
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
@@ -577,7 +612,8 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k,
   __shared__ __align__(16) uint4 answer;
   __shared__ uint32_t tmem_base_sh;
   __shared__ volatile int abort_flag;
-  __shared__ Unit unit_sh[2];
+  __shared__ Unit unit_sh[2], odd_sh[2];
+  __shared__ volatile int odd_flag;
   const TcPipe pipe = {bar_full, bar_empty, bar_s, bar_o, &abort_flag, a.err};
 
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);
@@ -600,6 +636,7 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k,
     mbar_init(&bar_q, 1);
     mbar_init(&bar_answer, 1);
     abort_flag = 0;
+    odd_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -722,13 +759,15 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k,
         load_to(max(3, 2 * w.nT - 3));
         mbar_wait(&bar_taken, n & 1, &abort_flag, a.err, false);
         __syncwarp();
-        if (lane == 0) ask_block(&answer, &bar_answer);
+        // else the block ends: it has rows to form again
+        const bool ask = __shfl_sync(0xffffffffu, odd_flag, 0) == 0;
+        if (ask && lane == 0) ask_block(&answer, &bar_answer);
         load_to(2 * w.nT);
         live = __shfl_sync(0xffffffffu, live, 0);
-        id = answered();
+        id = ask ? answered() : -1;
         // No block is left: the next kernel may start.  TMEM is taken by now, as in the
         // active attention.
-        if (id < 0) pdl_trigger();
+        if (ask && id < 0) pdl_trigger();
         if (w.nT) {
           tc_pass<D>(w);
           ++done;
@@ -809,6 +848,7 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k,
     const uint32_t lane_off = (uint32_t)(wq * 32) << 16;
     const uint32_t tO = tmem + lane_off + C::kOCol0 + D * t;
     const float sl2 = a.scale_log2;
+    unsigned odd = 0;   // bit n & 1: rows of unit n are to be formed again
     for (int n = 0; take(n); ++n) {
       // Read where it is needed: held in registers over the key loop it would spill, to an
       // L1 that the tiles have left no room in.
@@ -895,13 +935,18 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k,
       if (ok) {
         fence_after();
         const int piece = u.parts > 1 ? u.slot + u.part : -1;
-        const bool odd =
-            store_rows<D>(a, &tm_o, u, piece, t * kBM + wq * 32, lane, tO, m_run, l_run,
-                          sKV + slot * C::kTileBytes + wq * (C::kTileBytes / 4));
-        if (odd && a.mask) {
-          if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        if (store_rows<D>(a, &tm_o, u, piece, t * kBM + wq * 32, lane, tO, m_run, l_run,
+                          sKV + slot * C::kTileBytes + wq * (C::kTileBytes / 4)) &&
+            a.mask) {
+          // Forming rows again may take longer than the other roles wait for one another, so
+          // it is left until they have ended.  The unit after this one may have been handed
+          // over already, no other follows.
+          odd |= 1u << (n & 1);
+          if (lane == 0) {
+            odd_sh[n & 1] = u;
+            odd_flag = 1;
+          }
           __syncwarp();
-          form_again<D>(a, u, piece, r, limit + (u.j0 + u.nT) * kBN, m_run, l_run);
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         fence_before();
@@ -916,6 +961,18 @@ packed_attention_kernel(const __grid_constant__ CUtensorMap tm_k,
       ++done;
     }
     if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+    if (a.mask) {
+      named_barrier_sync(kBarQ, 256);   // all stores have left shared memory
+      if (odd) {
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        __syncwarp();
+#pragma unroll 1
+        for (int i = 0; i < 2; ++i)
+          if (odd >> i & 1)
+            form_again<D>(a, odd_sh[i], t * kBM + wq * 32 + lane,
+                          reinterpret_cast<uint4 *>(sKV + (warp - 4) * (C::kTileBytes / 4)));
+      }
+    }
     fence_before();
     named_barrier_sync(kBarTeardown, kTcThreads);
   }

@@ -455,3 +455,24 @@ def test_wait_timeout_where_blocks_take_several_units(hsa, D):
     finally:
         hsa.hsa_test_inject_attention_stall(0)
     _check(hsa, lens, 16, 8, D, 1, 35, rows=13)
+
+
+def test_rows_formed_again_over_long_keys(hsa):
+    """Rows that took in a masked NaN are formed again on the CUDA cores, here for longer than
+    the warps wait for one another, in blocks that have another unit to do."""
+    H, D, lq, n, at = 8, 128, 10300, 1_200_000, 1_200_000 - 130
+    g = torch.Generator(DEV).manual_seed(50)
+    q, k, v = (torch.randn((m, H, D), generator=g, device=DEV, dtype=torch.bfloat16)
+               for m in (lq, n, n))
+    v[at] = float("nan")
+    out = torch.full_like(q, 9.0)
+    hsa.hsa_packed_attention(q, k, v, _cum([lq]).to(DEV), _cum([n]).to(DEV), out, mask=1)
+    assert hsa.hsa_get_device_error() == 0
+    first = lq - (n - at)   # the first row that sees the NaN
+    nan = out.isnan()
+    assert nan[first:].all() and not nan[:first].any()
+    for h, row in ((0, first - 1), (7, first - 40), (3, 5000)):
+        ks, vs = (t[:at, h:h + 1].cpu().double() for t in (k, v))
+        want, tol = ref.attention(q[row:row + 1, h:h + 1].cpu().double(), ks, vs,
+                                  [n - lq + row + 1])
+        assert ((out[row, h].cpu().double() - want[0, 0]).abs() <= tol[0, 0]).all()
