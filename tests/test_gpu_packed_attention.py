@@ -476,3 +476,24 @@ def test_rows_formed_again_over_long_keys(hsa):
         want, tol = ref.attention(q[row:row + 1, h:h + 1].cpu().double(), ks, vs,
                                   [n - lq + row + 1])
         assert ((out[row, h].cpu().double() - want[0, 0]).abs() <= tol[0, 0]).all()
+
+
+@pytest.mark.parametrize("mask", [0, 1])
+def test_blocks_of_several_units_beside_another_stream(hsa, mask):
+    """Two grids whose blocks take further units, at the same time: each takes its own."""
+    lens = [(90 + 11 * (b % 7), 90 + 300 * (b % 3)) for b in range(60)]
+    (q, k, v), cu_q, cu_k = _data(lens, 16, 8, 128, 36)
+    q, k, v, cu_q, cu_k = (t.to(DEV) for t in (q, k, v, cu_q, cu_k))
+    size = hsa.hsa_packed_attention_workspace_bytes(16, 8, 128)
+    outs = [torch.full_like(q, 9.0) for _ in range(7)]
+    wss = [torch.empty(size, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    hsa.hsa_packed_attention(q, k, v, cu_q, cu_k, outs[0], mask=mask, workspace=wss[0])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for i in range(6):
+        with torch.cuda.stream(streams[i % 2]):
+            hsa.hsa_packed_attention(q, k, v, cu_q, cu_k, outs[1 + i], mask=mask,
+                                     workspace=wss[i % 2])
+    torch.cuda.synchronize()
+    assert hsa.hsa_get_device_error() == 0
+    assert all(torch.equal(outs[0], out) for out in outs[1:])
