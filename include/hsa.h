@@ -377,6 +377,7 @@ int hsa_kv_dequant_gather(const void *k_cache, const void *v_cache, const uint8_
  *   v_pages      HSA_E4M3 as hsa_kv_quant_scatter writes it, with
  *   k_scale,     device, scales [n_pages, page_size, Hkv] (HSA_E4M3; else NULL), any
  *   v_scale      alignment; the aligned words of four bytes around those needed are read.
+ *                A row as fresh memory holds it, all bytes zero, stands for zeros.
  *   page_table   device, int32 [batch, max_pages]: key j of sequence b is row
  *                j % page_size of page page_table[b, j / page_size].  Entries past a
  *                sequence's last page are not read, nor rows past its last key.

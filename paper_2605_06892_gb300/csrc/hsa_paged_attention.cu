@@ -24,16 +24,19 @@
 // 8-bit cache.  A key's e4m3 codes are exact in fp16, and so is a bf16 query row after
 // scaling by a power of two (its values below 2^-39 of the largest aside), so the
 // products are exact and the key's 2^ks multiplies the score.  The value's 2^vs goes into
-// the probability: with t_j the score in log2 units, u_j = t_j + vs_j and M = max u_j,
-//   o = sum_j 2^(u_j - M) code_j / sum_j 2^(t_j - M),
-// where no factor 2^(u_j - M) exceeds 1 and the sum of the second lies within 2^-120 and
-// 2^100 n because vs does within [-100, 120].
+// the probability: with t_j the score in log2 units, u_j = t_j + vs_j, M = max u_j and R
+// about max t_j,
+//   o = 2^(M - R) sum_j 2^(u_j - M) code_j / sum_j 2^(t_j - R).
+// No factor 2^(u_j - M) exceeds 1.  The weights' sum has a reference of its own: relative to
+// M it would lie between 2^-120 and 2^100 n, since vs does within [-100, 120] (-127 in rows
+// of fresh memory), and long stretches of zero rows would overflow it.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <type_traits>
 
 #include "hsa_internal.cuh"
 #include "hsa_ptx.cuh"
@@ -47,6 +50,7 @@ constexpr int kMostRows = 32;         // query rows of a unit at most
 constexpr int kMaxPerSm = 4;          // CTAs per SM that the workspace is sized for
 constexpr float kLowest = -3.0e38f;   // running maximum before the first key
 constexpr float kPShift = 14.f;       // fp16 probabilities are 2^(u - M + 14)
+constexpr float kFar = 0x1p64f;       // a weights' sum above it takes a new reference
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
@@ -136,6 +140,8 @@ struct Cfg {
   static constexpr int kScales = kF8 ? kKW * 16 : 0;           // per key four words
   static constexpr int kStage = 2 * kHalf + kScales;
   static constexpr int kQ = kRows * D * 2;                     // a unit's query rows
+  static constexpr int kStat = kF8 ? 4 : 2;                    // per row of a part: M, l, R
+  static constexpr int kPart = kRows * (D + kStat);            // floats of a part
   static constexpr int kSmem = kWarps * kStages * kStage + kStages * kQ;
 };
 
@@ -253,7 +259,7 @@ paged_attention_kernel(const Args a) {
   constexpr int kRows = C::kRows;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int sh_sum[kWarps], sh_at[3];
-  __shared__ float sh_m[kWarps][kRows], sh_l[kWarps][kRows];
+  __shared__ float sh_m[kWarps][kRows], sh_l[kWarps][kRows], sh_r[kF8 ? kWarps : 1][kRows];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   uint8_t *ring = smem + warp * (C::kStages * C::kStage);
   pdl_wait();
@@ -412,7 +418,10 @@ paged_attention_kernel(const Args a) {
   // lane row 8 x + g of Q^T and P^T, rows 8 x + 2 t + j of S^T and O^T
   constexpr bool kLean = C::kLean;
   uint32_t qf[kLean ? 1 : kSteps][kNR][2];
-  float o[kMT][kNR][4], m[kNR][2], l[kNR][2], c2[kF8 ? kNR : 1][2];
+  float o[kMT][kNR][4], m[kNR][2], l[kNR][2];
+  // 8 bits: a query row's power of two times the scale, and the reference of this lane's
+  // weights' sum
+  float c2[kF8 ? kNR : 1][2], ref[kF8 ? kNR : 1][2];
   uint32_t sq_now = 0;   // kLean: the unit's rows
   int unit_tile0 = 0;    // the unit's tile that this run of it starts with
   bool fresh = true, first_unit = true;
@@ -466,7 +475,10 @@ paged_attention_kernel(const Args a) {
         }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          if (kF8) c2[kF8 ? x : 0][j] = __shfl_sync(0xffffffffu, scale, 4 * (2 * t + j));
+          if (kF8) {
+            c2[kF8 ? x : 0][j] = __shfl_sync(0xffffffffu, scale, 4 * (2 * t + j));
+            ref[kF8 ? x : 0][j] = kLowest;
+          }
           m[x][j] = kLowest;
           l[x][j] = 0.f;
         }
@@ -480,7 +492,7 @@ paged_attention_kernel(const Args a) {
       const uint32_t sk = ring_s + now, sv = sk + C::kHalf;
       uint4 *scales = reinterpret_cast<uint4 *>(ring + now + 2 * C::kHalf);
       if (kF8) {
-        // each lane makes 2^ks and vs of its key's scale bytes (within [27, 247])
+        // each lane makes 2^ks and vs of its key's scale bytes (within [27, 247], or 0)
         if (lane < C::kKW) {
           const uint4 w = scales[lane];
           const uint32_t ks = w.x >> (w.z & 0xffffu) & 255u, vs = w.y >> (w.z >> 16) & 255u;
@@ -533,45 +545,48 @@ paged_attention_kernel(const Args a) {
       };
 #pragma unroll
       for (int x = 0; x < kNR; ++x) mx[x][0] = m[x][0], mx[x][1] = m[x][1];
+      // 8 bits: the weights' sum as well, each lane's relative to its own reference, a score of
+      // before that is close to the largest (within 2^64)
+      float sum[kF8 ? kNR : 1][2];
+      bool far = false;
+      auto weigh = [&](auto masked) {
 #pragma unroll
-      for (int b = 0; b < kNB; ++b)
+        for (int b = 0; b < kNB; ++b)
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
-          const int row = 16 * b + 8 * n + key_of<kCh>(g);
-          float kf = 1.f;
-          if (kF8) {
-            const uint4 w = scales[row];
-            kf = __uint_as_float(w.x), ve[b][n] = __uint_as_float(w.y);
-          }
-#pragma unroll
-          for (int x = 0; x < kNR; ++x)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              float &y = s[b][x][2 * n + j];
-              y = kF8 ? fmaf(y * kf, c2[kF8 ? x : 0][j], ve[b][n]) : y * a.scale_log2;
+          for (int n = 0; n < 2; ++n) {
+            const int row = 16 * b + 8 * n + key_of<kCh>(g);
+            float kf = 1.f;
+            if (kF8) {
+              const uint4 w = scales[row];
+              kf = __uint_as_float(w.x), ve[b][n] = __uint_as_float(w.y);
             }
-        }
-      if (!ragged) {
-#pragma unroll
-        for (int b = 0; b < kNB; ++b)
-#pragma unroll
-          for (int x = 0; x < kNR; ++x)
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-              mx[x][j] = fmaxf(mx[x][j], fmaxf(s[b][x][j], s[b][x][2 + j]));
-      } else {
-#pragma unroll
-        for (int b = 0; b < kNB; ++b)
-#pragma unroll
-          for (int n = 0; n < 2; ++n)
 #pragma unroll
             for (int x = 0; x < kNR; ++x)
 #pragma unroll
               for (int j = 0; j < 2; ++j) {
+                const bool seen = !decltype(masked)::value || key0 + row < limit(x, j);
                 float &y = s[b][x][2 * n + j];
-                if (key0 + 16 * b + 8 * n + key_of<kCh>(g) >= limit(x, j)) y = -INFINITY;
+                if constexpr (kF8) {
+                  const float z = y * kf;
+                  const float w = fmaf(z, c2[x][j], -ref[x][j]);
+                  y = seen ? fmaf(z, c2[x][j], ve[b][n]) : -INFINITY;
+                  sum[x][j] += seen ? fast_exp2(w) : 0.f;
+                } else {
+                  y = seen ? y * a.scale_log2 : -INFINITY;
+                }
                 mx[x][j] = fmaxf(mx[x][j], y);
               }
+          }
+      };
+      if constexpr (kF8) {
+#pragma unroll
+        for (int x = 0; x < kNR; ++x) sum[x][0] = l[x][0], sum[x][1] = l[x][1];
+      }
+      if (!ragged) weigh(std::false_type());
+      else weigh(std::true_type());
+      if constexpr (kF8) {
+#pragma unroll
+        for (int x = 0; x < kNR; ++x) far |= !(sum[x][0] <= kFar && sum[x][1] <= kFar);
       }
       bool moved = false;
 #pragma unroll
@@ -583,17 +598,43 @@ paged_attention_kernel(const Args a) {
             mx[x][j] = fmaxf(mx[x][j], __shfl_xor_sync(0xffffffffu, mx[x][j], d));
           moved |= mx[x][j] != m[x][j];
         }
-      if (__any_sync(0xffffffffu, moved)) {
+      if (__any_sync(0xffffffffu, moved || far)) {
 #pragma unroll
         for (int x = 0; x < kNR; ++x)
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             const float f = fast_exp2(m[x][j] - mx[x][j]);
             m[x][j] = mx[x][j];
-            l[x][j] *= f;
+            if (!kF8) l[x][j] *= f;
 #pragma unroll
             for (int n = 0; n < kMT; ++n) o[n][x][j] *= f, o[n][x][2 + j] *= f;
           }
+        // A unit's first tile and a steep rise: the sum again, from the scores that are still
+        // there, relative to the largest of them and of the sum before (which then counts 1
+        // at most)
+        if (kF8 && __any_sync(0xffffffffu, far)) {
+#pragma unroll
+          for (int x = 0; x < (kF8 ? kNR : 0); ++x)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              float top = fmaxf(ref[x][j], ref[x][j] + __log2f(l[x][j]));
+#pragma unroll
+              for (int b = 0; b < kNB; ++b)
+#pragma unroll
+                for (int n = 0; n < 2; ++n) top = fmaxf(top, s[b][x][2 * n + j] - ve[b][n]);
+              sum[x][j] = l[x][j] * fast_exp2(ref[x][j] - top);
+              ref[x][j] = top;
+#pragma unroll
+              for (int b = 0; b < kNB; ++b)
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+                  sum[x][j] += fast_exp2(s[b][x][2 * n + j] - ve[b][n] - top);
+            }
+        }
+      }
+      if constexpr (kF8) {
+#pragma unroll
+        for (int x = 0; x < kNR; ++x) l[x][0] = sum[x][0], l[x][1] = sum[x][1];
       }
       // ---- probabilities, as the 16 x 8 B operand of O^T += V^T P^T
       uint32_t p[kNB][kNR][2];
@@ -606,11 +647,8 @@ paged_attention_kernel(const Args a) {
             float y[2];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-              // 8 bits: 2^(t - M) by itself, not 2^(u - M) times 2^-vs: the first may be far
-              // below the least number where the second is not
-              const float z = s[b][x][2 * n + j] - (kF8 ? m[x][j] - kPShift : m[x][j]);
-              y[j] = fast_exp2(z);
-              l[x][j] += kF8 ? fast_exp2(z - ve[b][n]) : y[j];
+              y[j] = fast_exp2(s[b][x][2 * n + j] - (kF8 ? m[x][j] - kPShift : m[x][j]));
+              if (!kF8) l[x][j] += y[j];
             }
             p[b][x][n] = transposed(kF8 ? pack_f16(y[0], y[1]) : pack_bf16(y[0], y[1]));
           }
@@ -725,6 +763,14 @@ paged_attention_kernel(const Args a) {
       for (int x = 0; x < kNR; ++x)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
+          if constexpr (kF8) {   // one reference for the lanes of a row
+            float top = ref[x][j];
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1)
+              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+            l[x][j] *= fast_exp2(ref[x][j] - top);
+            if (g == 0) sh_r[warp][8 * x + 2 * t + j] = top;
+          }
 #pragma unroll
           for (int d = 4; d < 32; d <<= 1) l[x][j] += __shfl_xor_sync(0xffffffffu, l[x][j], d);
           if (g == 0) {
@@ -738,7 +784,7 @@ paged_attention_kernel(const Args a) {
       constexpr int kAt = kFit < 1 ? 0 : kFit < kNR ? kFit : kNR;
       static_assert(kAt > 0 && kNR % kAt == 0, "a stage takes the sums of a column block");
       const bool whole = unit_tile0 == 0 && unit_done;
-      float *part = a.ws + (size_t)(2 * blockIdx.x + (first_unit ? 0 : 1)) * (kRows * (D + 2));
+      float *part = a.ws + (size_t)(2 * blockIdx.x + (first_unit ? 0 : 1)) * C::kPart;
 #pragma unroll
       for (int x0 = 0; x0 < kNR; x0 += kAt) {
         if (x0) __syncthreads();
@@ -753,18 +799,25 @@ paged_attention_kernel(const Args a) {
         __syncthreads();
 #pragma unroll
         for (int x = x0; x < x0 + kAt; ++x) {
-          float f[2][kWarps], M[2], sum[2];
+          float f[2][kWarps], M[2], R[2], sum[2];
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             const int r = 8 * x + 2 * t + j;
             M[j] = sh_m[0][r];
 #pragma unroll
             for (int w = 1; w < kWarps; ++w) M[j] = fmaxf(M[j], sh_m[w][r]);
+            R[j] = M[j];
+            if constexpr (kF8) {
+              R[j] = sh_r[0][r];
+#pragma unroll
+              for (int w = 1; w < kWarps; ++w) R[j] = fmaxf(R[j], sh_r[w][r]);
+            }
             sum[j] = 0.f;
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
               f[j][w] = fast_exp2(sh_m[w][r] - M[j]);
-              sum[j] = fmaf(sh_l[w][r], f[j][w], sum[j]);
+              sum[j] = fmaf(sh_l[w][r], kF8 ? fast_exp2(sh_r[kF8 ? w : 0][r] - R[j]) : f[j][w],
+                            sum[j]);
             }
           }
           float y[kQuarter][4];
@@ -790,12 +843,14 @@ paged_attention_kernel(const Args a) {
             if (r >= a.rows) continue;
             if (whole) {
               const float inv = sum[j] > 0.f ? 1.f / sum[j] : sum[j] == 0.f ? 0.f : sum[j];
+              const float up = kF8 ? fast_exp2(M[j] - R[j] - kPShift) : 1.f;
               const int i = quotient(r, a.group);
               __nv_bfloat16 *dst = a.out + ((size_t)((size_t)cur.b * a.n_new + i) * a.Hq +
                                             h * (int)a.group.d + (r - i * (int)a.group.d)) * D + d;
               uint32_t w[kQuarter];
 #pragma unroll
-              for (int n = 0; n < kQuarter; ++n) w[n] = pack_bf16(y[n][j] * inv, y[n][2 + j] * inv);
+              for (int n = 0; n < kQuarter; ++n)
+                w[n] = pack_bf16(y[n][j] * inv * up, y[n][2 + j] * inv * up);
               if constexpr (kQuarter == 2)
                 *reinterpret_cast<uint2 *>(dst) = make_uint2(w[0], w[kQuarter - 1]);
               else
@@ -806,8 +861,10 @@ paged_attention_kernel(const Args a) {
                 *reinterpret_cast<float2 *>(part + rr * D + d + 2 * n) =
                     make_float2(y[n][j], y[n][2 + j]);
               if (warp == 0 && g == 0) {
-                part[kRows * D + 2 * rr] = M[j];
-                part[kRows * D + 2 * rr + 1] = sum[j];
+                float *stat = part + kRows * D + C::kStat * rr;
+                stat[0] = M[j];
+                stat[1] = sum[j];
+                if (kF8) stat[2] = R[j];
               }
             }
           }
@@ -836,15 +893,19 @@ paged_attention_kernel(const Args a) {
 // Joins a row's parts where several blocks shared its unit: one block for each block of
 // the kernel before and each row, and most of them find that theirs ended no such unit.
 // A part takes D/4 lanes, four dimensions each; bound by the round trips to L2, so each
-// lane group loads eight parts at once, and statistics with sums.
+// lane group loads eight parts at once, and statistics with sums.  In 8 bits, with a third
+// statistic, four: with eight it fits an SM three blocks or spills (48 ragged sequences 9.4
+// against 6.6 us, 12 heads x 64 of 16 sequences 8.4 against 6.4).
 constexpr int kJoinThreads = 256;
 
-template <int D, int kNR>
-__global__ void __launch_bounds__(kJoinThreads)
+template <int D, bool kF8, int kNR>
+__global__ void __launch_bounds__(kJoinThreads, 4)
 paged_join_kernel(const Args a) {
-  constexpr int kRows = 8 * kNR, kL = D / 4, kGroups = kJoinThreads / kL, kAtOnce = 8;
+  using C = Cfg<D, kF8, kNR>;
+  constexpr int kRows = 8 * kNR, kL = D / 4, kGroups = kJoinThreads / kL;
+  constexpr int kAtOnce = kF8 ? 4 : 8;
   __shared__ float4 sh_o[kJoinThreads];
-  __shared__ float2 sh_ml[kGroups];
+  __shared__ float4 sh_stat[kGroups];    // M, l, R
   pdl_wait();
   pdl_trigger();
   const CutUnit u = a.cuts[blockIdx.x];
@@ -852,69 +913,74 @@ paged_join_kernel(const Args a) {
   const int h = u.unit / a.row_tiles, rr = blockIdx.y, r = (u.unit - h * a.row_tiles) * kRows + rr;
   if (r >= a.rows) return;
   const int sub = threadIdx.x % kL, group = threadIdx.x / kL;
-  float M = kLowest, L = 0.f;
+  // R: what the weights' sum is relative to, in bf16 M itself
+  float M = kLowest, R = kLowest, L = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int p0 = group; p0 < u.parts; p0 += kAtOnce * kGroups) {
-    float2 w[kAtOnce];
-    float4 x[kAtOnce];
-#pragma unroll
-    for (int y = 0; y < kAtOnce; ++y) {
-      const int p = p0 + y * kGroups;
-      w[y] = make_float2(kLowest, 0.f);
-      x[y] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (p < u.parts) {
-        const float *part = a.ws + (size_t)(p ? 2 * (u.first + p) : u.slot) * (kRows * (D + 2));
-        w[y] = *reinterpret_cast<const float2 *>(part + kRows * D + 2 * rr);
-        x[y] = *reinterpret_cast<const float4 *>(part + rr * D + 4 * sub);
-      }
-    }
-    float to = M;
-#pragma unroll
-    for (int y = 0; y < kAtOnce; ++y) to = fmaxf(to, w[y].x);
-    const float f0 = fast_exp2(M - to);
+  auto refer = [&](float to, float to_r) {   // M and R rise
+    const float f = fast_exp2(M - to);
+    L *= kF8 ? fast_exp2(R - to_r) : f;
     M = to;
-    L *= f0, acc.x *= f0, acc.y *= f0, acc.z *= f0, acc.w *= f0;
-#pragma unroll
-    for (int y = 0; y < kAtOnce; ++y) {
-      const float f = fast_exp2(w[y].x - M);
-      L = fmaf(f, w[y].y, L);
-      acc.x = fmaf(f, x[y].x, acc.x);
-      acc.y = fmaf(f, x[y].y, acc.y);
-      acc.z = fmaf(f, x[y].z, acc.z);
-      acc.w = fmaf(f, x[y].w, acc.w);
-    }
-  }
-  sh_o[threadIdx.x] = acc;
-  if (sub == 0) sh_ml[group] = make_float2(M, L);
-  __syncthreads();
-  if (group) return;
-#pragma unroll
-  for (int y = 0; y < kGroups; ++y) M = fmaxf(M, sh_ml[y].x);
-  L = 0.f;
-  acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-  for (int y = 0; y < kGroups; ++y) {
-    const float2 w = sh_ml[y];
-    const float4 x = sh_o[y * kL + sub];
+    R = to_r;
+    acc.x *= f, acc.y *= f, acc.z *= f, acc.w *= f;
+  };
+  auto add = [&](const float4 &w, const float4 &x) {
     const float f = fast_exp2(w.x - M);
-    L = fmaf(f, w.y, L);
+    L = fmaf(kF8 ? fast_exp2(w.z - R) : f, w.y, L);
     acc.x = fmaf(f, x.x, acc.x);
     acc.y = fmaf(f, x.y, acc.y);
     acc.z = fmaf(f, x.z, acc.z);
     acc.w = fmaf(f, x.w, acc.w);
+  };
+  for (int p0 = group; p0 < u.parts; p0 += kAtOnce * kGroups) {
+    float4 w[kAtOnce], x[kAtOnce];
+#pragma unroll
+    for (int y = 0; y < kAtOnce; ++y) {
+      const int p = p0 + y * kGroups;
+      w[y] = make_float4(kLowest, 0.f, kLowest, 0.f);
+      x[y] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (p < u.parts) {
+        const float *part = a.ws + (size_t)(p ? 2 * (u.first + p) : u.slot) * C::kPart;
+        const float *stat = part + kRows * D + C::kStat * rr;
+        if constexpr (kF8) {
+          w[y] = *reinterpret_cast<const float4 *>(stat);
+        } else {
+          const float2 z = *reinterpret_cast<const float2 *>(stat);
+          w[y].x = z.x, w[y].y = z.y;
+        }
+        x[y] = *reinterpret_cast<const float4 *>(part + rr * D + 4 * sub);
+      }
+    }
+    float to = M, to_r = R;
+#pragma unroll
+    for (int y = 0; y < kAtOnce; ++y) to = fmaxf(to, w[y].x), to_r = fmaxf(to_r, w[y].z);
+    refer(to, to_r);
+#pragma unroll
+    for (int y = 0; y < kAtOnce; ++y) add(w[y], x[y]);
   }
+  sh_o[threadIdx.x] = acc;
+  if (sub == 0) sh_stat[group] = make_float4(M, L, R, 0.f);
+  __syncthreads();
+  if (group) return;
+#pragma unroll
+  for (int y = 0; y < kGroups; ++y) M = fmaxf(M, sh_stat[y].x), R = fmaxf(R, sh_stat[y].z);
+  L = 0.f;
+  acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int y = 0; y < kGroups; ++y) add(sh_stat[y], sh_o[y * kL + sub]);
   const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;
+  const float up = kF8 ? fast_exp2(M - R - kPShift) : 1.f;
   const int i = quotient(r, a.group);
   reinterpret_cast<uint2 *>(a.out + ((size_t)((size_t)u.b * a.n_new + i) * a.Hq +
                                      h * (int)a.group.d +
                                      (r - i * (int)a.group.d)) * D)[sub] =
-      make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+      make_uint2(pack_bf16(acc.x * inv * up, acc.y * inv * up),
+                 pack_bf16(acc.z * inv * up, acc.w * inv * up));
 }
 
 // -------------------------------------------------------------- host side
 
 size_t workspace_bytes(int D) {
-  return (size_t)sm_count() * kMaxPerSm * (sizeof(CutUnit) + 2 * kMostRows * ((size_t)D + 2) * 4);
+  return (size_t)sm_count() * kMaxPerSm * (sizeof(CutUnit) + 2 * kMostRows * ((size_t)D + 4) * 4);
 }
 
 template <int D, bool kF8, int kNR>
@@ -933,7 +999,7 @@ int launch(Args &a, void *workspace, cudaStream_t stream) {
             cudaSuccess ||
         cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout,
                              cudaSharedmemCarveoutMaxShared) != cudaSuccess ||
-        cudaFuncSetAttribute(paged_join_kernel<D, kNR>,
+        cudaFuncSetAttribute(paged_join_kernel<D, kF8, kNR>,
                              cudaFuncAttributePreferredSharedMemoryCarveout,
                              cudaSharedmemCarveoutMaxShared) != cudaSuccess ||
         cudaOccupancyMaxActiveBlocksPerMultiprocessor(&nb, kernel, kThreads, C::kSmem) !=
@@ -954,7 +1020,7 @@ int launch(Args &a, void *workspace, cudaStream_t stream) {
   count_launches(2);
   launch_pdl(kernel, dim3((unsigned)grid), dim3(kThreads), C::kSmem, stream, a);
   if (cudaGetLastError() != cudaSuccess) return HSA_ERR_CUDA;
-  launch_pdl(paged_join_kernel<D, kNR>, dim3((unsigned)grid, (unsigned)std::min(a.rows, C::kRows)),
+  launch_pdl(paged_join_kernel<D, kF8, kNR>, dim3((unsigned)grid, (unsigned)std::min(a.rows, C::kRows)),
              dim3(kJoinThreads), 0, stream, a);
   return launch_status();
 }
