@@ -419,9 +419,9 @@ paged_attention_kernel(const Args a) {
   constexpr bool kLean = C::kLean;
   uint32_t qf[kLean ? 1 : kSteps][kNR][2];
   float o[kMT][kNR][4], m[kNR][2], l[kNR][2];
-  // 8 bits: a query row's power of two times the scale, and the reference of this lane's
-  // weights' sum
-  float c2[kF8 ? kNR : 1][2], ref[kF8 ? kNR : 1][2];
+  // 8 bits: a query row's power of two and the scale, in two factors, and the reference of
+  // this lane's weights' sum
+  float before[kF8 ? kNR : 1][2], after[kF8 ? kNR : 1][2], ref[kF8 ? kNR : 1][2];
   uint32_t sq_now = 0;   // kLean: the unit's rows
   int unit_tile0 = 0;    // the unit's tile that this run of it starts with
   bool fresh = true, first_unit = true;
@@ -446,7 +446,7 @@ paged_attention_kernel(const Args a) {
         big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
         const unsigned E = max(__float_as_uint(big) >> 23, 20u);   // biased
         f = __uint_as_float((268u - E) << 23);
-        return a.scale_log2 * __uint_as_float((E - 14u) << 23);
+        return __uint_as_float((E - 14u) << 23);
       };
       auto larger = [](float big, uint32_t w) {
         return fmaxf(big, fmaxf(fabsf(lo_bf16(w)), fabsf(hi_bf16(w))));
@@ -476,7 +476,12 @@ paged_attention_kernel(const Args a) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           if (kF8) {
-            c2[kF8 ? x : 0][j] = __shfl_sync(0xffffffffu, scale, 4 * (2 * t + j));
+            // A product y stands for y 2^ks 2^c: multiplied in this order, with 2^c first
+            // where it is below 1 and last else, it overflows only where the score does,
+            // whatever the keys' size.
+            const float c = __shfl_sync(0xffffffffu, scale, 4 * (2 * t + j));
+            before[kF8 ? x : 0][j] = fminf(c, 1.f);
+            after[kF8 ? x : 0][j] = fminf(fmaxf(c, 1.f) * a.scale_log2, 3.4e38f);
             ref[kF8 ? x : 0][j] = kLowest;
           }
           m[x][j] = kLowest;
@@ -567,9 +572,9 @@ paged_attention_kernel(const Args a) {
                 const bool seen = !decltype(masked)::value || key0 + row < limit(x, j);
                 float &y = s[b][x][2 * n + j];
                 if constexpr (kF8) {
-                  const float z = y * kf;
-                  const float w = fmaf(z, c2[x][j], -ref[x][j]);
-                  y = seen ? fmaf(z, c2[x][j], ve[b][n]) : -INFINITY;
+                  const float z = y * before[x][j] * kf;
+                  const float w = fmaf(z, after[x][j], -ref[x][j]);
+                  y = seen ? fmaf(z, after[x][j], ve[b][n]) : -INFINITY;
                   sum[x][j] += seen ? fast_exp2(w) : 0.f;
                 } else {
                   y = seen ? y * a.scale_log2 : -INFINITY;

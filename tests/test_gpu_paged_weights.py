@@ -1,6 +1,6 @@
 """8-bit paged attention where the weights' sum has far to go: long stretches of zero rows,
-scale bytes as fresh memory holds them, values at the top of the range.  Against the 64-bit
-reference, within its bounds."""
+scale bytes as fresh memory holds them, values at the top of the range; and where keys and
+queries differ far in size.  Against the 64-bit reference, within its bounds."""
 import numpy as np
 import pytest
 import torch
@@ -145,3 +145,14 @@ def test_scores_that_climb(hsa, D):
     q[..., 0] = torch.tensor([1.0, 0.25, -1.0, 0.0])
     v = _normal((n, 1, D), 16) * torch.exp2(-level / 8)[:, None, None]
     _check(hsa, Sequence(k, v), q.to(torch.bfloat16), scale=0.5)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("ek,eq", [(110, -112), (120, -100), (-98, 112), (100, 20), (-90, -30)])
+def test_keys_and_queries_of_very_different_size(hsa, ek, eq, D):
+    """Scores of ordinary size from keys of 2^ek and queries of 2^eq."""
+    n = 200
+    k, v = _normal((n, 2, D), 11) * 2.0 ** ek, _normal((n, 2, D), 12)
+    k[5], k[77] = 0.0, 0.0                        # scores of exactly zero
+    q = (_normal((1, 2, 4, D), 13) * 2.0 ** eq).to(torch.bfloat16)
+    _check(hsa, Sequence(k, v), q, scale=D ** -0.5 * 2.0 ** -(ek + eq))
