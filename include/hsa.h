@@ -425,8 +425,9 @@ size_t hsa_paged_attention_workspace_bytes(int batch, int n_new, int Hq, int Hkv
  *                calls with few rows and long keys be cut along the keys and joined (a
  *                second launch).  Overwritten; calls (and captured graphs) sharing one
  *                must not overlap on the GPU.  Its size depends on D and the device.
- * D in {64, 128}; pointers but cu_q and cu_k 16-byte aligned; Hq * D <= 2^24; batch,
- * total_k, total_q * Hq / Hkv and Hkv * (total_q * Hq / Hkv / 256 + batch) < 2^31 - 1024. */
+ * D in {64, 128}; pointers but cu_q and cu_k 16-byte aligned; Hq * D <= 2^24; batch * Hkv
+ * <= 2^23; total_k, total_q * Hq / Hkv and Hkv * (total_q * Hq / Hkv / 256 + batch) < 2^31 -
+ * 1024. */
 int hsa_packed_attention(const void *q, long long q_row, const void *k, long long k_row,
                          const void *v, long long v_row, const int32_t *cu_q,
                          const int32_t *cu_k, int batch, int total_q, int total_k, int Hq,

@@ -551,6 +551,11 @@ __device__ __forceinline__ bool store_rows(const PackedArgs &a, const CUtensorMa
   return odd;
 }
 
+// Sequences times K/V heads of a call at most.  Those without rows have ids all the same, and
+// a block that passes over many of them, or over many sequences, keeps its other warps
+// waiting for a unit: their waits are bounded (about a second, hsa_tc.cuh).
+constexpr long long kMaxSequences = 1LL << 23;
+
 // Asks for the id of a block that has not started, which then never does (cluster launch
 // control); by one thread.
 __device__ __forceinline__ void ask_block(uint4 *answer, uint64_t *bar) {
@@ -1186,7 +1191,7 @@ extern "C" int hsa_packed_attention(const void *q, long long q_row, const void *
   if (dtype != HSA_BF16 && dtype != HSA_F32) return HSA_ERR_INVALID_ARG;
   if (dtype == HSA_F32 || (D != 64 && D != 128) || (long long)Hq * D > (1LL << 24))
     return HSA_ERR_UNSUPPORTED;
-  if (batch > 0x7fffff00 || total_k > 0x7fffff00 ||
+  if ((long long)batch * Hkv > kMaxSequences || total_k > 0x7fffff00 ||
       (long long)total_q * (Hq / Hkv) > 0x7fffff00LL)
     return HSA_ERR_UNSUPPORTED;
   if (q_row < (long long)Hq * D || k_row < (long long)Hkv * D || v_row < (long long)Hkv * D ||
