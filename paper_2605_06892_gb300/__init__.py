@@ -390,9 +390,14 @@ def hsa_cached_euler_l1rel(x, v_cache, v_fresh, pos, dsigma: float, stat, weight
 
 # ------------------------------------------------ 8-bit cache, paged attention
 
+_MOST = 2 ** 31 - 1   # C's int: ctypes would pass on a larger number's low 32 bits
+
+
 def _rows_of(name, t, size, n):
     """Refuses fewer than n rows, or rows of other sizes than a cache of this shape has."""
     shape = t.shape
+    if n > _MOST:
+        raise ValueError(f"{name}: {n} rows are more than a call takes")
     if len(shape) != 3 or shape[1] != size[-2] or shape[2] != size[-1] or not 0 <= n <= shape[0]:
         raise ValueError(f"{name} has shape {tuple(shape)}, not {n} or more rows of {size[-2]} "
                          f"heads x {size[-1]}")
@@ -412,13 +417,16 @@ def _cache8(k_cache, v_cache, k_scale, v_scale, size, device):
     if code is not torch.float8_e4m3fn and code is not torch.uint8:
         raise TypeError(f"the cache's codes have dtype {code}, not float8_e4m3fn or uint8")
     *lead, H, D = size
+    N = math.prod(lead)
+    if N > _MOST:
+        raise ValueError(f"k_cache holds {N} rows, more than a call takes")
     scales = (*lead, H)
     _sized("v_cache", v_cache, size)
     _sized("k_scale", k_scale, scales)
     _sized("v_scale", v_scale, scales)
     return (_place("k_cache", k_cache, code, device), _place("v_cache", v_cache, code, device),
             _place("k_scale", k_scale, torch.uint8, device),
-            _place("v_scale", v_scale, torch.uint8, device), math.prod(lead), H, D)
+            _place("v_scale", v_scale, torch.uint8, device), N, H, D)
 
 
 def hsa_kv_quant_scatter(k_cache, v_cache, k_scale, v_scale, k_fresh, v_fresh, idx, n_active: int,
@@ -526,6 +534,8 @@ def hsa_packed_attention(q, k, v, cu_q, cu_k, out, mask: int = 0, scale: float =
     total_k, Hkv, Dk = keys
     if Dk != D or len(ends) != 1:
         raise ValueError("q and k disagree on the head dimension, or cu_q is not a vector")
+    if not -_MOST <= mask <= _MOST:
+        raise ValueError(f"mask is {mask}, not 0 or a frame's tokens")
     _sized("v", v, keys)
     _sized("cu_k", cu_k, ends)
     _sized("out", out, size)
