@@ -24,12 +24,13 @@
 // 8-bit cache.  A key's e4m3 codes are exact in fp16, and so is a bf16 query row after
 // scaling by a power of two (its values below 2^-39 of the largest aside), so the
 // products are exact and the key's 2^ks multiplies the score.  The value's 2^vs goes into
-// the probability: with t_j the score in log2 units, u_j = t_j + vs_j, M = max u_j and R
-// about max t_j,
-//   o = 2^(M - R) sum_j 2^(u_j - M) code_j / sum_j 2^(t_j - R).
+// the probability: with t_j the score in log2 units, R about max t_j, u_j = t_j - R + vs_j
+// and M = max u_j,
+//   o = 2^M sum_j 2^(u_j - M) code_j / sum_j 2^(t_j - R).
 // No factor 2^(u_j - M) exceeds 1.  The weights' sum has a reference of its own: relative to
-// M it would lie between 2^-120 and 2^100 n, since vs does within [-100, 120] (-127 in rows
-// of fresh memory), and long stretches of zero rows would overflow it.
+// that of the other sum it would lie between 2^-120 and 2^100 n, since vs does within
+// [-100, 120] (-127 in rows of fresh memory), and long stretches of zero rows would overflow
+// it.  All else is relative to R, so that scores of any size lose nothing beside vs.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -50,7 +51,7 @@ constexpr int kMostRows = 32;         // query rows of a unit at most
 constexpr int kMaxPerSm = 4;          // CTAs per SM that the workspace is sized for
 constexpr float kLowest = -3.0e38f;   // running maximum before the first key
 constexpr float kPShift = 14.f;       // fp16 probabilities are 2^(u - M + 14)
-constexpr float kFar = 0x1p64f;       // a weights' sum above it takes a new reference
+constexpr float kFar = 0x1p64f;       // a lane's weights' sum above it takes a new R
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
@@ -419,22 +420,27 @@ paged_attention_kernel(const Args a) {
   constexpr bool kLean = C::kLean;
   uint32_t qf[kLean ? 1 : kSteps][kNR][2];
   float o[kMT][kNR][4], m[kNR][2], l[kNR][2];
-  // 8 bits: a query row's power of two and the scale, in two factors, and the reference of
-  // this lane's weights' sum
+  // 8 bits: a query row's power of two and the scale, in two factors, and its R
   float before[kF8 ? kNR : 1][2], after[kF8 ? kNR : 1][2], ref[kF8 ? kNR : 1][2];
   uint32_t sq_now = 0;   // kLean: the unit's rows
   int unit_tile0 = 0;    // the unit's tile that this run of it starts with
   bool fresh = true, first_unit = true;
+  // 8 bits: R is the largest score of the warp's first tile of the unit; where one rises 2^64
+  // above it later, that tile is taken again against a new one.
+  bool first = true, again = false;
   uint32_t now = 0;      // the stage of tile `it`
 
-  for (int it = 0; it < n_tiles; ++it) {
-    wait_all_but<C::kStages - 2>();
-    if (fresh) __syncthreads();   // the query rows are every thread's copies
-    else __syncwarp();
-    load_tile();
+  for (int it = 0; it < n_tiles;) {
+    if (!kF8 || !again) {
+      wait_all_but<C::kStages - 2>();
+      if (fresh) __syncthreads();   // the query rows are every thread's copies
+      else __syncwarp();
+      load_tile();
+    }
 
     if (fresh) {
       fresh = false;
+      first = true;
       unit_tile0 = cur.tile;
       const uint32_t from = smem_addr(sq + q_now * C::kQ);
       q_now = q_now + 1 == C::kStages ? 0 : q_now + 1;
@@ -496,7 +502,7 @@ paged_attention_kernel(const Args a) {
     if (key0 < cur.len) {
       const uint32_t sk = ring_s + now, sv = sk + C::kHalf;
       uint4 *scales = reinterpret_cast<uint4 *>(ring + now + 2 * C::kHalf);
-      if (kF8) {
+      if (kF8 && !again) {
         // each lane makes 2^ks and vs of its key's scale bytes (within [27, 247], or 0)
         if (lane < C::kKW) {
           const uint4 w = scales[lane];
@@ -505,8 +511,15 @@ paged_attention_kernel(const Args a) {
         }
         __syncwarp();
       }
+      const bool ragged = key0 + C::kKW > cur.len - a.n_new + 1;
+      // keys that row 8 x + 2 t + j sees, where that matters
+      auto limit = [&](int x, int j) {
+        return cur.len - a.n_new + 1 +
+               (int)quotient((cur.unit % a.row_tiles) * kRows + 8 * x + 2 * t + j, a.group);
+      };
+      float s[kNB][kNR][4], ve[kNB][2], mx[kNR][2], sum[kF8 ? kNR : 1][2];
+      bool refer = false;   // 8 bits: R is to be found
       // ---- scores: MMA row n (n + 8) of block b is key 16 b + key_of(n) (+ 8)
-      float s[kNB][kNR][4];
 #pragma unroll
       for (int b = 0; b < kNB; ++b) {
 #pragma unroll
@@ -540,20 +553,45 @@ paged_attention_kernel(const Args a) {
           }
         }
       }
-      // ---- log2 units, the mask, the running maximum
-      float ve[kNB][2], mx[kNR][2];   // s: u; u - ve: t
-      const bool ragged = key0 + C::kKW > cur.len - a.n_new + 1;
-      // keys that row 8 x + 2 t + j sees, where that matters
-      auto limit = [&](int x, int j) {
-        return cur.len - a.n_new + 1 +
-               (int)quotient((cur.unit % a.row_tiles) * kRows + 8 * x + 2 * t + j, a.group);
+      // ---- log2 units, the mask, the running maximum.  R and what is subtracted from it are
+      // the same rounded score: by an FMA a large one would differ from itself.
+      auto score = [&](float y, float kf, int x, int j) {
+        return __fmul_rn(y * before[x][j] * kf, after[x][j]);
       };
+      if constexpr (kF8) {
+        refer = first || again;
+        if (refer) {
 #pragma unroll
-      for (int x = 0; x < kNR; ++x) mx[x][0] = m[x][0], mx[x][1] = m[x][1];
-      // 8 bits: the weights' sum as well, each lane's relative to its own reference, a score of
-      // before that is close to the largest (within 2^64)
-      float sum[kF8 ? kNR : 1][2];
-      bool far = false;
+          for (int x = 0; x < kNR; ++x)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              // at least the sum so far, so that it starts from 1 at most
+              float top = first ? kLowest : fmaxf(ref[x][j], ref[x][j] + __log2f(l[x][j]));
+#pragma unroll
+              for (int b = 0; b < kNB; ++b)
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                  const int row = 16 * b + 8 * n + key_of<kCh>(g);
+                  const float kf = __uint_as_float(scales[row].x);
+                  if (!ragged || key0 + row < limit(x, j))
+                    top = fmaxf(top, score(s[b][x][2 * n + j], kf, x, j));
+                }
+#pragma unroll
+              for (int d = 4; d < 32; d <<= 1)
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+              if (!first) {
+                l[x][j] *= fast_exp2(ref[x][j] - top);
+                m[x][j] = fmaxf(m[x][j] + (ref[x][j] - top), kLowest);
+              }
+              ref[x][j] = top;
+            }
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < kNR; ++x) {
+        mx[x][0] = m[x][0], mx[x][1] = m[x][1];
+        if constexpr (kF8) sum[x][0] = l[x][0], sum[x][1] = l[x][1];
+      }
       auto weigh = [&](auto masked) {
 #pragma unroll
         for (int b = 0; b < kNB; ++b)
@@ -572,28 +610,23 @@ paged_attention_kernel(const Args a) {
                 const bool seen = !decltype(masked)::value || key0 + row < limit(x, j);
                 float &y = s[b][x][2 * n + j];
                 if constexpr (kF8) {
-                  const float z = y * before[x][j] * kf;
-                  const float w = fmaf(z, after[x][j], -ref[x][j]);
-                  y = seen ? fmaf(z, after[x][j], ve[b][n]) : -INFINITY;
+                  const float w = score(y, kf, x, j) - ref[x][j];
+                  y = seen ? w + ve[b][n] : -INFINITY;
                   sum[x][j] += seen ? fast_exp2(w) : 0.f;
                 } else {
-                  y = seen ? y * a.scale_log2 : -INFINITY;
+                  y = seen ? __fmul_rn(y, a.scale_log2) : -INFINITY;
                 }
                 mx[x][j] = fmaxf(mx[x][j], y);
               }
           }
       };
-      if constexpr (kF8) {
-#pragma unroll
-        for (int x = 0; x < kNR; ++x) sum[x][0] = l[x][0], sum[x][1] = l[x][1];
-      }
       if (!ragged) weigh(std::false_type());
       else weigh(std::true_type());
+      bool moved = false, far = false;
       if constexpr (kF8) {
 #pragma unroll
-        for (int x = 0; x < kNR; ++x) far |= !(sum[x][0] <= kFar && sum[x][1] <= kFar);
+        for (int x = 0; x < kNR; ++x) far |= sum[x][0] > kFar || sum[x][1] > kFar;
       }
-      bool moved = false;
 #pragma unroll
       for (int x = 0; x < kNR; ++x)
 #pragma unroll
@@ -604,6 +637,10 @@ paged_attention_kernel(const Args a) {
           moved |= mx[x][j] != m[x][j];
         }
       if (__any_sync(0xffffffffu, moved || far)) {
+        if (kF8 && !refer && __any_sync(0xffffffffu, far)) {
+          again = true;
+          continue;
+        }
 #pragma unroll
         for (int x = 0; x < kNR; ++x)
 #pragma unroll
@@ -614,30 +651,9 @@ paged_attention_kernel(const Args a) {
 #pragma unroll
             for (int n = 0; n < kMT; ++n) o[n][x][j] *= f, o[n][x][2 + j] *= f;
           }
-        // A unit's first tile and a steep rise: the sum again, from the scores that are still
-        // there, relative to the largest of them and of the sum before (which then counts 1
-        // at most)
-        if (kF8 && __any_sync(0xffffffffu, far)) {
-#pragma unroll
-          for (int x = 0; x < (kF8 ? kNR : 0); ++x)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              float top = fmaxf(ref[x][j], ref[x][j] + __log2f(l[x][j]));
-#pragma unroll
-              for (int b = 0; b < kNB; ++b)
-#pragma unroll
-                for (int n = 0; n < 2; ++n) top = fmaxf(top, s[b][x][2 * n + j] - ve[b][n]);
-              sum[x][j] = l[x][j] * fast_exp2(ref[x][j] - top);
-              ref[x][j] = top;
-#pragma unroll
-              for (int b = 0; b < kNB; ++b)
-#pragma unroll
-                for (int n = 0; n < 2; ++n)
-                  sum[x][j] += fast_exp2(s[b][x][2 * n + j] - ve[b][n] - top);
-            }
-        }
       }
       if constexpr (kF8) {
+        first = again = false;
 #pragma unroll
         for (int x = 0; x < kNR; ++x) l[x][0] = sum[x][0], l[x][1] = sum[x][1];
       }
@@ -768,19 +784,12 @@ paged_attention_kernel(const Args a) {
       for (int x = 0; x < kNR; ++x)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          if constexpr (kF8) {   // one reference for the lanes of a row
-            float top = ref[x][j];
-#pragma unroll
-            for (int d = 4; d < 32; d <<= 1)
-              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-            l[x][j] *= fast_exp2(ref[x][j] - top);
-            if (g == 0) sh_r[warp][8 * x + 2 * t + j] = top;
-          }
 #pragma unroll
           for (int d = 4; d < 32; d <<= 1) l[x][j] += __shfl_xor_sync(0xffffffffu, l[x][j], d);
           if (g == 0) {
             sh_m[warp][8 * x + 2 * t + j] = m[x][j];
             sh_l[warp][8 * x + 2 * t + j] = l[x][j];
+            if constexpr (kF8) sh_r[warp][8 * x + 2 * t + j] = ref[x][j];
           }
         }
       __syncwarp();   // every lane has read the stage
@@ -808,19 +817,23 @@ paged_attention_kernel(const Args a) {
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             const int r = 8 * x + 2 * t + j;
-            M[j] = sh_m[0][r];
-#pragma unroll
-            for (int w = 1; w < kWarps; ++w) M[j] = fmaxf(M[j], sh_m[w][r]);
-            R[j] = M[j];
+            // 8 bits: the warps' M relative to the largest R
+            R[j] = 0.f;
             if constexpr (kF8) {
               R[j] = sh_r[0][r];
 #pragma unroll
               for (int w = 1; w < kWarps; ++w) R[j] = fmaxf(R[j], sh_r[w][r]);
             }
+            auto level = [&](int w) {
+              return kF8 ? sh_r[kF8 ? w : 0][r] - R[j] + sh_m[w][r] : sh_m[w][r];
+            };
+            M[j] = level(0);
+#pragma unroll
+            for (int w = 1; w < kWarps; ++w) M[j] = fmaxf(M[j], level(w));
             sum[j] = 0.f;
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
-              f[j][w] = fast_exp2(sh_m[w][r] - M[j]);
+              f[j][w] = fast_exp2(level(w) - M[j]);
               sum[j] = fmaf(sh_l[w][r], kF8 ? fast_exp2(sh_r[kF8 ? w : 0][r] - R[j]) : f[j][w],
                             sum[j]);
             }
@@ -848,7 +861,7 @@ paged_attention_kernel(const Args a) {
             if (r >= a.rows) continue;
             if (whole) {
               const float inv = sum[j] > 0.f ? 1.f / sum[j] : sum[j] == 0.f ? 0.f : sum[j];
-              const float up = kF8 ? fast_exp2(M[j] - R[j] - kPShift) : 1.f;
+              const float up = kF8 ? fast_exp2(M[j] - kPShift) : 1.f;
               const int i = quotient(r, a.group);
               __nv_bfloat16 *dst = a.out + ((size_t)((size_t)cur.b * a.n_new + i) * a.Hq +
                                             h * (int)a.group.d + (r - i * (int)a.group.d)) * D + d;
@@ -888,7 +901,7 @@ paged_attention_kernel(const Args a) {
       fresh = true;
     }
     now = now + C::kStage == C::kStages * C::kStage ? 0 : now + C::kStage;
-    if (it + 1 < n_tiles) step(a, cur, C::kTile);
+    if (++it < n_tiles) step(a, cur, C::kTile);
   }
   wait_all_but<0>();
   if (threadIdx.x == 0) a.cuts[blockIdx.x] = cut;
@@ -918,18 +931,18 @@ paged_join_kernel(const Args a) {
   const int h = u.unit / a.row_tiles, rr = blockIdx.y, r = (u.unit - h * a.row_tiles) * kRows + rr;
   if (r >= a.rows) return;
   const int sub = threadIdx.x % kL, group = threadIdx.x / kL;
-  // R: what the weights' sum is relative to, in bf16 M itself
+  // in 8 bits L and M are relative to R
   float M = kLowest, R = kLowest, L = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  auto refer = [&](float to, float to_r) {   // M and R rise
-    const float f = fast_exp2(M - to);
-    L *= kF8 ? fast_exp2(R - to_r) : f;
-    M = to;
+  auto level = [&](const float4 &w) { return kF8 ? w.z - R + w.x : w.x; };
+  auto refer = [&](float to_r) {   // R rises
+    if (!kF8) return;
+    L *= fast_exp2(R - to_r);
+    M = fmaxf(M + (R - to_r), kLowest);
     R = to_r;
-    acc.x *= f, acc.y *= f, acc.z *= f, acc.w *= f;
   };
   auto add = [&](const float4 &w, const float4 &x) {
-    const float f = fast_exp2(w.x - M);
+    const float f = fast_exp2(level(w) - M);
     L = fmaf(kF8 ? fast_exp2(w.z - R) : f, w.y, L);
     acc.x = fmaf(f, x.x, acc.x);
     acc.y = fmaf(f, x.y, acc.y);
@@ -955,10 +968,17 @@ paged_join_kernel(const Args a) {
         x[y] = *reinterpret_cast<const float4 *>(part + rr * D + 4 * sub);
       }
     }
-    float to = M, to_r = R;
+    float to_r = R;
 #pragma unroll
-    for (int y = 0; y < kAtOnce; ++y) to = fmaxf(to, w[y].x), to_r = fmaxf(to_r, w[y].z);
-    refer(to, to_r);
+    for (int y = 0; y < kAtOnce; ++y) to_r = fmaxf(to_r, w[y].z);
+    refer(to_r);
+    float to = M;
+#pragma unroll
+    for (int y = 0; y < kAtOnce; ++y) to = fmaxf(to, level(w[y]));
+    const float f0 = fast_exp2(M - to);
+    M = to;
+    if (!kF8) L *= f0;
+    acc.x *= f0, acc.y *= f0, acc.z *= f0, acc.w *= f0;
 #pragma unroll
     for (int y = 0; y < kAtOnce; ++y) add(w[y], x[y]);
   }
@@ -967,13 +987,16 @@ paged_join_kernel(const Args a) {
   __syncthreads();
   if (group) return;
 #pragma unroll
-  for (int y = 0; y < kGroups; ++y) M = fmaxf(M, sh_stat[y].x), R = fmaxf(R, sh_stat[y].z);
+  for (int y = 0; y < kGroups; ++y) R = fmaxf(R, sh_stat[y].z);
+  M = kLowest;
+#pragma unroll
+  for (int y = 0; y < kGroups; ++y) M = fmaxf(M, level(sh_stat[y]));
   L = 0.f;
   acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
   for (int y = 0; y < kGroups; ++y) add(sh_stat[y], sh_o[y * kL + sub]);
   const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;
-  const float up = kF8 ? fast_exp2(M - R - kPShift) : 1.f;
+  const float up = kF8 ? fast_exp2(M - kPShift) : 1.f;
   const int i = quotient(r, a.group);
   reinterpret_cast<uint2 *>(a.out + ((size_t)((size_t)u.b * a.n_new + i) * a.Hq +
                                      h * (int)a.group.d +
@@ -1025,8 +1048,9 @@ int launch(Args &a, void *workspace, cudaStream_t stream) {
   count_launches(2);
   launch_pdl(kernel, dim3((unsigned)grid), dim3(kThreads), C::kSmem, stream, a);
   if (cudaGetLastError() != cudaSuccess) return HSA_ERR_CUDA;
-  launch_pdl(paged_join_kernel<D, kF8, kNR>, dim3((unsigned)grid, (unsigned)std::min(a.rows, C::kRows)),
-             dim3(kJoinThreads), 0, stream, a);
+  launch_pdl(paged_join_kernel<D, kF8, kNR>,
+             dim3((unsigned)grid, (unsigned)std::min(a.rows, C::kRows)), dim3(kJoinThreads), 0,
+             stream, a);
   return launch_status();
 }
 

@@ -1,6 +1,7 @@
 """8-bit paged attention where the weights' sum has far to go: long stretches of zero rows,
-scale bytes as fresh memory holds them, values at the top of the range; and where keys and
-queries differ far in size.  Against the 64-bit reference, within its bounds."""
+scale bytes as fresh memory holds them, values at the top of the range; where keys and queries
+differ far in size; and where scores are very large.  Against the 64-bit reference, within its
+bounds."""
 import numpy as np
 import pytest
 import torch
@@ -156,3 +157,57 @@ def test_keys_and_queries_of_very_different_size(hsa, ek, eq, D):
     k[5], k[77] = 0.0, 0.0                        # scores of exactly zero
     q = (_normal((1, 2, 4, D), 13) * 2.0 ** eq).to(torch.bfloat16)
     _check(hsa, Sequence(k, v), q, scale=D ** -0.5 * 2.0 ** -(ek + eq))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("power", [10, 20, 25, 26, 31, 60, 100])
+def test_scores_of_any_size(hsa, D, sign, power):
+    """Scores are small numbers times 2^power, exactly, so that the keys that share the largest
+    have all the weight, in equal parts, whatever their values' sizes: off by the rounding of
+    probabilities and output and by 2^-20 for the exponentials (2^-22.5) and 32-bit sums."""
+    n, Hq = 2000, 3
+    g = torch.Generator().manual_seed(17)
+    c = torch.randint(1, 8, (n,), generator=g)
+    k = torch.zeros((n, 1, D))
+    k[:, 0, 0] = c * (2.0 ** (power // 2) * sign)
+    v = _normal((n, 1, D), 18) * torch.exp2(torch.randint(-8, 9, (n, 1, 1), generator=g).float())
+    q = torch.zeros((1, 1, Hq, D))
+    q[..., 0] = 2.0 ** (power - power // 2)
+    seq = Sequence(k, v)
+    codes, scales = seq.pool()
+    got = _attend(hsa, q.to(torch.bfloat16), codes, scales, torch.arange(seq.P, dtype=torch.int32)[None],
+                  torch.tensor([n], dtype=torch.int32), 0.6931471805599453)[0, 0]
+    best = seq.held[1][(c * sign == (c * sign).max()), 0]
+    want = best.mean(0)
+    tol = 2.0 ** -8 * want.abs() + (2.0 ** -11 + 2.0 ** -20) * best.abs().mean(0)
+    assert ((got - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("f8", [True, False])
+@pytest.mark.parametrize("power", [12, 30, 50, 90])
+def test_largest_score_takes_all(hsa, f8, D, power):
+    """Scores of any digits times 2^power.  The largest is further from the next than the sums'
+    rounding, so that the output is its value: off by the output's rounding, and by 2^-20 for
+    the exponential and the division."""
+    n, Hq = 2000, 4
+    k, v = _normal((n, 1, D), 19) * 2.0 ** (power // 2), _normal((n, 1, D), 20)
+    q = (_normal((1, 1, Hq, D), 21) * 2.0 ** (power - power // 2)).to(torch.bfloat16)
+    k, v = k.to(torch.bfloat16), v.to(torch.bfloat16)
+    seq = Sequence(k, v)
+    codes, scales = seq.pool()
+    held = seq.held
+    if not f8:
+        held = [k.double(), v.double()]
+        codes = [torch.nn.functional.pad(x, (0, 0, 0, 0, 0, seq.P * PAGE - n)).view(seq.P, PAGE, 1, D).to(DEV)
+                 for x in (k, v)]
+        scales = [None, None]
+    got = _attend(hsa, q, codes, scales, torch.arange(seq.P, dtype=torch.int32)[None],
+                  torch.tensor([n], dtype=torch.int32))[0, 0]
+    s = (q[0, 0].double() @ held[0][:, 0].T) * D ** -0.5
+    top, at = s.topk(2, dim=1)
+    apart = (q[0, 0].double().abs() @ held[0][:, 0].abs().T).amax(1) * D ** -0.5 * (D + 2) * 2.0 ** -23
+    assert ((top[:, 0] - top[:, 1]) > apart + 40).all()
+    want = held[1][at[:, 0], 0]
+    assert ((got - want).abs() <= (2.0 ** -8 + 2.0 ** -20) * want.abs() + 2.0 ** -39 * want.abs().amax()).all()
