@@ -352,8 +352,8 @@ size_t hsa_active_attention_workspace_bytes(int n_active, int N, int H, int D,
  * one bf16 buffer of a layer's size then serves every layer.  An idx entry outside
  * [0, N) leaves its output rows untouched (HSA_ERR_INDEX).
  *
- * Both: D a multiple of 8 up to 256, n * H < 2^31, pointers but the scales 16-byte
- * aligned. */
+ * Both: D a multiple of 8 up to 256, H <= 2^24, n * H < 2^31, pointers but the scales
+ * 16-byte aligned. */
 int hsa_kv_quant_scatter(void *k_cache, void *v_cache, uint8_t *k_scale, uint8_t *v_scale,
                          const void *k_fresh, const void *v_fresh, const int32_t *idx,
                          int n_active, int N, int H, int D, hsa_dtype dtype,
@@ -388,10 +388,13 @@ int hsa_kv_dequant_gather(const void *k_cache, const void *v_cache, const uint8_
  *                aligned, overwritten; calls (and captured graphs) sharing one must
  *                not overlap on the GPU.  Its size depends on D and the device only.
  * D in {64, 128}; Hq < 2^16; page_size a power of two; max_pages * page_size < 2^31 - 256;
- * batch * Hkv * ceil(rows / 8) * max_pages * page_size / 64 < 2^31 with rows = n_new * Hq /
- * Hkv.  A page id outside [0, n_pages) reads as rows of zeros (HSA_ERR_INDEX).  Two launches;
- * the result does not depend on what else runs.  A flat cache of N rows is a cache of
- * ceil(N / page_size) pages with the identity as its table. */
+ * n_pages * page_size < 2^31; batch * Hkv * rows < 2^31 - 256 and batch * Hkv * ceil(rows / 8)
+ * * max_pages * page_size / 64 < 2^31 with rows = n_new * Hq / Hkv.  A page id outside
+ * [0, n_pages) reads as rows of zeros (HSA_ERR_INDEX).  Two launches; the result does not
+ * depend on what else runs.  A flat cache of N rows is a cache of ceil(N / page_size) pages
+ * with the identity as its table.
+ * HSA_E4M3: a key's weight times the power of two of its value row is held to 2^-39 of the
+ * row's largest such product; what lies further below adds nothing to out. */
 int hsa_paged_attention(const void *q, int batch, int n_new, int Hq, const void *k_pages,
                         const void *v_pages, const uint8_t *k_scale, const uint8_t *v_scale,
                         int n_pages, int page_size, int Hkv, int D, hsa_dtype cache_dtype,
@@ -416,8 +419,8 @@ size_t hsa_paged_attention_workspace_bytes(int batch, int n_new, int Hq, int Hkv
  *   cu_q, cu_k   device, int32 [batch + 1], not falling, within [0, total_q] and
  *                [0, total_k]; other values are moved inside and reported
  *                (HSA_ERR_INDEX; what is computed is then unspecified).
- *   total_q,     rows that q and out (k and v) hold; rows before cu[0] or from
- *   total_k      cu[batch] on are neither read nor written.
+ *   total_q,     rows that q and out (k and v) hold; those before cu[0] or from cu[batch]
+ *   total_k      on, whatever they hold, do not reach the result, and are not written.
  *   out          device, bf16 [total_q, Hq, D] compact, written; overlaps no input.
  *   dtype        HSA_BF16.
  *   workspace    device, optional (NULL = none), >=
@@ -425,9 +428,11 @@ size_t hsa_paged_attention_workspace_bytes(int batch, int n_new, int Hq, int Hkv
  *                calls with few rows and long keys be cut along the keys and joined (a
  *                second launch).  Overwritten; calls (and captured graphs) sharing one
  *                must not overlap on the GPU.  Its size depends on D and the device.
- * D in {64, 128}; pointers but cu_q and cu_k 16-byte aligned; Hq * D <= 2^24; batch * Hkv
- * <= 2^23; total_k, total_q * Hq / Hkv and Hkv * (total_q * Hq / Hkv / 256 + batch) < 2^31 -
- * 1024. */
+ * D in {64, 128}; pointers but cu_q and cu_k 16-byte aligned; Hq * D <= 2^24; q_row, k_row,
+ * v_row <= 2^31; batch * Hkv <= 2^23; total_k, total_q * Hq / Hkv and Hkv * (total_q * Hq /
+ * Hkv / 256 + batch) < 2^31 - 1024.  A row that sees a score, scale * <q, k>, of magnitude
+ * 2^30 or more is unspecified.  A NaN or infinity among values that some rows of a block of
+ * 256 see and others do not is slow: those others are formed again, at 4 us a key. */
 int hsa_packed_attention(const void *q, long long q_row, const void *k, long long k_row,
                          const void *v, long long v_row, const int32_t *cu_q,
                          const int32_t *cu_k, int batch, int total_q, int total_k, int Hq,
