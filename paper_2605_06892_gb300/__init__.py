@@ -194,7 +194,7 @@ def _sized(name, t, shape):
 
 
 def _device() -> int:
-    """The current CUDA device; -1, which no tensor is on, where there is none."""
+    """The current CUDA device; -2 where there is none, since a CPU tensor says -1."""
     if _current_device and torch.cuda.is_initialized():
         return _current_device()
     return torch.cuda.current_device() if torch.cuda.is_available() else -2

@@ -22,10 +22,10 @@
 // transposing loads; P^T is transposed on its way by movmatrix.
 //
 // 8-bit cache.  A key's e4m3 codes are exact in fp16, and so is a bf16 query row after
-// scaling by a power of two (its values below 2^-39 of the largest aside), so the
-// products are exact and the key's 2^ks multiplies the score.  The value's 2^vs goes into
-// the probability: with t_j the score in log2 units, R about max t_j, u_j = t_j - R + vs_j
-// and M = max u_j,
+// scaling by a power of two (its values below 2^-31 of the largest aside: those are rounded,
+// by 2^-39 of the largest at most), so the products are exact and the key's 2^ks multiplies
+// the score.  The value's 2^vs goes into the probability: with t_j the score in log2 units, R
+// about max t_j, u_j = t_j - R + vs_j and M = max u_j,
 //   o = 2^M sum_j 2^(u_j - M) code_j / sum_j 2^(t_j - R).
 // No factor 2^(u_j - M) exceeds 1.  The weights' sum has a reference of its own: relative to
 // that of the other sum it would lie between 2^-120 and 2^100 n, since vs does within
@@ -657,7 +657,13 @@ paged_attention_kernel(const Args a) {
 #pragma unroll
         for (int x = 0; x < kNR; ++x) l[x][0] = sum[x][0], l[x][1] = sum[x][1];
       }
-      // ---- probabilities, as the 16 x 8 B operand of O^T += V^T P^T
+      // ---- probabilities, as the 16 x 8 B operand of O^T += V^T P^T.  They are rounded to the
+      // 16 bits that the MMA takes: bf16 beside bf16 values, and fp16 beside 8-bit ones, which
+      // are exact in it and leave the probabilities three bits more.  Each is off by half a
+      // step at most (2^-8 or 2^-11 of itself), up or down, and an output by no more than that
+      // of its row's sum of |p v|; the sum l takes them unrounded, which adds nothing to it.
+      // In fp16 those with u more than 28 below M lose further bits, and more than 39 below
+      // they are zero.
       uint32_t p[kNB][kNR][2];
 #pragma unroll
       for (int b = 0; b < kNB; ++b)

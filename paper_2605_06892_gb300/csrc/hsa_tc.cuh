@@ -257,7 +257,13 @@ struct TcCfg {
 
 // P = 2^(s*scale*log2e - m) for this thread's 128 scores, as bf16 pairs
 // written over the first 64 S columns (all scores are in registers, so P may
-// overwrite S); returns the row sum of the fp32 values.
+// overwrite S); returns the row sum of the fp32 values.  bf16 is what the MMA
+// takes beside bf16 values, and its range lets P stand far above 1 (the fast
+// path below).  Each P is off by 2^-8 of itself at most, up or down, and an
+// output by no more than that of its row's sum of |p v|; the sum takes P
+// unrounded, which adds nothing to it.  The product is exact and m rounded, so
+// a row's P are all off by one factor, 2^(half a step of m), which the division
+// by their sum takes out: for |m| below 2^31 it is 2^64 at most.
 __device__ __forceinline__ float exp_store_tile(uint32_t tS, const uint32_t (&r)[128],
                                                 float sl2, float m) {
   // x = s*scale*log2e - m for a pair of scores in one packed FMA; p = 2^x.
