@@ -25,7 +25,7 @@
 // scaling by a power of two (its values below 2^-31 of the largest aside: those are rounded,
 // by 2^-39 of the largest at most), so the products are exact and the key's 2^ks multiplies
 // the score.  The value's 2^vs goes into the probability: with t_j the score in log2 units, R
-// about max t_j, u_j = t_j - R + vs_j and M = max u_j,
+// within 64 of max t_j, u_j = t_j - R + vs_j and M = max u_j,
 //   o = 2^M sum_j 2^(u_j - M) code_j / sum_j 2^(t_j - R).
 // No factor 2^(u_j - M) exceeds 1.  The weights' sum has a reference of its own: relative to
 // that of the other sum it would lie between 2^-120 and 2^100 n, since vs does within
@@ -188,7 +188,7 @@ struct Args {
   int batch, n_new, Hq, Hkv, rows, row_tiles;   // rows = n_new G
   Divider group;                                // by G = Hq / Hkv
   int n_pages, page_log2, max_pages, sms;
-  float scale_log2;
+  float scale_log2, scale_digits, scale_power;   // the first is the others' product
 };
 
 // What every block of a launch derives from the lengths: the key tiles of all units, cut
@@ -249,6 +249,121 @@ __device__ __forceinline__ void clear_empty(const Args &a) {
     const long long n = (long long)a.n_new * a.Hq * (D / 8);
     uint4 *dst = reinterpret_cast<uint4 *>(a.out) + b * n;
     for (long long i = threadIdx.x; i < n; i += kThreads) dst[i] = make_uint4(0u, 0u, 0u, 0u);
+  }
+}
+
+// The products of a warp's keys of a tile at sk with the query rows: MMA row n (n + 8) of block
+// b is key 16 b + key_of(n) (+ 8).  rows(step, x): this lane's part of column block x.
+template <int D, bool kF8, int kNR, typename Rows>
+__device__ __forceinline__ void score_tile(uint32_t sk, int g, int t,
+                                           float (&s)[Cfg<D, kF8, kNR>::kKW / 16][kNR][4],
+                                           Rows &&rows) {
+  using C = Cfg<D, kF8, kNR>;
+  constexpr int kCh = C::kChunks;
+#pragma unroll
+  for (int b = 0; b < C::kKW / 16; ++b) {
+#pragma unroll
+    for (int x = 0; x < kNR; ++x) s[b][x][0] = s[b][x][1] = s[b][x][2] = s[b][x][3] = 0.f;
+    const int row = 16 * b + key_of<kCh>(g);
+#pragma unroll
+    for (int i = 0; i < kCh / 4; ++i) {
+      const uint32_t at = 16 * k_chunk<kCh>(t + 4 * i, row);   // the same for row + 8
+      const uint4 w0 = lds128(sk + row * C::kRowBytes + at);
+      const uint4 w1 = lds128(sk + (row + 8) * C::kRowBytes + at);
+#pragma unroll
+      for (int e = 0; e < (kF8 ? 4 : 2); ++e) {
+        uint32_t k[4];
+        if (kF8) {
+          k[0] = f16x2_of_e4m3x2(word(w0, e)), k[2] = f16x2_of_e4m3x2(word(w0, e) >> 16);
+          k[1] = f16x2_of_e4m3x2(word(w1, e)), k[3] = f16x2_of_e4m3x2(word(w1, e) >> 16);
+        } else {
+          k[0] = word(w0, 2 * e), k[2] = word(w0, 2 * e + 1);
+          k[1] = word(w1, 2 * e), k[3] = word(w1, 2 * e + 1);
+        }
+#pragma unroll
+        for (int x = 0; x < kNR; ++x) {
+          const uint2 q = rows((kF8 ? 4 : 2) * i + e, x);
+          mma<kF8>(s[b][x], k, q.x, q.y);
+        }
+      }
+    }
+  }
+}
+
+__device__ __forceinline__ uint64_t both(float lo, float hi) {
+  return pack2(__float_as_uint(lo), __float_as_uint(hi));
+}
+
+// 8 bits: the products of two rows with one key times the query rows' power of two (where it
+// is below 1) and the key's, w = (kf, kf, vs, vs).  Only the key's factor holds digits, the
+// scale's, so that a score is rounded here and the powers of two after it are exact: R, one of
+// the scores, and the scores inside the FMA that subtracts it are the same numbers.  (A product
+// rounded as it is subtracted would differ from itself, by a half step of it.)
+__device__ __forceinline__ uint64_t product8(const float (&y)[4], int n, const float (&before)[2],
+                                             const uint4 &w) {
+  return mul2(mul2(both(y[2 * n], y[2 * n + 1]), both(before[0], before[1])), pack2(w.x, w.y));
+}
+
+// 8 bits: R is zero to begin with.  Where scores are beyond +-64 of it, so that a lane's sum
+// leaves the range that holds all that counts, the warp takes the tile again, here, against the
+// largest score so far.
+template <int D, int kNR>
+struct Tile8 {
+  uint2 q[D / 16][kNR];
+  float before[kNR][2], after[kNR][2];
+  int limit[kNR][2];                            // keys of the tile that a row sees
+  float ref[kNR][2], l[kNR][2], m[kNR][2];      // those before the tile; then the new R, l with
+  float s[2][kNR][4], mx[kNR][2];               // the tile's, the old m relative to R, u
+};
+template <int D, int kNR>
+__device__ __noinline__ void take_again(Tile8<D, kNR> &z, uint32_t sk, const uint4 *scales,
+                                        bool first) {
+  using C = Cfg<D, true, kNR>;
+  constexpr int kCh = C::kChunks;
+  static_assert(C::kKW == 32, "two blocks of 16 keys");
+  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  score_tile<D, true, kNR>(sk, g, t, z.s, [&](int step, int x) { return z.q[step][x]; });
+#pragma unroll 1
+  for (int x = 0; x < kNR; ++x) {
+    uint64_t score[4];
+    float top[2], l[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)   // at least the sum so far, which is then 1 at most
+      top[j] = first ? kLowest : fmaxf(z.ref[x][j], z.ref[x][j] + __log2f(z.l[x][j]));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = 8 * i + key_of<kCh>(g);
+      score[i] = mul2(product8(z.s[i >> 1][x], i & 1, z.before[x], scales[row]),
+                      both(z.after[x][0], z.after[x][1]));
+      if (row < z.limit[x][0]) top[0] = fmaxf(top[0], lo_f(score[i]));
+      if (row < z.limit[x][1]) top[1] = fmaxf(top[1], hi_f(score[i]));
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+#pragma unroll
+      for (int d = 4; d < 32; d <<= 1)
+        top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], d));
+      const float down = z.ref[x][j] - top[j];
+      l[j] = first ? 0.f : z.l[x][j] * fast_exp2(down);
+      z.m[x][j] = first ? kLowest : fmaxf(z.m[x][j] + down, kLowest);
+      z.mx[x][j] = z.m[x][j];
+      z.ref[x][j] = top[j];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = 8 * i + key_of<kCh>(g);
+      const float ve = __uint_as_float(scales[row].z);
+      const float d[2] = {lo_f(score[i]) - top[0], hi_f(score[i]) - top[1]};
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const bool seen = row < z.limit[x][j];
+        const float u = seen ? d[j] + ve : -INFINITY;
+        if (seen) l[j] += fast_exp2(d[j]);
+        z.s[i >> 1][x][2 * (i & 1) + j] = u;
+        z.mx[x][j] = fmaxf(z.mx[x][j], u);
+      }
+    }
+    z.l[x][0] = l[0], z.l[x][1] = l[1];
   }
 }
 
@@ -420,23 +535,20 @@ paged_attention_kernel(const Args a) {
   constexpr bool kLean = C::kLean;
   uint32_t qf[kLean ? 1 : kSteps][kNR][2];
   float o[kMT][kNR][4], m[kNR][2], l[kNR][2];
-  // 8 bits: a query row's power of two and the scale, in two factors, and its R
+  // 8 bits: a query row's power of two times the scale's, in two factors, and its R; rows 2 t
+  // and 2 t + 1 go together through packed instructions
   float before[kF8 ? kNR : 1][2], after[kF8 ? kNR : 1][2], ref[kF8 ? kNR : 1][2];
   uint32_t sq_now = 0;   // kLean: the unit's rows
   int unit_tile0 = 0;    // the unit's tile that this run of it starts with
   bool fresh = true, first_unit = true;
-  // 8 bits: R is the largest score of the warp's first tile of the unit; where one rises 2^64
-  // above it later, that tile is taken again against a new one.
-  bool first = true, again = false;
+  bool first = true;     // this warp has none of the unit's keys yet
   uint32_t now = 0;      // the stage of tile `it`
 
-  for (int it = 0; it < n_tiles;) {
-    if (!kF8 || !again) {
-      wait_all_but<C::kStages - 2>();
-      if (fresh) __syncthreads();   // the query rows are every thread's copies
-      else __syncwarp();
-      load_tile();
-    }
+  for (int it = 0; it < n_tiles; ++it) {
+    wait_all_but<C::kStages - 2>();
+    if (fresh) __syncthreads();   // the query rows are every thread's copies
+    else __syncwarp();
+    load_tile();
 
     if (fresh) {
       fresh = false;
@@ -482,13 +594,13 @@ paged_attention_kernel(const Args a) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           if (kF8) {
-            // A product y stands for y 2^ks 2^c: multiplied in this order, with 2^c first
-            // where it is below 1 and last else, it overflows only where the score does,
-            // whatever the keys' size.
+            // A product y stands for y 2^ks c, c a power of two: multiplied in this order, with
+            // c first where it is below 1 and last else, it overflows only where the product of
+            // query and key does, whatever their sizes.
             const float c = __shfl_sync(0xffffffffu, scale, 4 * (2 * t + j));
             before[kF8 ? x : 0][j] = fminf(c, 1.f);
-            after[kF8 ? x : 0][j] = fminf(fmaxf(c, 1.f) * a.scale_log2, 3.4e38f);
-            ref[kF8 ? x : 0][j] = kLowest;
+            after[kF8 ? x : 0][j] = fminf(fmaxf(c, 1.f) * a.scale_power, 0x1p127f);
+            ref[kF8 ? x : 0][j] = 0.f;
           }
           m[x][j] = kLowest;
           l[x][j] = 0.f;
@@ -502,12 +614,15 @@ paged_attention_kernel(const Args a) {
     if (key0 < cur.len) {
       const uint32_t sk = ring_s + now, sv = sk + C::kHalf;
       uint4 *scales = reinterpret_cast<uint4 *>(ring + now + 2 * C::kHalf);
-      if (kF8 && !again) {
-        // each lane makes 2^ks and vs of its key's scale bytes (within [27, 247], or 0)
+      if (kF8) {
+        // each lane makes 2^ks, times the scale's digits, and vs of its key's scale bytes
+        // (within [27, 247], or 0), each twice
         if (lane < C::kKW) {
           const uint4 w = scales[lane];
           const uint32_t ks = w.x >> (w.z & 0xffffu) & 255u, vs = w.y >> (w.z >> 16) & 255u;
-          scales[lane] = make_uint4(ks << 23, __float_as_uint((float)((int)vs - 127)), 0u, 0u);
+          const uint32_t ve = __float_as_uint((float)((int)vs - 127));
+          const uint32_t kf = __float_as_uint(__uint_as_float(ks << 23) * a.scale_digits);
+          scales[lane] = make_uint4(kf, kf, ve, ve);
         }
         __syncwarp();
       }
@@ -517,76 +632,16 @@ paged_attention_kernel(const Args a) {
         return cur.len - a.n_new + 1 +
                (int)quotient((cur.unit % a.row_tiles) * kRows + 8 * x + 2 * t + j, a.group);
       };
-      float s[kNB][kNR][4], ve[kNB][2], mx[kNR][2], sum[kF8 ? kNR : 1][2];
-      bool refer = false;   // 8 bits: R is to be found
-      // ---- scores: MMA row n (n + 8) of block b is key 16 b + key_of(n) (+ 8)
-#pragma unroll
-      for (int b = 0; b < kNB; ++b) {
-#pragma unroll
-        for (int x = 0; x < kNR; ++x) s[b][x][0] = s[b][x][1] = s[b][x][2] = s[b][x][3] = 0.f;
-        const int row = 16 * b + key_of<kCh>(g);
-#pragma unroll
-        for (int i = 0; i < kCh / 4; ++i) {
-          const uint32_t at = 16 * k_chunk<kCh>(t + 4 * i, row);   // the same for row + 8
-          const uint4 w0 = lds128(sk + row * C::kRowBytes + at);
-          const uint4 w1 = lds128(sk + (row + 8) * C::kRowBytes + at);
-#pragma unroll
-          for (int e = 0; e < (kF8 ? 4 : 2); ++e) {
-            const int step = (kF8 ? 4 : 2) * i + e;
-            uint32_t k[4];
-            if (kF8) {
-              k[0] = f16x2_of_e4m3x2(word(w0, e)), k[2] = f16x2_of_e4m3x2(word(w0, e) >> 16);
-              k[1] = f16x2_of_e4m3x2(word(w1, e)), k[3] = f16x2_of_e4m3x2(word(w1, e) >> 16);
-            } else {
-              k[0] = word(w0, 2 * e), k[2] = word(w0, 2 * e + 1);
-              k[1] = word(w1, 2 * e), k[3] = word(w1, 2 * e + 1);
-            }
-#pragma unroll
-            for (int x = 0; x < kNR; ++x) {
-              if constexpr (kLean) {
-                const uint2 w = lds64(sq_now + query_place<D, kF8>(8 * x + g, step, t));
-                mma<kF8>(s[b][x], k, w.x, w.y);
-              } else {
-                mma<kF8>(s[b][x], k, qf[step][x][0], qf[step][x][1]);
-              }
-            }
-          }
-        }
-      }
-      // ---- log2 units, the mask, the running maximum.  R and what is subtracted from it are
-      // the same rounded score: by an FMA a large one would differ from itself.
-      auto score = [&](float y, float kf, int x, int j) {
-        return __fmul_rn(y * before[x][j] * kf, after[x][j]);
-      };
-      if constexpr (kF8) {
-        refer = first || again;
-        if (refer) {
-#pragma unroll
-          for (int x = 0; x < kNR; ++x)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              // at least the sum so far, so that it starts from 1 at most
-              float top = first ? kLowest : fmaxf(ref[x][j], ref[x][j] + __log2f(l[x][j]));
-#pragma unroll
-              for (int b = 0; b < kNB; ++b)
-#pragma unroll
-                for (int n = 0; n < 2; ++n) {
-                  const int row = 16 * b + 8 * n + key_of<kCh>(g);
-                  const float kf = __uint_as_float(scales[row].x);
-                  if (!ragged || key0 + row < limit(x, j))
-                    top = fmaxf(top, score(s[b][x][2 * n + j], kf, x, j));
-                }
-#pragma unroll
-              for (int d = 4; d < 32; d <<= 1)
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-              if (!first) {
-                l[x][j] *= fast_exp2(ref[x][j] - top);
-                m[x][j] = fmaxf(m[x][j] + (ref[x][j] - top), kLowest);
-              }
-              ref[x][j] = top;
-            }
-        }
-      }
+      float s[kNB][kNR][4], mx[kNR][2], sum[kF8 ? kNR : 1][2];
+      if constexpr (kLean)
+        score_tile<D, kF8, kNR>(sk, g, t, s, [&](int step, int x) {
+          return lds64(sq_now + query_place<D, kF8>(8 * x + g, step, t));
+        });
+      else
+        score_tile<D, kF8, kNR>(sk, g, t, s, [&](int step, int x) {
+          return make_uint2(qf[step][x][0], qf[step][x][1]);
+        });
+      // ---- log2 units, the mask, the running maximum; in 8 bits the weights' sum as well
 #pragma unroll
       for (int x = 0; x < kNR; ++x) {
         mx[x][0] = m[x][0], mx[x][1] = m[x][1];
@@ -598,35 +653,83 @@ paged_attention_kernel(const Args a) {
 #pragma unroll
           for (int n = 0; n < 2; ++n) {
             const int row = 16 * b + 8 * n + key_of<kCh>(g);
-            float kf = 1.f;
-            if (kF8) {
+            if constexpr (kF8) {
               const uint4 w = scales[row];
-              kf = __uint_as_float(w.x), ve[b][n] = __uint_as_float(w.y);
-            }
 #pragma unroll
-            for (int x = 0; x < kNR; ++x)
-#pragma unroll
-              for (int j = 0; j < 2; ++j) {
-                const bool seen = !decltype(masked)::value || key0 + row < limit(x, j);
-                float &y = s[b][x][2 * n + j];
-                if constexpr (kF8) {
-                  const float w = score(y, kf, x, j) - ref[x][j];
-                  y = seen ? w + ve[b][n] : -INFINITY;
-                  sum[x][j] += seen ? fast_exp2(w) : 0.f;
-                } else {
-                  y = seen ? __fmul_rn(y, a.scale_log2) : -INFINITY;
+              for (int x = 0; x < kNR; ++x) {
+                const uint64_t z =
+                    fma2(product8(s[b][x], n, before[x], w), both(after[x][0], after[x][1]),
+                         both(-ref[x][0], -ref[x][1]));
+                const uint64_t u = add2(z, pack2(w.z, w.w));
+                float &y0 = s[b][x][2 * n], &y1 = s[b][x][2 * n + 1];
+                float e0 = fast_exp2(lo_f(z)), e1 = fast_exp2(hi_f(z));
+                y0 = lo_f(u), y1 = hi_f(u);
+                if (decltype(masked)::value) {
+                  if (key0 + row >= limit(x, 0)) y0 = -INFINITY, e0 = 0.f;
+                  if (key0 + row >= limit(x, 1)) y1 = -INFINITY, e1 = 0.f;
                 }
-                mx[x][j] = fmaxf(mx[x][j], y);
+                const uint64_t w2 = add2(both(sum[x][0], sum[x][1]), both(e0, e1));
+                sum[x][0] = lo_f(w2), sum[x][1] = hi_f(w2);
+                mx[x][0] = fmaxf(mx[x][0], y0), mx[x][1] = fmaxf(mx[x][1], y1);
               }
+            } else {
+#pragma unroll
+              for (int x = 0; x < kNR; ++x)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                  const bool seen = !decltype(masked)::value || key0 + row < limit(x, j);
+                  float &y = s[b][x][2 * n + j];
+                  y = seen ? __fmul_rn(y, a.scale_log2) : -INFINITY;
+                  mx[x][j] = fmaxf(mx[x][j], y);
+                }
+            }
           }
       };
       if (!ragged) weigh(std::false_type());
       else weigh(std::true_type());
-      bool moved = false, far = false;
       if constexpr (kF8) {
+        // Out of line, so that what is rare costs the usual path no registers.
+        float most = 0.f;
 #pragma unroll
-        for (int x = 0; x < kNR; ++x) far |= sum[x][0] > kFar || sum[x][1] > kFar;
+        for (int x = 0; x < kNR; ++x) most = max3f(most, sum[x][0], sum[x][1]);
+        bool far = most > kFar;
+        if (first) {
+#pragma unroll
+          for (int x = 0; x < kNR; ++x)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) far |= sum[x][j] < 1.f / kFar && mx[x][j] > kLowest;
+        }
+        if (__any_sync(0xffffffffu, far)) {
+          Tile8<D, kNR> z;
+#pragma unroll
+          for (int x = 0; x < kNR; ++x) {
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i)
+              z.q[i][x] = make_uint2(qf[kLean ? 0 : i][x][0], qf[kLean ? 0 : i][x][1]);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              z.before[x][j] = before[x][j], z.after[x][j] = after[x][j];
+              z.limit[x][j] = ragged ? limit(x, j) - key0 : C::kKW;
+              z.ref[x][j] = ref[x][j], z.l[x][j] = l[x][j], z.m[x][j] = m[x][j];
+            }
+          }
+          take_again<D, kNR>(z, sk, scales, first);
+#pragma unroll
+          for (int x = 0; x < kNR; ++x) {
+#pragma unroll
+            for (int b = 0; b < kNB; ++b)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) s[b][x][i] = z.s[b][x][i];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              ref[x][j] = z.ref[x][j], sum[x][j] = z.l[x][j];
+              m[x][j] = z.m[x][j], mx[x][j] = z.mx[x][j];
+            }
+          }
+        }
+        first = false;
       }
+      bool moved = false;
 #pragma unroll
       for (int x = 0; x < kNR; ++x)
 #pragma unroll
@@ -636,11 +739,7 @@ paged_attention_kernel(const Args a) {
             mx[x][j] = fmaxf(mx[x][j], __shfl_xor_sync(0xffffffffu, mx[x][j], d));
           moved |= mx[x][j] != m[x][j];
         }
-      if (__any_sync(0xffffffffu, moved || far)) {
-        if (kF8 && !refer && __any_sync(0xffffffffu, far)) {
-          again = true;
-          continue;
-        }
+      if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
         for (int x = 0; x < kNR; ++x)
 #pragma unroll
@@ -653,7 +752,6 @@ paged_attention_kernel(const Args a) {
           }
       }
       if constexpr (kF8) {
-        first = again = false;
 #pragma unroll
         for (int x = 0; x < kNR; ++x) l[x][0] = sum[x][0], l[x][1] = sum[x][1];
       }
@@ -672,10 +770,16 @@ paged_attention_kernel(const Args a) {
 #pragma unroll
           for (int n = 0; n < 2; ++n) {
             float y[2];
+            if constexpr (kF8) {
+              const uint64_t z = add2(both(s[b][x][2 * n], s[b][x][2 * n + 1]),
+                                      both(kPShift - m[x][0], kPShift - m[x][1]));
+              y[0] = fast_exp2(lo_f(z)), y[1] = fast_exp2(hi_f(z));
+            } else {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              y[j] = fast_exp2(s[b][x][2 * n + j] - (kF8 ? m[x][j] - kPShift : m[x][j]));
-              if (!kF8) l[x][j] += y[j];
+              for (int j = 0; j < 2; ++j) {
+                y[j] = fast_exp2(s[b][x][2 * n + j] - m[x][j]);
+                l[x][j] += y[j];
+              }
             }
             p[b][x][n] = transposed(kF8 ? pack_f16(y[0], y[1]) : pack_bf16(y[0], y[1]));
           }
@@ -795,7 +899,7 @@ paged_attention_kernel(const Args a) {
           if (g == 0) {
             sh_m[warp][8 * x + 2 * t + j] = m[x][j];
             sh_l[warp][8 * x + 2 * t + j] = l[x][j];
-            if constexpr (kF8) sh_r[warp][8 * x + 2 * t + j] = ref[x][j];
+            if constexpr (kF8) sh_r[warp][8 * x + 2 * t + j] = l[x][j] == 0.f ? kLowest : ref[x][j];
           }
         }
       __syncwarp();   // every lane has read the stage
@@ -907,7 +1011,7 @@ paged_attention_kernel(const Args a) {
       fresh = true;
     }
     now = now + C::kStage == C::kStages * C::kStage ? 0 : now + C::kStage;
-    if (++it < n_tiles) step(a, cur, C::kTile);
+    if (it + 1 < n_tiles) step(a, cur, C::kTile);
   }
   wait_all_but<0>();
   if (threadIdx.x == 0) a.cuts[blockIdx.x] = cut;
@@ -1140,6 +1244,9 @@ extern "C" int hsa_paged_attention(const void *q, int batch, int n_new, int Hq, 
   a.page_log2 = 0;
   while ((1 << a.page_log2) < page_size) ++a.page_log2;
   a.scale_log2 = scale * 1.4426950408889634f;
+  int power = 0;
+  a.scale_digits = 2.f * std::frexp(std::min(a.scale_log2, 3.4e38f), &power);   // in [1, 2)
+  a.scale_power = std::ldexp(1.f, power - 1);
   cudaStream_t s = (cudaStream_t)stream;
   if (f8)
     return D == 128 ? launch_rows<128, true>(a, workspace, s)
