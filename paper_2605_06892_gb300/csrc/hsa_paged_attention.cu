@@ -1168,8 +1168,9 @@ int launch(Args &a, void *workspace, cudaStream_t stream) {
 // Further units read the keys again, from L2, and by then the products bound the time: a
 // unit of four blocks takes 1.6 to 1.7 times one of two (4 sequences of 9000 to 30000 keys,
 // 8 K/V heads: 24 rows 48 against 57 us at D = 64, 82 against 99 at D = 128; 40 rows 77
-// against 75, 143 against 135).  8-bit keys at D = 128 leave it too few registers (24 rows
-// 84 against 73 us).
+// against 75, 143 against 135; 24 rows at D = 64 in 8 bits 55 against 66).  8-bit keys at
+// D = 128 leave it too few registers (24 rows, with the sum of the weights relative to the
+// probabilities' maximum, 84 against 73 us).
 template <int D, bool kF8>
 int launch_rows(Args &a, void *workspace, cudaStream_t stream) {
   if (a.rows <= 8) return launch<D, kF8, 1>(a, workspace, stream);
