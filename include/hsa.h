@@ -432,7 +432,8 @@ size_t hsa_paged_attention_workspace_bytes(int batch, int n_new, int Hq, int Hkv
  * v_row <= 2^31; batch * Hkv <= 2^23; total_k, total_q * Hq / Hkv and Hkv * (total_q * Hq /
  * Hkv / 256 + batch) < 2^31 - 1024.  A row that sees a score, scale * <q, k>, of magnitude
  * 2^30 or more is unspecified.  A NaN or infinity among values that some rows of a block of
- * 256 see and others do not is slow: those others are formed again, at 4 us a key. */
+ * 256 see and others do not is slow: those others are formed again, at 4 us a key, but where
+ * they see NaN in the same dimensions themselves. */
 int hsa_packed_attention(const void *q, long long q_row, const void *k, long long k_row,
                          const void *v, long long v_row, const int32_t *cu_q,
                          const int32_t *cu_k, int batch, int total_q, int total_k, int Hq,

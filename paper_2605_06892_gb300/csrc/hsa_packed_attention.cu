@@ -337,10 +337,31 @@ __device__ __forceinline__ int sum_place(int r, int x) {
   return (((r >> 5) * 2 + x / kV) * 32 + (r & 31)) * kV + ((y & ~7) | ((y ^ r) & 7));
 }
 
+// A row of V's elements that are not finite (kNan: that are NaN), a bit each.
+template <int D, bool kNan>
+__device__ __forceinline__ void odd_elements(const __nv_bfloat16 *v, uint32_t (&bits)[D / 32]) {
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint4 w = __ldg(reinterpret_cast<const uint4 *>(v + 32 * c + 8 * i));
+      const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t lo = x[e] << 16 & 0x7fff0000u, hi = x[e] & 0x7fff0000u;
+        constexpr uint32_t kFrom = kNan ? 0x7f810000u : 0x7f800000u;
+        bits[c] |= (uint32_t)(lo >= kFrom) << (8 * i + 2 * e);
+        bits[c] |= (uint32_t)(hi >= kFrom) << (8 * i + 2 * e + 1);
+      }
+    }
+}
+
 // Forms and stores those of this warp's rows again (r: this lane's) whose sums took in a
 // masked value that is not finite: the softmax over the row's own keys of the unit or piece,
 // on the CUDA cores, 32 keys at a time by way of `st`, 64 D bytes of the warp's own.  Rare and
-// slow (4 us a key); out of line so that it costs the usual path no registers.
+// slow (4 us a key); out of line so that it costs the usual path no registers.  A row stays as
+// it is where one of its own last keys has NaN in each dimension that a masked value spoils:
+// it is NaN there in any case, and so values that are NaN throughout cost no more than a look.
 template <int D>
 __device__ __noinline__ void form_again(const PackedArgs &a, const Unit &u, int r, uint4 *st) {
   const int lane = threadIdx.x & 31;
@@ -354,14 +375,22 @@ __device__ __noinline__ void form_again(const PackedArgs &a, const Unit &u, int 
   const __nv_bfloat16 *Q = a.q + (size_t)(u.seq.q0 + tok) * a.q_row +
                            (u.head * (int)a.group.d + (valid ? R - tok * (int)a.group.d : 0)) * D;
   bool bad = false;
-  if (valid)
-    for (int j = max(limit, k0); j < k1 && !bad; ++j)
-      for (int d = 0; d < D; d += 8) {
-        const uint4 w = __ldg(reinterpret_cast<const uint4 *>(V + (size_t)j * a.v_row + d));
-        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-        for (int i = 0; i < 4; ++i)
-          bad |= (x[i] & 0x7f80u) == 0x7f80u || (x[i] & 0x7f800000u) == 0x7f800000u;
-      }
+  if (valid) {
+    uint32_t spoilt[D / 32] = {}, own[D / 32] = {};
+    auto left = [&]() {
+      uint32_t any = 0;
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) any |= spoilt[c] & ~own[c];
+      return any != 0;
+    };
+    for (int j = max(limit, k0); j < k1; ++j)
+      odd_elements<D, false>(V + (size_t)j * a.v_row, spoilt);
+    bad = left();
+    for (int j = min(limit, k1) - 1, n = 0; j >= k0 && n < 32 && bad; --j, ++n) {
+      odd_elements<D, true>(V + (size_t)j * a.v_row, own);
+      bad = left();
+    }
+  }
   const int end = bad ? min(limit, k1) : 0;
   const int most = __reduce_max_sync(0xffffffffu, end);
   if (!__any_sync(0xffffffffu, bad)) return;
