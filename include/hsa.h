@@ -45,8 +45,10 @@ typedef struct CUstream_st *hsa_stream_t;
 typedef enum {
     HSA_BF16 = 0,   /* bfloat16 storage, fp32 accumulation */
     HSA_F32 = 1,    /* fp32 storage and arithmetic */
-    HSA_E4M3 = 2    /* 8-bit KV cache: e4m3 codes with one power of two per row; only where
+    HSA_E4M3 = 2,   /* 8-bit KV cache: e4m3 codes with one power of two per row; only where
                        a call names it */
+    HSA_E2M1 = 3    /* 4-bit KV cache: e2m1 codes with a word per row; only where a call
+                       names it */
 } hsa_dtype;
 
 typedef enum {
@@ -363,6 +365,119 @@ int hsa_kv_dequant_gather(const void *k_cache, const void *v_cache, const uint8_
                           const uint8_t *v_scale, const int32_t *idx, int n, int N, int H,
                           int D, void *k_out, void *v_out, hsa_dtype dtype,
                           hsa_stream_t stream);
+
+/* ------------------------------------------------- the KV cache in 4 bits */
+
+/* A KV cache of N rows of H heads x D values in 4 bits a value and a word a row; D is 64
+ * or 128.  The row of one token and head is held as D e2m1 codes (OCP 4-bit floating
+ * point: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives), dimension 2i in the low half of
+ * byte i, and a 32-bit word: factors m_0 .. m_3 of six bits each from the lowest bit on,
+ * and a byte s above them.  Dimension d is of group (d / (D/32)) mod 4 and stands for
+ * code * m_group * 2^(s - 127):
+ *   codes   [N, H, D/2] bytes;   words  [N, H], 4-byte aligned.
+ * Written from values x: with A the largest |x_d| of the row, e is the least integer with
+ * A <= 378 * 2^e, at least -100; s = e + 127; with a_g the largest |x_d| of group g,
+ * m_g = ceil(a_g / (6 * 2^e)); codes are x / (m_g * 2^e) rounded to nearest, ties to even
+ * (a zero may have either sign).  The values held are exact in bf16 and fp32.  A magnitude
+ * above 252 * 2^120 counts as that.  A row with a NaN or infinite element is held as NaN
+ * throughout (s = 255) and reported (HSA_ERR_NONFINITE).
+ *
+ * hsa_kv4_quant_scatter, hsa_kv4_dequant_gather: as hsa_kv_quant_scatter and
+ * hsa_kv_dequant_gather (the same arguments otherwise, caches in pages and the rotation of K
+ * included), but
+ *   k_row,       elements from one fresh token's row to the next: H * D where they are
+ *   v_row        compact, more in a fused projection's output; multiples of 16 bytes, at
+ *                most 2^31.
+ *   idx          -1 is a place that holds no token: its row is skipped, and not reported.
+ * Both: H <= 2^24, n * H < 2^31, pointers but the words 16-byte aligned. */
+int hsa_kv4_quant_scatter(void *k_cache, void *v_cache, uint32_t *k_scale, uint32_t *v_scale,
+                          const void *k_fresh, long long k_row, const void *v_fresh,
+                          long long v_row, const int32_t *idx, int n_active, int N, int H, int D,
+                          hsa_dtype dtype, const float *table, const int32_t *table_idx,
+                          int table_rows, hsa_stream_t stream);
+int hsa_kv4_dequant_gather(const void *k_cache, const void *v_cache, const uint32_t *k_scale,
+                           const uint32_t *v_scale, const int32_t *idx, int n, int N, int H,
+                           int D, void *k_out, void *v_out, hsa_dtype dtype,
+                           hsa_stream_t stream);
+
+/* ------------------------------------- queries and keys normed and rotated */
+
+/* The active rows' queries and keys on their way into the attention, and K and V into the
+ * cache, in one launch: for q (weights q_weight) and k (k_weight)
+ *   y = x / sqrt(mean(x^2) + eps) * weight,
+ * the mean over each head's D values (across == 0) or over all of the token's heads
+ * (across != 0), then, with a table, each pair (y0, y1) of a head becomes (y0 c - y1 s,
+ * y0 s + y1 c) by row t of the table (hsa_rope_table), t = table_idx[j] for row j, or
+ * k_idx[j] where table_idx is NULL, or j where both are.  32-bit arithmetic, rounded once to
+ * dtype.  v is copied.
+ *   q, k, v       device, token rows of Hq (Hkv, Hkv) heads x D values of dtype (HSA_BF16 or
+ *                 HSA_F32), q_row (k_row, v_row) elements from one token to the next: Hq * D
+ *                 where they are compact, more in a fused projection's output; multiples of
+ *                 16 bytes, at most 2^31.  v may be NULL, with v_out.
+ *   q_weight,     device, fp32 [D], or with `across` [Hq, D] ([Hkv, D]); NULL: ones.
+ *   k_weight
+ *   eps           at least 1e-30.
+ *   table         device, fp32 [table_rows, D/2, 2] or NULL: no rotation.  table_idx needs one.
+ *   q_out         device, [n, Hq, D] compact, written; may be q where q is compact.
+ *   k_out, v_out  device, written: [n, Hkv, D] compact (may be k and v where those are), or
+ *                 with k_idx [k_rows, Hkv, D]: row k_idx[j] takes row j, others stay as they
+ *                 are.  A cache in pages [n_pages, page, Hkv, D] has n_pages * page rows.
+ *   k_idx         device, int32 [n], distinct values in [0, k_rows), or NULL.
+ * -1 in k_idx is a place that holds no token: its K and V are skipped, and its q too where
+ * its table row is that; so is all of a row whose table_idx is -1.  Other values out of
+ * range skip the same and are reported (HSA_ERR_INDEX).
+ * D a multiple of 8 up to 256; Hq, Hkv <= 2^20; with `across` max(Hq, Hkv) * D <= 32768; n
+ * times max(1, the heads of q, k and v) < 2^31; pointers but the indices 16-byte aligned. */
+int hsa_qk_norm_rope(const void *q, long long q_row, const void *k, long long k_row,
+                     const void *v, long long v_row, const float *q_weight,
+                     const float *k_weight, float eps, int across, const float *table,
+                     const int32_t *table_idx, int table_rows, int n, int Hq, int Hkv, int D,
+                     hsa_dtype dtype, void *q_out, void *k_out, void *v_out,
+                     const int32_t *k_idx, int k_rows, hsa_stream_t stream);
+
+/* ------------------------------------------------------ pages and places */
+
+/* The bookkeeping of caches in pages before a step of several sequences: sequence b has
+ * lens[b] tokens in the cache and shall have want[b].  With H = ceil(lens[b] / page_size)
+ * pages before and W = ceil(want[b] / page_size) after:
+ *   - Where W < H (tokens withdrawn, or a sequence ended: want[b] = 0) pages W .. H-1 of
+ *     page_table[b] go onto the stack of free pages, in the order of b and page.
+ *   - After that sequences grow, in the order of b, while pages and places last: b grows if
+ *     W == H or the pages that the growing sequences up to and with b ask for are there, and
+ *     if their new tokens number at most max_new.  What does not grow keeps lens[b] and gets
+ *     no tokens; lens_out tells.  page_table[b] H .. W-1 take the pages from the stack's top.
+ *   lens, want    device, int32 [batch], in [0, max_pages * page_size]; a value outside is
+ *                 taken as the nearer end and reported (HSA_ERR_INDEX).
+ *   page_table    device, int32 [batch, max_pages], updated in place, as
+ *                 hsa_paged_attention reads it.  Entries past a sequence's last page are not
+ *                 read, and stay as they are.
+ *   free_pages    device, int32 [n_pages], updated in place: the first n_free[0] are the
+ *                 stack, its top the last of them.  An id outside [0, n_pages) that is taken
+ *                 or given back, or more given back than there is room for, is reported
+ *                 (HSA_ERR_INDEX).
+ *   n_free        device, int32 [1];  n_free_out  device, int32 [1], written.
+ *   lens_out      device, int32 [batch], written: the new lengths.
+ *   cu_q          device, int32 [batch + 1], written: the new tokens before sequence b (as
+ *                 hsa_packed_attention takes it).
+ *   slots,        device, int32 [max_new], written: for new token i of sequence b, in element
+ *   positions     cu_q[b] + i, its row in the cache, page id * page_size + place in the page
+ *                 (as the scatter calls' idx), and its position lens[b] + i (as their
+ *                 table_idx).  -1 in the elements from cu_q[batch] on.
+ *   cu_k          device, int32 [batch + 1] or NULL, written: the tokens of lens_out before b.
+ *   key_rows      device, int32 [max_keys] or NULL, written: the cache rows of all tokens of
+ *                 lens_out, in order (for the calls that read rows back), -1 from
+ *                 cu_k[batch] on; needs cu_k.  Tokens past max_keys are reported
+ *                 (HSA_ERR_INDEX).
+ * A row in a page whose id lies outside [0, n_pages) is -1 (HSA_ERR_INDEX).  lens_out may be
+ * lens or want, and n_free_out n_free; no other two may overlap.  page_size a power of two;
+ * n_pages * page_size < 2^31; max_pages * page_size < 2^31 - 256; max_new, max_keys < 2^31 -
+ * 256; sums past 2^31 - 1 count as that.  One launch, or two where max_new + max_keys is
+ * above 8192. */
+int hsa_page_plan(const int32_t *lens, const int32_t *want, int batch, int page_size,
+                  int32_t *page_table, int max_pages, int32_t *free_pages, int n_pages,
+                  const int32_t *n_free, int32_t *n_free_out, int32_t *lens_out, int32_t *cu_q,
+                  int32_t *slots, int32_t *positions, int max_new, int32_t *cu_k,
+                  int32_t *key_rows, int max_keys, hsa_stream_t stream);
 
 /* ------------------------------- attention over paged caches, packed prompts */
 

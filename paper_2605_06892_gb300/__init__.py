@@ -31,6 +31,8 @@ __all__ = [
     "HSA_E4M3", "hsa_kv_quant_scatter", "hsa_kv_dequant_gather",
     "hsa_paged_attention", "hsa_paged_attention_workspace_bytes",
     "hsa_packed_attention", "hsa_packed_attention_workspace_bytes",
+    "HSA_E2M1", "hsa_kv4_quant_scatter", "hsa_kv4_dequant_gather", "hsa_qk_norm_rope",
+    "hsa_page_plan",
     "hsa_get_device_error", "hsa_launch_count", "hsa_test_inject_attention_stall",
     "hsa_test_f32_cluster",
 ]
@@ -38,7 +40,7 @@ __all__ = [
 _HERE = os.path.dirname(os.path.abspath(__file__))
 library_path = os.path.join(_HERE, "libhsa.so")
 
-HSA_BF16, HSA_F32, HSA_E4M3 = 0, 1, 2
+HSA_BF16, HSA_F32, HSA_E4M3, HSA_E2M1 = 0, 1, 2, 3
 HSA_PARTITION_STATIC_MAX_TOKENS = 524288
 STATUS = {0: "HSA_OK", -1: "HSA_ERR_INVALID_ARG", -2: "HSA_ERR_NOT_DIVISOR",
           -3: "HSA_ERR_BAD_COUNTS", -4: "HSA_ERR_UNSUPPORTED", -5: "HSA_ERR_NONFINITE",
@@ -97,6 +99,13 @@ _SIGS = {
     "hsa_packed_attention": ([_c_p, _c_ll, _c_p, _c_ll, _c_p, _c_ll, _c_p, _c_p] + [_c_int] * 7 +
                              [_c_f, _c_p, _c_int, _c_p, _c_sz, _c_p], _c_int),
     "hsa_packed_attention_workspace_bytes": ([_c_int] * 3, _c_sz),
+    "hsa_kv4_quant_scatter": ([_c_p] * 5 + [_c_ll, _c_p, _c_ll, _c_p] + [_c_int] * 5 +
+                              [_c_p, _c_p, _c_int, _c_p], _c_int),
+    "hsa_kv4_dequant_gather": ([_c_p] * 5 + [_c_int] * 4 + [_c_p, _c_p, _c_int, _c_p], _c_int),
+    "hsa_qk_norm_rope": ([_c_p, _c_ll] * 3 + [_c_p, _c_p, _c_f, _c_int, _c_p, _c_p] +
+                         [_c_int] * 6 + [_c_p] * 4 + [_c_int, _c_p], _c_int),
+    "hsa_page_plan": ([_c_p, _c_p, _c_int, _c_int, _c_p, _c_int, _c_p, _c_int] + [_c_p] * 6 +
+                      [_c_int, _c_p, _c_p, _c_int, _c_p], _c_int),
     "hsa_get_device_error": ([_c_p], _c_int),
     "hsa_launch_count": ([], ctypes.c_ulonglong),
     "hsa_test_inject_attention_stall": ([_c_int], _c_int),
@@ -508,17 +517,18 @@ def hsa_packed_attention_workspace_bytes(Hq: int, Hkv: int, D: int) -> int:
     return lib().hsa_packed_attention_workspace_bytes(Hq, Hkv, D)
 
 
-def _token_rows(name, t, device):
-    """Address of bf16 token rows [tokens, H, D] on the device whose heads lie together, and
-    the elements from a row to the next: the rows may lie apart, as in a fused projection's
+def _token_rows(name, t, device, dtype=torch.bfloat16):
+    """Address of token rows [tokens, H, D] on the device whose heads lie together, and the
+    elements from a row to the next: the rows may lie apart, as in a fused projection's
     output."""
     tokens, H, D = t.shape
     if t.is_contiguous():
-        return _place(name, t, torch.bfloat16, device), H * D
+        return _place(name, t, dtype, device), H * D
     row, head, one = t.stride()
     if one != 1 or (head != D and H > 1):
         raise ValueError(f"{name} is not rows of {H} heads x {D} that lie together")
-    _place(name, t[0], torch.bfloat16, device)
+    if t.dtype is not dtype or t.get_device() != device:
+        _place(name, t[0], dtype, device)   # says why not
     return t.data_ptr(), row
 
 
@@ -548,6 +558,155 @@ def hsa_packed_attention(q, k, v, cu_q, cu_k, out, mask: int = 0, scale: float =
         _place("cu_k", cu_k, torch.int32, dev), ends[0] - 1, total_q, total_k, Hq, Hkv, D, mask,
         float(scale), _place("out", out, torch.bfloat16, dev), HSA_BF16, where, room,
         _stream(stream)), "hsa_packed_attention")
+
+
+# ------------------------- 4-bit cache, normed and rotated rows, page plans
+
+def _cache4(k_cache, v_cache, k_scale, v_scale, device):
+    """Addresses of a 4-bit cache's four tensors, its rows, heads and dimensions."""
+    *lead, H, half = size = k_cache.shape
+    N = math.prod(lead)
+    if N > _MOST:
+        raise ValueError(f"k_cache holds {N} rows, more than a call takes")
+    _sized("v_cache", v_cache, size)
+    _sized("k_scale", k_scale, (*lead, H))
+    _sized("v_scale", v_scale, (*lead, H))
+    return (_place("k_cache", k_cache, torch.uint8, device),
+            _place("v_cache", v_cache, torch.uint8, device),
+            _place("k_scale", k_scale, torch.int32, device),
+            _place("v_scale", v_scale, torch.int32, device), N, H, 2 * half)
+
+
+def hsa_kv4_quant_scatter(k_cache, v_cache, k_scale, v_scale, k_fresh, v_fresh, idx, n_active: int,
+                          table=None, table_idx=None, stream=None) -> None:
+    """Fresh rows [>= n_active, H, D] (bf16 or fp32; they may be slices of a wider tensor) into
+    rows idx of a 4-bit cache: codes [N, H, D/2] (uint8) and words [N, H] (int32); a cache in
+    pages [P, page, H, D/2] with words [P, page, H] counts as P * page rows.  idx -1: no row.
+    table: K is rotated first (bf16), by the table's rows table_idx (idx where that is None)."""
+    dev, size, dt = _device(), k_cache.shape, k_fresh.dtype
+    size = (*size[:-1], 2 * size[-1])
+    _sized("v_fresh", v_fresh, _rows_of("k_fresh", k_fresh, size, n_active))
+    if table is not None:
+        _sized("table", table, (table.shape[0], size[-1] // 2, 2))
+    kc, vc, ks, vs, N, H, D = _cache4(k_cache, v_cache, k_scale, v_scale, dev)
+    tp = ip = None
+    rows = 0
+    if table is not None:
+        rows, tp = table.shape[0], _place("table", table, torch.float32, dev)
+    if table_idx is not None:
+        ip = _ids("table_idx", table_idx, n_active, dev)
+    kp, k_row = _token_rows("k_fresh", k_fresh, dev, dt)
+    vp, v_row = _token_rows("v_fresh", v_fresh, dev, dt)
+    _check(lib().hsa_kv4_quant_scatter(
+        kc, vc, ks, vs, kp, k_row, vp, v_row, _ids("idx", idx, n_active, dev), n_active, N, H, D,
+        _dtype_code(k_fresh), tp, ip, rows, _stream(stream)), "hsa_kv4_quant_scatter")
+
+
+def hsa_kv4_dequant_gather(k_cache, v_cache, k_scale, v_scale, idx, n: int, k_out, v_out,
+                           stream=None) -> None:
+    """k_out[:n], v_out[:n] ([>= n, H, D], bf16 or fp32) <- rows idx[:n] of a 4-bit cache
+    (idx None: rows 0 .. n-1; -1: none); the cache as for hsa_kv4_quant_scatter."""
+    dev, size, dt = _device(), k_cache.shape, k_out.dtype
+    _sized("v_out", v_out, _rows_of("k_out", k_out, (*size[:-1], 2 * size[-1]), n))
+    kc, vc, ks, vs, N, H, D = _cache4(k_cache, v_cache, k_scale, v_scale, dev)
+    _check(lib().hsa_kv4_dequant_gather(
+        kc, vc, ks, vs, None if idx is None else _ids("idx", idx, n, dev), n, N, H, D,
+        _place("k_out", k_out, dt, dev), _place("v_out", v_out, dt, dev), _dtype_code(k_out),
+        _stream(stream)), "hsa_kv4_dequant_gather")
+
+
+def hsa_qk_norm_rope(q, k, q_weight, k_weight, q_out, k_out, eps: float = 1e-6,
+                     across: bool = False, table=None, table_idx=None, v=None, v_out=None,
+                     k_idx=None, stream=None) -> None:
+    """q_out [n, Hq, D] <- q [n, Hq, D] normed per head (or with `across` over all heads of a
+    token), times q_weight (fp32 [D], or [Hq, D]; None: ones), rotated by the table's rows
+    table_idx (k_idx where that is None); k [n, Hkv, D] likewise into k_out [n, Hkv, D], or
+    into rows k_idx of a cache [N, Hkv, D] or [P, page, Hkv, D], and v, copied, into v_out.
+    q, k and v may be slices of a wider tensor.  Index -1: no row."""
+    dev, size, dt = _device(), q.shape, q.dtype
+    n, Hq, D = size
+    m, Hkv, Dk = keys = k.shape
+    if Dk != D or m != n:
+        raise ValueError("q and k disagree on the rows or the head dimension")
+    _sized("q_out", q_out, size)
+    to = k_out.shape
+    rows = 0
+    if k_idx is None:
+        _sized("k_out", k_out, keys)
+    else:
+        *lead, H, Do = to
+        rows = math.prod(lead)
+        if H != Hkv or Do != D or rows > _MOST:
+            raise ValueError(f"k_out has shape {tuple(to)}, not rows of {Hkv} heads x {D}")
+        if k_idx.shape != (n,):
+            raise ValueError(f"k_idx does not hold {n} indices")
+    if q_weight is not None:
+        _sized("q_weight", q_weight, (Hq, D) if across else (D,))
+    if k_weight is not None:
+        _sized("k_weight", k_weight, (Hkv, D) if across else (D,))
+    table_rows = 0
+    if table is not None:
+        table_rows = table.shape[0]
+        _sized("table", table, (table_rows, D // 2, 2))
+    if table_idx is not None and table_idx.numel() < n:
+        raise ValueError(f"table_idx holds fewer than {n} indices")
+    vp = vo = None
+    v_row = 0
+    if v is not None and v_out is not None:
+        _sized("v", v, keys)
+        _sized("v_out", v_out, to)
+        vp, v_row = _token_rows("v", v, dev, dt)
+        vo = _place("v_out", v_out, dt, dev)
+    elif v is not None or v_out is not None:
+        raise TypeError("v and v_out go together")
+    f32, i32 = torch.float32, torch.int32
+    qp, q_row = _token_rows("q", q, dev, dt)
+    kp, k_row = _token_rows("k", k, dev, dt)
+    _check(lib().hsa_qk_norm_rope(
+        qp, q_row, kp, k_row, vp, v_row,
+        None if q_weight is None else _place("q_weight", q_weight, f32, dev),
+        None if k_weight is None else _place("k_weight", k_weight, f32, dev),
+        eps, across, None if table is None else _place("table", table, f32, dev),
+        None if table_idx is None else _place("table_idx", table_idx, i32, dev), table_rows, n, Hq,
+        Hkv, D, _dtype_code(q), _place("q_out", q_out, dt, dev), _place("k_out", k_out, dt, dev),
+        vo, None if k_idx is None else _place("k_idx", k_idx, i32, dev), rows, _stream(stream)),
+        "hsa_qk_norm_rope")
+
+
+def hsa_page_plan(lens, want, page_size: int, page_table, free_pages, n_free, n_free_out, lens_out,
+                  cu_q, slots, positions, cu_k=None, key_rows=None, stream=None) -> None:
+    """Pages, cache rows and positions of a step that takes each sequence from lens[b] to
+    want[b] tokens: page_table [batch, max_pages] and the stack free_pages [n_pages] with
+    n_free [1] entries are updated; n_free_out [1], lens_out [batch], cu_q [batch + 1], slots
+    and positions [room for new tokens], and if given cu_k [batch + 1] and key_rows [room for
+    all tokens] are written.  All int32."""
+    dev, i32 = _device(), torch.int32
+    (B,), (rows, cols), (n_pages,) = lens.shape, page_table.shape, free_pages.shape
+    _sized("want", want, (B,))
+    _sized("lens_out", lens_out, (B,))
+    _sized("cu_q", cu_q, (B + 1,))
+    _sized("n_free", n_free, (1,))
+    _sized("n_free_out", n_free_out, (1,))
+    if rows != B:
+        raise ValueError(f"page_table has {rows} rows, not {B}")
+    _sized("positions", positions, slots.shape)
+    kp = rp = None
+    max_keys = 0
+    if cu_k is not None:
+        _sized("cu_k", cu_k, (B + 1,))
+        kp = _place("cu_k", cu_k, i32, dev)
+    if key_rows is not None:
+        max_keys, rp = key_rows.numel(), _place("key_rows", key_rows, i32, dev)
+    if max(page_size, cols, n_pages, slots.numel(), max_keys) > _MOST or page_size < -_MOST:
+        raise ValueError("a size is more than a call takes")
+    _check(lib().hsa_page_plan(
+        _place("lens", lens, i32, dev), _place("want", want, i32, dev), B, page_size,
+        _place("page_table", page_table, i32, dev), cols,
+        _place("free_pages", free_pages, i32, dev), n_pages, _place("n_free", n_free, i32, dev),
+        _place("n_free_out", n_free_out, i32, dev), _place("lens_out", lens_out, i32, dev),
+        _place("cu_q", cu_q, i32, dev), _place("slots", slots, i32, dev),
+        _place("positions", positions, i32, dev), slots.numel(), kp, rp, max_keys,
+        _stream(stream)), "hsa_page_plan")
 
 
 def hsa_get_device_error(stream=None) -> int:
