@@ -489,9 +489,11 @@ int hsa_page_plan(const int32_t *lens, const int32_t *want, int batch, int page_
  * keys is zero.  scale <= 0 selects 1/sqrt(D).
  *   q            device, bf16 [batch, n_new, Hq, D].
  *   k_pages,     device, [n_pages, page_size, Hkv, D] of cache_dtype: HSA_BF16, or
- *   v_pages      HSA_E4M3 as hsa_kv_quant_scatter writes it, with
- *   k_scale,     device, scales [n_pages, page_size, Hkv] (HSA_E4M3; else NULL), any
- *   v_scale      alignment; the aligned words of four bytes around those needed are read.
+ *   v_pages      HSA_E4M3 as hsa_kv_quant_scatter writes it, or HSA_E2M1 as
+ *                hsa_kv4_quant_scatter does ([n_pages, page_size, Hkv, D/2] bytes), with
+ *   k_scale,     device, scales [n_pages, page_size, Hkv] (HSA_E4M3), any alignment; the
+ *   v_scale      aligned words of four bytes around those needed are read.  HSA_E2M1: the
+ *                words [n_pages, page_size, Hkv], 4-byte aligned.  HSA_BF16: NULL.
  *                A row as fresh memory holds it, all bytes zero, stands for zeros.
  *   page_table   device, int32 [batch, max_pages]: key j of sequence b is row
  *                j % page_size of page page_table[b, j / page_size].  Entries past a
@@ -508,8 +510,9 @@ int hsa_page_plan(const int32_t *lens, const int32_t *want, int batch, int page_
  * [0, n_pages) reads as rows of zeros (HSA_ERR_INDEX).  Two launches; the result does not
  * depend on what else runs.  A flat cache of N rows is a cache of ceil(N / page_size) pages
  * with the identity as its table.
- * HSA_E4M3: a key's weight times the power of two of its value row is held to 2^-39 of the
- * row's largest such product; what lies further below adds nothing to out. */
+ * HSA_E4M3, HSA_E2M1: a key's weight times the power of two of its value row is held to 2^-39
+ * (HSA_E2M1: 2^-35) of the row's largest such product; what lies further below adds nothing to
+ * out.  HSA_E2M1: a row of NaN reaches the rows that see its key, in every dimension. */
 int hsa_paged_attention(const void *q, int batch, int n_new, int Hq, const void *k_pages,
                         const void *v_pages, const uint8_t *k_scale, const uint8_t *v_scale,
                         int n_pages, int page_size, int Hkv, int D, hsa_dtype cache_dtype,

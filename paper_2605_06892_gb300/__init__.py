@@ -483,13 +483,15 @@ def hsa_paged_attention(q, k_pages, v_pages, page_table, seq_lens, out, k_scale=
     """out = attention of the newest tokens q [batch, n_new, Hq, D] over each sequence's
     seq_lens[b] keys, held in pages [n_pages, page, Hkv, D] named by page_table [batch,
     max_pages]; bf16 pages, or 8-bit ones (float8_e4m3fn or uint8) with their scale bytes
-    [n_pages, page, Hkv].  workspace: uint8 device tensor of at least
+    [n_pages, page, Hkv] (uint8), or 4-bit ones [n_pages, page, Hkv, D/2] (uint8) with their
+    words [n_pages, page, Hkv] (int32).  workspace: uint8 device tensor of at least
     hsa_paged_attention_workspace_bytes(...) bytes."""
     dev, size, pool = _device(), q.shape, k_pages.shape
     B, n_new, Hq, D = size
     n_pages, page, Hkv, Dk = pool
     batch, cols = page_table.shape
-    if Dk != D or batch != B or seq_lens.shape != (B,):
+    four = k_scale is not None and k_scale.dtype is torch.int32
+    if (2 * Dk if four else Dk) != D or batch != B or seq_lens.shape != (B,):
         raise ValueError("q, k_pages, page_table and seq_lens disagree on the batch or the head "
                          "dimension")
     _sized("out", out, size)
@@ -500,7 +502,10 @@ def hsa_paged_attention(q, k_pages, v_pages, page_table, seq_lens, out, k_scale=
         vp = _place("v_pages", v_pages, torch.bfloat16, dev)
         ks, vs, code = None, None, HSA_BF16
     elif k_scale is None or v_scale is None:
-        raise TypeError("an 8-bit cache has both k_scale and v_scale")
+        raise TypeError("an 8-bit or 4-bit cache has both k_scale and v_scale")
+    elif four:
+        kp, vp, ks, vs, *_ = _cache4(k_pages, v_pages, k_scale, v_scale, dev)
+        code = HSA_E2M1
     else:
         kp, vp, ks, vs, *_ = _cache8(k_pages, v_pages, k_scale, v_scale, pool, dev)
         code = HSA_E4M3

@@ -14,44 +14,47 @@ def group_of(D):
     return np.arange(D) // (D // 32) % 4
 
 
+def encode_rows(x):
+    """(codes of two a byte, words, any row not finite) of float64 rows x[..., D].  Products of
+    numbers of few bits are exact, so every border is decided by exact comparisons."""
+    x = np.asarray(x, dtype=np.float64)
+    finite = np.isfinite(x).all(-1)
+    g = group_of(x.shape[-1])
+    y = np.where(finite[..., None], np.clip(x, -TOP, TOP), 0.0)
+    a = np.stack([np.abs(y[..., g == h]).max(-1) for h in range(4)], -1)
+    top = a.max(-1)
+    e = np.full(top.shape, LEAST, dtype=np.int64)
+    while (more := top > 378.0 * np.exp2(e.astype(float))).any():
+        e += more
+    m = np.zeros(a.shape, dtype=np.int64)
+    while (more := a > 6.0 * m * np.exp2(e.astype(float))[..., None]).any():
+        m += more
+    unit = (m * np.exp2(e.astype(float))[..., None])[..., g]
+    code = np.zeros(x.shape, dtype=np.int64)
+    for i in range(7):
+        border = (GRID[i] + GRID[i + 1]) / 2 * unit
+        # a tie goes to the even code
+        code += (np.abs(y) > border) | ((np.abs(y) == border) & (i % 2 == 1) & (unit > 0))
+    code += 8 * np.signbit(y)
+    word = (e + 127) << 24
+    for h in range(4):
+        word |= m[..., h] << (6 * h)
+    pair = (code[..., 0::2] | code[..., 1::2] << 4).astype(np.uint8)
+    return (np.where(finite[..., None], pair, 0).astype(np.uint8),
+            np.where(finite, word, NAN_ROW).astype(np.uint32), not finite.all())
+
+
 def quantise_rows(x):
     """(values held, words, any row not finite) of float64 rows x[..., D]."""
-    x = np.asarray(x, dtype=np.float64)
-    D, g = x.shape[-1], group_of(x.shape[-1])
-    flat = x.reshape(-1, D)
-    held, words = np.zeros_like(flat), np.zeros(flat.shape[0], dtype=np.uint32)
-    odd = False
-    for r, row in enumerate(flat):
-        if not np.isfinite(row).all():
-            held[r], words[r], odd = np.nan, NAN_ROW, True
-            continue
-        row = np.clip(row, -TOP, TOP)
-        a = np.abs(row).max()
-        e = LEAST
-        while a > 378.0 * 2.0 ** e:
-            e += 1
-        word = (e + 127) << 24
-        for h in range(4):
-            part = row[g == h]
-            m = 0
-            while 6.0 * m * 2.0 ** e < np.abs(part).max():
-                m += 1
-            word |= m << (6 * h)
-            unit = m * 2.0 ** e
-            mid = (GRID[:-1] + GRID[1:]) / 2 * unit      # exact
-            at = np.searchsorted(mid, np.abs(part))      # borders below the value
-            tie = (at < 7) & (np.abs(part) == mid[np.minimum(at, 6)])
-            at = np.where(tie & (at % 2 == 1), at + 1, at)
-            held[r, g == h] = np.copysign(GRID[at] * unit, part) if m else 0.0
-        words[r] = word
-    return held.reshape(x.shape), words.reshape(x.shape[:-1]), odd
+    pair, word, odd = encode_rows(x)
+    return values(pair, word), word, odd
 
 
 def values(pair, word):
     """What codes [..., D/2] (uint8) with words [...] (int32 or uint32) stand for, float64."""
     pair = np.asarray(pair).astype(np.int64)
     word = np.asarray(word).astype(np.int64) & 0xffffffff
-    code = np.stack([pair & 15, pair >> 4], -1).reshape(*pair.shape[:-1], -1)
+    code = np.stack([pair & 15, pair >> 4], -1).reshape(*pair.shape[:-1], 2 * pair.shape[-1])
     m = word[..., None] >> (6 * group_of(code.shape[-1])) & 63
     s = (word >> 24)[..., None]
     v = np.where(code > 7, -GRID[code & 7], GRID[code & 7]) * m * np.exp2(s - 127.0)
@@ -79,6 +82,29 @@ def norm_rope(x, weight, eps, across, table, rows, out_step):
         a, b = a.abs(), b.abs()
         size = torch.stack([a * c.abs() + b * s.abs(), a * s.abs() + b * c.abs()], -1).flatten(-2)
     return y, out_step * y.abs() + steps * 2.0 ** -24 * size + 1e-38
+
+
+# A 4-bit attention's probabilities are rounded to fp16 and again after a factor of a group: at
+# most 2^-11 of themselves each.
+P_STEP = 2.0 ** -10 + 2.0 ** -22
+
+
+def small_weights(q, k, v_word, limit, scale=None):
+    """What the fp16 probabilities may lose below their normal range [n, Hq, 1]: a key's weight
+    times the power of two of its value row is held within 2^-35 of the largest such product, and
+    its product with a factor again; each meets a factor of up to 63 and a code of up to 6."""
+    n, Hq, D = q.shape
+    m, Hkv = k.shape[:2]
+    scale = D ** -0.5 if scale is None else scale
+    power = torch.from_numpy(np.exp2((np.asarray(v_word).astype(np.int64) >> 24 & 255) - 127.0))
+    out = torch.zeros((n, Hq, 1), dtype=torch.float64)
+    for h in range(Hq):
+        for i in range(n):
+            c = int(limit[i])
+            if c > 0:
+                w = torch.softmax((k[:c, h * Hkv // Hq] @ q[i, h]) * scale, 0)
+                out[i, h] = c * 2.0 ** -35 * (378 + 6) * (w * power[:c, h * Hkv // Hq]).max()
+    return out
 
 
 MOST = 2 ** 31 - 1

@@ -184,3 +184,34 @@ def test_binding_refuses_what_c_cannot_see(hsa, monkeypatch):
                          ("cu_k", dict(cu_k=new)), ("more than", dict(page_size=1 << 32))):
         with pytest.raises((ValueError, TypeError), match=name):
             hsa.hsa_page_plan(**{**ok, **change})
+
+
+def test_attention_over_4_bits_refusals(hsa, monkeypatch):
+    def call(q=P, B=2, new=1, Hq=8, k=P, v=P, ks=P, vs=P, pages=10, page=16, Hkv=2, D=64, table=P, cols=4, lens=P,
+             out=P, ws=P, size=1 << 30):
+        return hsa.lib().hsa_paged_attention(q, B, new, Hq, k, v, ks, vs, pages, page, Hkv, D, 3, table, cols, lens,
+                                             0.0, out, ws, size, None)
+    c0 = hsa.hsa_launch_count()
+    assert call(B=0, q=None, ws=None) == 0 and call(new=0, out=None) == 0
+    for bad in (dict(ks=None), dict(vs=None), dict(ks=BYTE), dict(vs=BYTE), dict(k=ODD), dict(v=ODD), dict(Hq=7),
+                dict(table=None), dict(lens=None), dict(q=None)):
+        assert call(**bad) == -1, bad
+    for bad in (dict(D=96), dict(D=32), dict(page=48)):
+        assert call(**bad) == -4, bad
+    for bad in (dict(ws=None), dict(size=1000)):
+        assert call(**bad) == -9, bad
+    assert hsa.hsa_launch_count() == c0
+
+    monkeypatch.setattr(hsa, "lib", lambda: None)
+    q, t, n = torch.zeros((1, 1, 4, 64), dtype=torch.bfloat16), torch.zeros((1, 2), dtype=torch.int32), torch.zeros(
+        1, dtype=torch.int32)
+    c, w = torch.zeros((2, 16, 2, 32), dtype=torch.uint8), torch.zeros((2, 16, 2), dtype=torch.int32)
+    with pytest.raises(ValueError, match="CUDA"):
+        hsa.hsa_paged_attention(q, c, c, t, n, q, k_scale=w, v_scale=w)
+    monkeypatch.setattr(hsa, "_device", lambda: -1)     # what a tensor of the CPU says
+    for name, args in (("head", (torch.zeros((2, 16, 2, 64), dtype=torch.uint8), c, w, w)),
+                       ("v_cache", (c, c[:1], w, w)), ("k_scale", (c, c, w[:1], w)), ("v_scale", (c, c, w, w[:1]))):
+        with pytest.raises(ValueError, match=name):
+            hsa.hsa_paged_attention(q, *args[:2], t, n, q, k_scale=args[2], v_scale=args[3])
+    with pytest.raises(TypeError):
+        hsa.hsa_paged_attention(q, c, c, t, n, q, k_scale=w)
