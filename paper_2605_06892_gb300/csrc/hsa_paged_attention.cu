@@ -31,40 +31,15 @@
 // that of the other sum it would lie between 2^-120 and 2^100 n, since vs does within
 // [-100, 120] (-127 in rows of fresh memory), and long stretches of zero rows would overflow
 // it.  All else is relative to R, so that scores of any size lose nothing beside vs.
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-
 #include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <type_traits>
 
-#include "hsa_internal.cuh"
-#include "hsa_ptx.cuh"
+#include "hsa_paged.cuh"
 
 namespace hsa {
 namespace {
-
-constexpr int kWarps = 4;
-constexpr int kThreads = 32 * kWarps;
-constexpr int kMostRows = 32;         // query rows of a unit at most
-constexpr int kMaxPerSm = 4;          // CTAs per SM that the workspace is sized for
-constexpr float kLowest = -3.0e38f;   // running maximum before the first key
-// fp16 probabilities are 2^(u - M + 14); in 4 bits 2^(u - M + 10), for the factors of up to 63
-template <int kBits>
-constexpr float kPShift = kBits == 4 ? 10.f : 14.f;
-constexpr float kFar = 0x1p64f;       // a lane's weights' sum above it takes a new R
-
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t *>(&v);
-}
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
-  const __half2 v = __floats2half2_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t *>(&v);
-}
-__device__ __forceinline__ float lo_bf16(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float hi_bf16(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
 __device__ __forceinline__ uint32_t f16x2_of_e4m3x2(uint32_t codes16) {
   uint32_t h;
@@ -72,445 +47,101 @@ __device__ __forceinline__ uint32_t f16x2_of_e4m3x2(uint32_t codes16) {
   return h;
 }
 
-// The values of eight e2m1 codes, in pairs.
-__device__ __forceinline__ void f16_of_e2m1x8(uint32_t w, uint32_t (&h)[4]) {
-  asm("{\n.reg .b8 a, b, c, e;\n"
-      "mov.b32 {a, b, c, e}, %4;\n"
-      "cvt.rn.f16x2.e2m1x2 %0, a;\n"
-      "cvt.rn.f16x2.e2m1x2 %1, b;\n"
-      "cvt.rn.f16x2.e2m1x2 %2, c;\n"
-      "cvt.rn.f16x2.e2m1x2 %3, e;\n}"
-      : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
-      : "r"(w));
-}
-
-// d += a b, 16 rows x 8 columns x 16.
-template <bool kF16>
-__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0,
-                                    uint32_t b1) {
-  if (kF16)
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
-        "{%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-  else
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
-        "{%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-
-// An 8 x 8 block of 16-bit values, a pair per lane, transposed.
-__device__ __forceinline__ uint32_t transposed(uint32_t w) {
-  uint32_t r;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(w));
-  return r;
-}
-
-// 16 bytes into shared memory, zeros where !ok.
-__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool ok) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src),
-               "r"(ok ? 16 : 0)
-               : "memory");
-}
-__device__ __forceinline__ void copy4(uint32_t dst, const void *src) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int n>
-__device__ __forceinline__ void wait_all_but() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(n) : "memory");
-}
-__device__ __forceinline__ uint4 lds128(uint32_t a) {
-  uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
-  return v;
-}
-__device__ __forceinline__ uint2 lds64(uint32_t a) {
-  uint2 v;
-  asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
-  return v;
-}
-__device__ __forceinline__ uint32_t lds32(uint32_t a) {
-  uint32_t v;
-  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a));
-  return v;
-}
-__device__ __forceinline__ uint32_t word(const uint4 &v, int i) {
-  return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w;
-}
-
-template <int D, int kBits, int kNR>
+template <int D, bool kF8, int kNR>
 struct Cfg {
-  static constexpr bool kCode = kBits < 16;                    // codes with powers of two
   static constexpr int kRows = 8 * kNR;                        // query rows of a unit
-  static constexpr int kRowBytes = D * kBits / 8;
+  static constexpr int kRowBytes = D * (kF8 ? 1 : 2);
   static constexpr int kChunks = kRowBytes / 16;               // 16-byte chunks per row
   // Four column blocks at D = 128 leave no registers for the query rows, which are then
   // read from shared memory at each product.
   static constexpr bool kLean = D == 128 && kNR == 4;
-  static_assert(!(kLean && kCode), "the rows in shared memory are bf16");
+  static_assert(!(kLean && kF8), "the rows in shared memory are bf16");
   static constexpr int kKW = kRowBytes == 256 ? 16 : 32;       // keys per warp and tile
   static constexpr int kTile = kWarps * kKW;                   // keys per tile
   static constexpr int kStages = 2;
   static constexpr int kBlocks = kNR == 1 ? (D == 64 ? 4 : 3) : 2;   // per SM: registers
   static constexpr int kHalf = kKW * kRowBytes;                // K (or V) bytes of a stage
-  // per key four words; in 4 bits four factors of K more, and half of a pair's of V
-  static constexpr int kScales = kBits == 8 ? kKW * 16 : kBits == 4 ? kKW * 40 : 0;
+  static constexpr int kScales = kF8 ? kKW * 16 : 0;           // per key four words
   static constexpr int kStage = 2 * kHalf + kScales;
   static constexpr int kQ = kRows * D * 2;                     // a unit's query rows
-  static constexpr int kStat = kCode ? 4 : 2;                    // per row of a part: M, l, R
-  static constexpr int kPart = kRows * (D + kStat);            // floats of a part
+  static constexpr int kStat = part_stats(kF8);
+  static constexpr int kPart = part_floats(D, kF8, kRows);
   static constexpr int kSmem = kWarps * kStages * kStage + kStages * kQ;
 };
 
 // The key (row of an 8-key block) of MMA index n.  The 16-byte loads of K (a quarter-warp:
 // keys of n = 2x, 2x+1; four chunks) and of V (keys of n = 0, 2, 4, 6 or 1, 3, 5, 7; two
-// chunks) then fall into distinct banks under the swizzles below; rows of two chunks take
-// 8-byte loads of K (a half-warp: keys of n = 0 .. 3 or 4 .. 7) and 4-byte ones of V (n = 0, 2,
-// 4, 6 or 1, 3, 5, 7), and four of them that differ mod 4 fill the banks.
+// chunks) then fall into distinct banks under the swizzles below.
 template <int kChunks>
 __device__ __forceinline__ int key_of(int n) {
-  return kChunks == 2   ? n ^ (n >> 2 & 1)
-         : kChunks == 4 ? n ^ ((n >> 1) & 1)
-                        : (n >> 1) | ((n & 1) << 2);
+  return kChunks == 4 ? n ^ ((n >> 1) & 1) : (n >> 1) | ((n & 1) << 2);
 }
 template <int kChunks>
 __device__ __forceinline__ int k_chunk(int c, int row) {
-  return kChunks <= 4 ? c : c ^ (row & 7);
+  return kChunks == 4 ? c : c ^ (row & 7);
 }
 template <int kChunks>
 __device__ __forceinline__ int v_chunk(int c, int row) {
-  return kChunks == 2 ? c : kChunks == 4 ? c ^ (((row >> 2) & 1) << 1) : c ^ ((row & 3) << 1);
-}
-// Whether key `row` of an 8-key block has an even MMA index. (Its pair's other key is row ^ 1,
-// and the pair's index row / 2.)
-template <int kChunks>
-__device__ __forceinline__ bool is_even(int row) {
-  static_assert(kChunks <= 4, "pairs of neighbouring keys");
-  return (row & 1) == (row >> (kChunks == 2 ? 2 : 1) & 1);
+  return kChunks == 4 ? c ^ (((row >> 2) & 1) << 1) : c ^ ((row & 3) << 1);
 }
 
 // Where a query row's dimensions of K = 16 step s lie in shared memory that lane t of a
 // quad multiplies: those that its K fragments hold (chunk c of row r lies at c ^ (r & 7)).
-// In 4 bits a step stays within a group (dimension d is of group (d / (D/32)) mod 4), two steps
-// to a group at D = 128; at D = 64 it takes two pairs that lie eight dimensions apart.
-template <int D, int kBits>
+template <int D, bool kF8>
 __device__ __forceinline__ int query_place(int r, int s, int t) {
-  const int d = kBits == 4   ? D / 4 * t + (D == 128 ? 4 * (s / 2) + 16 * (s % 2) : 2 * s)
-                : kBits == 8 ? 16 * (t + 4 * (s / 4)) + 4 * (s % 4)
-                             : 8 * (t + 4 * (s / 2)) + 4 * (s % 2);
-  return r * (2 * D) + 16 * ((d / 8) ^ (r & 7)) + (d & 6) * 2;
-}
-// The four dimensions there.
-template <int D, int kBits>
-__device__ __forceinline__ uint2 query_at(uint32_t rows, int r, int s, int t) {
-  const uint32_t at = rows + query_place<D, kBits>(r, s, t);
-  if constexpr (kBits == 4 && D == 64)   // d and d + 8: the chunks' lowest bit apart
-    return make_uint2(lds32(at), lds32(at ^ 16));
-  else
-    return lds64(at);
-}
-
-// What the join has to know of a unit that several blocks shared, from the block that
-// ended it: how many, the first, and that one's slot; parts = 0: that block ended none.
-struct CutUnit {
-  int parts, first, slot, b, unit, pad[3];
-};
-
-struct Args {
-  CutUnit *cuts;                   // [blocks]
-  const __nv_bfloat16 *q;
-  const uint8_t *k, *v;            // pages [n_pages][page][Hkv][D]
-  const uint8_t *ks, *vs;          // [n_pages][page][Hkv]
-  const int32_t *table, *lens;
-  __nv_bfloat16 *out;
-  float *ws;
-  unsigned *err;
-  int batch, n_new, Hq, Hkv, rows, row_tiles;   // rows = n_new G
-  Divider group;                                // by G = Hq / Hkv
-  int n_pages, page_log2, max_pages, sms;
-  float scale_log2, scale_digits, scale_power;   // the first is the others' product
-};
-
-// What every block of a launch derives from the lengths: the key tiles of all units, cut
-// into `ctas` runs of `base` or base + 1 tiles.  A tile per block up to one block per SM,
-// then at least two, which overlap (one token against 4001 keys of 8 heads 10.3 us, 11.7
-// with 456 blocks of one or two).
-struct Plan {
-  int total, ctas, base, more;     // more: how many runs have one tile more, the first ones
-};
-__device__ __forceinline__ Plan plan_of(int total, int grid, int sms) {
-  Plan p;
-  p.total = total;
-  p.ctas = max(1, min(grid, max(min(total, sms), total / 2)));
-  p.base = total / p.ctas;
-  p.more = total - p.base * p.ctas;
-  return p;
-}
-__device__ __forceinline__ int first_tile(const Plan &p, int cta) {
-  return cta * p.base + min(cta, p.more);
-}
-__device__ __forceinline__ int cta_of(const Plan &p, int tile) {
-  const int longer = p.more * (p.base + 1);
-  return tile < longer ? tile / (p.base + 1) : p.more + (tile - longer) / p.base;
-}
-
-// len_b, checked: negative, or more than the table's pages hold.
-__device__ __forceinline__ int length(const Args &a, int b) {
-  const int n = __ldg(a.lens + b);
-  const long long most = (long long)a.max_pages << a.page_log2;
-  if (n < 0 || n > most) {
-    set_error(a.err, kErrIndex);
-    return n < 0 ? 0 : (int)most;
-  }
-  return n;
-}
-
-// A place in the row of key tiles.
-struct Cursor {
-  int b, unit, tile, tiles, len;   // unit: head * row_tiles + row tile
-};
-__device__ __forceinline__ void step(const Args &a, Cursor &c, int tile) {
-  if (++c.tile < c.tiles) return;
-  c.tile = 0;
-  if (++c.unit < a.Hkv * a.row_tiles) return;
-  c.unit = 0;
-  do {
-    if (++c.b >= a.batch) return;   // past the end: not used any more
-    c.len = length(a, c.b);
-    c.tiles = (c.len + tile - 1) / tile;
-  } while (c.tiles == 0);
-}
-
-// Zeros for the rows of sequences without keys; the blocks share the sequences out.
-template <int D>
-__device__ __forceinline__ void clear_empty(const Args &a) {
-  for (int b = blockIdx.x; b < a.batch; b += gridDim.x) {
-    if (length(a, b) != 0) continue;
-    const long long n = (long long)a.n_new * a.Hq * (D / 8);
-    uint4 *dst = reinterpret_cast<uint4 *>(a.out) + b * n;
-    for (long long i = threadIdx.x; i < n; i += kThreads) dst[i] = make_uint4(0u, 0u, 0u, 0u);
-  }
-}
-
-__device__ __forceinline__ uint64_t both(float lo, float hi) {
-  return pack2(__float_as_uint(lo), __float_as_uint(hi));
+  const int d = kF8 ? 16 * (t + 4 * (s / 4)) + 4 * (s % 4) : 8 * (t + 4 * (s / 2)) + 4 * (s % 2);
+  return r * (2 * D) + 16 * ((d / 8) ^ (r & 7)) + (d & 4) * 2;
 }
 
 // The products of a warp's keys of a tile at sk with the query rows: MMA row n (n + 8) of block
 // b is key 16 b + key_of(n) (+ 8).  rows(step, x): this lane's part of column block x.
-// In 4 bits they are sums over each group times the key's factor for it (m: four to a key).
-template <int D, int kNR, typename Rows>
-__device__ __forceinline__ void score_tile4(uint32_t sk, const uint4 *m, int g, int t,
-                                            float (&s)[Cfg<D, 4, kNR>::kKW / 16][kNR][4],
-                                            Rows &&rows) {
-  using C = Cfg<D, 4, kNR>;
+template <int D, bool kF8, int kNR, typename Rows>
+__device__ __forceinline__ void score_tile(uint32_t sk, int g, int t,
+                                           float (&s)[Cfg<D, kF8, kNR>::kKW / 16][kNR][4],
+                                           Rows &&rows) {
+  using C = Cfg<D, kF8, kNR>;
+  constexpr int kCh = C::kChunks;
 #pragma unroll
   for (int b = 0; b < C::kKW / 16; ++b) {
 #pragma unroll
     for (int x = 0; x < kNR; ++x) s[b][x][0] = s[b][x][1] = s[b][x][2] = s[b][x][3] = 0.f;
-    const int row = 16 * b + key_of<C::kChunks>(g);
-    const uint32_t a0 = sk + row * C::kRowBytes, a1 = a0 + 8 * C::kRowBytes;
-    const uint4 m0 = m[row], m1 = m[row + 8];
-    // words w and w + kW of the lane's part hold the same groups, D / 64 each
-    constexpr int kW = D / 64;
-    uint32_t k0[2 * kW], k1[2 * kW];
-    if constexpr (D == 128) {
-      const uint4 y = lds128(a0 + 16 * t), z = lds128(a1 + 16 * t);
-      k0[0] = y.x, k0[1] = y.y, k0[2 * kW - 2] = y.z, k0[2 * kW - 1] = y.w;
-      k1[0] = z.x, k1[1] = z.y, k1[2 * kW - 2] = z.z, k1[2 * kW - 1] = z.w;
-    } else {
-      const uint2 y = lds64(a0 + 8 * t), z = lds64(a1 + 8 * t);
-      k0[0] = y.x, k0[1] = y.y, k1[0] = z.x, k1[1] = z.y;
-    }
+    const int row = 16 * b + key_of<kCh>(g);
 #pragma unroll
-    for (int w = 0; w < kW; ++w) {
-      uint32_t h0[2][4], h1[2][4];   // [first or second half of the part][pair]
+    for (int i = 0; i < kCh / 4; ++i) {
+      const uint32_t at = 16 * k_chunk<kCh>(t + 4 * i, row);   // the same for row + 8
+      const uint4 w0 = lds128(sk + row * C::kRowBytes + at);
+      const uint4 w1 = lds128(sk + (row + 8) * C::kRowBytes + at);
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        f16_of_e2m1x8(k0[w + kW * half], h0[half]);
-        f16_of_e2m1x8(k1[w + kW * half], h1[half]);
-      }
-#pragma unroll
-      for (int e = 0; e < 4 / kW; ++e) {
-        const int group = 4 / kW * w + e;
-        const float f0 = __uint_as_float(word(m0, group)), f1 = __uint_as_float(word(m1, group));
-        float y[kNR][4] = {};
-#pragma unroll
-        for (int j = 0; j < kW; ++j) {
-          // D = 128: the group's four dimensions of one half; D = 64: two of each
-          const uint32_t k[4] = {D == 128 ? h0[j][2 * e % 4] : h0[0][e],
-                                 D == 128 ? h1[j][2 * e % 4] : h1[0][e],
-                                 D == 128 ? h0[j][(2 * e + 1) % 4] : h0[1][e],
-                                 D == 128 ? h1[j][(2 * e + 1) % 4] : h1[1][e]};
-#pragma unroll
-          for (int x = 0; x < kNR; ++x) {
-            const uint2 q = rows(kW * group + j, x);
-            mma<true>(y[x], k, q.x, q.y);
-          }
+      for (int e = 0; e < (kF8 ? 4 : 2); ++e) {
+        uint32_t k[4];
+        if (kF8) {
+          k[0] = f16x2_of_e4m3x2(word(w0, e)), k[2] = f16x2_of_e4m3x2(word(w0, e) >> 16);
+          k[1] = f16x2_of_e4m3x2(word(w1, e)), k[3] = f16x2_of_e4m3x2(word(w1, e) >> 16);
+        } else {
+          k[0] = word(w0, 2 * e), k[2] = word(w0, 2 * e + 1);
+          k[1] = word(w1, 2 * e), k[3] = word(w1, 2 * e + 1);
         }
 #pragma unroll
         for (int x = 0; x < kNR; ++x) {
-          float(&z)[4] = s[b][x];
-          const uint64_t lo = fma2(both(y[x][0], y[x][1]), both(f0, f0), both(z[0], z[1]));
-          const uint64_t hi = fma2(both(y[x][2], y[x][3]), both(f1, f1), both(z[2], z[3]));
-          z[0] = lo_f(lo), z[1] = hi_f(lo), z[2] = lo_f(hi), z[3] = hi_f(hi);
+          const uint2 q = rows((kF8 ? 4 : 2) * i + e, x);
+          mma<kF8>(s[b][x], k, q.x, q.y);
         }
       }
     }
   }
-}
-
-template <int D, int kBits, int kNR, typename Rows>
-__device__ __forceinline__ void score_tile(uint32_t sk, const uint4 *m, int g, int t,
-                                           float (&s)[Cfg<D, kBits, kNR>::kKW / 16][kNR][4],
-                                           Rows &&rows) {
-  using C = Cfg<D, kBits, kNR>;
-  constexpr bool kCode = C::kCode;
-  constexpr int kCh = C::kChunks;
-  if constexpr (kBits == 4) {
-    score_tile4<D, kNR>(sk, m, g, t, s, rows);
-  } else {
-#pragma unroll
-    for (int b = 0; b < C::kKW / 16; ++b) {
-#pragma unroll
-      for (int x = 0; x < kNR; ++x) s[b][x][0] = s[b][x][1] = s[b][x][2] = s[b][x][3] = 0.f;
-      const int row = 16 * b + key_of<kCh>(g);
-#pragma unroll
-      for (int i = 0; i < kCh / 4; ++i) {
-        const uint32_t at = 16 * k_chunk<kCh>(t + 4 * i, row);   // the same for row + 8
-        const uint4 w0 = lds128(sk + row * C::kRowBytes + at);
-        const uint4 w1 = lds128(sk + (row + 8) * C::kRowBytes + at);
-#pragma unroll
-        for (int e = 0; e < (kCode ? 4 : 2); ++e) {
-          uint32_t k[4];
-          if (kCode) {
-            k[0] = f16x2_of_e4m3x2(word(w0, e)), k[2] = f16x2_of_e4m3x2(word(w0, e) >> 16);
-            k[1] = f16x2_of_e4m3x2(word(w1, e)), k[3] = f16x2_of_e4m3x2(word(w1, e) >> 16);
-          } else {
-            k[0] = word(w0, 2 * e), k[2] = word(w0, 2 * e + 1);
-            k[1] = word(w1, 2 * e), k[3] = word(w1, 2 * e + 1);
-          }
-#pragma unroll
-          for (int x = 0; x < kNR; ++x) {
-            const uint2 q = rows((kCode ? 4 : 2) * i + e, x);
-            mma<kCode>(s[b][x], k, q.x, q.y);
-          }
-        }
-      }
-    }
-  }
-}
-
-// 4 bits: O^T += V^T P^T over 16 keys, block b of a tile at sv, with the keys' factors for each
-// group in the probabilities (factors: four pairs for each two keys).  sees(x, k): whether row
-// 8 x + g sees key k of the tile, where some do not (`part`).
-template <int D, int kNR, typename Sees>
-__device__ __forceinline__ void add_values4(float (&o)[D / 16][kNR][4],
-                                            const uint32_t (&p)[kNR][2], uint32_t sv,
-                                            const uint4 *factors, int b, int g, int t, bool part,
-                                            Sees &&sees) {
-  using C = Cfg<D, 4, kNR>;
-  constexpr int kCh = C::kChunks, kNT = D / 8, kMT = D / 16;
-  uint32_t vf[kNT][2];
-  // A byte holds two dimensions of a key: the low halves of both keys' bytes make a pair
-  // of one dimension, the high halves of the next.
-  constexpr uint32_t kLow = 0x0f0f0f0fu;
-  uint32_t factor[2][4];
-#pragma unroll
-  for (int hi = 0; hi < 2; ++hi) {
-    const int ra = 16 * b + 8 * hi + key_of<kCh>(2 * t);
-    const int rb = 16 * b + 8 * hi + key_of<kCh>(2 * t + 1);
-    const uint32_t pa = sv + ra * C::kRowBytes, pb = sv + rb * C::kRowBytes;
-    uint32_t wa[2] = {}, wb[2] = {};
-    if (D == 128) {
-      const uint2 y = lds64(pa + 16 * v_chunk<kCh>(g >> 1, ra) + 8 * (g & 1));
-      const uint2 z = lds64(pb + 16 * v_chunk<kCh>(g >> 1, rb) + 8 * (g & 1));
-      wa[0] = y.x, wa[1] = y.y, wb[0] = z.x, wb[1] = z.y;
-    } else {
-      wa[0] = lds32(pa + 4 * g), wb[0] = lds32(pb + 4 * g);
-    }
-    const uint4 f = factors[8 * b + 4 * hi + t];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) factor[hi][i] = word(f, i);
-#pragma unroll
-    for (int w = 0; w < D / 64; ++w) {
-      uint32_t h0[4], h1[4];
-      f16_of_e2m1x8((wa[w] & kLow) | (wb[w] << 4 & ~kLow), h0);
-      f16_of_e2m1x8((wa[w] >> 4 & kLow) | (wb[w] & ~kLow), h1);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        vf[8 * w + 2 * i][hi] = h0[i], vf[8 * w + 2 * i + 1][hi] = h1[i];
-    }
-  }
-  // The factors of a row of NaN are NaN: they must not reach the rows that may not see
-  // it by 0 * NaN, so what newer keys than a row's are worth is zero after the product.
-  uint32_t keep[kNR][2];
-  if (part) {
-#pragma unroll
-    for (int x = 0; x < kNR; ++x)
-#pragma unroll
-      for (int hi = 0; hi < 2; ++hi) {
-        const int k = 16 * b + 8 * hi;
-        keep[x][hi] = (sees(x, k + key_of<kCh>(2 * t)) ? 0xffffu : 0u) |
-                      (sees(x, k + key_of<kCh>(2 * t + 1)) ? 0xffff0000u : 0u);
-      }
-  }
-  constexpr int kIn = kMT / 4;   // MMA blocks of a group
-#pragma unroll
-  for (int group = 0; group < 4; ++group)
-#pragma unroll
-    for (int x = 0; x < kNR; ++x) {
-      uint32_t y[2];
-#pragma unroll
-      for (int hi = 0; hi < 2; ++hi) {
-        const __half2 z = __hmul2(*reinterpret_cast<const __half2 *>(&p[x][hi]),
-                                  *reinterpret_cast<const __half2 *>(&factor[hi][group]));
-        y[hi] = *reinterpret_cast<const uint32_t *>(&z);
-        if (part) y[hi] &= keep[x][hi];
-      }
-#pragma unroll
-      for (int n = kIn * group; n < kIn * (group + 1); ++n) {
-        const uint32_t v[4] = {vf[2 * n][0], vf[2 * n + 1][0], vf[2 * n][1], vf[2 * n + 1][1]};
-        mma<true>(o[n][x], v, y[0], y[1]);
-      }
-    }
-}
-
-// 8 bits: the products of two rows with one key times the query rows' power of two (where it
-// is below 1) and the key's, w = (kf, kf, vs, vs).  Only the key's factor holds digits, the
-// scale's, so that a score is rounded here and the powers of two after it are exact: R, one of
-// the scores, and the scores inside the FMA that subtracts it are the same numbers.  (A product
-// rounded as it is subtracted would differ from itself, by a half step of it.)
-__device__ __forceinline__ uint64_t product8(const float (&y)[4], int n, const float (&before)[2],
-                                             const uint4 &w) {
-  return mul2(mul2(both(y[2 * n], y[2 * n + 1]), both(before[0], before[1])), pack2(w.x, w.y));
 }
 
 // 8 bits: R is zero to begin with.  Where scores are beyond +-64 of it, so that a lane's sum
 // leaves the range that holds all that counts, the warp takes the tile again, here, against the
 // largest score so far.
 template <int D, int kNR>
-struct TileCode {
-  uint2 q[D / 16][kNR];
-  float before[kNR][2], after[kNR][2];
-  int limit[kNR][2];                            // keys of the tile that a row sees
-  float ref[kNR][2], l[kNR][2], m[kNR][2];      // those before the tile; then the new R, l with
-  float s[2][kNR][4], mx[kNR][2];               // the tile's, the old m relative to R, u
-};
-template <int D, int kBits, int kNR>
-__device__ __noinline__ void take_again(TileCode<D, kNR> &z, uint32_t sk, const uint4 *scales,
+__device__ __noinline__ void take_again(CodeTile<D, kNR> &z, uint32_t sk, const uint4 *scales,
                                         bool first) {
-  using C = Cfg<D, kBits, kNR>;
+  using C = Cfg<D, true, kNR>;
   constexpr int kCh = C::kChunks;
   static_assert(C::kKW == 32, "two blocks of 16 keys");
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  score_tile<D, kBits, kNR>(sk, scales + C::kKW, g, t, z.s,
-                            [&](int step, int x) { return z.q[step][x]; });
+  score_tile<D, true, kNR>(sk, g, t, z.s, [&](int step, int x) { return z.q[step][x]; });
 #pragma unroll 1
   for (int x = 0; x < kNR; ++x) {
     uint64_t score[4];
@@ -521,7 +152,7 @@ __device__ __noinline__ void take_again(TileCode<D, kNR> &z, uint32_t sk, const 
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int row = 8 * i + key_of<kCh>(g);
-      score[i] = mul2(product8(z.s[i >> 1][x], i & 1, z.before[x], scales[row]),
+      score[i] = mul2(code_product(z.s[i >> 1][x], i & 1, z.before[x], scales[row]),
                       both(z.after[x][0], z.after[x][1]));
       if (row < z.limit[x][0]) top[0] = fmaxf(top[0], lo_f(score[i]));
       if (row < z.limit[x][1]) top[1] = fmaxf(top[1], hi_f(score[i]));
@@ -555,16 +186,15 @@ __device__ __noinline__ void take_again(TileCode<D, kNR> &z, uint32_t sk, const 
   }
 }
 
-template <int D, int kBits, int kNR>
-__global__ void __launch_bounds__(kThreads, (Cfg<D, kBits, kNR>::kBlocks))
-paged_attention_kernel(const Args a) {
-  using C = Cfg<D, kBits, kNR>;
-  constexpr bool kCode = C::kCode;
+template <int D, bool kF8, int kNR>
+__global__ void __launch_bounds__(kThreads, (Cfg<D, kF8, kNR>::kBlocks))
+paged_attention_kernel(const PagedArgs a) {
+  using C = Cfg<D, kF8, kNR>;
   constexpr int kCh = C::kChunks, kNB = C::kKW / 16, kSteps = D / 16, kNT = D / 8, kMT = D / 16;
   constexpr int kRows = C::kRows;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int sh_sum[kWarps], sh_at[3];
-  __shared__ float sh_m[kWarps][kRows], sh_l[kWarps][kRows], sh_r[kCode ? kWarps : 1][kRows];
+  __shared__ float sh_m[kWarps][kRows], sh_l[kWarps][kRows], sh_r[kF8 ? kWarps : 1][kRows];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   uint8_t *ring = smem + warp * (C::kStages * C::kStage);
   pdl_wait();
@@ -681,27 +311,20 @@ paged_attention_kernel(const Args a) {
       if (!ok && key < ahead.len) set_error(a.err, kErrIndex);
       const int slot = ok ? (page << a.page_log2) + (key & ((1 << a.page_log2) - 1)) : 0;
       const unsigned have = __ballot_sync(0xffffffffu, ok);   // rows that there are
-      if (kCode && lane < C::kKW) {
+      if (kF8 && lane < C::kKW) {
         // The aligned words around the key's scale bytes, and the bytes' place in them: the
         // bytes need not be waited for here.  A word that holds a byte of the scales can be
         // read whole, whatever the other three are.  No page: a row of zeros, times one.
         const size_t at = (size_t)slot * a.Hkv + h;
         const uintptr_t ks = (uintptr_t)(a.ks + at), vs = (uintptr_t)(a.vs + at);
         uint32_t *to = reinterpret_cast<uint32_t *>(ring + fill + 2 * C::kHalf) + 4 * lane;
-        if (kBits == 4) {   // the words themselves; no page: factors of zero
-          if (ok) {
-            copy4(smem_addr(to), a.ks + 4 * at);
-            copy4(smem_addr(to + 1), a.vs + 4 * at);
-          } else {
-            to[0] = to[1] = 0;
-          }
-        } else if (ok) {
+        if (ok) {
           copy4(smem_addr(to), (const void *)(ks & ~(uintptr_t)3));
           copy4(smem_addr(to + 1), (const void *)(vs & ~(uintptr_t)3));
         } else {
           to[0] = to[1] = 0x7f7f7f7fu;
         }
-        if (kBits == 8) to[2] = (uint32_t)(ks & 3) * 8 + ((uint32_t)(vs & 3) * 8 << 16);
+        to[2] = (uint32_t)(ks & 3) * 8 + ((uint32_t)(vs & 3) * 8 << 16);
       }
       const uint8_t *kb = a.k + (size_t)h * C::kRowBytes + 16 * (lane % kCh);
       const uint8_t *vb = a.v + (size_t)h * C::kRowBytes + 16 * (lane % kCh);
@@ -733,7 +356,7 @@ paged_attention_kernel(const Args a) {
   float o[kMT][kNR][4], m[kNR][2], l[kNR][2];
   // 8 bits: a query row's power of two times the scale's, in two factors, and its R; rows 2 t
   // and 2 t + 1 go together through packed instructions
-  float before[kCode ? kNR : 1][2], after[kCode ? kNR : 1][2], ref[kCode ? kNR : 1][2];
+  float before[kF8 ? kNR : 1][2], after[kF8 ? kNR : 1][2], ref[kF8 ? kNR : 1][2];
   uint32_t sq_now = 0;   // kLean: the unit's rows
   int unit_tile0 = 0;    // the unit's tile that this run of it starts with
   bool fresh = true, first_unit = true;
@@ -774,12 +397,12 @@ paged_attention_kernel(const Args a) {
           float big = 0.f, f;
 #pragma unroll
           for (int s = 0; s < kSteps; ++s) {
-            const uint2 w = query_at<D, kBits>(from, r, s, t);
+            const uint2 w = lds64(from + query_place<D, kF8>(r, s, t));
             qf[s][x][0] = w.x;
             qf[s][x][1] = w.y;
-            if (kCode) big = larger(larger(big, w.x), w.y);
+            if (kF8) big = larger(larger(big, w.x), w.y);
           }
-          if (kCode) {
+          if (kF8) {
             scale = scales_of(big, f);
 #pragma unroll
             for (int s = 0; s < kSteps; ++s)
@@ -789,14 +412,14 @@ paged_attention_kernel(const Args a) {
         }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          if (kCode) {
+          if (kF8) {
             // A product y stands for y 2^ks c, c a power of two: multiplied in this order, with
             // c first where it is below 1 and last else, it overflows only where the product of
             // query and key does, whatever their sizes.
             const float c = __shfl_sync(0xffffffffu, scale, 4 * (2 * t + j));
-            before[kCode ? x : 0][j] = fminf(c, 1.f);
-            after[kCode ? x : 0][j] = fminf(fmaxf(c, 1.f) * a.scale_power, 0x1p127f);
-            ref[kCode ? x : 0][j] = 0.f;
+            before[kF8 ? x : 0][j] = fminf(c, 1.f);
+            after[kF8 ? x : 0][j] = fminf(fmaxf(c, 1.f) * a.scale_power, 0x1p127f);
+            ref[kF8 ? x : 0][j] = 0.f;
           }
           m[x][j] = kLowest;
           l[x][j] = 0.f;
@@ -810,39 +433,10 @@ paged_attention_kernel(const Args a) {
     if (key0 < cur.len) {
       const uint32_t sk = ring_s + now, sv = sk + C::kHalf;
       uint4 *scales = reinterpret_cast<uint4 *>(ring + now + 2 * C::kHalf);
-      if (kCode) {
+      if (kF8) {
         // each lane makes 2^ks, times the scale's digits, and vs of its key's scale bytes
         // (within [27, 247], or 0), each twice
-        if constexpr (kBits == 4) {
-          static_assert(C::kKW == 32, "a key to a lane");
-          const uint4 w = scales[lane];
-          const uint32_t ks = w.x >> 24, vs = w.y >> 24;
-          // rows of NaN have 255: K's factor, and V's factors, are NaN
-          const uint32_t kf = ks == 255u ? 0x7fffffffu
-                                         : __float_as_uint(__uint_as_float(ks << 23) * a.scale_digits);
-          const uint32_t ve = __float_as_uint((float)((int)(vs == 255u ? 127u : vs) - 127));
-          scales[lane] = make_uint4(kf, kf, ve, ve);
-          auto factor = [&](int i) {
-            return __float_as_uint(__uint_as_float(0x4b000000u | (w.x >> (6 * i) & 63u)) - 0x1p23f);
-          };
-          scales[C::kKW + lane] = make_uint4(factor(0), factor(1), factor(2), factor(3));
-          // V's factors in fp16, beside the pair's other key's: this lane makes two groups' of
-          // both, the key of the even MMA index low
-          const uint32_t other = __shfl_xor_sync(0xffffffffu, w.y, 1);
-          const bool even = is_even<kCh>(lane & 7);
-          const uint32_t lo = even ? w.y : other, hi = even ? other : w.y;
-          auto pair = [&](int i) {
-            __half2 z;
-            *reinterpret_cast<uint32_t *>(&z) =
-                0x64006400u | (lo >> (6 * i) & 63u) | (hi >> (6 * i) & 63u) << 16;
-            z = __hsub2(z, __float2half2_rn(1024.f));
-            return *reinterpret_cast<uint32_t *>(&z) | (lo >> 24 == 255u ? 0x7fffu : 0u) |
-                   (hi >> 24 == 255u ? 0x7fff0000u : 0u);
-          };
-          const int first = even ? 0 : 2;
-          reinterpret_cast<uint2 *>(scales + 2 * C::kKW)[2 * (lane >> 1) + (even ? 0 : 1)] =
-              make_uint2(pair(first), pair(first + 1));
-        } else if (lane < C::kKW) {
+        if (lane < C::kKW) {
           const uint4 w = scales[lane];
           const uint32_t ks = w.x >> (w.z & 0xffffu) & 255u, vs = w.y >> (w.z >> 16) & 255u;
           const uint32_t ve = __float_as_uint((float)((int)vs - 127));
@@ -857,20 +451,20 @@ paged_attention_kernel(const Args a) {
         return cur.len - a.n_new + 1 +
                (int)quotient((cur.unit % a.row_tiles) * kRows + 8 * x + 2 * t + j, a.group);
       };
-      float s[kNB][kNR][4], mx[kNR][2], sum[kCode ? kNR : 1][2];
+      float s[kNB][kNR][4], mx[kNR][2], sum[kF8 ? kNR : 1][2];
       if constexpr (kLean)
-        score_tile<D, kBits, kNR>(sk, scales + C::kKW, g, t, s, [&](int step, int x) {
-          return query_at<D, kBits>(sq_now, 8 * x + g, step, t);
+        score_tile<D, kF8, kNR>(sk, g, t, s, [&](int step, int x) {
+          return lds64(sq_now + query_place<D, kF8>(8 * x + g, step, t));
         });
       else
-        score_tile<D, kBits, kNR>(sk, scales + C::kKW, g, t, s, [&](int step, int x) {
+        score_tile<D, kF8, kNR>(sk, g, t, s, [&](int step, int x) {
           return make_uint2(qf[step][x][0], qf[step][x][1]);
         });
       // ---- log2 units, the mask, the running maximum; in 8 bits the weights' sum as well
 #pragma unroll
       for (int x = 0; x < kNR; ++x) {
         mx[x][0] = m[x][0], mx[x][1] = m[x][1];
-        if constexpr (kCode) sum[x][0] = l[x][0], sum[x][1] = l[x][1];
+        if constexpr (kF8) sum[x][0] = l[x][0], sum[x][1] = l[x][1];
       }
       auto weigh = [&](auto masked) {
 #pragma unroll
@@ -878,12 +472,12 @@ paged_attention_kernel(const Args a) {
 #pragma unroll
           for (int n = 0; n < 2; ++n) {
             const int row = 16 * b + 8 * n + key_of<kCh>(g);
-            if constexpr (kCode) {
+            if constexpr (kF8) {
               const uint4 w = scales[row];
 #pragma unroll
               for (int x = 0; x < kNR; ++x) {
                 const uint64_t z =
-                    fma2(product8(s[b][x], n, before[x], w), both(after[x][0], after[x][1]),
+                    fma2(code_product(s[b][x], n, before[x], w), both(after[x][0], after[x][1]),
                          both(-ref[x][0], -ref[x][1]));
                 const uint64_t u = add2(z, pack2(w.z, w.w));
                 float &y0 = s[b][x][2 * n], &y1 = s[b][x][2 * n + 1];
@@ -912,7 +506,7 @@ paged_attention_kernel(const Args a) {
       };
       if (!ragged) weigh(std::false_type());
       else weigh(std::true_type());
-      if constexpr (kCode) {
+      if constexpr (kF8) {
         // Out of line, so that what is rare costs the usual path no registers.
         float most = 0.f;
 #pragma unroll
@@ -925,7 +519,7 @@ paged_attention_kernel(const Args a) {
             for (int j = 0; j < 2; ++j) far |= sum[x][j] < 1.f / kFar && mx[x][j] > kLowest;
         }
         if (__any_sync(0xffffffffu, far)) {
-          TileCode<D, kNR> z;
+          CodeTile<D, kNR> z;
 #pragma unroll
           for (int x = 0; x < kNR; ++x) {
 #pragma unroll
@@ -938,7 +532,7 @@ paged_attention_kernel(const Args a) {
               z.ref[x][j] = ref[x][j], z.l[x][j] = l[x][j], z.m[x][j] = m[x][j];
             }
           }
-          take_again<D, kBits, kNR>(z, sk, scales, first);
+          take_again<D, kNR>(z, sk, scales, first);
 #pragma unroll
           for (int x = 0; x < kNR; ++x) {
 #pragma unroll
@@ -971,12 +565,12 @@ paged_attention_kernel(const Args a) {
           for (int j = 0; j < 2; ++j) {
             const float f = fast_exp2(m[x][j] - mx[x][j]);
             m[x][j] = mx[x][j];
-            if (!kCode) l[x][j] *= f;
+            if (!kF8) l[x][j] *= f;
 #pragma unroll
             for (int n = 0; n < kMT; ++n) o[n][x][j] *= f, o[n][x][2 + j] *= f;
           }
       }
-      if constexpr (kCode) {
+      if constexpr (kF8) {
 #pragma unroll
         for (int x = 0; x < kNR; ++x) l[x][0] = sum[x][0], l[x][1] = sum[x][1];
       }
@@ -995,9 +589,9 @@ paged_attention_kernel(const Args a) {
 #pragma unroll
           for (int n = 0; n < 2; ++n) {
             float y[2];
-            if constexpr (kCode) {
+            if constexpr (kF8) {
               const uint64_t z = add2(both(s[b][x][2 * n], s[b][x][2 * n + 1]),
-                                      both(kPShift<kBits> - m[x][0], kPShift<kBits> - m[x][1]));
+                                      both(kPShift - m[x][0], kPShift - m[x][1]));
               y[0] = fast_exp2(lo_f(z)), y[1] = fast_exp2(hi_f(z));
             } else {
 #pragma unroll
@@ -1006,110 +600,101 @@ paged_attention_kernel(const Args a) {
                 l[x][j] += y[j];
               }
             }
-            p[b][x][n] = transposed(kCode ? pack_f16(y[0], y[1]) : pack_bf16(y[0], y[1]));
+            p[b][x][n] = transposed(kF8 ? pack_f16(y[0], y[1]) : pack_bf16(y[0], y[1]));
           }
       // ---- O^T += V^T P^T, 16 keys at a time
 #pragma unroll
       for (int b = 0; b < kNB; ++b) {
-        if constexpr (kBits == 4) {
-          add_values4<D, kNR>(o, p[b], sv, scales + 2 * C::kKW, b, g, t, ragged && a.n_new > 1,
-                              [&](int x, int k) {
-            return key0 + k < cur.len - a.n_new + 1 +
-                                  (int)quotient((cur.unit % a.row_tiles) * kRows + 8 * x + g,
-                                                a.group);
-          });
-        } else {
-          // This lane's V rows: the keys of MMA indices 2t, 2t+1 (+ 8).  vf[n][hi] holds their
-          // values of dimension E g + n (bf16: + 56 for n >= 8), E = kNT in 8 bits, else 8.
-          uint32_t vf[kNT][2];
+        // This lane's V rows: the keys of MMA indices 2t, 2t+1 (+ 8).  vf[n][hi] holds their
+        // values of dimension E g + n (bf16: + 56 for n >= 8), E = kNT in 8 bits, else 8.
+        uint32_t vf[kNT][2];
 #pragma unroll
-          for (int hi = 0; hi < 2; ++hi) {
-            const int ra = 16 * b + 8 * hi + key_of<kCh>(2 * t);
-            const int rb = 16 * b + 8 * hi + key_of<kCh>(2 * t + 1);
-            const uint32_t pa = sv + ra * C::kRowBytes, pb = sv + rb * C::kRowBytes;
-            if (kCode) {
-              uint32_t wa[4] = {0, 0, 0, 0}, wb[4] = {0, 0, 0, 0};
-              if (D == 128) {
-                const uint4 y = lds128(pa + 16 * v_chunk<kCh>(g, ra));
-                const uint4 z = lds128(pb + 16 * v_chunk<kCh>(g, rb));
-                wa[0] = y.x, wa[1] = y.y, wa[2] = y.z, wa[3] = y.w;
-                wb[0] = z.x, wb[1] = z.y, wb[2] = z.z, wb[3] = z.w;
-              } else {
-                const uint2 y = lds64(pa + 16 * v_chunk<kCh>(g >> 1, ra) + 8 * (g & 1));
-                const uint2 z = lds64(pb + 16 * v_chunk<kCh>(g >> 1, rb) + 8 * (g & 1));
-                wa[0] = y.x, wa[1] = y.y, wb[0] = z.x, wb[1] = z.y;
-              }
-#pragma unroll
-              for (int w = 0; w < kNT / 4; ++w) {
-                const uint32_t y = __byte_perm(wa[w], wb[w], 0x5140);
-                const uint32_t z = __byte_perm(wa[w], wb[w], 0x7362);
-                vf[4 * w][hi] = f16x2_of_e4m3x2(y);
-                vf[4 * w + 1][hi] = f16x2_of_e4m3x2(y >> 16);
-                vf[4 * w + 2][hi] = f16x2_of_e4m3x2(z);
-                vf[4 * w + 3][hi] = f16x2_of_e4m3x2(z >> 16);
-              }
+        for (int hi = 0; hi < 2; ++hi) {
+          const int ra = 16 * b + 8 * hi + key_of<kCh>(2 * t);
+          const int rb = 16 * b + 8 * hi + key_of<kCh>(2 * t + 1);
+          const uint32_t pa = sv + ra * C::kRowBytes, pb = sv + rb * C::kRowBytes;
+          if (kF8) {
+            uint32_t wa[4] = {0, 0, 0, 0}, wb[4] = {0, 0, 0, 0};
+            if (D == 128) {
+              const uint4 y = lds128(pa + 16 * v_chunk<kCh>(g, ra));
+              const uint4 z = lds128(pb + 16 * v_chunk<kCh>(g, rb));
+              wa[0] = y.x, wa[1] = y.y, wa[2] = y.z, wa[3] = y.w;
+              wb[0] = z.x, wb[1] = z.y, wb[2] = z.z, wb[3] = z.w;
             } else {
-#pragma unroll
-              for (int half = 0; half < kNT / 8; ++half) {
-                const uint4 y = lds128(pa + 16 * v_chunk<kCh>(g + 8 * half, ra));
-                const uint4 z = lds128(pb + 16 * v_chunk<kCh>(g + 8 * half, rb));
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                  vf[8 * half + 2 * w][hi] = __byte_perm(word(y, w), word(z, w), 0x5410);
-                  vf[8 * half + 2 * w + 1][hi] = __byte_perm(word(y, w), word(z, w), 0x7632);
-                }
-              }
+              const uint2 y = lds64(pa + 16 * v_chunk<kCh>(g >> 1, ra) + 8 * (g & 1));
+              const uint2 z = lds64(pb + 16 * v_chunk<kCh>(g >> 1, rb) + 8 * (g & 1));
+              wa[0] = y.x, wa[1] = y.y, wb[0] = z.x, wb[1] = z.y;
             }
-          }
-          // A key that some of the rows may not see must not reach them by 0 * NaN: where a
-          // value among the newest keys is not finite, each token's rows take the product
-          // with the keys behind their own as zeros.
-          bool apart = false;
-          if (ragged && a.n_new > 1) {
-            bool odd = false;
-            constexpr uint32_t kExp = kCode ? 0x7c00u : 0x7f80u;
 #pragma unroll
-            for (int n = 0; n < kNT; ++n)
-#pragma unroll
-              for (int hi = 0; hi < 2; ++hi)
-                odd |= (vf[n][hi] & kExp) == kExp || (vf[n][hi] >> 16 & kExp) == kExp;
-            apart = __any_sync(0xffffffffu, odd);
-          }
-          if (!apart) {
-#pragma unroll
-            for (int n = 0; n < kMT; ++n) {
-              const uint32_t v[4] = {vf[2 * n][0], vf[2 * n + 1][0], vf[2 * n][1], vf[2 * n + 1][1]};
-#pragma unroll
-              for (int x = 0; x < kNR; ++x) mma<kCode>(o[n][x], v, p[b][x][0], p[b][x][1]);
+            for (int w = 0; w < kNT / 4; ++w) {
+              const uint32_t y = __byte_perm(wa[w], wb[w], 0x5140);
+              const uint32_t z = __byte_perm(wa[w], wb[w], 0x7362);
+              vf[4 * w][hi] = f16x2_of_e4m3x2(y);
+              vf[4 * w + 1][hi] = f16x2_of_e4m3x2(y >> 16);
+              vf[4 * w + 2][hi] = f16x2_of_e4m3x2(z);
+              vf[4 * w + 3][hi] = f16x2_of_e4m3x2(z >> 16);
             }
           } else {
-            const int r0 = (cur.unit % a.row_tiles) * kRows;
-            const int i1 = (min(a.rows, r0 + kRows) - 1) / (int)a.group.d;
-            for (int i = r0 / (int)a.group.d; i <= i1; ++i) {
-              const int lim = cur.len - a.n_new + i + 1;
-              uint32_t keep[2];
 #pragma unroll
-              for (int hi = 0; hi < 2; ++hi) {
-                const int k = key0 + 16 * b + 8 * hi;
-                keep[hi] = (k + key_of<kCh>(2 * t) < lim ? 0xffffu : 0u) |
-                           (k + key_of<kCh>(2 * t + 1) < lim ? 0xffff0000u : 0u);
+            for (int half = 0; half < kNT / 8; ++half) {
+              const uint4 y = lds128(pa + 16 * v_chunk<kCh>(g + 8 * half, ra));
+              const uint4 z = lds128(pb + 16 * v_chunk<kCh>(g + 8 * half, rb));
+#pragma unroll
+              for (int w = 0; w < 4; ++w) {
+                vf[8 * half + 2 * w][hi] = __byte_perm(word(y, w), word(z, w), 0x5410);
+                vf[8 * half + 2 * w + 1][hi] = __byte_perm(word(y, w), word(z, w), 0x7632);
               }
-              // the other tokens' sums stand aside: they take nothing, not 0 * NaN
+            }
+          }
+        }
+        // A key that some of the rows may not see must not reach them by 0 * NaN: where a
+        // value among the newest keys is not finite, each token's rows take the product
+        // with the keys behind their own as zeros.
+        bool apart = false;
+        if (ragged && a.n_new > 1) {
+          bool odd = false;
+          constexpr uint32_t kExp = kF8 ? 0x7c00u : 0x7f80u;
 #pragma unroll
-              for (int n = 0; n < kMT; ++n) {
-                const uint32_t v[4] = {vf[2 * n][0] & keep[0], vf[2 * n + 1][0] & keep[0],
-                                       vf[2 * n][1] & keep[1], vf[2 * n + 1][1] & keep[1]};
+          for (int n = 0; n < kNT; ++n)
 #pragma unroll
-                for (int x = 0; x < kNR; ++x) {
-                  float y[4] = {0.f, 0.f, 0.f, 0.f};
-                  mma<kCode>(y, v, p[b][x][0], p[b][x][1]);
+            for (int hi = 0; hi < 2; ++hi)
+              odd |= (vf[n][hi] & kExp) == kExp || (vf[n][hi] >> 16 & kExp) == kExp;
+          apart = __any_sync(0xffffffffu, odd);
+        }
+        if (!apart) {
 #pragma unroll
-                  for (int j = 0; j < 2; ++j)
-                    if (limit(x, j) == lim && r0 + 8 * x + 2 * t + j < a.rows) {
-                      o[n][x][j] += y[j];
-                      o[n][x][2 + j] += y[2 + j];
-                    }
-                }
+          for (int n = 0; n < kMT; ++n) {
+            const uint32_t v[4] = {vf[2 * n][0], vf[2 * n + 1][0], vf[2 * n][1], vf[2 * n + 1][1]};
+#pragma unroll
+            for (int x = 0; x < kNR; ++x) mma<kF8>(o[n][x], v, p[b][x][0], p[b][x][1]);
+          }
+        } else {
+          const int r0 = (cur.unit % a.row_tiles) * kRows;
+          const int i1 = (min(a.rows, r0 + kRows) - 1) / (int)a.group.d;
+          for (int i = r0 / (int)a.group.d; i <= i1; ++i) {
+            const int lim = cur.len - a.n_new + i + 1;
+            uint32_t keep[2];
+#pragma unroll
+            for (int hi = 0; hi < 2; ++hi) {
+              const int k = key0 + 16 * b + 8 * hi;
+              keep[hi] = (k + key_of<kCh>(2 * t) < lim ? 0xffffu : 0u) |
+                         (k + key_of<kCh>(2 * t + 1) < lim ? 0xffff0000u : 0u);
+            }
+            // the other tokens' sums stand aside: they take nothing, not 0 * NaN
+#pragma unroll
+            for (int n = 0; n < kMT; ++n) {
+              const uint32_t v[4] = {vf[2 * n][0] & keep[0], vf[2 * n + 1][0] & keep[0],
+                                     vf[2 * n][1] & keep[1], vf[2 * n + 1][1] & keep[1]};
+#pragma unroll
+              for (int x = 0; x < kNR; ++x) {
+                float y[4] = {0.f, 0.f, 0.f, 0.f};
+                mma<kF8>(y, v, p[b][x][0], p[b][x][1]);
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                  if (limit(x, j) == lim && r0 + 8 * x + 2 * t + j < a.rows) {
+                    o[n][x][j] += y[j];
+                    o[n][x][2 + j] += y[2 + j];
+                  }
               }
             }
           }
@@ -1133,7 +718,7 @@ paged_attention_kernel(const Args a) {
           if (g == 0) {
             sh_m[warp][8 * x + 2 * t + j] = m[x][j];
             sh_l[warp][8 * x + 2 * t + j] = l[x][j];
-            if constexpr (kCode) sh_r[warp][8 * x + 2 * t + j] = l[x][j] == 0.f ? kLowest : ref[x][j];
+            if constexpr (kF8) sh_r[warp][8 * x + 2 * t + j] = l[x][j] == 0.f ? kLowest : ref[x][j];
           }
         }
       __syncwarp();   // every lane has read the stage
@@ -1163,13 +748,13 @@ paged_attention_kernel(const Args a) {
             const int r = 8 * x + 2 * t + j;
             // 8 bits: the warps' M relative to the largest R
             R[j] = 0.f;
-            if constexpr (kCode) {
+            if constexpr (kF8) {
               R[j] = sh_r[0][r];
 #pragma unroll
               for (int w = 1; w < kWarps; ++w) R[j] = fmaxf(R[j], sh_r[w][r]);
             }
             auto level = [&](int w) {
-              return kCode ? sh_r[kCode ? w : 0][r] - R[j] + sh_m[w][r] : sh_m[w][r];
+              return kF8 ? sh_r[kF8 ? w : 0][r] - R[j] + sh_m[w][r] : sh_m[w][r];
             };
             M[j] = level(0);
 #pragma unroll
@@ -1178,7 +763,7 @@ paged_attention_kernel(const Args a) {
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
               f[j][w] = fast_exp2(level(w) - M[j]);
-              sum[j] = fmaf(sh_l[w][r], kCode ? fast_exp2(sh_r[kCode ? w : 0][r] - R[j]) : f[j][w],
+              sum[j] = fmaf(sh_l[w][r], kF8 ? fast_exp2(sh_r[kF8 ? w : 0][r] - R[j]) : f[j][w],
                             sum[j]);
             }
           }
@@ -1196,7 +781,7 @@ paged_attention_kernel(const Args a) {
             }
           }
           // block n holds dimensions E g + 2 n and the next (bf16: + 56 from n = 4 on)
-          constexpr int kE = kCode ? kNT : 8;
+          constexpr int kE = kF8 ? kNT : 8;
           const int n0 = warp * kQuarter;
           const int d = kE * g + (kE == 8 ? (n0 / 4) * 64 + 2 * (n0 % 4) : 2 * n0);
 #pragma unroll
@@ -1205,7 +790,7 @@ paged_attention_kernel(const Args a) {
             if (r >= a.rows) continue;
             if (whole) {
               const float inv = sum[j] > 0.f ? 1.f / sum[j] : sum[j] == 0.f ? 0.f : sum[j];
-              const float up = kCode ? fast_exp2(M[j] - kPShift<kBits>) : 1.f;
+              const float up = kF8 ? fast_exp2(M[j] - kPShift) : 1.f;
               const int i = quotient(r, a.group);
               __nv_bfloat16 *dst = a.out + ((size_t)((size_t)cur.b * a.n_new + i) * a.Hq +
                                             h * (int)a.group.d + (r - i * (int)a.group.d)) * D + d;
@@ -1226,7 +811,7 @@ paged_attention_kernel(const Args a) {
                 float *stat = part + kRows * D + C::kStat * rr;
                 stat[0] = M[j];
                 stat[1] = sum[j];
-                if (kCode) stat[2] = R[j];
+                if (kF8) stat[2] = R[j];
               }
             }
           }
@@ -1252,114 +837,12 @@ paged_attention_kernel(const Args a) {
   clear_empty<D>(a);
 }
 
-// Joins a row's parts where several blocks shared its unit: one block for each block of
-// the kernel before and each row, and most of them find that theirs ended no such unit.
-// A part takes D/4 lanes, four dimensions each; bound by the round trips to L2, so each
-// lane group loads eight parts at once, and statistics with sums.  In 8 bits, with a third
-// statistic, four: with eight it fits an SM three blocks or spills (48 ragged sequences 9.4
-// against 6.6 us, 12 heads x 64 of 16 sequences 8.4 against 6.4).
-constexpr int kJoinThreads = 256;
-
-template <int D, int kBits, int kNR>
-__global__ void __launch_bounds__(kJoinThreads, 4)
-paged_join_kernel(const Args a) {
-  using C = Cfg<D, kBits, kNR>;
-  constexpr bool kCode = C::kCode;
-  constexpr int kRows = 8 * kNR, kL = D / 4, kGroups = kJoinThreads / kL;
-  constexpr int kAtOnce = kCode ? 4 : 8;
-  __shared__ float4 sh_o[kJoinThreads];
-  __shared__ float4 sh_stat[kGroups];    // M, l, R
-  pdl_wait();
-  pdl_trigger();
-  const CutUnit u = a.cuts[blockIdx.x];
-  if (u.parts == 0) return;
-  const int h = u.unit / a.row_tiles, rr = blockIdx.y, r = (u.unit - h * a.row_tiles) * kRows + rr;
-  if (r >= a.rows) return;
-  const int sub = threadIdx.x % kL, group = threadIdx.x / kL;
-  // in 8 bits L and M are relative to R
-  float M = kLowest, R = kLowest, L = 0.f;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  auto level = [&](const float4 &w) { return kCode ? w.z - R + w.x : w.x; };
-  auto refer = [&](float to_r) {   // R rises
-    if (!kCode) return;
-    L *= fast_exp2(R - to_r);
-    M = fmaxf(M + (R - to_r), kLowest);
-    R = to_r;
-  };
-  auto add = [&](const float4 &w, const float4 &x) {
-    const float f = fast_exp2(level(w) - M);
-    L = fmaf(kCode ? fast_exp2(w.z - R) : f, w.y, L);
-    acc.x = fmaf(f, x.x, acc.x);
-    acc.y = fmaf(f, x.y, acc.y);
-    acc.z = fmaf(f, x.z, acc.z);
-    acc.w = fmaf(f, x.w, acc.w);
-  };
-  for (int p0 = group; p0 < u.parts; p0 += kAtOnce * kGroups) {
-    float4 w[kAtOnce], x[kAtOnce];
-#pragma unroll
-    for (int y = 0; y < kAtOnce; ++y) {
-      const int p = p0 + y * kGroups;
-      w[y] = make_float4(kLowest, 0.f, kLowest, 0.f);
-      x[y] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (p < u.parts) {
-        const float *part = a.ws + (size_t)(p ? 2 * (u.first + p) : u.slot) * C::kPart;
-        const float *stat = part + kRows * D + C::kStat * rr;
-        if constexpr (kCode) {
-          w[y] = *reinterpret_cast<const float4 *>(stat);
-        } else {
-          const float2 z = *reinterpret_cast<const float2 *>(stat);
-          w[y].x = z.x, w[y].y = z.y;
-        }
-        x[y] = *reinterpret_cast<const float4 *>(part + rr * D + 4 * sub);
-      }
-    }
-    float to_r = R;
-#pragma unroll
-    for (int y = 0; y < kAtOnce; ++y) to_r = fmaxf(to_r, w[y].z);
-    refer(to_r);
-    float to = M;
-#pragma unroll
-    for (int y = 0; y < kAtOnce; ++y) to = fmaxf(to, level(w[y]));
-    const float f0 = fast_exp2(M - to);
-    M = to;
-    if (!kCode) L *= f0;
-    acc.x *= f0, acc.y *= f0, acc.z *= f0, acc.w *= f0;
-#pragma unroll
-    for (int y = 0; y < kAtOnce; ++y) add(w[y], x[y]);
-  }
-  sh_o[threadIdx.x] = acc;
-  if (sub == 0) sh_stat[group] = make_float4(M, L, R, 0.f);
-  __syncthreads();
-  if (group) return;
-#pragma unroll
-  for (int y = 0; y < kGroups; ++y) R = fmaxf(R, sh_stat[y].z);
-  M = kLowest;
-#pragma unroll
-  for (int y = 0; y < kGroups; ++y) M = fmaxf(M, level(sh_stat[y]));
-  L = 0.f;
-  acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-  for (int y = 0; y < kGroups; ++y) add(sh_stat[y], sh_o[y * kL + sub]);
-  const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;
-  const float up = kCode ? fast_exp2(M - kPShift<kBits>) : 1.f;
-  const int i = quotient(r, a.group);
-  reinterpret_cast<uint2 *>(a.out + ((size_t)((size_t)u.b * a.n_new + i) * a.Hq +
-                                     h * (int)a.group.d +
-                                     (r - i * (int)a.group.d)) * D)[sub] =
-      make_uint2(pack_bf16(acc.x * inv * up, acc.y * inv * up),
-                 pack_bf16(acc.z * inv * up, acc.w * inv * up));
-}
-
 // -------------------------------------------------------------- host side
 
-size_t workspace_bytes(int D) {
-  return (size_t)sm_count() * kMaxPerSm * (sizeof(CutUnit) + 2 * kMostRows * ((size_t)D + 4) * 4);
-}
-
-template <int D, int kBits, int kNR>
-int launch(Args &a, void *workspace, cudaStream_t stream) {
-  using C = Cfg<D, kBits, kNR>;
-  auto kernel = paged_attention_kernel<D, kBits, kNR>;
+template <int D, bool kF8, int kNR>
+int launch(PagedArgs &a, void *workspace, cudaStream_t stream) {
+  using C = Cfg<D, kF8, kNR>;
+  auto kernel = paged_attention_kernel<D, kF8, kNR>;
   static std::atomic<int> per_sm[64];
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return HSA_ERR_CUDA;
@@ -1372,7 +855,7 @@ int launch(Args &a, void *workspace, cudaStream_t stream) {
             cudaSuccess ||
         cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout,
                              cudaSharedmemCarveoutMaxShared) != cudaSuccess ||
-        cudaFuncSetAttribute(paged_join_kernel<D, kBits, kNR>,
+        cudaFuncSetAttribute(paged_join_kernel<D, kF8, kNR>,
                              cudaFuncAttributePreferredSharedMemoryCarveout,
                              cudaSharedmemCarveoutMaxShared) != cudaSuccess ||
         cudaOccupancyMaxActiveBlocksPerMultiprocessor(&nb, kernel, kThreads, C::kSmem) !=
@@ -1393,7 +876,7 @@ int launch(Args &a, void *workspace, cudaStream_t stream) {
   count_launches(2);
   launch_pdl(kernel, dim3((unsigned)grid), dim3(kThreads), C::kSmem, stream, a);
   if (cudaGetLastError() != cudaSuccess) return HSA_ERR_CUDA;
-  launch_pdl(paged_join_kernel<D, kBits, kNR>,
+  launch_pdl(paged_join_kernel<D, kF8, kNR>,
              dim3((unsigned)grid, (unsigned)std::min(a.rows, C::kRows)), dim3(kJoinThreads), 0,
              stream, a);
   return launch_status();
@@ -1406,13 +889,13 @@ int launch(Args &a, void *workspace, cudaStream_t stream) {
 // against 75, 143 against 135; 24 rows at D = 64 in 8 bits 55 against 66).  8-bit keys at
 // D = 128 leave it too few registers (24 rows, with the sum of the weights relative to the
 // probabilities' maximum, 84 against 73 us).
-template <int D, int kBits>
-int launch_rows(Args &a, void *workspace, cudaStream_t stream) {
-  if (a.rows <= 8) return launch<D, kBits, 1>(a, workspace, stream);
-  if constexpr (kBits == 16 || (kBits == 8 && D == 64))
+template <int D, bool kF8>
+int launch_rows(PagedArgs &a, void *workspace, cudaStream_t stream) {
+  if (a.rows <= 8) return launch<D, kF8, 1>(a, workspace, stream);
+  if constexpr (!(kF8 && D == 128))
     if (5 * ((a.rows + 31) / 32) < 3 * ((a.rows + 15) / 16))
-      return launch<D, kBits, 4>(a, workspace, stream);
-  return launch<D, kBits, 2>(a, workspace, stream);
+      return launch<D, kF8, 4>(a, workspace, stream);
+  return launch<D, kF8, 2>(a, workspace, stream);
 }
 
 }  // namespace
@@ -1456,7 +939,7 @@ extern "C" int hsa_paged_attention(const void *q, int batch, int n_new, int Hq, 
     return HSA_ERR_INVALID_ARG;
   if (!workspace || !aligned16(workspace) || size < workspace_bytes(D)) return HSA_ERR_WORKSPACE;
   if (!(scale > 0.f) || !std::isfinite(scale)) scale = 1.f / std::sqrt((float)D);
-  Args a;
+  PagedArgs a;
   a.q = static_cast<const __nv_bfloat16 *>(q);
   a.k = static_cast<const uint8_t *>(k_pages);
   a.v = static_cast<const uint8_t *>(v_pages);
@@ -1479,6 +962,7 @@ extern "C" int hsa_paged_attention(const void *q, int batch, int n_new, int Hq, 
   a.n_pages = n_pages;
   a.max_pages = n_pages > 0 ? max_pages : 0;
   a.sms = sm_count();
+  a.side = 1;
   a.page_log2 = 0;
   while ((1 << a.page_log2) < page_size) ++a.page_log2;
   a.scale_log2 = scale * 1.4426950408889634f;
@@ -1486,9 +970,10 @@ extern "C" int hsa_paged_attention(const void *q, int batch, int n_new, int Hq, 
   a.scale_digits = 2.f * std::frexp(std::min(a.scale_log2, 3.4e38f), &power);   // in [1, 2)
   a.scale_power = std::ldexp(1.f, power - 1);
   cudaStream_t s = (cudaStream_t)stream;
-  if (f4)
-    return D == 128 ? launch_rows<128, 4>(a, workspace, s) : launch_rows<64, 4>(a, workspace, s);
+  if (f4) return launch_paged4(a, D, workspace, s);
   if (f8)
-    return D == 128 ? launch_rows<128, 8>(a, workspace, s) : launch_rows<64, 8>(a, workspace, s);
-  return D == 128 ? launch_rows<128, 16>(a, workspace, s) : launch_rows<64, 16>(a, workspace, s);
+    return D == 128 ? launch_rows<128, true>(a, workspace, s)
+                    : launch_rows<64, true>(a, workspace, s);
+  return D == 128 ? launch_rows<128, false>(a, workspace, s)
+                  : launch_rows<64, false>(a, workspace, s);
 }

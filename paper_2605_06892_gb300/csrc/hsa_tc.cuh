@@ -4,92 +4,18 @@
 // work together.
 #pragma once
 
-#include <cuda.h>
-#include <cudaTypedefs.h>
 #include <cuda_bf16.h>
 
 #include <atomic>
 
 #include "hsa_internal.cuh"
 #include "hsa_ptx.cuh"
+#include "hsa_tma.cuh"
 
 namespace hsa {
 namespace {
 
 // ----------------------------------------------------------- PTX wrappers
-
-__device__ __forceinline__ void mbar_init(uint64_t *b, uint32_t count) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(b)), "r"(count)
-               : "memory");
-}
-
-__device__ __forceinline__ void mbar_expect_tx(uint64_t *b, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_addr(b)),
-               "r"(bytes)
-               : "memory");
-}
-
-__device__ __forceinline__ void mbar_arrive(uint64_t *b) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(b)) : "memory");
-}
-
-// Non-blocking test of phase `parity` (never suspends the thread).
-__device__ __forceinline__ bool mbar_peek(uint64_t *b, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n"
-      " selp.u32 %0, 1, 0, p;\n}\n"
-      : "=r"(ok)
-      : "r"(smem_addr(b)), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-
-// try_wait that lets the hardware suspend the thread for up to ~0.5 ms while
-// the phase is incomplete, so waiting warps take no issue slots from the
-// working ones.
-__device__ __forceinline__ bool mbar_test_suspend(uint64_t *b, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n"
-      " selp.u32 %0, 1, 0, p;\n}\n"
-      : "=r"(ok)
-      : "r"(smem_addr(b)), "r"(parity), "r"(500000u)
-      : "memory");
-  return ok != 0;
-}
-
-// About one second at the GB300 clock.
-constexpr long long kWaitCycles = 2000000000LL;
-
-// Bounded wait on phase `parity` of barrier b.  Gives up when the time runs
-// out (records the timeout and raises the CTA's abort flag) or, if
-// `honor_abort`, as soon as another role has raised the abort flag.  The
-// first test is a non-blocking test_wait (a try_wait costs far more even on a
-// completed phase); between tests the thread suspends in try_wait.
-__device__ __forceinline__ bool mbar_wait(uint64_t *b, uint32_t parity, volatile int *abort_flag,
-                                          unsigned *err, bool honor_abort = true) {
-  if (mbar_peek(b, parity)) return true;
-  const long long t0 = clock64();
-  while (true) {
-    if (mbar_test_suspend(b, parity)) return true;
-    if (honor_abort && *abort_flag) return false;
-    if (clock64() - t0 > kWaitCycles) {
-      set_error(err, kErrTimeout);
-      *abort_flag = 1;
-      return false;
-    }
-  }
-}
-
-__device__ __forceinline__ void tma_load_2d(void *dst, const CUtensorMap *map, uint64_t *bar,
-                                            int x, int y) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes"
-      " [%0], [%1, {%3, %4}], [%2];" ::"r"(smem_addr(dst)),
-      "l"(map), "r"(smem_addr(bar)), "r"(x), "r"(y)
-      : "memory");
-}
 
 __device__ __forceinline__ void fence_before() {
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -110,14 +36,6 @@ __device__ __forceinline__ uint64_t sdesc(uint32_t saddr, uint32_t lbo, uint32_t
 __host__ __device__ constexpr uint32_t idesc_bf16(int M, int N, int b_mn_major) {
   return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)b_mn_major << 16) |
          ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
-}
-
-// One lane of the warp: 1 in it, 0 in the others.
-__device__ __forceinline__ uint32_t elect_one() {
-  uint32_t r;
-  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n"
-               : "=r"(r));
-  return r;
 }
 
 // The MMAs and commits are issued by the lane with lead != 0, but every lane of
@@ -670,22 +588,6 @@ __device__ __forceinline__ void tc_watch_s(const TcPipe &p, const TcSpan &w) {
 }
 
 // -------------------------------------------------------------- host side
-
-inline PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
-  static std::atomic<PFN_cuTensorMapEncodeTiled_v12000> fn{nullptr};
-  PFN_cuTensorMapEncodeTiled_v12000 f = fn.load();
-  if (!f) {
-    cudaDriverEntryPointQueryResult q;
-    void *p = nullptr;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault,
-                                         &q) != cudaSuccess ||
-        q != cudaDriverEntryPointSuccess)
-      return nullptr;
-    f = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
-    fn.store(f);
-  }
-  return f;
-}
 
 // 2-D map over N rows of `cols` bf16 values, `row` elements apart: boxes of 64 columns x
 // 128 rows, 128-byte swizzle, rows past N read as zero.

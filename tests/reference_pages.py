@@ -91,7 +91,7 @@ P_STEP = 2.0 ** -10 + 2.0 ** -22
 
 def small_weights(q, k, v_word, limit, scale=None):
     """What the fp16 probabilities may lose below their normal range [n, Hq, 1]: a key's weight
-    times the power of two of its value row is held within 2^-35 of the largest such product, and
+    times the power of two of its value row is held within 2^-31 of the largest such product, and
     its product with a factor again; each meets a factor of up to 63 and a code of up to 6."""
     n, Hq, D = q.shape
     m, Hkv = k.shape[:2]
@@ -103,7 +103,7 @@ def small_weights(q, k, v_word, limit, scale=None):
             c = int(limit[i])
             if c > 0:
                 w = torch.softmax((k[:c, h * Hkv // Hq] @ q[i, h]) * scale, 0)
-                out[i, h] = c * 2.0 ** -35 * (378 + 6) * (w * power[:c, h * Hkv // Hq]).max()
+                out[i, h] = c * 2.0 ** -31 * (378 + 6) * (w * power[:c, h * Hkv // Hq]).max()
     return out
 
 
