@@ -10,9 +10,13 @@
 // vectors of eight values a thread, and the warps' sums meet in shared memory.
 #include <cuda_bf16.h>
 
+#include <algorithm>
+#include <atomic>
 #include <cmath>
 
 #include "hsa_internal.cuh"
+#include "hsa_ptx.cuh"
+#include "hsa_tma.cuh"
 
 namespace hsa {
 namespace {
@@ -21,6 +25,7 @@ constexpr int kThreads = 256;
 constexpr int kMaxD = 256;
 constexpr int kHeads = 4;        // heads of a lane group at a time
 constexpr float kDown = 0x1p-80f;
+constexpr int kRingTokens = 1;   // tokens per SM from which on the ring takes them
 
 __device__ __forceinline__ uint4 ld16(const void *p) {
   uint4 v;   // not the read-only path: the rows may be written in place
@@ -50,77 +55,106 @@ __device__ __forceinline__ void store8(uint8_t *p, const Eight<kF32> &v) {
   reinterpret_cast<uint4 *>(p)[0] = v.w[0];
   if (kF32) reinterpret_cast<uint4 *>(p)[kF32 ? 1 : 0] = v.w[kF32 ? 1 : 0];
 }
+// Eight values in 32 bits, the even ones apart from the odd: (x0, x2), (x4, x6), (x1, x3),
+// (x5, x7), so that two pairs turn in one packed instruction.
+struct Values {
+  uint64_t a[2], b[2];
+};
 template <bool kF32>
-__device__ __forceinline__ void unpack8(const Eight<kF32> &v, float (&x)[8]) {
-  const uint32_t w[4] = {v.w[0].x, v.w[0].y, v.w[0].z, v.w[0].w};
+__device__ __forceinline__ Values unpack8(const Eight<kF32> &v) {
+  Values x;
+  const uint4 &p = v.w[0], &q = v.w[kF32 ? 1 : 0];
   if (kF32) {
-    const uint4 &q = v.w[kF32 ? 1 : 0];
-    const uint32_t u[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(w[i]), x[4 + i] = __uint_as_float(u[i]);
+    x.a[0] = pack2(p.x, p.z), x.b[0] = pack2(p.y, p.w);
+    x.a[1] = pack2(q.x, q.z), x.b[1] = pack2(q.y, q.w);
   } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    constexpr uint32_t kHigh = 0xffff0000u;
+    x.a[0] = pack2(p.x << 16, p.y << 16), x.b[0] = pack2(p.x & kHigh, p.y & kHigh);
+    x.a[1] = pack2(p.z << 16, p.w << 16), x.b[1] = pack2(p.z & kHigh, p.w & kHigh);
   }
+  return x;
 }
 template <bool kF32>
-__device__ __forceinline__ Eight<kF32> pack8(const float (&x)[8]) {
+__device__ __forceinline__ Eight<kF32> pack8(const Values &x) {
   Eight<kF32> v;
   if (kF32) {
-    v.w[0] = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]),
-                        __float_as_uint(x[3]));
-    v.w[kF32 ? 1 : 0] = make_uint4(__float_as_uint(x[4]), __float_as_uint(x[5]),
-                                   __float_as_uint(x[6]), __float_as_uint(x[7]));
+    v.w[0] = make_uint4((uint32_t)x.a[0], (uint32_t)x.b[0], x.a[0] >> 32, x.b[0] >> 32);
+    v.w[kF32 ? 1 : 0] = make_uint4((uint32_t)x.a[1], (uint32_t)x.b[1], x.a[1] >> 32, x.b[1] >> 32);
   } else {
-    v.w[0] = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]),
-                        pack_bf16(x[6], x[7]));
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      w[2 * i] = pack_bf16(lo_f(x.a[i]), lo_f(x.b[i]));
+      w[2 * i + 1] = pack_bf16(hi_f(x.a[i]), hi_f(x.b[i]));
+    }
+    v.w[0] = make_uint4(w[0], w[1], w[2], w[3]);
   }
   return v;
 }
+__device__ __forceinline__ uint64_t twice(float f) {
+  return pack2(__float_as_uint(f), __float_as_uint(f));
+}
 
-template <bool kF32>
-__device__ __forceinline__ float squares(const Eight<kF32> &v, float f) {
-  float x[8], s = 0.f;
-  unpack8<kF32>(v, x);
+__device__ __forceinline__ float squares(const Values &x) {
+  const uint64_t s = fma2(x.b[1], x.b[1], fma2(x.a[1], x.a[1], fma2(x.b[0], x.b[0],
+                                                                    mul2(x.a[0], x.a[0]))));
+  return lo_f(s) + hi_f(s);
+}
+// The squares of x 2^-80.
+__device__ __forceinline__ float small_squares(Values x) {
+  const uint64_t f = twice(kDown);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float y = x[i] * f;
-    s = fmaf(y, y, s);
-  }
-  return s;
+  for (int i = 0; i < 2; ++i) x.a[i] = mul2(x.a[i], f), x.b[i] = mul2(x.b[i], f);
+  return squares(x);
+}
+// 1 / sqrt(x) for x >= 1e-30: the approximation (within 2^-22), and where the result keeps more
+// than eight bits a step of Newton's method after it; zero for infinity.
+template <bool kF32>
+__device__ __forceinline__ float inverse_root(float x) {
+  float r;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  if (kF32) r = r > 0.f ? fmaf(0.5f * r, fmaf(-x * r, r, 1.f), r) : r;
+  return r;
 }
 
 // What a lane keeps of the weights and of the table's row for its eight dimensions.
 struct Turn {
-  float w[8], cs[8];   // cs: (cos, sin) of the four pairs
+  Values w;
+  uint64_t c[2], s[2], minus_s[2];   // of its pairs 0, 1 and 2, 3
 };
-__device__ __forceinline__ void read8(const float *p, float (&x)[8]) {
-  const float4 a = __ldg(reinterpret_cast<const float4 *>(p));
-  const float4 b = __ldg(reinterpret_cast<const float4 *>(p) + 1);
-  x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
-  x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+__device__ __forceinline__ Values values_of(const float4 &x, const float4 &y) {
+  Eight<true> v;
+  v.w[0] = make_uint4(__float_as_uint(x.x), __float_as_uint(x.y), __float_as_uint(x.z),
+                      __float_as_uint(x.w));
+  v.w[1] = make_uint4(__float_as_uint(y.x), __float_as_uint(y.y), __float_as_uint(y.z),
+                      __float_as_uint(y.w));
+  return unpack8<true>(v);
+}
+__device__ __forceinline__ Values weights_at(const float *p) {
+  if (!p) return Values{{twice(1.f), twice(1.f)}, {twice(1.f), twice(1.f)}};
+  return values_of(__ldg(reinterpret_cast<const float4 *>(p)),
+                   __ldg(reinterpret_cast<const float4 *>(p) + 1));
+}
+// (cos, sin) of four pairs at p.
+__device__ __forceinline__ void turn_by(Turn &t, const float4 &x, const float4 &y) {
+  const Values v = values_of(x, y);
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    t.c[i] = v.a[i], t.s[i] = v.b[i], t.minus_s[i] = v.b[i] ^ 0x8000000080000000ull;
 }
 
-// x times r (1 / the root), times the weights, turned.  `down`: the row's squares overflow in
-// 32 bits, and r is for x 2^-80.
+// x r (r: one over the root), times the weights, turned.
 template <bool kF32>
-__device__ __forceinline__ Eight<kF32> normed(const Eight<kF32> &v, float r, bool down,
-                                              const Turn &t, bool turn) {
-  float x[8];
-  unpack8<kF32>(v, x);
-  if (down) {
+__device__ __forceinline__ Eight<kF32> normed(Values x, float r, const Turn &t, bool turn) {
+  const uint64_t f = twice(r);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] *= kDown;
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = x[i] * r * t.w[i];
-  if (turn) {
-#pragma unroll
-    for (int i = 0; i < 8; i += 2) {
-      const float a = x[i], b = x[i + 1], c = t.cs[i], s = t.cs[i + 1];
-      x[i] = fmaf(a, c, -(b * s));
-      x[i + 1] = fmaf(a, s, b * c);
+  for (int i = 0; i < 2; ++i) {
+    x.a[i] = mul2(mul2(x.a[i], f), t.w.a[i]);
+    x.b[i] = mul2(mul2(x.b[i], f), t.w.b[i]);
+    if (turn) {
+      const uint64_t a = x.a[i], b = x.b[i];
+      x.a[i] = fma2(a, t.c[i], mul2(b, t.minus_s[i]));
+      x.b[i] = fma2(a, t.s[i], mul2(b, t.c[i]));
     }
   }
   return pack8<kF32>(x);
@@ -163,15 +197,59 @@ __device__ __forceinline__ Place place_of(const Args &a, int of, unsigned j) {
   return p;
 }
 
+// Lanes that share a head: known to the compiler for D = 64 and 128 (kLog), or any.
+template <int kLog>
+__device__ __forceinline__ int log_lanes(const Args &a) {
+  return kLog >= 0 ? kLog : a.lpr_log2;
+}
+
+// One over the roots of the mean squares of kN heads that a lane holds parts of, s: the lane's
+// sums.  Where a sum overflows (rare), from those of x 2^-80, next to which eps is nothing.  All
+// lanes call it.
+template <bool kF32, int kLog, int kN>
+__device__ __forceinline__ void head_roots(const Args &a, const Eight<kF32> (&v)[kN],
+                                           float (&r)[kN]) {
+  const int log = log_lanes<kLog>(a);
+  float s[kN];
+#pragma unroll
+  for (int y = 0; y < kN; ++y) s[y] = squares(unpack8<kF32>(v[y]));
+#pragma unroll
+  for (int o = 0; o < (kLog >= 0 ? kLog : 5); ++o)
+    if (kLog >= 0 || o < log)
+#pragma unroll
+      for (int y = 0; y < kN; ++y) s[y] += __shfl_xor_sync(0xffffffffu, s[y], 1 << o);
+  bool down = false;
+#pragma unroll
+  for (int y = 0; y < kN; ++y) {
+    r[y] = inverse_root<kF32>(fmaf(s[y], a.inv, a.eps));
+    down |= s[y] == INFINITY;
+  }
+  if (__any_sync(0xffffffffu, down)) {
+#pragma unroll 1
+    for (int y = 0; y < kN; ++y) {
+      float z = 0.f, was = 0.f;
+#pragma unroll
+      for (int i = 0; i < kN; ++i)
+        if (i == y) z = small_squares(unpack8<kF32>(v[i])), was = s[i];
+      for (int o = 0; o < log; ++o) z += __shfl_xor_sync(0xffffffffu, z, 1 << o);
+      z = inverse_root<kF32>(z * a.inv) * kDown;
+#pragma unroll
+      for (int i = 0; i < kN; ++i)
+        if (i == y && was == INFINITY) r[i] = z;
+    }
+  }
+}
+
 // A unit is the kHeads lane groups' heads of one token and tensor.
-template <bool kF32>
-__global__ void __launch_bounds__(kThreads) norm_heads_kernel(const Args a) {
+template <bool kF32, int kLog>
+__global__ void __launch_bounds__(kThreads, 3) norm_heads_kernel(const Args a) {
   pdl_wait();
   pdl_trigger();
   constexpr int kVec = kF32 ? 32 : 16;
-  const int L = 1 << a.lpr_log2, lane = threadIdx.x & 31, c = lane & (L - 1);
-  const int group = lane >> a.lpr_log2, groups = 32 >> a.lpr_log2;
-  const bool in = 8 * c < a.D;
+  const int log = log_lanes<kLog>(a), lane = threadIdx.x & 31, c = lane & ((1 << log) - 1);
+  const int group = lane >> log, groups = 32 >> log;
+  const int vecs8 = kLog >= 0 ? 1 << kLog : a.D / 8;
+  const bool in = kLog >= 0 || c < vecs8;
   const unsigned warps = gridDim.x * (kThreads / 32);
   for (unsigned long long i = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); i < a.items;
        i += warps) {
@@ -179,43 +257,32 @@ __global__ void __launch_bounds__(kThreads) norm_heads_kernel(const Args a) {
     const int u = (unsigned)i - j * a.units.d;
     const int of = u < a.first[1] ? 0 : u < a.first[2] ? 1 : 2;
     const int h0 = (u - a.first[of]) * groups * kHeads + group;
-    const Place p = place_of(a, of, j);
-    if (p.to < 0) continue;
+    const Place place = place_of(a, of, j);
+    if (place.to < 0) continue;
     Eight<kF32> v[kHeads] = {};
     const uint8_t *src = a.x[of] + (long long)j * a.in_row[of] + c * kVec;
-    uint8_t *dst = a.y[of] + p.to * a.out_row[of] + c * kVec;
+    uint8_t *dst = a.y[of] + place.to * a.out_row[of] + c * kVec;
 #pragma unroll
     for (int y = 0; y < kHeads; ++y)
       if (in && h0 + y * groups < a.H[of])
-        v[y] = load8<kF32>(src + (size_t)(h0 + y * groups) * (a.D / 8) * kVec);
+        v[y] = load8<kF32>(src + (size_t)(h0 + y * groups) * vecs8 * kVec);
     if (of < 2) {
       Turn t;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) t.w[e] = 1.f;
-      if (in && a.weight[of]) read8(a.weight[of] + 8 * c, t.w);
-      if (in && a.table) read8(a.table + (size_t)p.trow * a.D + 8 * c, t.cs);
-      float s[kHeads];
-#pragma unroll
-      for (int y = 0; y < kHeads; ++y) s[y] = squares<kF32>(v[y], 1.f);
-      for (int o = 1; o < L; o <<= 1)
-#pragma unroll
-        for (int y = 0; y < kHeads; ++y) s[y] += __shfl_xor_sync(0xffffffffu, s[y], o);
-#pragma unroll
-      for (int y = 0; y < kHeads; ++y) {
-        const bool down = s[y] == INFINITY;
-        float r = __frsqrt_rn(fmaf(s[y], a.inv, a.eps));
-        if (__any_sync(0xffffffffu, down)) {   // rare
-          float z = squares<kF32>(v[y], kDown);
-          for (int o = 1; o < L; o <<= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
-          if (down) r = __frsqrt_rn(z * a.inv);
-        }
-        v[y] = normed<kF32>(v[y], r, down, t, a.table != nullptr);
+      t.w = weights_at(in && a.weight[of] ? a.weight[of] + 8 * c : nullptr);
+      if (in && a.table) {
+        const float4 *row = reinterpret_cast<const float4 *>(a.table + (size_t)place.trow * a.D);
+        turn_by(t, __ldg(row + 2 * c), __ldg(row + 2 * c + 1));
       }
+      float r[kHeads];
+      head_roots<kF32, kLog, kHeads>(a, v, r);
+#pragma unroll
+      for (int y = 0; y < kHeads; ++y)
+        v[y] = normed<kF32>(unpack8<kF32>(v[y]), r[y], t, a.table != nullptr);
     }
 #pragma unroll
     for (int y = 0; y < kHeads; ++y)
       if (in && h0 + y * groups < a.H[of])
-        store8<kF32>(dst + (size_t)(h0 + y * groups) * (a.D / 8) * kVec, v[y]);
+        store8<kF32>(dst + (size_t)(h0 + y * groups) * vecs8 * kVec, v[y]);
   }
 }
 
@@ -246,12 +313,13 @@ norm_row_kernel(const Args a) {
 #pragma unroll
   for (int y = 0; y < kVectors; ++y)
     if (sub + y * kT < vecs) v[y] = load8<kF32>(src + (size_t)(sub + y * kT) * kVec);
-  float r = 0.f;
-  bool down = false;
-  auto total = [&](float f, float (&part)[kBlock / 32]) {
+  auto total = [&](bool small, float (&part)[kBlock / 32]) {
     float s = 0.f;
 #pragma unroll
-    for (int y = 0; y < kVectors; ++y) s += squares<kF32>(v[y], f);
+    for (int y = 0; y < kVectors; ++y) {
+      const Values x = unpack8<kF32>(v[y]);
+      s += small ? small_squares(x) : squares(x);
+    }
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     if (kT > 32) {
@@ -264,12 +332,12 @@ norm_row_kernel(const Args a) {
     return s;
   };
   const float inv = of < 2 ? 1.f / (float)(a.H[of] * a.D) : 0.f;
-  const float s = total(1.f, sh[0]);
-  r = __frsqrt_rn(fmaf(s, inv, a.eps));
-  down = s == INFINITY;
+  const float s = total(false, sh[0]);
+  float r = inverse_root<kF32>(fmaf(s, inv, a.eps));
+  const bool down = s == INFINITY;
   if (__syncthreads_or(down)) {   // rare
-    const float z = total(kDown, sh[1]);
-    if (down) r = __frsqrt_rn(z * inv);
+    const float z = total(true, sh[1]);
+    if (down) r = inverse_root<kF32>(z * inv) * kDown;
   }
   uint8_t *dst = a.y[of] + p.to * a.out_row[of];
 #pragma unroll
@@ -278,13 +346,205 @@ norm_row_kernel(const Args a) {
     if (at >= vecs) continue;
     if (of < 2) {
       Turn t;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) t.w[e] = 1.f;
-      if (a.weight[of]) read8(a.weight[of] + 8 * at, t.w);
-      if (a.table) read8(a.table + (size_t)p.trow * a.D + 8 * (at % vecs8), t.cs);
-      v[y] = normed<kF32>(v[y], r, down, t, a.table != nullptr);
+      t.w = weights_at(a.weight[of] ? a.weight[of] + 8 * at : nullptr);
+      if (a.table) {
+        const float4 *row = reinterpret_cast<const float4 *>(a.table + (size_t)p.trow * a.D);
+        const int q = 2 * (at % vecs8);
+        turn_by(t, __ldg(row + q), __ldg(row + q + 1));
+      }
+      v[y] = normed<kF32>(unpack8<kF32>(v[y]), r, t, a.table != nullptr);
     }
     store8<kF32>(dst + (size_t)at * kVec, v[y]);
+  }
+}
+
+// Across the heads, many tokens: a block takes whole tokens, one after the other, and their rows
+// of q, k, v and the table come by bulk copies into a ring of stages, so that what is in flight
+// does not depend on registers and occupancy; v goes out again without passing through them.  A
+// thread holds the same kY vectors of q and of k of every token, so that their weights stay in
+// registers, and (a head's vectors divide the block's threads) one place in a head.
+constexpr int kMostStages = 8;
+constexpr int kRingThreads = 512;   // at most
+
+struct RingArgs {
+  Args a;
+  int n, stages, stage;       // tokens; stages of `stage` bytes
+  int bytes[4], at[4];        // of q, k, v and the table's row in a stage
+  float inv[2];               // 1 / values of q's and k's mean
+};
+
+template <bool kF32, int kY>
+__global__ void __maxnreg__((kY == 1 ? 64 : 96)) norm_ring_kernel(const RingArgs z) {
+  constexpr int kVec = kF32 ? 32 : 16, kMostWarps = kRingThreads / 32;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ uint64_t full[kMostStages];
+  __shared__ __align__(16) float part[2][2][kMostWarps];
+  __shared__ int abort_flag;
+  const Args &a = z.a;
+  const int threads = blockDim.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const bool leads = threadIdx.x == 0;
+  if (leads) {
+    for (int s = 0; s < z.stages; ++s) mbar_init(&full[s], 2);
+    abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (threadIdx.x < 4 * kMostWarps) (&part[0][0][0])[threadIdx.x] = 0.f;
+  __syncthreads();
+  pdl_wait();
+  pdl_trigger();
+  const int step = gridDim.x;
+  auto slot_of = [&](int j) { return a.kidx ? __ldg(a.kidx + j) : j; };
+  auto trow_of = [&](int j, int slot) { return a.tidx ? __ldg(a.tidx + j) : slot; };
+  auto load_rows = [&](int j, int s) {
+    mbar_expect_tx(&full[s], z.bytes[0] + z.bytes[1] + z.bytes[2]);
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+      if (z.bytes[i])
+        bulk_load(smem_addr(smem) + s * z.stage + z.at[i], a.x[i] + (long long)j * a.in_row[i],
+                  z.bytes[i], &full[s]);
+  };
+  auto load_table = [&](int trow, int s) {
+    if (a.table && trow >= 0 && trow < a.table_rows) {
+      mbar_expect_tx(&full[s], z.bytes[3]);
+      bulk_load(smem_addr(smem) + s * z.stage + z.at[3], a.table + (size_t)trow * a.D, z.bytes[3],
+                &full[s]);
+    } else {
+      mbar_arrive(&full[s]);
+    }
+  };
+  if (leads) {
+    for (int s = 0, j = blockIdx.x; s < z.stages && j < z.n; ++s, j += step) load_rows(j, s);
+    for (int s = 0, j = blockIdx.x; s < z.stages && j < z.n; ++s, j += step)
+      load_table(trow_of(j, slot_of(j)), s);
+  }
+  const int vecs8 = a.D / 8, in_head = threadIdx.x % vecs8;
+  Values w[2][kY];
+  bool mine[2][kY];
+#pragma unroll
+  for (int of = 0; of < 2; ++of)
+#pragma unroll
+    for (int y = 0; y < kY; ++y) {
+      const int at = threadIdx.x + y * threads;
+      mine[of][y] = at < a.H[of] * vecs8;
+      w[of][y] = weights_at(mine[of][y] && a.weight[of] ? a.weight[of] + 8 * at : nullptr);
+    }
+  int s = 0;                  // the present stage
+  uint32_t phase = 0;
+  int loaded = z.stages * step + blockIdx.x;   // the next token to load
+  int late_trow = -1;         // its table row
+  int slot = 0, trow = 0;
+  if ((int)blockIdx.x < z.n) {
+    slot = slot_of(blockIdx.x);
+    trow = trow_of(blockIdx.x, slot);
+  }
+  for (int j = blockIdx.x, it = 0; j < z.n; j += step, ++it) {
+    // the next token's places, and the table's row of the token that this stage takes next
+    int slot_next = 0, trow_next = 0, trow_far = -1;
+    if (j + step < z.n) {
+      slot_next = slot_of(j + step);
+      trow_next = trow_of(j + step, slot_next);
+    }
+    if (leads && j + z.stages * step < z.n)
+      trow_far = trow_of(j + z.stages * step, slot_of(j + z.stages * step));
+    bool all = true, kv = true;   // whether q, and whether k and v are written
+    if (a.kidx && (slot < 0 || slot >= a.k_rows)) {
+      kv = false;
+      if (leads && slot != -1) set_error(a.err, kErrIndex);
+    }
+    if (a.table && (trow < 0 || trow >= a.table_rows)) {
+      all = kv = false;
+      if (leads && trow != -1) set_error(a.err, kErrIndex);
+    }
+    mbar_wait(&full[s], phase, &abort_flag, a.err);
+    const uint8_t *stage = smem + s * z.stage;
+    if (leads && z.bytes[2] && kv)
+      bulk_store(a.y[2] + (long long)slot * a.out_row[2], smem_addr(stage) + z.at[2], z.bytes[2]);
+    Eight<kF32> v[2][kY] = {};
+    float sum[2], r[2];
+#pragma unroll
+    for (int of = 0; of < 2; ++of) {
+      sum[of] = 0.f;
+#pragma unroll
+      for (int y = 0; y < kY; ++y) {
+        if (mine[of][y]) {
+          const uint4 *p = reinterpret_cast<const uint4 *>(
+              stage + z.at[of] + (threadIdx.x + y * threads) * kVec);
+          v[of][y].w[0] = p[0];
+          if (kF32) v[of][y].w[kF32 ? 1 : 0] = p[kF32 ? 1 : 0];
+        }
+        sum[of] += squares(unpack8<kF32>(v[of][y]));
+      }
+    }
+    Turn t;
+    if (a.table) {
+      const float4 *p = reinterpret_cast<const float4 *>(stage + z.at[3]) + 2 * in_head;
+      turn_by(t, p[0], p[1]);
+    }
+    auto total = [&]() {
+#pragma unroll
+      for (int of = 0; of < 2; ++of) {
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) sum[of] += __shfl_xor_sync(0xffffffffu, sum[of], o);
+        if (lane == 0) part[it & 1][of][warp] = sum[of];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int of = 0; of < 2; ++of) {
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < kMostWarps / 4; ++i) {   // those of warps that are not there are zero
+          const float4 q = reinterpret_cast<const float4 *>(part[it & 1][of])[i];
+          x.x += q.x, x.y += q.y, x.z += q.z, x.w += q.w;
+        }
+        sum[of] = (x.x + x.y) + (x.z + x.w);
+      }
+    };
+    total();
+    // every thread has left the stage before: it takes the next token to load
+    if (leads && it > 0 && loaded < z.n && !*(volatile int *)&abort_flag) {
+      bulk_stores_read();
+      const int late = s == 0 ? z.stages - 1 : s - 1;
+      load_rows(loaded, late);
+      load_table(late_trow, late);
+      loaded += step;
+    }
+    const bool down[2] = {sum[0] == INFINITY, sum[1] == INFINITY};
+#pragma unroll
+    for (int of = 0; of < 2; ++of) r[of] = inverse_root<kF32>(fmaf(sum[of], z.inv[of], a.eps));
+    if (down[0] || down[1]) {   // rare, and the same for all threads
+#pragma unroll
+      for (int of = 0; of < 2; ++of) {
+        sum[of] = 0.f;
+#pragma unroll
+        for (int y = 0; y < kY; ++y) sum[of] += small_squares(unpack8<kF32>(v[of][y]));
+      }
+      __syncthreads();
+      total();
+#pragma unroll
+      for (int of = 0; of < 2; ++of)
+        if (down[of]) r[of] = inverse_root<kF32>(sum[of] * z.inv[of]) * kDown;
+    }
+#pragma unroll
+    for (int of = 0; of < 2; ++of) {
+      uint8_t *out = a.y[of] + (long long)(of ? slot : j) * a.out_row[of];
+#pragma unroll
+      for (int y = 0; y < kY; ++y)
+        if (mine[of][y] && (of ? kv : all)) {
+          t.w = w[of][y];
+          store8<kF32>(out + (size_t)(threadIdx.x + y * threads) * kVec,
+                       normed<kF32>(unpack8<kF32>(v[of][y]), r[of], t, a.table != nullptr));
+        }
+    }
+    late_trow = trow_far;
+    slot = slot_next;
+    trow = trow_next;
+    if (++s == z.stages) s = 0, phase ^= 1;
+  }
+  if (leads) bulk_stores_written();
+  if (leads && abort_flag) {   // a wait ran out: copies in flight land before the block ends
+    const int count = (loaded - (int)blockIdx.x) / step;
+    for (int i = max(0, count - z.stages); i < count && blockIdx.x + i * step < (unsigned)z.n; ++i)
+      mbar_wait(&full[i % z.stages], i / z.stages & 1, &abort_flag, a.err, false);
   }
 }
 
@@ -303,6 +563,63 @@ void launch_row(const Args &a, int threads, cudaStream_t s) {
     case 512: return go(norm_row_kernel<kF32, 512>, 512);
     default: return go(norm_row_kernel<kF32, 1024>, 1024);
   }
+}
+
+// Registers of a ring kernel's thread, which may from now on use all of an SM's shared memory on
+// this device; 0 where that failed.
+template <bool kF32, int kY>
+int ring_registers() {
+  static std::atomic<int> known[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+  int regs = known[dev].load(std::memory_order_acquire);
+  if (regs) return regs;
+  cudaFuncAttributes f;
+  if (cudaFuncSetAttribute(norm_ring_kernel<kF32, kY>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                           226 * 1024 - 1024) != cudaSuccess ||
+      cudaFuncGetAttributes(&f, norm_ring_kernel<kF32, kY>) != cudaSuccess)
+    return 0;
+  known[dev].store(regs = (f.numRegs + 7) & ~7, std::memory_order_release);
+  return regs;
+}
+
+// Launches the ring for n tokens where it is the better: false where the other kernel takes the
+// call, for few tokens, rows that 512 threads or two stages do not hold, or head dimensions whose
+// vectors do not divide as many threads.
+template <bool kF32>
+bool launch_ring(const Args &a, int n, bool with_v, cudaStream_t s) {
+  constexpr int kRoom = 227 * 1024, kOwn = 1024 + 1024;   // an SM's; a block's, and its statics
+  const int vecs8 = a.D / 8, most = std::max(a.H[0], a.H[1]) * vecs8;
+  if (n < kRingTokens * sm_count()) return false;
+  int unit = 32;                                          // whole warps and whole heads
+  while (unit % vecs8) unit += 32;
+  const int y = most <= kRingThreads ? 1 : 2;
+  const int threads = ((most + y - 1) / y + unit - 1) / unit * unit;
+  if (threads > kRingThreads) return false;
+  const int regs = y == 1 ? ring_registers<kF32, 1>() : ring_registers<kF32, 2>();
+  if (!regs) return false;
+  RingArgs z;
+  z.a = a;
+  z.n = n;
+  z.stage = 0;
+  for (int i = 0; i < 4; ++i) {
+    z.bytes[i] = i == 3 ? (a.table ? 4 * a.D : 0)
+                 : i == 2 && !with_v ? 0 : a.H[i] * a.D * (kF32 ? 4 : 2);
+    z.at[i] = z.stage;
+    z.stage += z.bytes[i];
+  }
+  for (int i = 0; i < 2; ++i) z.inv[i] = 1.f / (float)(a.H[i] * a.D);
+  z.stage = (z.stage + 127) & ~127;
+  int nb = std::min(4, 65536 / (regs * threads));
+  for (; nb >= 1; --nb) {
+    z.stages = std::min(kMostStages, (kRoom / nb - kOwn) / z.stage);
+    if (z.stages >= 3 || (nb == 1 && z.stages == 2)) break;
+  }
+  if (nb < 1) return false;
+  const int blocks = std::min(n, nb * sm_count());
+  launch_pdl(y == 1 ? norm_ring_kernel<kF32, 1> : norm_ring_kernel<kF32, 2>, dim3(blocks),
+             dim3(threads), (size_t)z.stages * z.stage, s, z);
+  return true;
 }
 
 }  // namespace
@@ -367,16 +684,24 @@ extern "C" int hsa_qk_norm_rope(const void *q, long long q_row, const void *k, l
   a.eps = eps;
   a.inv = 1.f / (float)D;
   cudaStream_t s = (cudaStream_t)stream;
+  const bool f32 = dtype == HSA_F32;
   count_launches(1);
   if (!across) {
     const long long need = (items + kThreads / 32 - 1) / (kThreads / 32);
     const long long cap = (long long)sm_count() * 32;
-    launch_pdl(dtype == HSA_F32 ? norm_heads_kernel<true> : norm_heads_kernel<false>,
+    const int known = D == 64 ? 3 : D == 128 ? 4 : -1;
+    launch_pdl(f32 ? (known == 3   ? norm_heads_kernel<true, 3>
+                      : known == 4 ? norm_heads_kernel<true, 4>
+                                   : norm_heads_kernel<true, -1>)
+                   : (known == 3   ? norm_heads_kernel<false, 3>
+                      : known == 4 ? norm_heads_kernel<false, 4>
+                                   : norm_heads_kernel<false, -1>),
                dim3((unsigned)(need < cap ? need : cap)), dim3(kThreads), 0, s, a);
-  } else {
+  } else if (!(f32 ? launch_ring<true>(a, n, v != nullptr, s)
+                   : launch_ring<false>(a, n, v != nullptr, s))) {
     int t = 32;
     while (t * kVectors < most * (D / 8)) t *= 2;
-    if (dtype == HSA_F32) launch_row<true>(a, t, s);
+    if (f32) launch_row<true>(a, t, s);
     else launch_row<false>(a, t, s);
   }
   return launch_status();
