@@ -21,8 +21,8 @@
 // borders m_g 0.25 .. m_g 5 themselves, which are exact.
 //
 // Both kernels are bound by HBM: 2.5 bytes move per element of a bf16 tensor, so there are few
-// issue slots for each.  A lane group (a power of two) holds a head's row, of K and of V: two
-// vectors of eight elements a lane when quantising, one when reading back.
+// issue slots for each.  A lane group (a power of two) holds a head's row, of K and of V: four
+// vectors of eight elements a lane when quantising (two in fp32), one when reading back.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -117,28 +117,29 @@ __device__ __forceinline__ uint32_t rotate2(uint32_t w, float c, float s) {
   return pack_bf16(__fmaf_rn(a, c, -__fmul_rn(b, s)), __fmaf_rn(a, s, __fmul_rn(b, c)));
 }
 
-// A lane's vectors are c and c + L of a row's D / 8, L = D / 16.  A vector holds D = 128: four
-// dimensions of group 0 and four of 1 (c even), or of 2 and of 3 (c odd); D = 64: two of each
-// group.  kG groups a lane.
-template <int D>
+// A lane's vectors are c, c + L, .. of a row's D / 8, kN of them (what is done per row and not
+// per element is a third of the work with two).  A vector holds, at D = 128, four dimensions of
+// group 0 and four of 1 (c even), or of 2 and of 3 (c odd); at D = 64 two of each group.  kG groups
+// a lane.
+template <int D, bool kF32>
 struct Lay {
-  static constexpr int kL = D / 16, kG = D == 128 ? 2 : 4, kRun = 8 / kG;
+  static constexpr int kN = kF32 ? 2 : 4, kL = D / 8 / kN, kG = D == 128 ? 2 : 4, kRun = 8 / kG;
 };
 
 // The largest magnitudes of the lane's groups over the row, as bits of fp32.
-template <int D, bool kF32>
-__device__ __forceinline__ void largest(const Eight<kF32> (&v)[2], uint32_t (&m)[Lay<D>::kG]) {
-  constexpr int kG = Lay<D>::kG, kL = Lay<D>::kL;
+template <int D, bool kF32, typename Y = Lay<D, kF32>>
+__device__ __forceinline__ void largest(const Eight<kF32> (&v)[Y::kN], uint32_t (&m)[Y::kG]) {
+  constexpr int kG = Y::kG, kL = Y::kL, kN = Y::kN;
   if (kF32) {
 #pragma unroll
     for (int i = 0; i < kG; ++i) m[i] = 0;
 #pragma unroll
-    for (int y = 0; y < 2; ++y) {
+    for (int y = 0; y < kN; ++y) {
       float x[8];
       unpack8(v[y], x);
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        m[i / Lay<D>::kRun] = max(m[i / Lay<D>::kRun], __float_as_uint(x[i]) & 0x7fffffffu);
+        m[i / Y::kRun] = max(m[i / Y::kRun], __float_as_uint(x[i]) & 0x7fffffffu);
     }
 #pragma unroll
     for (int o = kG == 2 ? 2 : 1; o < kL; o <<= 1)
@@ -147,18 +148,22 @@ __device__ __forceinline__ void largest(const Eight<kF32> (&v)[2], uint32_t (&m)
   } else {
     // magnitudes of bf16 are ordered as their bits: two groups to a word
     constexpr uint32_t kM = 0x7fff7fffu;
-    const uint4 &p = v[0].w[0], &q = v[1].w[0];
-    const uint32_t w0 = __vmaxu2(p.x & kM, q.x & kM), w1 = __vmaxu2(p.y & kM, q.y & kM);
-    const uint32_t w2 = __vmaxu2(p.z & kM, q.z & kM), w3 = __vmaxu2(p.w & kM, q.w & kM);
+    uint32_t w[4] = {};
+#pragma unroll
+    for (int y = 0; y < kN; ++y) {
+      const uint4 &p = v[y].w[0];
+      w[0] = __vmaxu2(w[0], p.x & kM), w[1] = __vmaxu2(w[1], p.y & kM);
+      w[2] = __vmaxu2(w[2], p.z & kM), w[3] = __vmaxu2(w[3], p.w & kM);
+    }
     auto across = [](uint32_t a, uint32_t b) {   // (largest half of a, of b)
       return __vmaxu2(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632));
     };
     uint32_t r[kG / 2];
     if (kG == 2) {
-      r[0] = across(__vmaxu2(w0, w1), __vmaxu2(w2, w3));
+      r[0] = across(__vmaxu2(w[0], w[1]), __vmaxu2(w[2], w[3]));
     } else {
-      r[0] = across(w0, w1);
-      r[kG / 2 - 1] = across(w2, w3);
+      r[0] = across(w[0], w[1]);
+      r[kG / 2 - 1] = across(w[2], w[3]);
     }
 #pragma unroll
     for (int o = kG == 2 ? 2 : 1; o < kL; o <<= 1)
@@ -169,31 +174,33 @@ __device__ __forceinline__ void largest(const Eight<kF32> (&v)[2], uint32_t (&m)
   }
 }
 
-// The codes of a lane's two vectors and the row's word, all lanes of the warp together.  `bad`
-// is set where the row holds what is not finite: it is then NaN throughout.
-template <int D, bool kF32>
-__device__ __forceinline__ void quantise(Eight<kF32> (&v)[2], uint32_t (&code)[2], uint32_t &word,
-                                         bool &bad) {
-  constexpr int kG = Lay<D>::kG, kRun = Lay<D>::kRun;
+// The codes of a lane's vectors and the row's word, all lanes of the warp together.  `bad` is set
+// where the row holds what is not finite: it is then NaN throughout.
+template <int D, bool kF32, typename Y = Lay<D, kF32>>
+__device__ __forceinline__ void quantise(Eight<kF32> (&v)[Y::kN], uint32_t (&code)[Y::kN],
+                                         uint32_t &word, bool &bad) {
+  constexpr int kG = Y::kG, kRun = Y::kRun, kN = Y::kN;
   uint32_t m[kG];
   largest<D, kF32>(v, m);
   uint32_t top = max(m[0], m[1]);
   if (kG == 4) top = max(top, max(m[kG - 2], m[kG - 1]));
   if (kG == 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-  bool odd = top >= 0x7f800000u;
+  const bool odd = top >= 0x7f800000u;
   if (top > kTop) {   // rare
     top = kTop;
 #pragma unroll
     for (int i = 0; i < kG; ++i) m[i] = min(m[i], kTop);
 #pragma unroll
-    for (int y = 0; y < 2; ++y)
+    for (int y = 0; y < kN; ++y)
 #pragma unroll
       for (int i = 0; i < (kF32 ? 2 : 1); ++i) {
         uint32_t w[4] = {v[y].w[i].x, v[y].w[i].y, v[y].w[i].z, v[y].w[i].w};
 #pragma unroll
-        for (int z = 0; z < 4; ++z)
+        for (int z = 0; z < 4; ++z) {
           w[z] = kF32 ? min(w[z] & 0x7fffffffu, kTop) | (w[z] & 0x80000000u)
                       : __vminu2(w[z] & 0x7fff7fffu, kTop | kTop >> 16) | (w[z] & 0x80008000u);
+          if (odd) w[z] = 0;
+        }
         v[y].w[i] = make_uint4(w[0], w[1], w[2], w[3]);
       }
   }
@@ -207,12 +214,16 @@ __device__ __forceinline__ void quantise(Eight<kF32> (&v)[2], uint32_t (&code)[2
 #pragma unroll
   for (int i = 0; i < kG; ++i) {
     const float a = __uint_as_float(m[i]) * f;         // exact, at most 378
-    // a / 6, a little less, and up: the factor, or for what is within 2^-21 of 6 n one too few
-    float n = ceilf(a * __uint_as_float(0x3e2aaaa8u));
-    if (n * 6.f < a) n += 1.f;
-    unit[i] = n;
-    per[i] = n > 0.f ? f * __frcp_rn(n) : 0.f;
-    factors |= (uint32_t)n << (6 * i);
+    // ceil(a / 6): a times a little less than 1/6, rounded up to a whole number as it joins
+    // 2^23.  Of bf16 values a is 6 n or above it by 2^-8 of itself and so well above a little
+    // less; of fp32 ones it may be one too few.
+    float n = __fadd_ru(a * __uint_as_float(0x3e2aaaa8u), 0x1p23f);
+    if (kF32 && (n - 0x1p23f) * 6.f < a) n += 1.f;
+    factors |= (__float_as_uint(n) & 63u) << (6 * i);
+    unit[i] = n - 0x1p23f;
+    float inverse;   // within 2^-23; of a group of zeros any will do
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inverse) : "f"(fmaxf(unit[i], 1.f)));
+    per[i] = f * inverse;
   }
   if (kG == 2) {
     const uint32_t other = __shfl_xor_sync(0xffffffffu, factors, 1);
@@ -221,7 +232,7 @@ __device__ __forceinline__ void quantise(Eight<kF32> (&v)[2], uint32_t (&code)[2
   }
   word = odd ? kNanRow : s << 24 | factors;
 #pragma unroll
-  for (int y = 0; y < 2; ++y) {
+  for (int y = 0; y < kN; ++y) {
     float x[8];
     unpack8(v[y], x);
     if (kF32) {
@@ -247,7 +258,6 @@ __device__ __forceinline__ void quantise(Eight<kF32> (&v)[2], uint32_t (&code)[2
       }
       code[y] = codes8(x);
     }
-    if (odd) code[y] = 0;
   }
 }
 
@@ -264,12 +274,15 @@ struct QuantArgs {
   int N, table_rows;
 };
 
+constexpr int kQuantBlocks = 3;   // per SM, all resident at once
+
 // One item is a (token, head) of the fresh rows, K and V.
 template <int D, bool kF32, bool kRope>
-__global__ void __launch_bounds__(kThreads, kF32 ? 4 : 6)
+__global__ void __launch_bounds__(kThreads, kQuantBlocks)
 kv4_quant_scatter_kernel(const QuantArgs a) {
   pdl_wait();
-  constexpr int kL = Lay<D>::kL;
+  using Y = Lay<D, kF32>;
+  constexpr int kL = Y::kL, kN = Y::kN;
   const int lane = threadIdx.x & 31, c = lane & (kL - 1);
   const unsigned step = gridDim.x * (unsigned)(kThreads / kL);
   const unsigned first = (blockIdx.x * (unsigned)kThreads + threadIdx.x) / kL;
@@ -278,13 +291,13 @@ kv4_quant_scatter_kernel(const QuantArgs a) {
     const bool there = i < a.items;
     const unsigned j = quotient((unsigned)i, a.heads), h = (unsigned)i - j * a.heads.d;
     int slot = -1, trow = 0;
-    Eight<kF32> k[2] = {}, v[2] = {};
+    Eight<kF32> k[kN] = {}, v[kN] = {};
     if (there) {
       slot = __ldg(a.idx + j);
       trow = !kRope ? 0 : a.tidx ? __ldg(a.tidx + j) : slot;
       const size_t in_row = (size_t)h * D + 8 * c;
 #pragma unroll
-      for (int y = 0; y < 2; ++y) {
+      for (int y = 0; y < kN; ++y) {
         k[y] = load8<kF32>(a.kf, (size_t)j * a.k_row + in_row + 8 * kL * y);
         v[y] = load8<kF32>(a.vf, (size_t)j * a.v_row + in_row + 8 * kL * y);
       }
@@ -294,7 +307,7 @@ kv4_quant_scatter_kernel(const QuantArgs a) {
     if (kRope && ok) {
       const float4 *t = reinterpret_cast<const float4 *>(a.table + (size_t)trow * D) + 2 * c;
 #pragma unroll
-      for (int y = 0; y < 2; ++y) {
+      for (int y = 0; y < kN; ++y) {
         const float4 t0 = __ldg(t + 2 * kL * y), t1 = __ldg(t + 2 * kL * y + 1);
         uint4 &w = k[y].w[0];
         w.x = rotate2(w.x, t0.x, t0.y);
@@ -304,14 +317,14 @@ kv4_quant_scatter_kernel(const QuantArgs a) {
       }
     }
     bool bad = false;
-    uint32_t wk, wv, ck[2], cv[2];
+    uint32_t wk, wv, ck[kN], cv[kN];
     quantise<D, kF32>(k, ck, wk, bad);
     quantise<D, kF32>(v, cv, wv, bad);
     if (!ok) continue;
     if (bad) set_error(a.err, kErrNonfinite);
     const size_t row = (size_t)slot * a.heads.d + h, to = row * (D / 2) + 4 * c;
 #pragma unroll
-    for (int y = 0; y < 2; ++y) {
+    for (int y = 0; y < kN; ++y) {
       *reinterpret_cast<uint32_t *>(a.kc + to + 4 * kL * y) = ck[y];
       *reinterpret_cast<uint32_t *>(a.vc + to + 4 * kL * y) = cv[y];
     }
@@ -467,19 +480,20 @@ extern "C" int hsa_kv4_quant_scatter(void *k_cache, void *v_cache, uint32_t *k_s
   a.items = (unsigned)n_active * (unsigned)H;
   a.N = N;
   a.table_rows = table_rows;
-  auto go = [&](auto kernel, int per_sm) {
-    launch_pdl(kernel, dim3(grid_for(a.items, D / 16, 1, per_sm)), dim3(kThreads), 0,
+  const int lanes = D / 8 / (dtype == HSA_F32 ? 2 : 4);
+  auto go = [&](auto kernel) {
+    launch_pdl(kernel, dim3(grid_for(a.items, lanes, 1, kQuantBlocks)), dim3(kThreads), 0,
                (cudaStream_t)stream, a);
   };
   count_launches(1);
   if (D == 128) {
-    if (dtype == HSA_F32) go(kv4_quant_scatter_kernel<128, true, false>, 4);
-    else if (table) go(kv4_quant_scatter_kernel<128, false, true>, 6);
-    else go(kv4_quant_scatter_kernel<128, false, false>, 6);
+    if (dtype == HSA_F32) go(kv4_quant_scatter_kernel<128, true, false>);
+    else if (table) go(kv4_quant_scatter_kernel<128, false, true>);
+    else go(kv4_quant_scatter_kernel<128, false, false>);
   } else {
-    if (dtype == HSA_F32) go(kv4_quant_scatter_kernel<64, true, false>, 4);
-    else if (table) go(kv4_quant_scatter_kernel<64, false, true>, 6);
-    else go(kv4_quant_scatter_kernel<64, false, false>, 6);
+    if (dtype == HSA_F32) go(kv4_quant_scatter_kernel<64, true, false>);
+    else if (table) go(kv4_quant_scatter_kernel<64, false, true>);
+    else go(kv4_quant_scatter_kernel<64, false, false>);
   }
   return launch_status();
 }
