@@ -472,7 +472,7 @@ int hsa_qk_norm_rope(const void *q, long long q_row, const void *k, long long k_
  * lens or want, and n_free_out n_free; no other two may overlap.  page_size a power of two;
  * n_pages * page_size < 2^31; max_pages * page_size < 2^31 - 256; max_new, max_keys < 2^31 -
  * 256; sums past 2^31 - 1 count as that.  One launch, or two where max_new + max_keys is
- * above 8192. */
+ * above 8192 or batch above 1024. */
 int hsa_page_plan(const int32_t *lens, const int32_t *want, int batch, int page_size,
                   int32_t *page_table, int max_pages, int32_t *free_pages, int n_pages,
                   const int32_t *n_free, int32_t *n_free_out, int32_t *lens_out, int32_t *cu_q,

@@ -7,10 +7,11 @@
 // the step is a few prefix sums and, between them, the moves.  A few kilobytes move: what
 // bounds it is the chain of loads, sums and barriers, and the launch.
 //
-// One block does the sums and moves the pages, 1024 sequences at a time.  The sums saturate
-// at 2^31 - 1, where min(a + b, 2^31 - 1) is still associative, so 32 bits serve whatever the
-// lengths are.  The rows of tokens and keys are filled by the same block where they are few,
-// else by a second grid.
+// One block does the sums and moves the pages: of up to 256 or 1024 sequences, a thread each,
+// with one exchange of all four sums, or of 1024 at a time.  The sums saturate at 2^31 - 1,
+// where min(a + b, 2^31 - 1) is still associative, so 32 bits serve whatever the lengths are.
+// The rows of tokens and keys are filled by the same block where they are few, else by a second
+// grid.
 #include "hsa_internal.cuh"
 
 namespace hsa {
@@ -30,9 +31,9 @@ struct Args {
 __device__ __forceinline__ unsigned add_up(unsigned a, unsigned b) { return min(a + b, kMost); }
 
 // Inclusive prefix sums of kN numbers per thread over the block, and the totals.
-template <int kN>
+template <int kN, int kW>
 __device__ __forceinline__ void block_scan(unsigned (&x)[kN], unsigned (&total)[kN],
-                                           unsigned (&sh)[kN][kWarps]) {
+                                           unsigned (&sh)[kN][kW]) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
   for (int i = 0; i < kN; ++i) {
@@ -46,13 +47,13 @@ __device__ __forceinline__ void block_scan(unsigned (&x)[kN], unsigned (&total)[
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < kN; ++i) {
-    unsigned s = sh[i][lane];   // as many warps as lanes
+    unsigned s = lane < kW ? sh[i][lane] : 0;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
+    for (int o = 1; o < kW; o <<= 1) {
       const unsigned y = __shfl_up_sync(0xffffffffu, s, o);
       if (lane >= o) s = add_up(s, y);
     }
-    total[i] = __shfl_sync(0xffffffffu, s, 31);
+    total[i] = __shfl_sync(0xffffffffu, s, kW - 1);
     const unsigned before = __shfl_sync(0xffffffffu, s, (warp + 31) & 31);
     if (warp) x[i] = add_up(x[i], before);
   }
@@ -74,15 +75,15 @@ __device__ __forceinline__ int first_above(int n, unsigned v, Get &&get) {
 // Cache rows of elements i .. i + 3 of the batch: element i of sequence b, cu[b] <= i <
 // cu[b + 1], is its (i - cu[b])th key, or the like of its newest tokens.  Those from cu[batch]
 // on get -1.
-__device__ __forceinline__ void fill4(const Args &a, const int32_t *cu, int i, int n,
-                                      int32_t *rows, int32_t *positions) {
+__device__ __forceinline__ void fill4(const Args &a, const int32_t *cu, const int32_t *lens, int i,
+                                      int n, int32_t *rows, int32_t *positions) {
   int b = first_above(a.batch, (unsigned)i, [&](int m) { return (unsigned)cu[m + 1]; });
   int begin = 0, end = 0, first = 0;
   auto look = [&]() {
     if (b >= a.batch) return;
     begin = cu[b];
     end = cu[b + 1];
-    first = positions ? a.lens_out[b] - (end - begin) : 0;
+    first = positions ? lens[b] - (end - begin) : 0;
   };
   look();
 #pragma unroll
@@ -104,17 +105,137 @@ __device__ __forceinline__ void fill4(const Args &a, const int32_t *cu, int i, i
   }
 }
 
-// Elements of slots, then of key_rows, four a thread.
-__device__ __forceinline__ void fill_rows(const Args &a, unsigned first, unsigned step) {
+// Elements of slots, then of key_rows, four a thread, with the offsets and lengths at cu_q, cu_k
+// and lens.
+__device__ __forceinline__ void fill_rows(const Args &a, const int32_t *cu_q, const int32_t *cu_k,
+                                          const int32_t *lens, unsigned first, unsigned step) {
   const unsigned tokens = ((unsigned)a.max_new + 3) / 4;
   const unsigned all = tokens + (a.key_rows ? ((unsigned)a.max_keys + 3) / 4 : 0);
   for (unsigned e = first; e < all; e += step) {
-    if (e < tokens) fill4(a, a.cu_q, 4 * e, a.max_new, a.slots, a.positions);
-    else fill4(a, a.cu_k, 4 * (e - tokens), a.max_keys, a.key_rows, nullptr);
+    if (e < tokens) fill4(a, cu_q, lens, 4 * e, a.max_new, a.slots, a.positions);
+    else fill4(a, cu_k, lens, 4 * (e - tokens), a.max_keys, a.key_rows, nullptr);
   }
 }
 
-template <bool kFill>
+__device__ __forceinline__ int pages_of(const Args &a, int n) {
+  return (n >> a.page_log2) + ((n & ((1 << a.page_log2) - 1)) != 0);
+}
+// A length, checked.
+__device__ __forceinline__ int checked(const Args &a, int n) {
+  const long long most = (long long)a.max_pages << a.page_log2;
+  if (n >= 0 && n <= most) return n;
+  set_error(a.err, kErrIndex);
+  return n < 0 ? 0 : (int)most;
+}
+__device__ __forceinline__ int checked_stack(const Args &a, int n) {
+  if (n >= 0 && n <= a.n_pages) return n;
+  if (threadIdx.x == 0) set_error(a.err, kErrIndex);
+  return n < 0 ? 0 : a.n_pages;
+}
+// Page e of those given back goes onto the stack at `at`.
+__device__ __forceinline__ void push(const Args &a, long long at, const int32_t *from) {
+  const int id = *from;
+  if (at < a.n_pages) a.free_pages[at] = id;
+  if (at >= a.n_pages || id < 0 || id >= a.n_pages) set_error(a.err, kErrIndex);
+}
+__device__ __forceinline__ int pop(const Args &a, unsigned at, int32_t *to) {
+  const int id = a.free_pages[at];
+  if (id < 0 || id >= a.n_pages) set_error(a.err, kErrIndex);
+  return *to = id;
+}
+
+// Up to kT sequences, a thread each.
+template <int kT, bool kFill>
+__global__ void __launch_bounds__(kT) page_plan_one_kernel(const Args a) {
+  __shared__ unsigned sh_sum[4][kT / 32];
+  __shared__ unsigned sh_back[kT], sh_get[kT];     // pages moved, up to and with each sequence
+  __shared__ int sh_to[kT], sh_from[kT];           // first page that moves
+  __shared__ int32_t sh_cu[2][kFill ? kT + 1 : 1], sh_len[kFill ? kT : 1];
+  pdl_wait();
+  pdl_trigger();
+  const int b = threadIdx.x, P1 = (1 << a.page_log2) - 1;
+  int l = 0, w = 0;
+  if (b < a.batch) {
+    l = a.lens[b];
+    w = a.want[b];
+  }
+  int n_free = *a.n_free;
+  l = checked(a, l);
+  w = checked(a, w);
+  n_free = checked_stack(a, n_free);
+  int32_t *row = a.table + (size_t)b * a.max_pages;
+  const int from = pages_of(a, l), to = pages_of(a, w), fresh = max(0, w - l);
+  // the page that the first new token goes to, where the sequence holds it already
+  int held = -1;
+  if (fresh && (l & P1)) held = row[l >> a.page_log2];
+  const unsigned back = max(0, from - to), get = max(0, to - from);
+  unsigned x[4] = {back, get, (unsigned)fresh, (unsigned)w}, total[4];
+  block_scan(x, total, sh_sum);
+  const unsigned back_total = total[0], back_end = x[0];
+  const unsigned count = min((unsigned)n_free + back_total, (unsigned)a.n_pages);
+  // a sequence grows where its pages and its tokens' places last for it and all that grow
+  // before it
+  const bool ok = fresh == 0 || ((get == 0 || x[1] <= count) && x[2] <= (unsigned)a.max_new);
+  sh_back[b] = back_end;
+  sh_to[b] = to;
+  if (__syncthreads_or(!ok)) {   // rare: the sums again, without those
+    x[1] = ok ? get : 0;
+    x[2] = ok ? fresh : 0;
+    x[3] = ok ? w : l;
+    block_scan(x, total, sh_sum);
+  }
+  const int len = ok ? w : l, mine = ok ? fresh : 0;
+  if (b < a.batch) {
+    a.lens_out[b] = len;
+    a.cu_q[b + 1] = (int)x[2];
+    if (a.cu_k) a.cu_k[b + 1] = (int)x[3];
+  }
+  if (b == 0) {
+    a.cu_q[0] = 0;
+    if (a.cu_k) a.cu_k[0] = 0;
+    *a.n_free_out = (int)(count - total[1]);
+    if (a.key_rows && total[3] > (unsigned)a.max_keys) set_error(a.err, kErrIndex);
+  }
+  // ---- pages given back, in the order of the sequences, then those taken from the top
+  for (unsigned e = b; e < back_total; e += kT) {
+    const int s = first_above(kT, e, [&](int m) { return sh_back[m]; });
+    const unsigned j = e - (s ? sh_back[s - 1] : 0);
+    push(a, (long long)n_free + e, a.table + (size_t)s * a.max_pages + sh_to[s] + j);
+  }
+  sh_get[b] = x[1];
+  sh_from[b] = from;
+  if (kFill) {
+    sh_cu[0][b + 1] = (int)x[2];
+    sh_cu[1][b + 1] = (int)x[3];
+    sh_len[b] = len;
+    if (b == 0) sh_cu[0][0] = sh_cu[1][0] = 0;
+  }
+  // a token each at most, as in a decoder's step: its sequence's thread does it all
+  if (!__syncthreads_or(mine > 1) && kFill && !a.key_rows) {
+    if (mine) {
+      const int id = ok && get ? pop(a, count - x[1], row + from) : held;
+      int at = -1;
+      if (id >= 0 && id < a.n_pages) at = (id << a.page_log2) + (l & P1);
+      else set_error(a.err, kErrIndex);
+      a.slots[x[2] - 1] = at;
+      a.positions[x[2] - 1] = l;
+    }
+    for (unsigned i = total[2] + b; i < (unsigned)a.max_new; i += kT)
+      a.slots[i] = a.positions[i] = -1;
+    return;
+  }
+  for (unsigned e = b; e < total[1]; e += kT) {
+    const int s = first_above(kT, e, [&](int m) { return sh_get[m]; });
+    const unsigned j = e - (s ? sh_get[s - 1] : 0);
+    pop(a, count - 1 - e, a.table + (size_t)s * a.max_pages + sh_from[s] + j);
+  }
+  if (kFill) {
+    __syncthreads();
+    fill_rows(a, sh_cu[0], sh_cu[1], sh_len, b, kT);
+  }
+}
+
+// Any number of sequences, kThreads at a time.
 __global__ void __launch_bounds__(kThreads) page_plan_kernel(const Args a) {
   __shared__ unsigned sh_sum[3][kWarps];
   __shared__ unsigned sh_end[kThreads];   // pages moved, up to and with each sequence
@@ -122,24 +243,15 @@ __global__ void __launch_bounds__(kThreads) page_plan_kernel(const Args a) {
   auto &sh_one = *reinterpret_cast<unsigned(*)[1][kWarps]>(&sh_sum[0]);
   pdl_wait();
   pdl_trigger();
-  const long long most = (long long)a.max_pages << a.page_log2;
-  const int P1 = (1 << a.page_log2) - 1;
-  auto pages = [&](int n) { return (n >> a.page_log2) + ((n & P1) != 0); };
+  auto pages = [&](int n) { return pages_of(a, n); };
   int l = 0, w = 0;
   auto read = [&](int b) {
     l = w = 0;
     if (b >= a.batch) return;
-    l = a.lens[b];
-    w = a.want[b];
-    if (l < 0 || w < 0 || l > most || w > most) set_error(a.err, kErrIndex);
-    l = l < 0 ? 0 : l > most ? (int)most : l;
-    w = w < 0 ? 0 : w > most ? (int)most : w;
+    l = checked(a, a.lens[b]);
+    w = checked(a, a.want[b]);
   };
-  int n_free = *a.n_free;
-  if (n_free < 0 || n_free > a.n_pages) {
-    if (threadIdx.x == 0) set_error(a.err, kErrIndex);
-    n_free = n_free < 0 ? 0 : a.n_pages;
-  }
+  const int n_free = checked_stack(a, *a.n_free);
 
   // ---- pages given back, in the order of the sequences
   unsigned back_total = 0;
@@ -156,10 +268,8 @@ __global__ void __launch_bounds__(kThreads) page_plan_kernel(const Args a) {
       for (unsigned e = threadIdx.x; e < total[0]; e += kThreads) {
         const int s = first_above(kThreads, e, [&](int m) { return sh_end[m]; });
         const unsigned j = e - (s ? sh_end[s - 1] : 0);
-        const int id = a.table[(size_t)(b0 + s) * a.max_pages + sh_page[s] + j];
-        const long long at = (long long)n_free + back_total + e;
-        if (at < a.n_pages) a.free_pages[at] = id;
-        if (at >= a.n_pages || id < 0 || id >= a.n_pages) set_error(a.err, kErrIndex);
+        push(a, (long long)n_free + back_total + e,
+             a.table + (size_t)(b0 + s) * a.max_pages + sh_page[s] + j);
       }
       __syncthreads();
     }
@@ -176,7 +286,7 @@ __global__ void __launch_bounds__(kThreads) page_plan_kernel(const Args a) {
   }
   for (int b0 = 0; b0 < a.batch; b0 += kThreads) {
     const int b = b0 + threadIdx.x;
-    if (a.batch > kThreads) read(b);
+    read(b);
     const int from = pages(l);
     const unsigned get = max(0, pages(w) - from), fresh = max(0, w - l);
     unsigned x[3] = {get, fresh, (unsigned)w}, total[3];
@@ -202,9 +312,7 @@ __global__ void __launch_bounds__(kThreads) page_plan_kernel(const Args a) {
       for (unsigned e = threadIdx.x; e < total[0]; e += kThreads) {
         const int s = first_above(kThreads, e, [&](int m) { return sh_end[m]; });
         const unsigned j = e - (s ? sh_end[s - 1] : 0);
-        const int id = a.free_pages[count - 1 - got - e];
-        if (id < 0 || id >= a.n_pages) set_error(a.err, kErrIndex);
-        a.table[(size_t)(b0 + s) * a.max_pages + sh_page[s] + j] = id;
+        pop(a, count - 1 - got - e, a.table + (size_t)(b0 + s) * a.max_pages + sh_page[s] + j);
       }
       __syncthreads();
     }
@@ -217,21 +325,31 @@ __global__ void __launch_bounds__(kThreads) page_plan_kernel(const Args a) {
     *a.n_free_out = (int)(count - got);
     if (a.key_rows && sum_k > (unsigned)a.max_keys) set_error(a.err, kErrIndex);
   }
-  if (kFill) {
+}
+
+// The rows by a grid of their own; the offsets come to shared memory, where a search takes a
+// tenth of the time, as long as they fit.
+constexpr int kFillThreads = 256, kFillBatch = 1024;
+__global__ void __launch_bounds__(kFillThreads) page_rows_kernel(const Args a) {
+  __shared__ int32_t sh_cu[2][kFillBatch + 1], sh_len[kFillBatch];
+  pdl_wait();
+  pdl_trigger();
+  const unsigned first = blockIdx.x * kFillThreads + threadIdx.x;
+  if (a.batch <= kFillBatch) {
+    for (int i = threadIdx.x; i <= a.batch; i += kFillThreads) {
+      sh_cu[0][i] = __ldg(a.cu_q + i);
+      if (a.key_rows) sh_cu[1][i] = __ldg(a.cu_k + i);
+      if (i < a.batch) sh_len[i] = __ldg(a.lens_out + i);
+    }
     __syncthreads();
-    fill_rows(a, threadIdx.x, kThreads);
+    fill_rows(a, sh_cu[0], sh_cu[1], sh_len, first, gridDim.x * kFillThreads);
+  } else {
+    fill_rows(a, a.cu_q, a.cu_k, a.lens_out, first, gridDim.x * kFillThreads);
   }
 }
 
-constexpr int kFillThreads = 256;
-__global__ void __launch_bounds__(kFillThreads) page_rows_kernel(const Args a) {
-  pdl_wait();
-  pdl_trigger();
-  fill_rows(a, blockIdx.x * kFillThreads + threadIdx.x, gridDim.x * kFillThreads);
-}
-
 // Rows that the planning block fills itself.
-constexpr long long kOwnRows = 8 * kThreads;
+constexpr long long kOwnRows = 8192;
 
 }  // namespace
 }  // namespace hsa
@@ -279,10 +397,16 @@ extern "C" int hsa_page_plan(const int32_t *lens, const int32_t *want, int batch
   a.max_keys = a.key_rows ? max_keys : 0;
   cudaStream_t s = (cudaStream_t)stream;
   const long long rows = (long long)max_new + a.max_keys;
-  const bool own = rows <= kOwnRows;
+  const bool own = rows <= kOwnRows && batch <= kThreads;
   count_launches(own ? 1 : 2);
-  launch_pdl(own ? page_plan_kernel<true> : page_plan_kernel<false>, dim3(1), dim3(kThreads), 0, s,
-             a);
+  if (batch > kThreads)
+    launch_pdl(page_plan_kernel, dim3(1), dim3(kThreads), 0, s, a);
+  else if (batch > 256 || (own && rows > 2048))
+    launch_pdl(own ? page_plan_one_kernel<kThreads, true> : page_plan_one_kernel<kThreads, false>,
+               dim3(1), dim3(kThreads), 0, s, a);
+  else
+    launch_pdl(own ? page_plan_one_kernel<256, true> : page_plan_one_kernel<256, false>, dim3(1),
+               dim3(256), 0, s, a);
   if (own) return launch_status();
   if (cudaGetLastError() != cudaSuccess) return HSA_ERR_CUDA;
   const long long need = (rows / 4 + 2 + kFillThreads - 1) / kFillThreads;

@@ -85,6 +85,23 @@ def test_mixed_steps(hsa, B, page, most):
         _check(hsa, lens, want, page, table, free, n, max_new, max_keys, in_place=True)
 
 
+@pytest.mark.parametrize("B", [1, 3, 200, 256, 257, 1024, 1025])
+def test_decoders_steps(hsa, B):
+    """A token each at most: sequences at every place in a page, some that stand still or end."""
+    page = 8
+    lens = [(5 * b) % 40 for b in range(B)]
+    want = [0 if b % 7 == 3 else n if b % 11 == 5 else n + 1 for b, n in enumerate(lens)]
+    table, free, n = _state(lens, page, 6, B // 3 + 1, 9)
+    new = sum(w > h for h, w in zip(lens, want))
+    for max_new in (new, new + 5, new // 2, new + 9000):
+        for n_free in (n, n // 4, 0):
+            _check(hsa, lens, want, page, table, free, n_free, max_new, in_place=n_free == n)
+    _check(hsa, lens, want, page, table, free, n, new, sum(want))
+    bad = table.clone()
+    bad[B // 2, lens[B // 2] // page] = 1 << 20      # the page that a token goes to, or none
+    _check(hsa, lens, want, page, bad, free, n, new)
+
+
 @pytest.mark.parametrize("B", [6, 1300])
 def test_pages_and_places_that_do_not_last(hsa, B):
     """What no longer grows keeps its length; what needs no page still does; nothing is reported."""
