@@ -759,7 +759,8 @@ def profiled_traffic(w, n_of):
     src = os.path.join(ROOT, "paper_2605_06892_gb300", "csrc")
     try:
         digest = code_digest("\n".join(open(os.path.join(src, f)).read()
-                                       for f in ("hsa_tc.cuh", "hsa_attention.cu")))
+                                       for f in ("hsa_tma.cuh", "hsa_tc.cuh",
+                                                 "hsa_attention.cu")))
         per_head, sha = {}, None
         for line in open(path):
             if line.startswith("code_sha256:"):

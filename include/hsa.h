@@ -497,7 +497,8 @@ int hsa_page_plan(const int32_t *lens, const int32_t *want, int batch, int page_
  *                A row as fresh memory holds it, all bytes zero, stands for zeros.
  *   page_table   device, int32 [batch, max_pages]: key j of sequence b is row
  *                j % page_size of page page_table[b, j / page_size].  Entries past a
- *                sequence's last page are not read, nor rows past its last key.
+ *                sequence's last page are not read, nor rows past its last key (HSA_E2M1:
+ *                codes of such rows of its last page may be, and reach nothing).
  *   seq_lens     device, int32 [batch], in [0, max_pages * page_size]; a value
  *                outside is taken as the nearer end and reported (HSA_ERR_INDEX).
  *   out          device, bf16 [batch, n_new, Hq, D], written.

@@ -1,9 +1,9 @@
 /*
  * hsa_test.h -- test hooks of libhsa (not needed by applications).
  *
- * The attention kernel bounds every pipeline wait (about one second) and, when
- * one runs out, records HSA_ERR_TIMEOUT, stops issuing work, drains its own
- * copies and tensor-core operations, frees its tensor memory and returns, so
+ * The attention kernels, and the norm across heads, bound every pipeline wait (about
+ * one second) and, when one runs out, record HSA_ERR_TIMEOUT, stop issuing work, drain
+ * their own copies and tensor-core operations, free their tensor memory and return, so
  * the CUDA context stays usable.  The first hook lets a test drive that path on
  * a GPU without any fault: it withholds one internal signal so that a wait can
  * never complete.  The second shows a launch plan.  The paper has no counterpart.
@@ -20,7 +20,10 @@ extern "C" {
  *         hsa_packed_attention) launch that follows, each CTA
  *         never loads its first value tile, so the bounded wait for it runs
  *         out; the call then reports HSA_ERR_TIMEOUT through
- *         hsa_get_device_error and its output is unspecified.
+ *         hsa_get_device_error and its output is unspecified.  So does
+ *         hsa_paged_attention over a 4-bit cache, and hsa_qk_norm_rope across
+ *         the heads of as many tokens as the GPU has SMs or more, whose blocks
+ *         never get their first token's row of the table.
  * Process-wide, host side only; returns the previous mode, or
  * HSA_ERR_INVALID_ARG (-1) for an unknown mode. */
 int hsa_test_inject_attention_stall(int mode);

@@ -369,6 +369,7 @@ constexpr int kRingThreads = 512;   // at most
 struct RingArgs {
   Args a;
   int n, stages, stage;       // tokens; stages of `stage` bytes
+  int inject_stall;           // test hook (hsa_test.h)
   int bytes[4], at[4];        // of q, k, v and the table's row in a stage
   float inv[2];               // 1 / values of q's and k's mean
 };
@@ -415,7 +416,8 @@ __global__ void __maxnreg__((kY == 1 ? 64 : 96)) norm_ring_kernel(const RingArgs
   if (leads) {
     for (int s = 0, j = blockIdx.x; s < z.stages && j < z.n; ++s, j += step) load_rows(j, s);
     for (int s = 0, j = blockIdx.x; s < z.stages && j < z.n; ++s, j += step)
-      load_table(trow_of(j, slot_of(j)), s);
+      if (z.inject_stall != 1 || s)   // test hook: the first token's never comes
+        load_table(trow_of(j, slot_of(j)), s);
   }
   const int vecs8 = a.D / 8, in_head = threadIdx.x % vecs8;
   Values w[2][kY];
@@ -602,6 +604,7 @@ bool launch_ring(const Args &a, int n, bool with_v, cudaStream_t s) {
   z.a = a;
   z.n = n;
   z.stage = 0;
+  z.inject_stall = attention_stall();
   for (int i = 0; i < 4; ++i) {
     z.bytes[i] = i == 3 ? (a.table ? 4 * a.D : 0)
                  : i == 2 && !with_v ? 0 : a.H[i] * a.D * (kF32 ? 4 : 2);

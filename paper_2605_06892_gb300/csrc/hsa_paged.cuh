@@ -30,6 +30,7 @@ struct PagedArgs {
   Divider group;                                // by G = Hq / Hkv
   int n_pages, page_log2, max_pages, sms;
   int side;                        // units that run side by side (4 bits), or 1
+  int inject_stall;                // test hook (hsa_test.h)
   float scale_log2, scale_digits, scale_power;   // the first is the others' product
 };
 

@@ -963,6 +963,7 @@ extern "C" int hsa_paged_attention(const void *q, int batch, int n_new, int Hq, 
   a.max_pages = n_pages > 0 ? max_pages : 0;
   a.sms = sm_count();
   a.side = 1;
+  a.inject_stall = attention_stall();
   a.page_log2 = 0;
   while ((1 << a.page_log2) < page_size) ++a.page_log2;
   a.scale_log2 = scale * 1.4426950408889634f;

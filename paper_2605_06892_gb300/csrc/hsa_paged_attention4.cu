@@ -465,6 +465,7 @@ paged_attention4_kernel(const __grid_constant__ Maps maps, const PagedArgs a) {
       *w = make_uint2(0u, 0u);   // factors of zero
     }
     arrive_with_copies(bar);
+    const bool withheld = a.inject_stall == 1 && loaded == 0;   // test hook: V never loads
     if (boxes) {
       uint8_t *dst = ring + fill * C::kStage;
       const bool leads = elect_one();
@@ -473,8 +474,9 @@ paged_attention4_kernel(const __grid_constant__ Maps maps, const PagedArgs a) {
         const int y = __shfl_sync(0xffffffffu, slot, i);
         if (leads) {
           tma_load_2d(dst + i * C::kRowBytes, &maps.k, &full[warp][fill], h * C::kRowBytes, y);
-          tma_load_2d(dst + C::kHalf + i * C::kRowBytes, &maps.v, &full[warp][fill],
-                      h * C::kRowBytes, y);
+          if (!withheld)
+            tma_load_2d(dst + C::kHalf + i * C::kRowBytes, &maps.v, &full[warp][fill],
+                        h * C::kRowBytes, y);
         }
       }
     } else {
@@ -487,7 +489,7 @@ paged_attention4_kernel(const __grid_constant__ Maps maps, const PagedArgs a) {
 #pragma unroll
         for (int c = 0; c < C::kChunks; ++c) {
           bulk16(dst + place<D>(lane, c), a.k + at + 16 * c, bar);
-          bulk16(dst + C::kHalf + place<D>(lane, c), a.v + at + 16 * c, bar);
+          if (!withheld) bulk16(dst + C::kHalf + place<D>(lane, c), a.v + at + 16 * c, bar);
         }
       }
     }
