@@ -7,7 +7,7 @@
 // the step is a few prefix sums and, between them, the moves.  A few kilobytes move: what
 // bounds it is the chain of loads, sums and barriers, and the launch.
 //
-// One block does the sums and moves the pages: of up to 256 or 1024 sequences, a thread each,
+// One block does the sums and moves the pages: of up to 512 or 1024 sequences, a thread each,
 // with one exchange of all four sums, or of 1024 at a time.  The sums saturate at 2^31 - 1,
 // where min(a + b, 2^31 - 1) is still associative, so 32 bits serve whatever the lengths are.
 // The rows of tokens and keys are filled by the same block where they are few, else by a second
@@ -19,6 +19,10 @@ namespace {
 
 constexpr int kThreads = 1024;
 constexpr int kWarps = kThreads / 32;
+// Threads for as many sequences or fewer.  Replayed from a graph (an empty one takes 4.1 us), 64
+// sequences, a token each / six of them ended besides, with 750 pages given back: 256 threads
+// 4.1 / 8.2 us, 512 4.1 / 6.2, 1024 6.2 / 6.2.
+constexpr int kFew = 512;
 constexpr unsigned kMost = 0x7fffffffu;
 
 struct Args {
@@ -401,12 +405,12 @@ extern "C" int hsa_page_plan(const int32_t *lens, const int32_t *want, int batch
   count_launches(own ? 1 : 2);
   if (batch > kThreads)
     launch_pdl(page_plan_kernel, dim3(1), dim3(kThreads), 0, s, a);
-  else if (batch > 256 || (own && rows > 2048))
+  else if (batch > kFew || (own && rows > 4 * kFew))
     launch_pdl(own ? page_plan_one_kernel<kThreads, true> : page_plan_one_kernel<kThreads, false>,
                dim3(1), dim3(kThreads), 0, s, a);
   else
-    launch_pdl(own ? page_plan_one_kernel<256, true> : page_plan_one_kernel<256, false>, dim3(1),
-               dim3(256), 0, s, a);
+    launch_pdl(own ? page_plan_one_kernel<kFew, true> : page_plan_one_kernel<kFew, false>, dim3(1),
+               dim3(kFew), 0, s, a);
   if (own) return launch_status();
   if (cudaGetLastError() != cudaSuccess) return HSA_ERR_CUDA;
   const long long need = (rows / 4 + 2 + kFillThreads - 1) / kFillThreads;
