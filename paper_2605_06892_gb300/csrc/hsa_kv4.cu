@@ -17,7 +17,9 @@
 //
 // Borders are decided exactly.  A bf16 value has eight bits and a border, m_g times 0.25 .. 5,
 // at most nine, so x / m_g is at a border or at least 2^-10 from it: formed within 2^-20 and
-// rounded to multiples of 2^-14 it falls on the right side.  An fp32 value is compared with the
+// rounded to multiples of 2^-14 it falls on the right side.  In fp32 x / m_g, formed within
+// 2^-22 of itself and so within 2^-19, falls on the right side where it is 2^-18 or more from
+// each multiple of 1/4, which all borders are; nearer values (zeros too) are compared with the
 // borders m_g 0.25 .. m_g 5 themselves, which are exact.
 //
 // Both kernels are bound by HBM: 2.5 bytes move per element of a bf16 tensor, so there are few
@@ -43,6 +45,9 @@ __device__ __forceinline__ uint4 ld_stream(const void *p) {
                : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
   return v;
 }
+__device__ __forceinline__ void prefetch_l2(const void *p) {
+  asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
+}
 __device__ __forceinline__ uint32_t ld_codes(const void *p) {
   uint32_t v;
   asm volatile("ld.global.L1::no_allocate.u32 %0, [%1];" : "=r"(v) : "l"(p));
@@ -51,6 +56,9 @@ __device__ __forceinline__ uint32_t ld_codes(const void *p) {
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t *>(&v);
+}
+__device__ __forceinline__ uint64_t twice(float f) {
+  return pack2(__float_as_uint(f), __float_as_uint(f));
 }
 __device__ __forceinline__ float lo_bf16(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_bf16(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
@@ -236,6 +244,20 @@ __device__ __forceinline__ void quantise(Eight<kF32> (&v)[Y::kN], uint32_t (&cod
     float x[8];
     unpack8(v[y], x);
     if (kF32) {
+      float r[8], near = 1.f;   // x / m_g, and how far the closest is from a multiple of 1/4
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) {
+        const uint64_t z = mul2(pack2(__float_as_uint(x[i]), __float_as_uint(x[i + 1])),
+                                twice(per[i / kRun]));
+        const uint64_t quarters = add2(add2(z, twice(0x1.8p21f)), twice(-0x1.8p21f));
+        const uint64_t off = fma2(quarters, twice(-1.f), z);   // exact
+        near = fminf(near, fminf(fabsf(lo_f(off)), fabsf(hi_f(off))));
+        r[i] = lo_f(z), r[i + 1] = hi_f(z);
+      }
+      if (near >= 0x1p-18f) {
+        code[y] = codes8(r);
+        continue;
+      }
       uint32_t c = 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -249,11 +271,8 @@ __device__ __forceinline__ void quantise(Eight<kF32> (&v)[Y::kN], uint32_t (&cod
     } else {
 #pragma unroll
       for (int i = 0; i < 8; i += 2) {
-        const uint32_t p = __float_as_uint(per[i / kRun]);
-        const uint64_t z = add2(
-            fma2(pack2(__float_as_uint(x[i]), __float_as_uint(x[i + 1])), pack2(p, p),
-                 pack2(__float_as_uint(768.f), __float_as_uint(768.f))),
-            pack2(__float_as_uint(-768.f), __float_as_uint(-768.f)));
+        const uint64_t z = add2(fma2(pack2(__float_as_uint(x[i]), __float_as_uint(x[i + 1])),
+                                     twice(per[i / kRun]), twice(768.f)), twice(-768.f));
         x[i] = lo_f(z), x[i + 1] = hi_f(z);
       }
       code[y] = codes8(x);
@@ -276,7 +295,11 @@ struct QuantArgs {
 
 constexpr int kQuantBlocks = 3;   // per SM, all resident at once
 
-// One item is a (token, head) of the fresh rows, K and V.
+// One item is a (token, head) of the fresh rows, K and V.  18900 tokens of 40 heads of D = 128,
+// turned: 88 us, 0.84 of HBM's measured rate, and fp32 142, 0.91; 37800 of D = 64 99 us, 0.75, for
+// what is done per row is done twice as often.  At D = 128 rows are asked for one item ahead (90 us
+// without; at D = 64, where issue slots bind, that costs 2 us).  Four blocks of 64 registers 93 us,
+// five 104.
 template <int D, bool kF32, bool kRope>
 __global__ void __launch_bounds__(kThreads, kQuantBlocks)
 kv4_quant_scatter_kernel(const QuantArgs a) {
@@ -289,6 +312,14 @@ kv4_quant_scatter_kernel(const QuantArgs a) {
   // all lanes of a warp run as often as its first
   for (unsigned long long i = first; i - lane / kL < a.items; i += step) {
     const bool there = i < a.items;
+    if (D == 128 && i + step < a.items) {   // a line of the lane group's next rows, into L2
+      static_assert(D * (kF32 ? 4 : 2) / 128 * 2 == kL, "the lanes' lines are the rows'");
+      const unsigned n = (unsigned)i + step, nj = quotient(n, a.heads);
+      const bool of_k = c < kL / 2;
+      const size_t at = (size_t)nj * (of_k ? a.k_row : a.v_row) +
+                        (size_t)(n - nj * a.heads.d) * D + c % (kL / 2) * (kF32 ? 32 : 64);
+      prefetch_l2(static_cast<const uint8_t *>(of_k ? a.kf : a.vf) + at * (kF32 ? 4 : 2));
+    }
     const unsigned j = quotient((unsigned)i, a.heads), h = (unsigned)i - j * a.heads.d;
     int slot = -1, trow = 0;
     Eight<kF32> k[kN] = {}, v[kN] = {};
