@@ -15,11 +15,15 @@
 // equal parts, and MMAs over one group only.
 //
 // What bounds it.  68 bytes a key and head leave 370 issue slots of an SM's quarter for 16 keys
-// of one head at the memory's rate, and decoding (96 conversions and shuffles of bits), 16 MMAs
-// and the softmax need most of them.  So the tiles come by TMA, a box of a page's rows each,
-// which costs the lanes next to nothing, and the blocks of a key's heads run side by side: their
-// rows and words lie together, and what one block leaves of a line or sector the others find in
-// L2 (4 sequences of 95000 keys: 134 -> 112 us).
+// of one head at the memory's rate, and decoding (64 conversions and shuffles of bits), 16 MMAs
+// and the softmax need most of them; three warps a quarter, which is what the registers allow, use
+// half of the slots.  So what does not grow with the bytes is kept small: the tiles come by TMA, a
+// box of a page's rows each, a warp holds 64 keys of a tile and takes them 32 at a time, their
+// words wait in registers, and the blocks of a key's heads run side by side: their rows and words
+// lie together, and what one block leaves of a line or sector the others find in L2 (4 sequences
+// of 95000 keys: 134 -> 112 us).  32 query heads over 8 of D = 128: 4 sequences of 95000 keys 101
+// us, 4.1 TB/s, 0.60 of HBM's measured rate (tiles of 32 keys a warp 109); 48 of 4500 68 us, 0.48;
+// one of 4001 11.6 us.
 #include <algorithm>
 #include <atomic>
 #include <cstring>
@@ -31,8 +35,10 @@
 namespace hsa {
 namespace {
 
-constexpr int kKW = 32;                        // keys per warp and tile
-constexpr int kTile = kWarps * kKW;
+constexpr int kKW = 32;                        // keys that a warp takes at a time
+constexpr int kParts = 2;                      // parts of a tile's keys of one warp, kKW each
+constexpr int kHold = kParts * kKW;
+constexpr int kTile = kWarps * kHold;
 constexpr float kShift = 6.f;                  // probabilities are 2^(u - M + 6)
 constexpr float kSlack = 4.f;                  // u - M at most; then M rises
 
@@ -41,17 +47,16 @@ struct Cfg4 {
   static constexpr int kRows = 8 * kNR;        // query rows of a unit
   static constexpr int kRowBytes = D / 2;
   static constexpr int kChunks = kRowBytes / 16;
-  static constexpr int kStages = 3;
+  static constexpr int kStages = 2;
   static constexpr int kBlocks = kNR == 1 ? (D == 64 ? 4 : 3) : 2;   // per SM: registers
-  static constexpr int kHalf = kKW * kRowBytes;                      // K (or V) bytes of a stage
+  static constexpr int kHalf = kHold * kRowBytes;                      // K (or V) bytes of a stage
   static constexpr int kStage = 2 * kHalf;
-  static constexpr int kRaw = kStages * kKW * 8;                     // words of K and V per key
-  static constexpr int kMade = kKW * 40;                             // what a tile's words make
+  static constexpr int kMade = kKW * 40;                             // what kKW keys' words make
   static constexpr int kQ = kRows * D * 2;                           // a unit's query rows
   static constexpr int kPart = part_floats(D, true, kRows);
   static constexpr int kAlign = 512;                                 // the swizzle's period
   static constexpr int kSmem =
-      kAlign + kWarps * (kStages * kStage + kRaw + kMade) + kStages * kQ;
+      kAlign + kWarps * (kStages * kStage + kMade) + kStages * kQ;
 };
 
 // The key (row of an 8-key block) of MMA index n: the pairs 2t, 2t+1 are neighbours, and the
@@ -103,11 +108,6 @@ __device__ __forceinline__ void bulk16(uint32_t dst, const void *src, uint32_t b
           "r"(dst), "l"(src), "r"(bar)
       : "memory");
 }
-// The barrier's phase also waits for this thread's copies so far (counted in its arrivals).
-__device__ __forceinline__ void arrive_with_copies(uint32_t bar) {
-  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
-}
-
 // The four dimensions of a query row that lane t of a quad multiplies at step s of K = 16, in
 // the order of its K fragments (chunk c of row r lies at c ^ (r & 7)).  A step stays within a
 // group: two steps to one at D = 128; at D = 64 it takes two pairs eight dimensions apart.
@@ -336,12 +336,11 @@ paged_attention4_kernel(const __grid_constant__ Maps maps, const PagedArgs a) {
   uint8_t *smem = dyn + (-smem_addr(dyn) & (C::kAlign - 1));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   uint8_t *ring = smem + warp * (C::kStages * C::kStage);
-  uint8_t *words = smem + kWarps * C::kStages * C::kStage + warp * (C::kRaw + C::kMade);
-  uint2 *raw = reinterpret_cast<uint2 *>(words);                    // [stage][key]
-  uint4 *made = reinterpret_cast<uint4 *>(words + C::kRaw);         // of the present tile
-  uint8_t *sq = smem + kWarps * (C::kStages * C::kStage + C::kRaw + C::kMade);
+  uint4 *made = reinterpret_cast<uint4 *>(smem + kWarps * C::kStages * C::kStage +
+                                          warp * C::kMade);         // of the present keys
+  uint8_t *sq = smem + kWarps * (C::kStages * C::kStage + C::kMade);
   if (lane == 0)
-    for (int s = 0; s < C::kStages; ++s) mbar_init(&full[warp][s], 33);
+    for (int s = 0; s < C::kStages; ++s) mbar_init(&full[warp][s], 1);
   if (threadIdx.x == 0) abort_flag = 0;
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   // `side` neighbouring blocks take the same run of tiles, each for a unit of its own
@@ -399,33 +398,36 @@ paged_attention4_kernel(const __grid_constant__ Maps maps, const PagedArgs a) {
     __syncthreads();
   }
   const int n_tiles = first_tile(plan, run + 1) - first_tile(plan, run);
-  Place here;
-  Cursor &cur = here.c;
+  Cursor cur;
   cur.b = sh_at[0];
   cur.len = sh_at[1];
   cur.tiles = (cur.len + kTile - 1) / kTile;
   cur.unit = sh_at[2] / cur.tiles;
   cur.tile = sh_at[2] - cur.unit * cur.tiles;
   if (side > 1) cur.unit = blockIdx.x - run * side;   // from 0, of one unit
-  set_unit(a, here, kRows);
-  CutUnit cut = {};
+  if (threadIdx.x == 0) a.cuts[blockIdx.x].parts = 0;
 
-  // ---- the ring: `ahead` is the next tile to load; the page of this lane's key in it is read
+  // ---- the ring: `ahead` is the next tile to load; the pages of this lane's keys in it are read
   // one tile before, and looked at only then
-  Place next = here;
+  Place next = {cur, 0, 0};
   Cursor &ahead = next.c;
+  set_unit(a, next, kRows);
   int left = n_tiles, loaded = 0;           // tiles to load, and loaded
   int fill = 0;                             // the stage of the next one
   const uint32_t ring_s = smem_addr(ring), bars = smem_addr(&full[warp][0]);
-  // a box is a page's rows, or 32; boxes below 128 bytes go row by row instead
-  const int box = min(kKW, 1 << a.page_log2);
+  // a box is a page's rows, or kHold; boxes below 128 bytes go row by row instead
+  const int box = min(kHold, 1 << a.page_log2);
   const bool boxes = box * C::kRowBytes >= 128;
-  int page;
+  int page[kParts];
+  uint32_t wk[kParts], wv[kParts];          // the keys' words, loaded a tile before they are used
   auto look_up = [&]() {
-    const int key = ahead.tile * kTile + warp * kKW + lane;
-    page = -1;
-    if (key < ahead.len)
-      page = __ldg(a.table + (size_t)ahead.b * a.max_pages + (key >> a.page_log2));
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) {
+      const int key = ahead.tile * kTile + warp * kHold + i * kKW + lane;
+      page[i] = -1;
+      if (key < ahead.len)
+        page[i] = __ldg(a.table + (size_t)ahead.b * a.max_pages + (key >> a.page_log2));
+    }
   };
   look_up();
   int q_fill = 0, q_now = 0;                // buffers of the next unit's rows, and of this one's
@@ -449,29 +451,30 @@ paged_attention4_kernel(const __grid_constant__ Maps maps, const PagedArgs a) {
       }
       q_fill = q_fill + 1 == C::kStages ? 0 : q_fill + 1;
     }
-    const int key = ahead.tile * kTile + warp * kKW + lane;
-    const bool ok = page >= 0 && page < a.n_pages;
-    if (!ok && key < ahead.len) set_error(a.err, kErrIndex);
-    // a row that there is not lies past the last: TMA fills it with zeros
-    const int slot = ok ? (page << a.page_log2) + (key & ((1 << a.page_log2) - 1))
-                        : a.n_pages << a.page_log2;
     const uint32_t bar = bars + 8 * fill;
-    uint2 *w = raw + fill * kKW + lane;
-    if (ok) {
-      const size_t at = 4 * ((size_t)slot * a.Hkv + h);
-      copy4(smem_addr(w), a.ks + at);
-      copy4(smem_addr(w) + 4, a.vs + at);
-    } else {
-      *w = make_uint2(0u, 0u);   // factors of zero
+    int slot[kParts];
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) {
+      const int key = ahead.tile * kTile + warp * kHold + i * kKW + lane;
+      const bool ok = page[i] >= 0 && page[i] < a.n_pages;
+      if (!ok && key < ahead.len) set_error(a.err, kErrIndex);
+      // a row that there is not lies past the last: TMA fills it with zeros
+      slot[i] = ok ? (page[i] << a.page_log2) + (key & ((1 << a.page_log2) - 1))
+                   : a.n_pages << a.page_log2;
+      wk[i] = wv[i] = 0u;   // factors of zero
+      if (ok) {
+        const size_t at = (size_t)slot[i] * a.Hkv + h;
+        wk[i] = __ldg(reinterpret_cast<const uint32_t *>(a.ks) + at);
+        wv[i] = __ldg(reinterpret_cast<const uint32_t *>(a.vs) + at);
+      }
     }
-    arrive_with_copies(bar);
     const bool withheld = a.inject_stall == 1 && loaded == 0;   // test hook: V never loads
     if (boxes) {
       uint8_t *dst = ring + fill * C::kStage;
       const bool leads = elect_one();
       if (leads) mbar_expect_tx(&full[warp][fill], C::kStage);
-      for (int i = 0; i < kKW; i += box) {
-        const int y = __shfl_sync(0xffffffffu, slot, i);
+      for (int i = 0; i < kHold; i += box) {
+        const int y = __shfl_sync(0xffffffffu, i < kKW ? slot[0] : slot[kParts - 1], i % kKW);
         if (leads) {
           tma_load_2d(dst + i * C::kRowBytes, &maps.k, &full[warp][fill], h * C::kRowBytes, y);
           if (!withheld)
@@ -480,16 +483,22 @@ paged_attention4_kernel(const __grid_constant__ Maps maps, const PagedArgs a) {
         }
       }
     } else {
-      const unsigned have = __popc(__ballot_sync(0xffffffffu, ok));
+      const int none = a.n_pages << a.page_log2;
+      unsigned have = 0;
+#pragma unroll
+      for (int i = 0; i < kParts; ++i) have += __popc(__ballot_sync(0xffffffffu, slot[i] < none));
       if (lane == 0) mbar_expect_tx(&full[warp][fill], have * 2 * C::kRowBytes);
       __syncwarp();
-      if (ok) {   // what the stage held before is finite, and its factors are zero
+#pragma unroll
+      for (int i = 0; i < kParts; ++i) {
+        if (slot[i] >= none) continue;   // what the stage held is finite, and its factors are zero
         const uint32_t dst = ring_s + fill * C::kStage;
-        const size_t at = ((size_t)slot * a.Hkv + h) * C::kRowBytes;
+        const size_t at = ((size_t)slot[i] * a.Hkv + h) * C::kRowBytes;
 #pragma unroll
         for (int c = 0; c < C::kChunks; ++c) {
-          bulk16(dst + place<D>(lane, c), a.k + at + 16 * c, bar);
-          if (!withheld) bulk16(dst + C::kHalf + place<D>(lane, c), a.v + at + 16 * c, bar);
+          const uint32_t to = dst + place<D>(i * kKW + lane, c);
+          bulk16(to, a.k + at + 16 * c, bar);
+          if (!withheld) bulk16(to + C::kHalf, a.v + at + 16 * c, bar);
         }
       }
     }
@@ -515,6 +524,7 @@ paged_attention4_kernel(const __grid_constant__ Maps maps, const PagedArgs a) {
   bool first = true;     // this warp has none of the unit's keys yet
   bool live = true;      // no wait has run out
   int now = 0;           // the stage of tile `it`
+  auto row0 = [&]() { return cur.unit % a.row_tiles * kRows; };   // the unit's first row
   uint32_t phase = 0;
 
   for (int it = 0; it < n_tiles; ++it) {
@@ -526,6 +536,9 @@ paged_attention4_kernel(const __grid_constant__ Maps maps, const PagedArgs a) {
     } else {
       __syncwarp();
     }
+    uint32_t wk_now[kParts], wv_now[kParts];
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) wk_now[i] = wk[i], wv_now[i] = wv[i];
     if (live) load_tile();
 
     if (fresh) {
@@ -581,19 +594,24 @@ paged_attention4_kernel(const __grid_constant__ Maps maps, const PagedArgs a) {
       }
     }
 
-    const int key0 = cur.tile * kTile + warp * kKW;
-    if (key0 < cur.len) {
-      const uint32_t sk = ring_s + now * C::kStage, sv = sk + C::kHalf;
+#pragma unroll 1
+    for (int i = 0; i < kParts; ++i) {
+      const int key0 = cur.tile * kTile + warp * kHold + i * kKW;
+      if (key0 >= cur.len) break;
+      const uint32_t sk = ring_s + now * C::kStage + i * (C::kHalf / kParts), sv = sk + C::kHalf;
+      if (i) __syncwarp();   // the keys before have been taken
       {
         // A lane's key: (kf, kf, ve, ve) with kf = 2^ks times the scale's digits and ve = vs;
         // K's factors; V's in fp16, beside those of the pair's other key: this lane makes two
         // groups' of both, the key of the even MMA index low.  A row of NaN has s = 255: its
         // kf, and its V factors, are NaN.
-        const uint2 w = raw[now * kKW + lane];
+        const uint2 w = i == 0 ? make_uint2(wk_now[0], wv_now[0])
+                               : make_uint2(wk_now[kParts - 1], wv_now[kParts - 1]);
         const uint32_t ks = w.x >> 24, vs = w.y >> 24;
         const uint32_t kf =
             ks == 255u ? 0x7fffffffu : __float_as_uint(__uint_as_float(ks << 23) * a.scale_digits);
-        const uint32_t ve = __float_as_uint((float)((int)(vs == 255u ? 127u : vs) - 127));
+        const uint32_t ve = __float_as_uint(
+            __uint_as_float(0x4b000000u | (vs == 255u ? 127u : vs)) - (0x1p23f + 127.f));
         made[lane] = make_uint4(kf, kf, ve, ve);
         auto factor = [&](int i) {
           return __float_as_uint(__uint_as_float(0x4b000000u | (w.x >> (6 * i) & 63u)) - 0x1p23f);
@@ -619,7 +637,7 @@ paged_attention4_kernel(const __grid_constant__ Maps maps, const PagedArgs a) {
       // keys that row 8 x + 2 t + j sees, where that matters
       auto limit = [&](int x, int j) {
         return cur.len - a.n_new + 1 +
-               (int)quotient(here.row0 + 8 * x + 2 * t + j, a.group);
+               (int)quotient(row0() + 8 * x + 2 * t + j, a.group);
       };
       float s[kNB][kNR][4], mx[kNR][2], sum[kNR][2];
       score_tile<D, kNR>(sk, made + kKW, g, t, s, [&](int step, int x) {
@@ -748,7 +766,7 @@ paged_attention4_kernel(const __grid_constant__ Maps maps, const PagedArgs a) {
                 pack_f16(fast_exp2(s[b][x][2 * n]), fast_exp2(s[b][x][2 * n + 1])));
           }
         auto sees = [&](int x, int k) {
-          return key0 + k < cur.len - a.n_new + 1 + (int)quotient(here.row0 + 8 * x + g, a.group);
+          return key0 + k < cur.len - a.n_new + 1 + (int)quotient(row0() + 8 * x + g, a.group);
         };
         if (ragged && a.n_new > 1)
           add_values<D, kNR, true>(o, p, sv, made + 2 * kKW, b, g, t, sees);
@@ -763,7 +781,7 @@ paged_attention4_kernel(const __grid_constant__ Maps maps, const PagedArgs a) {
       // sums in the stage that it has just read, lane by lane, and takes a quarter of the
       // dimensions of all four.  TMA fills the stage again only after the barrier that starts
       // the next unit.
-      const int h = here.head, r0 = here.row0;
+      const int h = cur.unit / a.row_tiles, r0 = row0();
 #pragma unroll
       for (int x = 0; x < kNR; ++x)
 #pragma unroll
@@ -778,7 +796,7 @@ paged_attention4_kernel(const __grid_constant__ Maps maps, const PagedArgs a) {
         }
       __syncwarp();   // every lane has read the stage
       constexpr int kQuarter = kMT / kWarps;                // MMA blocks of 16 dimensions
-      static_assert(C::kStage == kMT * 512, "a stage takes the sums of a column block");
+      static_assert(C::kStage >= kMT * 512, "a stage takes the sums of a column block");
       const bool whole = unit_tile0 == 0 && unit_done;
       float *part = a.ws + (size_t)(2 * blockIdx.x + (first_unit ? 0 : 1)) * C::kPart;
 #pragma unroll
@@ -859,17 +877,17 @@ paged_attention4_kernel(const __grid_constant__ Maps maps, const PagedArgs a) {
       if (unit_done && !whole) {   // a run ends one such unit at most: its first
         const int t0 = first_tile(plan, run) - unit_tile0;
         const int c0 = cta_of(plan, t0);
-        cut.parts = run - c0 + 1;
-        cut.first = blockIdx.x - (run - c0) * side;
-        cut.slot = 2 * cut.first + (first_tile(plan, c0) == t0 ? 0 : 1);
-        cut.b = cur.b;
-        cut.unit = cur.unit;
+        const int first_block = blockIdx.x - (run - c0) * side;
+        if (threadIdx.x == 0)
+          a.cuts[blockIdx.x] = {run - c0 + 1, first_block,
+                                2 * first_block + (first_tile(plan, c0) == t0 ? 0 : 1), cur.b,
+                                cur.unit};
       }
       first_unit = false;
       fresh = true;
     }
     if (++now == C::kStages) now = 0, phase ^= 1;
-    if (it + 1 < n_tiles) advance(a, here, side, kRows);
+    if (it + 1 < n_tiles) step(a, cur, kTile, side);
   }
   wait_all_but<0>();
   if (!live) {
@@ -877,7 +895,6 @@ paged_attention4_kernel(const __grid_constant__ Maps maps, const PagedArgs a) {
     for (int i = max(0, loaded - C::kStages); i < loaded; ++i)
       mbar_wait(&full[warp][i % C::kStages], i / C::kStages & 1, &abort_flag, a.err, false);
   }
-  if (threadIdx.x == 0) a.cuts[blockIdx.x] = cut;
   clear_empty<D>(a);
 }
 
@@ -929,7 +946,7 @@ int launch(PagedArgs &a, void *workspace, cudaStream_t stream) {
   std::memset(&maps, 0, sizeof maps);
   if (tiles) {
     const long long rows = (long long)a.n_pages << a.page_log2;
-    const int box = std::min(kKW, 1 << a.page_log2);
+    const int box = std::min(kHold, 1 << a.page_log2);
     if (!make_map(maps.k, a.k, rows, a.Hkv, C::kRowBytes, box) ||
         !make_map(maps.v, a.v, rows, a.Hkv, C::kRowBytes, box))
       return HSA_ERR_CUDA;
