@@ -307,7 +307,8 @@ __global__ void __launch_bounds__(kThreads, kHeadBlocks) norm_heads_kernel(const
   }
 }
 
-// A unit is one token's row of one tensor, taken by kT threads of a block.
+// A unit is one token's row of one tensor, taken by kT threads of a block: fewer tokens than SMs,
+// where the ring has nothing to run ahead of, and rows that leave it no stages.
 constexpr int kVectors = 4;      // vectors of eight values a thread
 
 template <bool kF32, int kT>
@@ -383,7 +384,9 @@ norm_row_kernel(const Args a) {
 // of q, k, v and the table come by bulk copies into a ring of stages, so that what is in flight
 // does not depend on registers and occupancy; v goes out again without passing through them.  A
 // thread holds the same kY vectors of q and of k of every token, so that their weights stay in
-// registers, and (a head's vectors divide the block's threads) one place in a head.
+// registers, and (a head's vectors divide the block's threads) one place in a head.  bf16, 40 heads
+// of each, D = 128: 18900 tokens 181 us, 0.95 of HBM's measured rate (a group of warps per row
+// 397); 1200 14.4 (24.7), 600 10.3 (14.5), 300 8.2 (10.3).
 constexpr int kMostStages = 8;
 constexpr int kRingThreads = 512;   // at most
 

@@ -7,8 +7,8 @@
 //   2^ks sum_g m_g <q_g, code_g>,
 // sums of exact fp16 products over one group each, times the factors in 32 bits.  A value's
 // factors go into the probabilities, one group of dimensions after the other: P in fp16 is
-// 2^(u - M + 6), at most 2^10 * 63 with a factor (u is 4 above M at most), and its product with one is rounded to fp16
-// again (2^-11 of itself).  Codes are always finite; where a row is held as NaN its factors are.
+// 2^(u - M + 6), at most 2^10 * 63 with a factor (u is 4 above M at most), and its product with
+// one is rounded to fp16 again (2^-11 of itself).  Codes are always finite; where a row is held as NaN its factors are.
 //
 // The groups interleave (dimension d is of group (d / (D/32)) mod 4): the 16 (D = 64: 8) bytes
 // of a key that a lane of a quad multiplies, and the 8 (4) bytes of a value, hold all four in
@@ -977,8 +977,10 @@ int launch(PagedArgs &a, void *workspace, cudaStream_t stream) {
 
 int launch_paged4(PagedArgs &a, int D, void *workspace, cudaStream_t stream) {
   if (D == 128)
-    return a.rows <= 8 ? launch<128, 1>(a, workspace, stream) : launch<128, 2>(a, workspace, stream);
-  return a.rows <= 8 ? launch<64, 1>(a, workspace, stream) : launch<64, 2>(a, workspace, stream);
+    return a.rows <= 8 ? launch<128, 1>(a, workspace, stream)
+                       : launch<128, 2>(a, workspace, stream);
+  return a.rows <= 8 ? launch<64, 1>(a, workspace, stream)
+                     : launch<64, 2>(a, workspace, stream);
 }
 
 }  // namespace hsa
