@@ -134,6 +134,46 @@ def test_page_sizes(hsa, page):
     _check(hsa, [77, 300, 3], 2, 4, 2, 64, page, page)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("page", [4, 16, 32, 64, 128])
+def test_ends_of_tiles(hsa, page, D):
+    """Lengths about the ends of what a warp and a block hold, pages that end inside."""
+    lens = [47, 49, 191, 192, 193, 223, 225, 255, 256, 257, 289, 321, 511, 512, 513]
+    _check(hsa, lens, 1, 4, 2, D, page, 60 + page)
+    _check(hsa, [n + 2 for n in lens], 3, 2, 2, D, page, 61 + page)
+
+
+def test_two_graphs_that_share_a_workspace(hsa):
+    """Captured with different batches and row counts over one workspace, replayed in turn."""
+    calls = []
+    ws = torch.empty(max(hsa.hsa_paged_attention_workspace_bytes(2, 1, 8, 2, 128),
+                         hsa.hsa_paged_attention_workspace_bytes(3, 5, 4, 2, 64)), dtype=torch.uint8, device=DEV)
+    for lens, new, Hq, D in (([3000, 700], 1, 8, 128), ([5, 900, 4000], 5, 4, 64)):
+        pool = Pool(_random(lens, 2, D, 70 + D), 32, 2, D, 70 + D)
+        q = _normal((len(lens), new, Hq, D), 71).to(torch.bfloat16)
+        d = [t.to(DEV) for t in (q, *pool.codes, pool.table, torch.tensor(lens, dtype=torch.int32))]
+        words = [t.to(DEV) for t in pool.words]
+        out, graph = torch.empty_like(d[0]), torch.cuda.CUDAGraph()
+
+        def run():
+            hsa.hsa_paged_attention(*d, out, k_scale=words[0], v_scale=words[1], workspace=ws)
+        run()
+        first = out.clone()
+        for b in range(len(lens)):
+            want, tol = pool.want(b, q[b], new)
+            assert ((out[b].double().cpu() - want).abs() <= tol).all()
+        with torch.cuda.graph(graph):
+            run()
+        calls.append((graph, out, first, d, words))
+    for _ in range(3):
+        for _, out, *_ in calls:
+            out.fill_(9.0)
+        for graph, *_ in calls:
+            graph.replay()
+        assert all(torch.equal(out, first) for _, out, first, *_ in calls)
+    assert hsa.hsa_get_device_error() == 0
+
+
 def test_long_sequences_are_split_and_joined(hsa):
     _check(hsa, [30011], 1, 4, 1, 128, 64, 3)
     _check(hsa, [9000, 40, 12000, 0, 1, 130], 2, 4, 2, 64, 16, 4)
