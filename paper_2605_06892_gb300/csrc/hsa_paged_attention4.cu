@@ -8,7 +8,9 @@
 // sums of exact fp16 products over one group each, times the factors in 32 bits.  A value's
 // factors go into the probabilities, one group of dimensions after the other: P in fp16 is
 // 2^(u - M + 6), at most 2^10 * 63 with a factor (u is 4 above M at most), and its product with
-// one is rounded to fp16 again (2^-11 of itself).  Codes are always finite; where a row is held as NaN its factors are.
+// one is rounded to fp16 again (2^-11 of itself).  Codes and factors are always finite; where a
+// row is held as NaN its power is NaN, and so become the scores, or the weights, of the query
+// rows that see it and of no others.
 //
 // The groups interleave (dimension d is of group (d / (D/32)) mod 4): the 16 (D = 64: 8) bytes
 // of a key that a lane of a quad multiplies, and the 8 (4) bytes of a value, hold all four in
@@ -21,9 +23,9 @@
 // box of a page's rows each, a warp holds 64 keys of a tile and takes them 32 at a time, their
 // words wait in registers, and the blocks of a key's heads run side by side: their rows and words
 // lie together, and what one block leaves of a line or sector the others find in L2 (4 sequences
-// of 95000 keys: 134 -> 112 us).  32 query heads over 8 of D = 128: 4 sequences of 95000 keys 101
-// us, 4.1 TB/s, 0.60 of HBM's measured rate (tiles of 32 keys a warp 109); 48 of 4500 68 us, 0.48;
-// one of 4001 11.6 us.
+// of 95000 keys: 134 -> 112 us).  32 query heads over 8 of D = 128: 4 sequences of 95000 keys 96 us,
+// 4.3 TB/s, 0.63 of HBM's measured rate (tiles of 32 keys a warp 105); 48 of 4500 65 us, 0.51;
+// one of 4001 10.6 us.
 #include <algorithm>
 #include <atomic>
 #include <cstring>
@@ -184,18 +186,16 @@ __device__ __forceinline__ void score_tile(uint32_t sk, const uint4 *m, int g, i
 }
 
 // O^T += V^T P^T over 16 keys, block b of a tile at sv, with the keys' factors for each group in
-// the probabilities (factors: four pairs for each two keys).  sees(x, k): whether row 8 x + g
-// sees key k of the tile, where some do not (`part`).
-template <int D, int kNR, bool part, typename Sees>
+// the probabilities (factors: four pairs for each two keys).
+template <int D, int kNR>
 __device__ __forceinline__ void add_values(float (&o)[D / 16][kNR][4],
                                            const uint32_t (&p)[kNR][2], uint32_t sv,
-                                           const uint4 *factors, int b, int g, int t,
-                                           Sees &&sees) {
+                                           const uint4 *factors, int b, int g, int t) {
   constexpr int kW = D / 64;   // words of a lane's part of a row
   // A byte holds two dimensions of a key: the low halves of both keys' bytes make a pair of one
   // dimension, the high halves of the next.
   constexpr uint32_t kLow = 0x0f0f0f0fu;
-  uint32_t wa[2][kW], wb[2][kW], factor[2][4], keep[kNR][2];
+  uint32_t wa[2][kW], wb[2][kW], factor[2][4];
 #pragma unroll
   for (int hi = 0; hi < 2; ++hi) {
     const int ra = 16 * b + 8 * hi + key_of<D>(2 * t);
@@ -211,18 +211,6 @@ __device__ __forceinline__ void add_values(float (&o)[D / 16][kNR][4],
     const uint4 f = factors[8 * b + 4 * hi + t];
 #pragma unroll
     for (int i = 0; i < 4; ++i) factor[hi][i] = word(f, i);
-  }
-  // The factors of a row of NaN are NaN: they must not reach the rows that may not see it by
-  // 0 * NaN, so what newer keys than a row's are worth is zero after the product.
-  if (part) {
-#pragma unroll
-    for (int x = 0; x < kNR; ++x)
-#pragma unroll
-      for (int hi = 0; hi < 2; ++hi) {
-        const int k = 16 * b + 8 * hi;
-        keep[x][hi] = (sees(x, k + key_of<D>(2 * t)) ? 0xffffu : 0u) |
-                      (sees(x, k + key_of<D>(2 * t + 1)) ? 0xffff0000u : 0u);
-      }
   }
 #pragma unroll
   for (int w = 0; w < kW; ++w) {   // a word: four MMA blocks of 16 dimensions
@@ -244,7 +232,6 @@ __device__ __forceinline__ void add_values(float (&o)[D / 16][kNR][4],
                 __hmul2(*reinterpret_cast<const __half2 *>(&p[x][hi]),
                         *reinterpret_cast<const __half2 *>(&factor[hi][(4 * w + i) / kW]));
             y[hi] = *reinterpret_cast<const uint32_t *>(&z);
-            if (part) y[hi] &= keep[x][hi];
           }
         }
         const uint32_t v[4] = {even[0][i], odd[0][i], even[1][i], odd[1][i]};
@@ -603,15 +590,16 @@ paged_attention4_kernel(const __grid_constant__ Maps maps, const PagedArgs a) {
       {
         // A lane's key: (kf, kf, ve, ve) with kf = 2^ks times the scale's digits and ve = vs;
         // K's factors; V's in fp16, beside those of the pair's other key: this lane makes two
-        // groups' of both, the key of the even MMA index low.  A row of NaN has s = 255: its
-        // kf, and its V factors, are NaN.
+        // groups' of both, the key of the even MMA index low.  A row of NaN has s = 255: its kf,
+        // or ve, is NaN.
         const uint2 w = i == 0 ? make_uint2(wk_now[0], wv_now[0])
                                : make_uint2(wk_now[kParts - 1], wv_now[kParts - 1]);
         const uint32_t ks = w.x >> 24, vs = w.y >> 24;
         const uint32_t kf =
             ks == 255u ? 0x7fffffffu : __float_as_uint(__uint_as_float(ks << 23) * a.scale_digits);
-        const uint32_t ve = __float_as_uint(
-            __uint_as_float(0x4b000000u | (vs == 255u ? 127u : vs)) - (0x1p23f + 127.f));
+        const uint32_t ve =
+            vs == 255u ? 0x7fffffffu
+                       : __float_as_uint(__uint_as_float(0x4b000000u | vs) - (0x1p23f + 127.f));
         made[lane] = make_uint4(kf, kf, ve, ve);
         auto factor = [&](int i) {
           return __float_as_uint(__uint_as_float(0x4b000000u | (w.x >> (6 * i) & 63u)) - 0x1p23f);
@@ -625,8 +613,7 @@ paged_attention4_kernel(const __grid_constant__ Maps maps, const PagedArgs a) {
           *reinterpret_cast<uint32_t *>(&z) =
               0x64006400u | (lo >> (6 * i) & 63u) | (hi >> (6 * i) & 63u) << 16;
           z = __hsub2(z, __float2half2_rn(1024.f));
-          return *reinterpret_cast<uint32_t *>(&z) | (lo >> 24 == 255u ? 0x7fffu : 0u) |
-                 (hi >> 24 == 255u ? 0x7fff0000u : 0u);
+          return *reinterpret_cast<uint32_t *>(&z);
         };
         const int two = even ? 0 : 2;
         reinterpret_cast<uint2 *>(made + 2 * kKW)[2 * (lane >> 1) + (even ? 0 : 1)] =
@@ -765,13 +752,7 @@ paged_attention4_kernel(const __grid_constant__ Maps maps, const PagedArgs a) {
             p[x][n] = transposed(
                 pack_f16(fast_exp2(s[b][x][2 * n]), fast_exp2(s[b][x][2 * n + 1])));
           }
-        auto sees = [&](int x, int k) {
-          return key0 + k < cur.len - a.n_new + 1 + (int)quotient(row0() + 8 * x + g, a.group);
-        };
-        if (ragged && a.n_new > 1)
-          add_values<D, kNR, true>(o, p, sv, made + 2 * kKW, b, g, t, sees);
-        else
-          add_values<D, kNR, false>(o, p, sv, made + 2 * kKW, b, g, t, sees);
+        add_values<D, kNR>(o, p, sv, made + 2 * kKW, b, g, t);
       }
     }
 
