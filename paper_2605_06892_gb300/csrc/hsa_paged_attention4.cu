@@ -23,9 +23,9 @@
 // box of a page's rows each, a warp holds 64 keys of a tile and takes them 32 at a time, their
 // words wait in registers, and the blocks of a key's heads run side by side: their rows and words
 // lie together, and what one block leaves of a line or sector the others find in L2 (4 sequences
-// of 95000 keys: 134 -> 112 us).  32 query heads over 8 of D = 128: 4 sequences of 95000 keys 96 us,
-// 4.3 TB/s, 0.63 of HBM's measured rate (tiles of 32 keys a warp 105); 48 of 4500 65 us, 0.51;
-// one of 4001 10.6 us.
+// of 95000 keys: 134 -> 112 us).  32 query heads over 8 of D = 128: 4 sequences of 95000 keys 96
+// us, 4.3 TB/s, 0.63 of HBM's measured rate (tiles of 32 keys a warp took 8 us more); 48 of 4500 65 us,
+// 0.51; one of 4001 10.6 us.
 #include <algorithm>
 #include <atomic>
 #include <cstring>
