@@ -23,9 +23,9 @@
 // box of a page's rows each, a warp holds 64 keys of a tile and takes them 32 at a time, their
 // words wait in registers, and the blocks of a key's heads run side by side: their rows and words
 // lie together, and what one block leaves of a line or sector the others find in L2 (4 sequences
-// of 95000 keys: 134 -> 112 us).  32 query heads over 8 of D = 128: 4 sequences of 95000 keys 96
-// us, 4.3 TB/s, 0.63 of HBM's measured rate (tiles of 32 keys a warp took 8 us more); 48 of 4500 65 us,
-// 0.51; one of 4001 10.6 us.
+// of 95000 keys: 134 -> 112 us).  32 query heads over 8 of D = 128: 4 sequences of 95000 keys 94
+// us, 4.4 TB/s, 0.64 of HBM's measured rate (tiles of 32 keys a warp took 8 us more); 48 of 4500 64
+// us, 0.52; one of 4001 10.4 us.
 #include <algorithm>
 #include <atomic>
 #include <cstring>
@@ -637,34 +637,47 @@ paged_attention4_kernel(const __grid_constant__ Maps maps, const PagedArgs a) {
         mx[x][0] = mx[x][1] = -INFINITY;
         sum[x][0] = l[x][0], sum[x][1] = l[x][1];
       }
-      auto weigh = [&](auto masked) {
+      // (without masks first: one piece of code with the products, in which the two blocks overlap)
+      float e[kNB][kNR][4];
+#pragma unroll
+      for (int b = 0; b < kNB; ++b)
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+          const uint4 w = made[16 * b + 8 * n + key_of<D>(g)];
+#pragma unroll
+          for (int x = 0; x < kNR; ++x) {
+            const uint64_t z =
+                fma2(code_product(s[b][x], n, before[x], w), both(after[x][0], after[x][1]),
+                     both(down[x][0], down[x][1]));
+            const uint64_t u = add2(add2(z, pack2(w.z, w.w)), both(up[x][0], up[x][1]));
+            e[b][x][2 * n] = fast_exp2(lo_f(z)), e[b][x][2 * n + 1] = fast_exp2(hi_f(z));
+            s[b][x][2 * n] = lo_f(u), s[b][x][2 * n + 1] = hi_f(u);
+          }
+        }
+      if (ragged) {
+#pragma unroll
+        for (int b = 0; b < kNB; ++b)
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int x = 0; x < kNR; ++x)
+#pragma unroll
+              for (int j = 0; j < 2; ++j)
+                if (key0 + 16 * b + 8 * n + key_of<D>(g) >= limit(x, j))
+                  s[b][x][2 * n + j] = -INFINITY, e[b][x][2 * n + j] = 0.f;
+      }
+#pragma unroll
+      for (int x = 0; x < kNR; ++x)
 #pragma unroll
         for (int b = 0; b < kNB; ++b)
 #pragma unroll
           for (int n = 0; n < 2; ++n) {
-            const int row = 16 * b + 8 * n + key_of<D>(g);
-            const uint4 w = made[row];
-#pragma unroll
-            for (int x = 0; x < kNR; ++x) {
-              const uint64_t z =
-                  fma2(code_product(s[b][x], n, before[x], w), both(after[x][0], after[x][1]),
-                       both(down[x][0], down[x][1]));
-              const uint64_t u = add2(add2(z, pack2(w.z, w.w)), both(up[x][0], up[x][1]));
-              float &y0 = s[b][x][2 * n], &y1 = s[b][x][2 * n + 1];
-              float e0 = fast_exp2(lo_f(z)), e1 = fast_exp2(hi_f(z));
-              y0 = lo_f(u), y1 = hi_f(u);
-              if (decltype(masked)::value) {
-                if (key0 + row >= limit(x, 0)) y0 = -INFINITY, e0 = 0.f;
-                if (key0 + row >= limit(x, 1)) y1 = -INFINITY, e1 = 0.f;
-              }
-              const uint64_t w2 = add2(both(sum[x][0], sum[x][1]), both(e0, e1));
-              sum[x][0] = lo_f(w2), sum[x][1] = hi_f(w2);
-              mx[x][0] = fmaxf(mx[x][0], y0), mx[x][1] = fmaxf(mx[x][1], y1);
-            }
+            const uint64_t w2 = add2(both(sum[x][0], sum[x][1]),
+                                     both(e[b][x][2 * n], e[b][x][2 * n + 1]));
+            sum[x][0] = lo_f(w2), sum[x][1] = hi_f(w2);
+            mx[x][0] = fmaxf(mx[x][0], s[b][x][2 * n]);
+            mx[x][1] = fmaxf(mx[x][1], s[b][x][2 * n + 1]);
           }
-      };
-      if (!ragged) weigh(std::false_type());
-      else weigh(std::true_type());
       // Rare: the first tile, sums far from R, or a u further above M than fp16 has room for.  M
       // is a largest u, but rises only then: a new largest is in two thirds of the first 20
       // tiles, and O would be scaled each time.
