@@ -23,7 +23,7 @@
 // box of a page's rows each, a warp holds 64 keys of a tile and takes them 32 at a time, their
 // words wait in registers, and the blocks of a key's heads run side by side: their rows and words
 // lie together, and what one block leaves of a line or sector the others find in L2 (4 sequences
-// of 95000 keys: 134 -> 112 us).  32 query heads over 8 of D = 128: 4 sequences of 95000 keys 94
+// of 95000 keys: 134 -> 112 us).  32 query heads over 8 of D = 128: 4 sequences of 95000 keys 95
 // us, 4.4 TB/s, 0.64 of HBM's measured rate (tiles of 32 keys a warp took 8 us more); 48 of 4500 64
 // us, 0.52; one of 4001 10.4 us.
 #include <algorithm>
