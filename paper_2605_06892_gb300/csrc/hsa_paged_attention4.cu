@@ -23,9 +23,9 @@
 // box of a page's rows each, a warp holds 64 keys of a tile and takes them 32 at a time, their
 // words wait in registers, and the blocks of a key's heads run side by side: their rows and words
 // lie together, and what one block leaves of a line or sector the others find in L2 (4 sequences
-// of 95000 keys: 134 -> 112 us).  32 query heads over 8 of D = 128: 4 sequences of 95000 keys 95
-// us, 4.4 TB/s, 0.64 of HBM's measured rate (tiles of 32 keys a warp took 8 us more); 48 of 4500 64
-// us, 0.52; one of 4001 10.4 us.
+// of 95000 keys: 134 -> 112 us).  32 query heads over 8 of D = 128: 4 sequences of 95000 keys 90
+// us, 4.6 TB/s, 0.67 of HBM's measured rate (tiles of 32 keys a warp took 8 us more, the two parts
+// of a tile in a loop 4); 48 of 4500 61 us, 0.56; one of 4001 10.9 us.
 #include <algorithm>
 #include <atomic>
 #include <cstring>
@@ -581,7 +581,7 @@ paged_attention4_kernel(const __grid_constant__ Maps maps, const PagedArgs a) {
       }
     }
 
-#pragma unroll 1
+#pragma unroll
     for (int i = 0; i < kParts; ++i) {
       const int key0 = cur.tile * kTile + warp * kHold + i * kKW;
       if (key0 >= cur.len) break;
