@@ -436,6 +436,7 @@ paged_attention4_kernel(const __grid_constant__ Maps maps, const PagedArgs a) {
         copy16(to + r * (2 * D) + 16 * (c ^ (r & 7)),
                a.q + (((size_t)ahead.b * a.n_new + i) * a.Hq + head) * D + 8 * c, ok);
       }
+      commit();   // every thread: the unit's start waits for its own copies
       q_fill = q_fill + 1 == C::kStages ? 0 : q_fill + 1;
     }
     const uint32_t bar = bars + 8 * fill;
