@@ -413,7 +413,8 @@ __global__ void __maxnreg__((kY == 1 ? 64 : 96)) norm_ring_kernel(const RingArgs
     abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (threadIdx.x < 4 * kMostWarps) (&part[0][0][0])[threadIdx.x] = 0.f;
+  // a block may have fewer threads than these: those of warps that are not there stay zero
+  for (int i = threadIdx.x; i < 4 * kMostWarps; i += threads) (&part[0][0][0])[i] = 0.f;
   __syncthreads();
   pdl_wait();
   pdl_trigger();

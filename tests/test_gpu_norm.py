@@ -189,3 +189,31 @@ def test_same_as_the_rotation_by_itself(hsa):
                          table_idx=at.to(DEV))
     hsa.hsa_rope_rows(y, at.to(DEV), n, table.to(DEV))
     assert torch.equal(qo, y) and torch.equal(ko, y)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n,Hq,Hkv,D", [(6200, 4, 4, 64), (6200, 4, 1, 64), (6200, 1, 1, 8), (6200, 8, 3, 32),
+                                        (6200, 2, 2, 128), (6200, 1, 1, 256), (6200, 32, 32, 8), (3000, 5, 5, 80),
+                                        (3000, 12, 3, 96), (3000, 3, 3, 24), (1500, 32, 8, 128), (1500, 40, 40, 128)])
+def test_across_heads_token_after_token(hsa, n, Hq, Hkv, D, dtype):
+    """More tokens than blocks, so that a block takes several, from one warp a block to as many
+    threads as there are; with rows whose squares overflow, and rows of zeros.  The kernel before
+    has left NaN where sums are kept."""
+    (q, k, v), w, table, at, idx = _inputs(n, Hq, Hkv, D, torch.float32, n + D, True)
+    q[5::50] *= 2.0 ** 75
+    k[9::31] *= 2.0 ** 90
+    k[4::13] = 0.0
+    q, k, v = (x.to(dtype) for x in (q, k, v))
+    d = [t.to(DEV) for t in (q, k, v, *w, table, at, idx)]
+    nan = torch.full((1500, 32, 128), float("nan"), dtype=dtype, device=DEV)
+    for rows in (None, d[7]):
+        hsa.hsa_qk_norm_rope(nan, nan, None, None, torch.empty_like(nan), torch.empty_like(nan), across=True)
+        qo = torch.empty_like(d[0])
+        ko, vo = (torch.full((n if rows is None else 2 * n + 3, Hkv, D), 3.0, dtype=dtype, device=DEV) for _ in "kv")
+        hsa.hsa_qk_norm_rope(d[0], d[1], d[3], d[4], qo, ko, across=True, table=d[5], table_idx=d[6], v=d[2], v_out=vo,
+                             k_idx=rows)
+        assert hsa.hsa_get_device_error() == 0
+        ko, vo = (x if rows is None else x[rows.long()] for x in (ko, vo))
+        for got, x, weight in ((qo, q, w[0]), (ko, k, w[1])):
+            _close(got, *ref.norm_rope(x, weight, 1e-6, True, table, at, STEP[dtype]))
+        assert torch.equal(vo, d[2])
