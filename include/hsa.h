@@ -443,9 +443,10 @@ int hsa_qk_norm_rope(const void *q, long long q_row, const void *k, long long k_
  *   - Where W < H (tokens withdrawn, or a sequence ended: want[b] = 0) pages W .. H-1 of
  *     page_table[b] go onto the stack of free pages, in the order of b and page.
  *   - After that sequences grow, in the order of b, while pages and places last: b grows if
- *     W == H or the pages that the growing sequences up to and with b ask for are there, and
- *     if their new tokens number at most max_new.  What does not grow keeps lens[b] and gets
- *     no tokens; lens_out tells.  page_table[b] H .. W-1 take the pages from the stack's top.
+ *     W == H or the pages that all sequences up to and with b ask for are there, and if the new
+ *     tokens that they ask for number at most max_new; what a sequence asks for counts whether
+ *     it grows or not.  What does not grow keeps lens[b] and gets no tokens; lens_out tells.
+ *     page_table[b] H .. W-1 take the pages from the stack's top.
  *   lens, want    device, int32 [batch], in [0, max_pages * page_size]; a value outside is
  *                 taken as the nearer end and reported (HSA_ERR_INDEX).
  *   page_table    device, int32 [batch, max_pages], updated in place, as

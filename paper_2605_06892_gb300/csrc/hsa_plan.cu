@@ -177,8 +177,8 @@ __global__ void __launch_bounds__(kT) page_plan_one_kernel(const Args a) {
   block_scan(x, total, sh_sum);
   const unsigned back_total = total[0], back_end = x[0];
   const unsigned count = min((unsigned)n_free + back_total, (unsigned)a.n_pages);
-  // a sequence grows where its pages and its tokens' places last for it and all that grow
-  // before it
+  // a sequence grows where its pages and its tokens' places last for it and all that ask
+  // before it, whether they got theirs or not
   const bool ok = fresh == 0 || ((get == 0 || x[1] <= count) && x[2] <= (unsigned)a.max_new);
   sh_back[b] = back_end;
   sh_to[b] = to;
@@ -282,8 +282,9 @@ __global__ void __launch_bounds__(kThreads) page_plan_kernel(const Args a) {
   const unsigned count = min((unsigned)n_free + back_total, (unsigned)a.n_pages);
 
   // ---- growth: a sequence grows where its pages and its tokens' places last for it and all
-  // that grow before it
-  unsigned got = 0, asked = 0, sum_q = 0, sum_k = 0;   // of the sequences before these
+  // that ask before it, whether they got theirs or not
+  unsigned asked_pages = 0, asked = 0;          // of the sequences before these
+  unsigned got = 0, sum_q = 0, sum_k = 0;       // granted to them
   if (threadIdx.x == 0) {
     a.cu_q[0] = 0;
     if (a.cu_k) a.cu_k[0] = 0;
@@ -295,9 +296,9 @@ __global__ void __launch_bounds__(kThreads) page_plan_kernel(const Args a) {
     const unsigned get = max(0, pages(w) - from), fresh = max(0, w - l);
     unsigned x[3] = {get, fresh, (unsigned)w}, total[3];
     block_scan(x, total, sh_sum);
-    const bool ok = fresh == 0 || ((get == 0 || add_up(got, x[0]) <= count) &&
+    const bool ok = fresh == 0 || ((get == 0 || add_up(asked_pages, x[0]) <= count) &&
                                    add_up(asked, x[1]) <= (unsigned)a.max_new);
-    const unsigned want_total = total[1];
+    const unsigned want_pages = total[0], want_total = total[1];
     if (__syncthreads_or(!ok)) {   // rare: the sums again, without those
       x[0] = ok ? get : 0;
       x[1] = ok ? fresh : 0;
@@ -321,6 +322,7 @@ __global__ void __launch_bounds__(kThreads) page_plan_kernel(const Args a) {
       __syncthreads();
     }
     got += total[0];   // at most count
+    asked_pages = add_up(asked_pages, want_pages);
     asked = add_up(asked, want_total);
     sum_q = add_up(sum_q, total[1]);
     sum_k = add_up(sum_k, total[2]);

@@ -204,3 +204,40 @@ def test_launches_and_graph(hsa):
                      (ps, "positions")):
             assert torch.equal(x.cpu(), exp[k]), k
     assert hsa.hsa_get_device_error() == 0
+
+
+def test_pages_asked_for_count_across_groups_of_sequences(hsa):
+    """A sequence that asks for more pages than there are stops those behind it that need any,
+    wherever it stands."""
+    for B in (5, 1024, 1025, 1026, 2049):
+        lens, want = [0] * B, [48] + [0] * (B - 2) + [1]
+        table, free, n = _state(lens, 16, 4, 9, 7)
+        for n_free in range(5):
+            exp = _check(hsa, lens, want, 16, table, free, n_free, 200)
+            assert exp["lens_out"][-1] == (n_free == 4)
+    lens, want = [0] * 1025, [2] + [0] * 1023 + [1]
+    table, free, _ = _state(lens, 1, 4, 9, 7)
+    exp = _check(hsa, lens, want, 1, table, free, 1, 200)
+    assert not exp["lens_out"].any() and exp["n_free_out"].tolist() == [1]
+
+
+@pytest.mark.parametrize("B", [1023, 1024, 1025, 1026, 1027, 1028, 1029, 1030, 2049])
+def test_every_size_of_the_stack(hsa, B):
+    """Mixed needs on both sides of a border of 1024 sequences; any number of free pages, and of
+    places for tokens, from none to what is needed."""
+    page = 4
+    g = torch.Generator().manual_seed(B)
+    lens = torch.randint(0, 9, (B,), generator=g)
+    want = lens.clone()
+    some = torch.cat([torch.arange(3), torch.randint(0, B, (25,), generator=g), torch.arange(B - 10, B)])
+    want[some] += torch.randint(1, 4 * page, some.shape, generator=g)
+    want[torch.randint(0, B, (4,), generator=g)] = 0
+    lens, want = lens.tolist(), want.tolist()
+    asked = sum(max(0, w - h) for h, w in zip(lens, want))
+    need = sum(max(0, -(-w // page) - -(-h // page)) for h, w in zip(lens, want))
+    table, free, n = _state(lens, page, 8, need, 3)
+    for n_free in range(need + 1):
+        _check(hsa, lens, want, page, table, free, n_free, asked)
+    for max_new in range(0, asked + 1, 7):
+        _check(hsa, lens, want, page, table, free, n, max_new)
+        _check(hsa, lens, want, page, table, free, need // 2, max_new)
