@@ -203,6 +203,28 @@ struct CodeTile {
   float ref[kNR][2], l[kNR][2], m[kNR][2];      // those before the tile; then the new R, l with
   float s[2][kNR][4], mx[kNR][2];               // the tile's, the old m relative to R, u
 };
+
+// The end of a row's sums: x 2^h / l, by factors that are in range wherever the result is.  h may
+// lie beyond the exponents that 2^h has alone, where scores far from R meet values near the ends
+// of their range (l then has scores of that size too): l's exponent goes into it first, and what
+// is left in two halves.  Else the usual 2^h, and 1 / l.
+template <bool kCode>
+struct RowEnd {
+  float inv, up = 1.f, rest = 1.f;
+  __device__ __forceinline__ RowEnd(float l, float h) {
+    inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
+    if (!kCode) return;
+    if (fabsf(h) > 100.f && l > 0.f) {
+      const uint32_t w = __float_as_uint(l);
+      inv = 1.f / __uint_as_float((w & 0x7fffffu) | 0x3f800000u);
+      up = rest = fast_exp2(0.5f * (h - (float)((int)(w >> 23) - 127)));
+    } else {
+      up = fast_exp2(h);
+    }
+  }
+  __device__ __forceinline__ float operator()(float x) const { return x * inv * up * rest; }
+};
+
 // Joins a row's parts where several blocks shared its unit: one block for each block of
 // the kernel before and each row, and most of them find that theirs ended no such unit.
 // A part takes D/4 lanes, four dimensions each; bound by the round trips to L2, so each
@@ -290,14 +312,12 @@ paged_join_kernel(const PagedArgs a) {
   acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
   for (int y = 0; y < kGroups; ++y) add(sh_stat[y], sh_o[y * kL + sub]);
-  const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;
-  const float up = kCode ? fast_exp2(M - kPShift) : 1.f;
+  const RowEnd<kCode> end(L, M - kPShift);
   const int i = quotient(r, a.group);
   reinterpret_cast<uint2 *>(a.out + ((size_t)((size_t)u.b * a.n_new + i) * a.Hq +
                                      h * (int)a.group.d +
                                      (r - i * (int)a.group.d)) * D)[sub] =
-      make_uint2(pack_bf16(acc.x * inv * up, acc.y * inv * up),
-                 pack_bf16(acc.z * inv * up, acc.w * inv * up));
+      make_uint2(pack_bf16(end(acc.x), end(acc.y)), pack_bf16(end(acc.z), end(acc.w)));
 }
 
 size_t workspace_bytes(int D) {

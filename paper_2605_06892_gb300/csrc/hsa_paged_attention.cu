@@ -789,15 +789,14 @@ paged_attention_kernel(const PagedArgs a) {
             const int rr = 8 * x + 2 * t + j, r = r0 + rr;
             if (r >= a.rows) continue;
             if (whole) {
-              const float inv = sum[j] > 0.f ? 1.f / sum[j] : sum[j] == 0.f ? 0.f : sum[j];
-              const float up = kF8 ? fast_exp2(M[j] - kPShift) : 1.f;
+              const RowEnd<kF8> end(sum[j], M[j] - kPShift);
               const int i = quotient(r, a.group);
               __nv_bfloat16 *dst = a.out + ((size_t)((size_t)cur.b * a.n_new + i) * a.Hq +
                                             h * (int)a.group.d + (r - i * (int)a.group.d)) * D + d;
               uint32_t w[kQuarter];
 #pragma unroll
               for (int n = 0; n < kQuarter; ++n)
-                w[n] = pack_bf16(y[n][j] * inv * up, y[n][2 + j] * inv * up);
+                w[n] = pack_bf16(end(y[n][j]), end(y[n][2 + j]));
               if constexpr (kQuarter == 2)
                 *reinterpret_cast<uint2 *>(dst) = make_uint2(w[0], w[kQuarter - 1]);
               else

@@ -377,3 +377,21 @@ def test_pages_past_4_gib(hsa):
     want, tol = base.attention(q[0].double(), held[0][2], held[1][2], [n], p_step=ref.P_STEP)
     tol = tol + ref.small_weights(q[0].double(), held[0][2], held[1][1], [n])
     assert ((out[0].double().cpu() - want).abs() <= tol).all()
+
+
+FAR = [(30, 119), (30, 126), (60, 118), (60, 126), (-30, 126), (-60, -62), (-60, -90), (30, -95), (60, -95), (-60, 119)]
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("level,power", FAR)
+@pytest.mark.parametrize("n,new", [(100, 1), (7000, 1), (300, 3)])
+def test_scores_away_from_zero_beside_values_at_the_ends(hsa, n, new, level, power, D):
+    """All scores near 2^level's exponent, values near 2^power: the result is a mean of values,
+    whatever the two add up to; in one block and joined."""
+    g = torch.Generator().manual_seed(n + power)
+    k = torch.zeros((n, 1, D))
+    k[:, 0, 0] = level + 3 * torch.rand((n,), generator=g) - 1.5
+    q = torch.zeros((1, new, 2, D))
+    q[..., 0] = 1.0
+    v = (torch.rand((n, 1, D), generator=g) + 0.9) * 2.0 ** power
+    _compare(hsa, [(k, v)], q.to(torch.bfloat16), 128, scale=0.6931471805599453)

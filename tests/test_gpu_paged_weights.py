@@ -211,3 +211,21 @@ def test_largest_score_takes_all(hsa, f8, D, power):
     assert ((top[:, 0] - top[:, 1]) > apart + 40).all()
     want = held[1][at[:, 0], 0]
     assert ((got - want).abs() <= (2.0 ** -8 + 2.0 ** -20) * want.abs() + 2.0 ** -39 * want.abs().amax()).all()
+
+
+FAR = [(30, 119), (30, 126), (60, 118), (60, 126), (-30, 126), (-60, -62), (-60, -90), (30, -95), (60, -95), (-60, 119)]
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("level,power", FAR)
+@pytest.mark.parametrize("n,new", [(100, 1), (7000, 1), (300, 9)])
+def test_scores_away_from_zero_beside_values_at_the_ends(hsa, n, new, level, power, D):
+    """All scores near 2^level's exponent, values near 2^power: the result is a mean of values,
+    whatever the two add up to; in one block and joined."""
+    g = torch.Generator().manual_seed(n + power)
+    k = torch.zeros((n, 1, D))
+    k[:, 0, 0] = level + 3 * torch.rand((n,), generator=g) - 1.5
+    q = torch.zeros((1, new, 2, D))
+    q[..., 0] = 1.0
+    v = (torch.rand((n, 1, D), generator=g) + 0.9) * 2.0 ** power
+    _check(hsa, Sequence(k, v), q.to(torch.bfloat16), scale=0.6931471805599453)
