@@ -221,12 +221,15 @@ __device__ __forceinline__ void quantise(Eight<kF32> (&v)[Y::kN], uint32_t (&cod
   float unit[kG], per[kG];
 #pragma unroll
   for (int i = 0; i < kG; ++i) {
-    const float a = __uint_as_float(m[i]) * f;         // exact, at most 378
+    // at most 378, and exact, but for groups so far below the row that their factor is 1
+    const float a = __uint_as_float(m[i]) * f;
     // ceil(a / 6): a times a little less than 1/6, rounded up to a whole number as it joins
     // 2^23.  Of bf16 values a is 6 n or above it by 2^-8 of itself and so well above a little
     // less; of fp32 ones it may be one too few.
     float n = __fadd_ru(a * __uint_as_float(0x3e2aaaa8u), 0x1p23f);
     if (kF32 && (n - 0x1p23f) * 6.f < a) n += 1.f;
+    // a, or a sixth of it, may have vanished in 32 bits where the group is not zero
+    if (m[i]) n = fmaxf(n, 0x1p23f + 1.f);
     factors |= (__float_as_uint(n) & 63u) << (6 * i);
     unit[i] = n - 0x1p23f;
     float inverse;   // within 2^-23; of a group of zeros any will do

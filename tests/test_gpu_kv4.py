@@ -241,3 +241,22 @@ def test_another_stream_and_graph(hsa):
     assert all(torch.equal(a, b) for a, b in zip(d, eager))
     assert torch.equal(out[0], out[2]) and torch.equal(out[1], out[3])
     assert hsa.hsa_get_device_error() == 0
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("D", [64, 128])
+def test_groups_of_very_different_size(hsa, D, dtype):
+    """A group far below the row's largest, however far, has a factor of one."""
+    group = torch.from_numpy(ref.group_of(D))
+    f = torch.finfo(dtype)
+    rows = []
+    for i, (big, small) in enumerate((b, s) for b in (1e38, f.max, 2.0 ** 100, 1.0, 378.0 * 2.0 ** -100)
+                                     for s in (f.tiny, f.tiny / 64, 1e-38, 2.0 ** -60, 2.0 ** -48, 2.0 ** -49, 2.0 ** -50)):
+        x = torch.zeros(D)
+        x[group == i % 4] = torch.linspace(-big, big, D // 4)
+        x[group == (i + 1) % 4] = small
+        x[group == (i + 2) % 4] = torch.linspace(-small, small / 3, D // 4)
+        rows.append(x)
+    x = torch.stack(rows)[:, None].to(dtype)
+    assert (x.abs() > 0).any(-1).all()
+    _check(hsa, len(rows) + 3, 1, D, dtype, len(rows), 13, (x, -x))
