@@ -514,7 +514,9 @@ int hsa_page_plan(const int32_t *lens, const int32_t *want, int batch, int page_
  * with the identity as its table.
  * HSA_E4M3, HSA_E2M1: a key's weight times the power of two of its value row is held to 2^-39
  * (HSA_E2M1: 2^-31) of the row's largest such product; what lies further below adds nothing to
- * out.  HSA_E2M1: a row of NaN reaches the rows that see its key, in every dimension. */
+ * out.  Weights meet the codes in fp16, rounded once (HSA_BF16: in bf16), HSA_E2M1: and once more
+ * with a group's factor; their sum is of those not rounded.  HSA_E2M1: a row of NaN reaches the
+ * rows that see its key, in every dimension. */
 int hsa_paged_attention(const void *q, int batch, int n_new, int Hq, const void *k_pages,
                         const void *v_pages, const uint8_t *k_scale, const uint8_t *v_scale,
                         int n_pages, int page_size, int Hkv, int D, hsa_dtype cache_dtype,

@@ -413,7 +413,8 @@ __device__ __forceinline__ void store_values(void *base, size_t elem, int c, uin
 }
 
 // Reading back, an item is a (token, head) of the cache, K and V, a vector of eight a lane.  75600
-// tokens of 40 heads of D = 128, bf16: 307 us, 0.94 of HBM's measured rate.
+// tokens of 40 heads of D = 128, bf16: 308 us, 0.94 of HBM's measured rate; D = 64 158, 0.92.  fp32
+// 778 us, 0.66 (each of a lane's two 16-byte stores fills half of a sector, which may be why).
 constexpr int kU = 2;        // items of a lane at a time, reading back
 constexpr int kBlocks = 32;  // blocks per SM at most
 

@@ -26,7 +26,13 @@ constexpr int kMaxD = 256;
 constexpr int kHeads = 4;        // heads of a lane group at a time
 constexpr int kHeadBlocks = 3;   // blocks per SM of the kernel per head
 constexpr float kDown = 0x1p-80f;
-constexpr int kRingTokens = 1;   // tokens per SM from which on the ring takes them
+// Tokens per SM from which on the ring takes them.  Replayed from a graph, whose steps are about
+// 2.05 us, ring / group of warps: bf16 40 x 128, 16 to 150 tokens 6.2 / 6.2 us, 200 8.2 / 8.2, 300
+// 8.2 / 10.3, 600 10.2 / 14.4, 5000 55 / 109; fp32 16 tokens 8.2 / 6.2, 150 8.2 / 8.2, 300 10.3 /
+// 12.3, 5000 113 / 142; bf16 8 x 128 up to 600 tokens 6.2 / 6.2, 5000 20.5 / 22.8; 4 x 64, where a
+// warp holds a row and the ring's blocks are one warp, up to 150 tokens 6.2 / 4.1, 1200 8.2 / 6.2,
+// 5000 18.6 / 14.4.
+constexpr int kRingTokens = 1;
 
 __device__ __forceinline__ uint4 ld16(const void *p) {
   uint4 v;   // not the read-only path: the rows may be written in place
@@ -254,7 +260,9 @@ __device__ __forceinline__ void head_roots(const Args &a, const Eight<kF32> (&v)
 // are resident, so that each warp asks for its next unit's rows, into L2, before it takes the
 // present one: the loads that it waits for are then short ones.  bf16, 40 heads of each, D = 128,
 // 18900 tokens: 179 us, 0.96 of HBM's measured rate; without asking ahead 189, and with 32 blocks
-// per SM in turn instead, whose number hides the latency then, 193.
+// per SM in turn instead, whose number hides the latency then, 193.  fp32 428 us, 0.80; 20 heads of
+// D = 256 191, 0.90; 40 of D = 96 and of 80, where a quarter and more of a group's lanes hold
+// nothing, 180 both, 0.72 and 0.60.
 template <bool kF32, int kLog>
 __global__ void __launch_bounds__(kThreads, kHeadBlocks) norm_heads_kernel(const Args a) {
   pdl_wait();
@@ -385,8 +393,8 @@ norm_row_kernel(const Args a) {
 // does not depend on registers and occupancy; v goes out again without passing through them.  A
 // thread holds the same kY vectors of q and of k of every token, so that their weights stay in
 // registers, and (a head's vectors divide the block's threads) one place in a head.  bf16, 40 heads
-// of each, D = 128: 18900 tokens 181 us, 0.95 of HBM's measured rate (a group of warps per row
-// 397); 1200 14.4 (24.7), 600 10.3 (14.5), 300 8.2 (10.3).
+// of each, D = 128: 18900 tokens 182 us, 0.94 of HBM's measured rate (a group of warps per row
+// 397); fp32 395 us, 0.87.
 constexpr int kMostStages = 8;
 constexpr int kRingThreads = 512;   // at most
 

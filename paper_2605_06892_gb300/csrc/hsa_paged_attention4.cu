@@ -16,16 +16,18 @@
 // of a key that a lane of a quad multiplies, and the 8 (4) bytes of a value, hold all four in
 // equal parts, and MMAs over one group only.
 //
-// What bounds it.  68 bytes a key and head leave 370 issue slots of an SM's quarter for 16 keys
-// of one head at the memory's rate, and decoding (64 conversions and shuffles of bits), 16 MMAs
-// and the softmax need most of them; three warps a quarter, which is what the registers allow, use
-// half of the slots.  So what does not grow with the bytes is kept small: the tiles come by TMA, a
-// box of a page's rows each, a warp holds 64 keys of a tile and takes them 32 at a time, their
-// words wait in registers, and the blocks of a key's heads run side by side: their rows and words
-// lie together, and what one block leaves of a line or sector the others find in L2 (4 sequences
-// of 95000 keys: 134 -> 112 us).  32 query heads over 8 of D = 128: 4 sequences of 95000 keys 90
-// us, 4.6 TB/s, 0.67 of HBM's measured rate (tiles of 32 keys a warp took 8 us more, the two parts
-// of a tile in a loop 4); 48 of 4500 61 us, 0.56; one of 4001 10.9 us.
+// What bounds it is latency.  68 bytes a key and head leave 370 issue slots of an SM's quarter for
+// 16 keys of one head at the memory's rate, and decoding (64 conversions and shuffles of bits), 16
+// MMAs and the softmax take 292 of them; but three warps a quarter, which is what the registers
+// allow, issue once in about five cycles each, and so use half of the slots: what counts is a
+// warp's own chain of loads, wait, words, products and softmax.  So what does not grow with the
+// bytes is kept small: the tiles come by TMA, a box of a page's rows each, a warp holds 64 keys of a
+// tile and takes them 32 at a time, their words wait in registers, and the blocks of a key's heads
+// run side by side: their rows and words lie together, and what one block leaves of a line or sector
+// the others find in L2 (4 sequences of 95000 keys: 134 -> 112 us).  32 query heads over 8 of D =
+// 128: 4 sequences of 95000 keys 90 us, 4.6 TB/s, 0.67 of HBM's measured rate (tiles of 32 keys a
+// warp took 8 us more, the two parts of a tile in a loop 4); 48 of 4500 61 us, 0.56; one of 4001
+// 10.9 us.
 #include <algorithm>
 #include <atomic>
 #include <cstring>
@@ -969,6 +971,10 @@ int launch(PagedArgs &a, void *workspace, cudaStream_t stream) {
 
 }  // namespace
 
+// Column blocks of eight query rows per unit: one, or two that share the keys' fragments.  48
+// sequences of 4500 keys, 8 K/V heads, D = 128 (64): 4 and 8 rows a head 61 and 65 us (49); 16 rows
+// 97 (74), with units of eight rows, which decode the keys twice, 113 (86); 24 rows 161 (120)
+// against 153 (119), 32 rows 162 (121) against 203 (147).  More than two do not fit the registers.
 int launch_paged4(PagedArgs &a, int D, void *workspace, cudaStream_t stream) {
   if (D == 128)
     return a.rows <= 8 ? launch<128, 1>(a, workspace, stream)
